@@ -1,4 +1,5 @@
-"""ctypes binding of libolive_score.so (the C ABI of include/olive_score.h).
+"""ctypes binding of libolive_score.so (the C ABI of include/olive_score.h and
+include/olive_layers.h).
 
 Argument marshalling only: every function has the C name and forwards plain
 pointers, sizes and the HIP stream. Torch tensors are accepted wherever the C
@@ -42,6 +43,8 @@ OLIVE_FLAG_NARROW_TILE = 16
 OLIVE_GRAD_REUSE_FORWARD = 1
 OLIVE_TOPK = 16
 OLIVE_OUT_REGION_ONLY = 1
+OLIVE_ROPE_HALF = 0
+OLIVE_ROPE_PAIRS = 1
 
 
 class olive_score_desc(ctypes.Structure):
@@ -81,6 +84,42 @@ class olive_grad_outputs(ctypes.Structure):
 class olive_spans(ctypes.Structure):
     _fields_ = [("size", ctypes.c_int32), ("num_spans", ctypes.c_int32),
                 ("span_offsets", ctypes.c_void_p), ("spans", ctypes.c_void_p)]
+
+
+class olive_heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_token", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64)]
+
+
+class olive_qk_desc(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_int32), ("dtype", ctypes.c_int32), ("tokens", ctypes.c_int64),
+                ("heads_q", ctypes.c_int32), ("heads_k", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("positions", ctypes.c_void_p), ("num_positions", ctypes.c_int64),
+                ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p),
+                ("weight_q", ctypes.c_void_p), ("weight_k", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("slot_rows", ctypes.c_int64)]
+
+
+class olive_attn_desc(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("num_groups", ctypes.c_int32), ("num_seqs", ctypes.c_int32),
+                ("heads_q", ctypes.c_int32), ("heads_kv", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("max_q", ctypes.c_int32),
+                ("total_q", ctypes.c_int64), ("max_prefix", ctypes.c_int64),
+                ("max_suffix", ctypes.c_int64), ("prefix_rows", ctypes.c_int64),
+                ("suffix_rows", ctypes.c_int64), ("group_seqs", ctypes.c_void_p),
+                ("cu_q", ctypes.c_void_p), ("prefix_start", ctypes.c_void_p),
+                ("prefix_len", ctypes.c_void_p), ("suffix_len", ctypes.c_void_p),
+                ("suffix_start", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class olive_grad_tensor(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("dtype_out", ctypes.c_int32)]
 
 
 class OliveError(RuntimeError):
@@ -142,6 +181,28 @@ def load() -> ctypes.CDLL:
     lib.olive_score_last_stats.restype = st
     lib.olive_score_kernel_times.argtypes = [vp, ctypes.POINTER(ctypes.c_float), ctypes.c_int]
     lib.olive_score_kernel_times.restype = st
+    hp, qp = ctypes.POINTER(olive_heads), ctypes.POINTER(olive_qk_desc)
+    ap, i64 = ctypes.POINTER(olive_attn_desc), ctypes.c_int64
+    lib.olive_qk_norm_rope.argtypes = [qp] + [hp] * 6 + [vp]
+    lib.olive_qk_norm_rope.restype = st
+    lib.olive_qk_norm_rope_workspace.argtypes = [qp, ctypes.POINTER(i64)]
+    lib.olive_qk_norm_rope_workspace.restype = st
+    lib.olive_qk_norm_rope_backward.argtypes = [qp] + [hp] * 6 + [f32p, f32p, vp, i64, vp]
+    lib.olive_qk_norm_rope_backward.restype = st
+    lib.olive_prefix_attention_workspace.argtypes = [ap, ctypes.c_int32, ctypes.POINTER(i64)]
+    lib.olive_prefix_attention_workspace.restype = st
+    lib.olive_prefix_attention.argtypes = [ap] + [hp] * 6 + [f32p, vp, i64, vp]
+    lib.olive_prefix_attention.restype = st
+    lib.olive_prefix_attention_backward.argtypes = [ap] + [hp] * 6 + [f32p] + [hp] * 6 + \
+        [vp, i64, vp]
+    lib.olive_prefix_attention_backward.restype = st
+    lib.olive_grad_clip_init.argtypes = [ctypes.POINTER(ctypes.c_void_p),
+                                         ctypes.POINTER(olive_grad_tensor), ctypes.c_int32, vp]
+    lib.olive_grad_clip_init.restype = st
+    lib.olive_grad_clip.argtypes = [vp, ctypes.c_float, f32p, vp]
+    lib.olive_grad_clip.restype = st
+    lib.olive_grad_clip_free.argtypes = [vp]
+    lib.olive_grad_clip_free.restype = st
     _lib = lib
     return lib
 
@@ -349,3 +410,167 @@ def make_desc(vocab, d_student, d_teacher, dtype=OLIVE_BF16, w_layout=OLIVE_W_DV
     d.max_seqs = int(max_seqs)
     d.flags = int(flags)
     return d
+
+
+def make_heads(x) -> Optional[olive_heads]:
+    """An olive_heads over a [tokens, heads, head_dim] tensor whose last dimension is
+    contiguous (None stays None; the caller keeps the tensor alive)."""
+    if x is None or isinstance(x, olive_heads):
+        return x
+    if x.dim() != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
+        raise ValueError("expected [tokens, heads, head_dim] with contiguous heads")
+    return olive_heads(_ptr(x), x.stride(0), x.stride(1))
+
+
+def _heads(x):
+    h = make_heads(x)
+    return None if h is None else ctypes.byref(h)
+
+
+def _workspace(w):
+    return _ptr(w), (0 if w is None else w.numel() * w.element_size())
+
+
+def make_qk_desc(tokens, heads_q, heads_k, head_dim, positions=None, cos=None, sin=None,
+                 weight_q=None, weight_k=None, dtype=OLIVE_BF16, eps=1e-6, layout=OLIVE_ROPE_HALF,
+                 rot_dim=None, num_positions=None, slots=None, slot_rows=0) -> olive_qk_desc:
+    """cos and sin: fp32 [num_positions, rot_dim / 2], which give the default sizes."""
+    d = olive_qk_desc()
+    d.size = ctypes.sizeof(olive_qk_desc)
+    d.dtype, d.tokens = int(dtype), int(tokens)
+    d.heads_q, d.heads_k, d.head_dim = int(heads_q), int(heads_k), int(head_dim)
+    d.rot_dim = int(rot_dim if rot_dim is not None else 0 if cos is None else 2 * cos.shape[1])
+    d.num_positions = int(num_positions if num_positions is not None
+                          else 0 if cos is None else cos.shape[0])
+    d.layout, d.eps = int(layout), float(eps)
+    d.positions, d.cos, d.sin = _ptr(positions), _ptr(cos), _ptr(sin)
+    d.weight_q, d.weight_k = _ptr(weight_q), _ptr(weight_k)
+    d.slots, d.slot_rows = _ptr(slots), int(slot_rows)
+    return d
+
+
+def olive_qk_norm_rope(desc: olive_qk_desc, q, k, q_out, k_out, v=None, v_out=None, stream=None,
+                       check: bool = True) -> int:
+    s = load().olive_qk_norm_rope(ctypes.byref(desc), _heads(q), _heads(k), _heads(v),
+                                  _heads(q_out), _heads(k_out), _heads(v_out), _stream(stream))
+    if check:
+        _check(s, "olive_qk_norm_rope")
+    return s
+
+
+def olive_qk_norm_rope_workspace(desc: olive_qk_desc) -> int:
+    """Bytes of olive_qk_norm_rope_backward's workspace."""
+    n = ctypes.c_int64(0)
+    _check(load().olive_qk_norm_rope_workspace(ctypes.byref(desc), ctypes.byref(n)),
+           "olive_qk_norm_rope_workspace")
+    return n.value
+
+
+def olive_qk_norm_rope_backward(desc: olive_qk_desc, q, k, grad_q_out, grad_k_out, grad_q, grad_k,
+                                grad_weight_q=None, grad_weight_k=None, workspace=None,
+                                stream=None, check: bool = True) -> int:
+    s = load().olive_qk_norm_rope_backward(
+        ctypes.byref(desc), _heads(q), _heads(k), _heads(grad_q_out), _heads(grad_k_out),
+        _heads(grad_q), _heads(grad_k), _ptr(grad_weight_q), _ptr(grad_weight_k),
+        *_workspace(workspace), _stream(stream))
+    if check:
+        _check(s, "olive_qk_norm_rope_backward")
+    return s
+
+
+def make_attn_desc(heads_q, heads_kv, head_dim, group_seqs, cu_q, prefix_start, prefix_len,
+                   suffix_len, total_q, max_q, max_prefix, max_suffix, prefix_rows, suffix_rows,
+                   suffix_start=None, page_table=None, page_size=0, dtype=OLIVE_BF16,
+                   scale=None, num_groups=None, num_seqs=None) -> olive_attn_desc:
+    """Device tensors: group_seqs [G + 1], cu_q [B + 1], prefix_len [G], suffix_len [B] int32,
+    prefix_start [G], suffix_start [B] int64, page_table [B, pages] int32."""
+    d = olive_attn_desc()
+    d.size = ctypes.sizeof(olive_attn_desc)
+    d.dtype = int(dtype)
+    d.num_groups = int(num_groups if num_groups is not None else prefix_len.shape[0])
+    d.num_seqs = int(num_seqs if num_seqs is not None else suffix_len.shape[0])
+    d.heads_q, d.heads_kv, d.head_dim = int(heads_q), int(heads_kv), int(head_dim)
+    d.max_q, d.total_q = int(max_q), int(total_q)
+    d.max_prefix, d.max_suffix = int(max_prefix), int(max_suffix)
+    d.prefix_rows, d.suffix_rows = int(prefix_rows), int(suffix_rows)
+    d.group_seqs, d.cu_q = _ptr(group_seqs), _ptr(cu_q)
+    d.prefix_start, d.prefix_len = _ptr(prefix_start), _ptr(prefix_len)
+    d.suffix_len, d.suffix_start = _ptr(suffix_len), _ptr(suffix_start)
+    d.page_table, d.page_size = _ptr(page_table), int(page_size)
+    d.table_stride = 0 if page_table is None or isinstance(page_table, int) \
+        else page_table.stride(0)
+    d.scale = float(scale if scale is not None else head_dim ** -0.5)
+    return d
+
+
+def olive_prefix_attention_workspace(desc: olive_attn_desc, backward: bool = False) -> int:
+    """Bytes of the workspace of olive_prefix_attention, with `backward` of its backward's
+    where that is more."""
+    most = 0
+    for b in (0, 1) if backward else (0,):
+        n = ctypes.c_int64(0)
+        _check(load().olive_prefix_attention_workspace(ctypes.byref(desc), b, ctypes.byref(n)),
+               "olive_prefix_attention_workspace")
+        most = max(most, n.value)
+    return most
+
+
+def olive_prefix_attention(desc: olive_attn_desc, q, k_prefix, v_prefix, k_suffix, v_suffix, out,
+                           lse=None, workspace=None, stream=None, check: bool = True) -> int:
+    s = load().olive_prefix_attention(
+        ctypes.byref(desc), _heads(q), _heads(k_prefix), _heads(v_prefix), _heads(k_suffix),
+        _heads(v_suffix), _heads(out), _ptr(lse), *_workspace(workspace), _stream(stream))
+    if check:
+        _check(s, "olive_prefix_attention")
+    return s
+
+
+def olive_prefix_attention_backward(desc: olive_attn_desc, q, k_prefix, v_prefix, k_suffix,
+                                    v_suffix, out, lse, grad_out, grad_q, grad_k_prefix,
+                                    grad_v_prefix, grad_k_suffix, grad_v_suffix, workspace=None,
+                                    stream=None, check: bool = True) -> int:
+    s = load().olive_prefix_attention_backward(
+        ctypes.byref(desc), _heads(q), _heads(k_prefix), _heads(v_prefix), _heads(k_suffix),
+        _heads(v_suffix), _heads(out), _ptr(lse), _heads(grad_out), _heads(grad_q),
+        _heads(grad_k_prefix), _heads(grad_v_prefix), _heads(grad_k_suffix),
+        _heads(grad_v_suffix), *_workspace(workspace), _stream(stream))
+    if check:
+        _check(s, "olive_prefix_attention_backward")
+    return s
+
+
+def _dtype_of(x) -> int:
+    kinds = {"torch.bfloat16": OLIVE_BF16, "torch.float32": OLIVE_F32}
+    if str(x.dtype) not in kinds or not x.is_contiguous():
+        raise ValueError("a gradient is a contiguous bf16 or fp32 tensor")
+    return kinds[str(x.dtype)]
+
+
+def olive_grad_clip_init(grads, outs=None, stream=None) -> int:
+    """A context for a list of contiguous gradients, scaled in place, or into `outs` (None
+    entries: only counted). The caller keeps the tensors alive."""
+    outs = grads if outs is None else outs
+    if len(outs) != len(grads):
+        raise ValueError("one output for each gradient")
+    arr = (olive_grad_tensor * max(1, len(grads)))()
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        if o is not None and o.numel() != g.numel():
+            raise ValueError("an output has its gradient's size")
+        kind = _dtype_of(g)
+        arr[i] = olive_grad_tensor(_ptr(g), _ptr(o), g.numel(), kind,
+                                   kind if o is None else _dtype_of(o))
+    h = ctypes.c_void_p()
+    _check(load().olive_grad_clip_init(ctypes.byref(h), arr, len(grads), _stream(stream)),
+           "olive_grad_clip_init")
+    return h.value
+
+
+def olive_grad_clip(ctx, max_norm: float, norm=None, stream=None, check: bool = True) -> int:
+    s = load().olive_grad_clip(ctx, float(max_norm), _ptr(norm), _stream(stream))
+    if check:
+        _check(s, "olive_grad_clip")
+    return s
+
+
+def olive_grad_clip_free(ctx) -> int:
+    return load().olive_grad_clip_free(ctx)

@@ -1,0 +1,161 @@
+// The global norm over a list of gradients, and the gradients scaled to a limit.
+//
+// Two passes: the squares are summed chunk by chunk in 64 bits (a square of an fp32 value
+// neither overflows nor vanishes there, and the sum's error stays below fp32's rounding), a
+// partial sum a workgroup; every workgroup of the second pass adds the partial sums in the
+// same order and scales its chunks. Bound by memory: the values are read twice and written
+// once.
+#include "layers_internal.hpp"
+#include "olive_device.hpp"
+
+namespace olive {
+namespace {
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ double block_sum(double v) {
+    __shared__ double join[kThreads / 64];
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    if ((threadIdx.x & 63) == 0) join[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0;
+    for (int i = 0; i < kThreads / 64; ++i) v += join[i];
+    return v;
+}
+
+__device__ __forceinline__ void add_square(double &s, float x) { s = fma((double)x, (double)x, s); }
+
+__global__ __launch_bounds__(kThreads) void clip_norm_kernel(const ClipTensor *tensors,
+                                                             const ClipChunk *chunks,
+                                                             int64_t n_chunks, double *part) {
+    double s = 0.0;
+    for (int64_t c = blockIdx.x; c < n_chunks; c += gridDim.x) {
+        const ClipChunk ch = chunks[c];
+        const ClipTensor t = tensors[ch.tensor];
+        if (t.bf16_in) {
+            const uint16_t *p = (const uint16_t *)t.in + ch.start;
+            int i = 0;
+            if (((uintptr_t)p & 15) == 0) {
+                const uint4 *v = (const uint4 *)p;
+                for (int j = threadIdx.x; j < ch.n / 8; j += kThreads) {
+                    const uint4 u = v[j];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t w = ((const uint32_t *)&u)[k];
+                        add_square(s, __uint_as_float(w << 16));
+                        add_square(s, __uint_as_float(w & 0xffff0000u));
+                    }
+                }
+                i = ch.n / 8 * 8;
+            }
+            for (int j = i + threadIdx.x; j < ch.n; j += kThreads) add_square(s, bf16_bits_to_f32(p[j]));
+        } else {
+            const float *p = (const float *)t.in + ch.start;
+            int i = 0;
+            if (((uintptr_t)p & 15) == 0) {
+                const float4 *v = (const float4 *)p;
+                for (int j = threadIdx.x; j < ch.n / 4; j += kThreads) {
+                    const float4 u = v[j];
+                    add_square(s, u.x);
+                    add_square(s, u.y);
+                    add_square(s, u.z);
+                    add_square(s, u.w);
+                }
+                i = ch.n / 4 * 4;
+            }
+            for (int j = i + threadIdx.x; j < ch.n; j += kThreads) add_square(s, p[j]);
+        }
+    }
+    s = block_sum(s);
+    if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+template <typename TI>
+__device__ __forceinline__ float clip_get(const TI *p, int j) { return load_elem<TI>(p, j); }
+
+template <typename TI, typename TO>
+__device__ __forceinline__ void scale_chunk(const TI *in, TO *out, int n, float f) {
+    // 8 values a thread and step where both sides lie on 16 bytes
+    int i = 0;
+    if ((((uintptr_t)in | (uintptr_t)out) & 15) == 0) {
+        for (int j = threadIdx.x; j < n / 8; j += kThreads) {
+            float x[8];
+            if constexpr (sizeof(TI) == 2) {
+                const uint4 u = ((const uint4 *)in)[j];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t w = ((const uint32_t *)&u)[k];
+                    x[2 * k] = __uint_as_float(w << 16);
+                    x[2 * k + 1] = __uint_as_float(w & 0xffff0000u);
+                }
+            } else {
+                const float4 u = ((const float4 *)in)[2 * j], w = ((const float4 *)in)[2 * j + 1];
+                x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;
+                x[4] = w.x, x[5] = w.y, x[6] = w.z, x[7] = w.w;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] *= f;
+            if constexpr (sizeof(TO) == 2) {
+                uint4 u;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) ((uint32_t *)&u)[k] = pack_bf16x2(x[2 * k], x[2 * k + 1]);
+                ((uint4 *)out)[j] = u;
+            } else {
+                ((float4 *)out)[2 * j] = make_float4(x[0], x[1], x[2], x[3]);
+                ((float4 *)out)[2 * j + 1] = make_float4(x[4], x[5], x[6], x[7]);
+            }
+        }
+        i = n / 8 * 8;
+    }
+    for (int j = i + threadIdx.x; j < n; j += kThreads) {
+        const float x = load_elem<TI>(in, j) * f;
+        if constexpr (sizeof(TO) == 2) out[j] = (TO)(pack_bf16x2(x, x) & 0xffffu);
+        else out[j] = x;
+    }
+}
+
+// Chunks are taken from the last to the first: what the norm pass read last is still in the
+// chip's last-level cache.
+__global__ __launch_bounds__(kThreads) void clip_scale_kernel(const ClipTensor *tensors,
+                                                              const ClipChunk *chunks,
+                                                              int64_t n_chunks, const double *part,
+                                                              int parts, float max_norm,
+                                                              float *norm) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
+    const double n = sqrt(block_sum(s));
+    // 1 for a norm that is not finite: the values are left as they are
+    float f = 1.f;
+    if (n < __builtin_inf()) {
+        const double g = (double)max_norm / (n + 1e-6);
+        f = g < 1.0 ? (float)g : 1.f;
+    }
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
+    for (int64_t c = n_chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
+        const ClipChunk ch = chunks[c];
+        const ClipTensor t = tensors[ch.tensor];
+        if (!t.out || (t.out == t.in && f == 1.f)) continue;
+        if (t.bf16_in) {
+            const uint16_t *in = (const uint16_t *)t.in + ch.start;
+            if (t.bf16_out) scale_chunk(in, (uint16_t *)t.out + ch.start, ch.n, f);
+            else scale_chunk(in, (float *)t.out + ch.start, ch.n, f);
+        } else {
+            const float *in = (const float *)t.in + ch.start;
+            if (t.bf16_out) scale_chunk(in, (uint16_t *)t.out + ch.start, ch.n, f);
+            else scale_chunk(in, (float *)t.out + ch.start, ch.n, f);
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_clip(const ClipTensor *tensors, const ClipChunk *chunks, int64_t n_chunks,
+                       double *part, float max_norm, float *norm, hipStream_t st) {
+    const int grid = (int)(n_chunks < kClipBlocks ? (n_chunks > 0 ? n_chunks : 1) : kClipBlocks);
+    clip_norm_kernel<<<grid, kThreads, 0, st>>>(tensors, chunks, n_chunks, part);
+    clip_scale_kernel<<<grid, kThreads, 0, st>>>(tensors, chunks, n_chunks, part, grid, max_norm,
+                                                 norm);
+    return hipGetLastError();
+}
+
+}  // namespace olive

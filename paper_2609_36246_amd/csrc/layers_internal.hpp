@@ -1,0 +1,81 @@
+// Launchers of the layer operators (include/olive_layers.h): their argument structs and the
+// size rules that the host and the kernels share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "olive_layers.h"
+
+namespace olive {
+
+constexpr int kChipUnits = 256;      // compute units of an MI355X
+
+struct HeadsArg {                    // olive_heads with a typed use in the kernels
+    char *p;
+    int64_t st, sh;                  // elements between tokens and heads
+};
+
+// ---- norms of heads with the rotation ----------------------------------------------------
+struct QkArgs {
+    HeadsArg q, k, v, qo, ko, vo;    // backward: qo / ko hold the gradients of the outputs
+    HeadsArg gq, gk;                 // backward: gradients of q and k
+    int32_t tokens, hq, hk, hv, d, rot, layout;
+    float eps;
+    const int32_t *positions;
+    int64_t num_positions;
+    const float *cos, *sin;
+    const void *wq, *wk;
+    const int32_t *slots;
+    int64_t slot_rows;
+    float *gwq, *gwk;                // backward: weight gradients or NULL
+    float *part;                     // backward: [blocks][2][d] partial weight gradients
+};
+
+constexpr int kQkBwdBlocks = 1024;   // workgroups of the backward at most (its partial rows)
+
+hipError_t launch_qk_forward(const QkArgs &a, bool bf16, hipStream_t st);
+hipError_t launch_qk_backward(const QkArgs &a, bool bf16, hipStream_t st);
+
+// ---- gradient clipping -------------------------------------------------------------------
+struct ClipTensor {
+    const void *in;
+    void *out;
+    int64_t n;
+    int32_t bf16_in, bf16_out;
+};
+struct ClipChunk {
+    int64_t start;                   // first value of the chunk in its tensor
+    int32_t tensor;
+    int32_t n;                       // its values
+};
+constexpr int kClipChunk = 16384;    // values of a chunk
+constexpr int kClipBlocks = 2048;    // workgroups of the norm pass at most (its partial sums)
+
+hipError_t launch_clip(const ClipTensor *tensors, const ClipChunk *chunks, int64_t n_chunks,
+                       double *part, float max_norm, float *norm, hipStream_t st);
+
+// ---- attention on shared prefixes --------------------------------------------------------
+struct AttnArgs {
+    HeadsArg q, kp, vp, ks, vs, o;
+    float *lse;                      // [total_q][hq], forward: or NULL
+    HeadsArg go, gq, gkp, gvp, gks, gvs;   // backward
+    int32_t groups, seqs, hq, hk, d, max_q;
+    int64_t total_q, max_prefix, max_suffix, prefix_rows, suffix_rows;
+    const int32_t *group_seqs, *cu_q;
+    const int64_t *prefix_start;
+    const int32_t *prefix_len, *suffix_len;
+    const int64_t *suffix_start;
+    const int32_t *pages;
+    int64_t table_stride;
+    int32_t page_size;
+    float scale;
+    char *work;                      // workspace
+};
+
+int64_t attn_forward_bytes(const AttnArgs &a, bool bf16);
+int64_t attn_backward_bytes(const AttnArgs &a, bool bf16);
+hipError_t launch_attn_forward(const AttnArgs &a, bool bf16, hipStream_t st);
+hipError_t launch_attn_backward(const AttnArgs &a, bool bf16, hipStream_t st);
+
+}  // namespace olive
