@@ -14,7 +14,8 @@ LIB = os.path.join(PKG, "libolive_score.so")
 SOURCES = ["olive_abi.hip", "prep.hip", "score_simple.hip", "score_mfma.hip", "combine.hip",
            "fixup.hip", "topk.hip", "gemm_mfma.hip", "backward.hip",
            "filter.hip", "argmax.hip", "score_wide.hip",
-           "layers_abi.hip", "qk_rope.hip", "attn_generic.hip", "grad_clip.hip"]
+           "layers_abi.hip", "qk_rope.hip", "attn_generic.hip", "attn_fwd.hip",
+           "grad_clip.hip"]
 ARCH = "gfx950"
 
 

@@ -1,0 +1,637 @@
+// Attention on shared prefixes, bf16 on matrix instructions (head_dim a multiple of 8, rows on
+// 16 bytes).
+//
+// A workgroup of 4 wavefronts takes 32 WR query rows of one key head (a row is one query head
+// of one token) and a range of key tiles. The product is formed as z^T = K q^T, so that a lane
+// holds one query row's scores: the running maximum and sum are the lane's own, and the
+// exponentials, rounded to bf16, are the second operand of out^T = V^T p^T as they lie. V^T
+// comes out of LDS through the transposing read. With WR = 4 the wavefronts share every key;
+// with WR = 2 or 1 they take different keys of a tile (WK = 4 / WR of them a row) and join
+// their maxima, sums and outputs at the end: few rows are bound by the loads of the keys, and
+// all four wavefronts have to have loads in flight.
+//
+// Two ways to cut a call:
+//   own     rows of one sequence, its prefix and then its suffix in one pass; split along the
+//           keys where there are too few row tiles to fill the chip
+//   shared  (single tokens, short runs) the rows of all sequences of a group against the
+//           prefix, so that it is read once for 32 WR of them, and each sequence's rows
+//           against its suffix
+// Parts of a row meet in a second kernel through fp32 partial outputs.
+#include "attn_tile.hpp"
+
+namespace olive {
+namespace {
+
+constexpr float kRescale = 8.f;      // the running maximum may lag by 2^8 (see below)
+
+// How a call is cut: a function of the descriptor alone (the workspace goes by it).
+struct FwdPlan {
+    bool shared;
+    int wr;                          // 32-row blocks of a workgroup
+    int np, ns;                      // parts along the prefix and the suffix (own: np = 0, and
+                                     // ns along both)
+    int ptiles, stiles;              // row tiles: over all groups (a bound), of a sequence
+    int64_t p_units, s_units;        // workgroups
+    __host__ __device__ int parts() const { return np + ns; }
+    __host__ __device__ bool direct() const { return !shared && ns == 1; }
+};
+
+__host__ __device__ constexpr int tile_keys(int dp, int wr) {
+    return wr == 4 ? (dp == 256 ? 32 : 64) : wr == 2 ? 64 : 128;
+}
+inline int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+
+__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+FwdPlan make_plan(const AttnArgs &a) {
+    FwdPlan p{};
+    const int64_t g = a.hq / a.hk, dp = padded(a.d);
+    const int64_t seq_rows = a.max_q * g;
+    // rows of a group, if the groups are alike
+    const int64_t group_rows = ceil_div(a.total_q * g, a.groups);
+    p.shared = a.max_prefix > 0 && a.seqs > a.groups && seq_rows <= 64;
+    const auto pick = [&](int64_t rows) { return rows <= 32 && dp < 256 ? 1 : rows <= 64 ? 2 : 4; };
+    p.wr = pick(p.shared ? group_rows : seq_rows);
+    const int64_t kt = tile_keys((int)dp, p.wr), bm = 32 * p.wr;
+    const int64_t pk = ceil_div(a.max_prefix, kt), sk = ceil_div(a.max_suffix, kt);
+    p.stiles = (int)ceil_div(seq_rows, bm);
+    // two workgroups a compute unit; a part of at least two tiles
+    const auto split = [&](int64_t units, int64_t tiles, int64_t want) {
+        int64_t n = want / (units > 0 ? units : 1);
+        n = n < (tiles + 1) / 2 ? n : (tiles + 1) / 2;
+        return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+    };
+    if (p.shared) {
+        const int64_t likely = a.groups * ceil_div(group_rows, bm) * a.hk;
+        p.ptiles = (int)(ceil_div(a.total_q * g, bm) + a.groups);
+        p.np = split(likely, pk, 2 * kChipUnits);
+        p.ns = sk ? split((int64_t)a.seqs * p.stiles * a.hk, sk, 2 * kChipUnits) : 0;
+        p.p_units = (int64_t)p.ptiles * a.hk * p.np;
+        p.s_units = (int64_t)a.seqs * p.stiles * a.hk * p.ns;
+    } else {
+        const int64_t units = (int64_t)a.seqs * p.stiles * a.hk;
+        p.ns = split(units, pk + sk, 2 * kChipUnits);
+        p.s_units = units * p.ns;
+    }
+    return p;
+}
+
+// Key tiles [t0, t1) of part i of n.
+__device__ __forceinline__ void part_range(int tiles, int n, int i, int &t0, int &t1) {
+    t0 = (int)((int64_t)tiles * i / n);
+    t1 = (int)((int64_t)tiles * (i + 1) / n);
+}
+
+struct FwdArgs {
+    AttnArgs a;
+    FwdPlan p;
+    float *po;                       // [part][total_q hq][d]
+    float2 *pml;                     // [part][total_q hq]: maximum (log2 units), sum
+};
+
+// What one workgroup does.
+struct Work {
+    SeqView s;
+    int64_t rows;                    // query rows of the range that begins at token s.q0
+    int64_t r0;                      // first of this workgroup's
+    int kvh, part;
+    int pt;                          // prefix tiles come first
+    int t0, t1;
+};
+
+// The row tile of flat index i over the groups: groups of 64 a step, by prefix sums.
+__device__ __forceinline__ bool find_group(const AttnArgs &a, int g_heads, int bm, int64_t i, int &grp,
+                                           int64_t &tile) {
+    const int lane = threadIdx.x & 63;
+    for (int g0 = 0; g0 < a.groups; g0 += 64) {
+        const int g = g0 + lane;
+        int64_t n = 0;
+        if (g < a.groups) {
+            const int b0 = a.group_seqs[g], b1 = a.group_seqs[g + 1];
+            if (b0 >= 0 && b0 <= b1 && b1 <= a.seqs) {
+                const int64_t q0 = a.cu_q[b0], q1 = a.cu_q[b1];
+                if (q0 >= 0 && q0 <= q1 && q1 <= a.total_q) n = ceil_div((q1 - q0) * g_heads, bm);
+            }
+        }
+        int64_t sum = n;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int64_t v = __shfl_up(sum, o);
+            if (lane >= o) sum += v;
+        }
+        const uint64_t hit = __ballot(i < sum);
+        if (hit) {
+            const int l = __ffsll((unsigned long long)hit) - 1;
+            grp = __builtin_amdgcn_readfirstlane(g0 + l);
+            tile = i - (__shfl(sum, l) - __shfl(n, l));
+            return true;
+        }
+        i -= __shfl(sum, 63);
+    }
+    return false;
+}
+
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)v >> 32));
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+template <int DP, int WR>
+__device__ __forceinline__ bool find_work(const FwdArgs &f, int64_t u, Work &w) {
+    const AttnArgs &a = f.a;
+    constexpr int BM = 32 * WR, KT = tile_keys(DP, WR);
+    const int g = a.hq / a.hk;
+    if (u < f.p.p_units) {
+        const int64_t i = u % f.p.ptiles;
+        int v = (int)(u / f.p.ptiles);
+        w.kvh = v % a.hk;
+        w.part = v / a.hk;
+        int grp;
+        int64_t tile;
+        if (!find_group(a, g, BM, i, grp, tile) || !prefix_ok(a, grp)) return false;
+        w.s = SeqView{};
+        w.s.q0 = a.cu_q[a.group_seqs[grp]];
+        w.rows = (a.cu_q[a.group_seqs[grp + 1]] - w.s.q0) * g;
+        w.r0 = uniform64(tile) * BM;
+        w.s.plen = a.prefix_len[grp];
+        w.s.pstart = a.prefix_start[grp];
+        w.pt = (int)ceil_div(w.s.plen, KT);
+        part_range(w.pt, f.p.np, w.part, w.t0, w.t1);
+        return w.t0 < w.t1;
+    }
+    u -= f.p.p_units;
+    // the last row tiles of a sequence, which see the most keys, come first
+    const int rt = f.p.stiles - 1 - (int)(u % f.p.stiles);
+    u /= f.p.stiles;
+    w.kvh = (int)(u % a.hk);
+    u /= a.hk;
+    w.part = (int)(u % f.p.ns);
+    w.s = load_seq(a, (int)(u / f.p.ns));
+    w.rows = (int64_t)w.s.n * g;
+    w.r0 = (int64_t)rt * BM;
+    if (w.s.skip || w.r0 >= w.rows) return false;
+    if (w.s.bad) {
+        w.t0 = w.t1 = w.pt = 0;
+        return f.p.direct() && rt == 0;      // else the second kernel writes the NaN
+    }
+    const int last = (int)((min(w.rows, w.r0 + BM) - 1) / g);
+    const int st = (int)ceil_div(suffix_seen(w.s, last), KT);
+    w.pt = f.p.shared ? 0 : (int)ceil_div(w.s.plen, KT);
+    part_range(w.pt + st, f.p.ns, w.part, w.t0, w.t1);
+    w.part += f.p.np;
+    return w.t0 < w.t1 || f.p.direct();
+}
+
+// Keys and values on their way into LDS. A wavefront loads KT / 4 rows of each of a tile; rows
+// past the end are copies of the last one (their scores are masked).
+template <int DP, int KT>
+struct Loader {
+    using R = TileRow<DP>;
+    static constexpr int N = KT / 4 / R::PER_DMA;    // loads of a wavefront, keys and values each
+    static constexpr int BYTES = KT * R::BYTES;      // of the tile's keys; the values follow
+    // the segment being read, prefix or suffix (wave-uniform)
+    const char *k, *v;                               // its first key's head
+    int64_t kst, vst;                                // bytes between keys
+    int len, tile0;                                  // its keys, its first tile's index
+    bool paged;
+    int shift;                                       // log2 of the page size, or -1
+    int32_t page[N];                                 // table entries of the next tile's rows
+    bool bad = false;
+
+    __device__ __forceinline__ void open(const AttnArgs &a, const Work &w, bool pre) {
+        const HeadsArg &kh = pre ? a.kp : a.ks, &vh = pre ? a.vp : a.vs;
+        const int64_t at = pre ? w.s.pstart : w.s.sstart;
+        kst = kh.st * 2;
+        vst = vh.st * 2;
+        k = kh.p + (int64_t)w.kvh * kh.sh * 2 + at * kst;
+        v = vh.p + (int64_t)w.kvh * vh.sh * 2 + at * vst;
+        len = pre ? w.s.plen : w.s.slen;
+        tile0 = pre ? 0 : w.pt;
+        paged = !pre && w.s.pages;
+        shift = (a.page_size & (a.page_size - 1)) == 0 ? 31 - __clz(a.page_size | 1) : -1;
+    }
+    static __device__ __forceinline__ int row(int n) {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        return wave * (KT / 4) + n * R::PER_DMA + lane / R::CHUNKS;
+    }
+    __device__ __forceinline__ int page_of(const AttnArgs &a, int j) const {
+        return shift >= 0 ? j >> shift : j / a.page_size;
+    }
+    // Asks for the table entries of tile t; they are there at the next barrier.
+    __device__ __forceinline__ void look_up(const AttnArgs &a, const Work &w, int t) {
+        if (!w.s.pages || t < w.pt || t >= w.t1) return;
+        const int j0 = (t - w.pt) * KT;
+#pragma unroll
+        for (int n = 0; n < N; ++n) page[n] = w.s.pages[page_of(a, min(j0 + row(n), w.s.slen - 1))];
+    }
+    __device__ __forceinline__ void issue(const AttnArgs &a, const Work &w, int t, uint32_t lds) {
+        if (t == w.pt && t != w.t0) open(a, w, false);
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int nch = a.d / 8;
+        const int j0 = (t - tile0) * KT, last = len - 1 - j0;
+        const char *kt = k + j0 * kst, *vt = v + j0 * vst;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int full = row(n), r = min(full, last);
+            const int ch = (lane & (R::CHUNKS - 1)) ^ R::swz(full), c = ch * 16;
+            if (ch >= nch) continue;      // the slots past head_dim keep their zeros
+            const uint32_t to = lds + (wave * (KT / 4) + n * R::PER_DMA) * R::BYTES;
+            if (paged) {
+                const int j = j0 + r;
+                int64_t at = (int64_t)page[n] * a.page_size;
+                if (at < 0 || at > a.suffix_rows - a.page_size) {
+                    bad = true;
+                    at = 0;
+                } else {
+                    at += j - page_of(a, j) * a.page_size;
+                }
+                dma16(k + at * kst + c, to);
+                dma16(v + at * vst + c, to + BYTES);
+            } else {
+                // the launcher takes strides for which a tile's offsets fit 32 bits
+                dma16_sv<0>(kt, (uint32_t)r * (uint32_t)kst + c, to);
+                dma16_sv<0>(vt, (uint32_t)r * (uint32_t)vst + c, to + BYTES);
+            }
+        }
+    }
+};
+
+// acc + V^T p^T where some value is not finite and some row does not see its key: that row's
+// weight of it is 0, and the product would make a NaN of it. Rows that see such a value take
+// the product, the others the product without it. `seen` holds 1 where p's key is seen, and
+// `there` all bits where the key is one at all (past the end lie copies of the last one).
+__device__ __forceinline__ floatx16 mfma_special(bf16x8 v, bf16x8 p, uintx4 seen, uintx4 there, floatx16 acc) {
+    const uintx4 u = __builtin_bit_cast(uintx4, v) & there;
+    uintx4 fin, is;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const bool lo = (u[j] & 0x7f80u) == 0x7f80u, hi = (u[j] & 0x7f800000u) == 0x7f800000u;
+        fin[j] = u[j] & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
+        is[j] = (lo ? 0x3f80u : 0u) | (hi ? 0x3f800000u : 0u);
+    }
+    const floatx16 count = mfma(__builtin_bit_cast(bf16x8, is), __builtin_bit_cast(bf16x8, seen), zero16());
+    const floatx16 all = mfma(__builtin_bit_cast(bf16x8, u), p, acc);
+    floatx16 r = mfma(__builtin_bit_cast(bf16x8, fin), p, acc);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = count[i] > 0.f ? all[i] : r[i];
+    return r;
+}
+
+// One pass along the key tiles [w.t0, w.t1): out^T (unscaled), the maximum in log2 units and
+// this half's share of the sum, of the query row `lane % 32` of a wavefront. SPECIAL: with
+// mfma_special where rows see different keys.
+template <int DP, int WR, bool SPECIAL>
+__device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint32_t lds, int wk, int seen,
+                                         int least, const bf16x8 (&q)[DP / 16], floatx16 (&acc)[DP / 32],
+                                         float &m, float &l) {
+    constexpr int WK = 4 / WR, KT = tile_keys(DP, WR), NB = KT / 32 / WK, DB = DP / 32, KS = DP / 16;
+    using L = Loader<DP, KT>;
+    const int lane = threadIdx.x & 63;
+    const float c = a.scale * kLog2e;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) acc[d] = zero16();
+    m = kNegInf;
+    l = 0.f;
+    L load;
+    if (w.t0 < w.t1) {
+        load.open(a, w, w.t0 < w.pt);
+        load.look_up(a, w, w.t0);
+        load.issue(a, w, w.t0, lds);
+        load.look_up(a, w, w.t0 + 1);
+    }
+    for (int kt = w.t0; kt < w.t1; ++kt) {
+        const uint32_t kb = lds + ((kt - w.t0) & 1) * 2 * L::BYTES + wk * NB * 32 * TileRow<DP>::BYTES;
+        const uint32_t vb = kb + L::BYTES;
+        tile_barrier();
+        if (kt + 1 < w.t1) {
+            load.issue(a, w, kt + 1, lds + ((kt + 1 - w.t0) & 1) * 2 * L::BYTES);
+            load.look_up(a, w, kt + 2);
+        }
+        floatx16 z[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            z[b] = zero16();
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+                z[b] = mfma(read_row<DP>(kb + b * 32 * TileRow<DP>::BYTES, lane, s), q[s], z[b]);
+        }
+        // masks: the end of the prefix, and the suffix keys that a row does not see
+        const bool pre = kt < w.pt;
+        const int j0 = (pre ? kt : kt - w.pt) * KT + wk * NB * 32;
+        const int limit = pre ? w.s.plen : seen;
+        const bool masked = j0 + NB * 32 > (pre ? w.s.plen : least);
+        if (masked) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    z[b][i] = j0 + 32 * b + acc_row(i, lane) < limit ? z[b][i] : kNegInf;
+        }
+        float top = kNegInf;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, z[b][i]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * c;
+        // The maximum that the weights refer to follows the running one only when it falls
+        // more than 2^8 behind: fp32 sums have the room, and the outputs are seldom rescaled.
+        if (__any(top > m + kRescale)) {
+            const float m2 = fmaxf(m, top);
+            const float r = m2 == m ? 1.f : fast_exp2(m - m2);
+            m = m2;
+            l *= r;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) acc[d] *= r;
+        }
+        const float m0 = m == kNegInf ? 0.f : m;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                z[b][i] = fast_exp2(fmaf(z[b][i], c, -m0));
+                sum += z[b][i];
+            }
+            l += sum;
+#pragma unroll
+            for (int mm = 0; mm < 2; ++mm) {
+                const bf16x8 p = pack8(z[b], mm);
+                const uint32_t base = vb + (32 * b + 16 * mm) * TileRow<DP>::BYTES;
+                uintx4 on, there;
+#pragma unroll
+                for (int i = 0; SPECIAL && i < 4; ++i) {
+                    const int j = j0 + 32 * b + acc_row(8 * mm + 2 * i, lane), end = pre ? w.s.plen : w.s.slen;
+                    on[i] = (j < limit ? 0x3f80u : 0u) | (j + 1 < limit ? 0x3f800000u : 0u);
+                    there[i] = (j < end ? 0xffffu : 0u) | (j + 1 < end ? 0xffff0000u : 0u);
+                }
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const bf16x8 v = read_col<DP>(base, lane, d);
+                    acc[d] = SPECIAL ? mfma_special(v, p, on, there, acc[d])
+                                     : mfma(v, p, acc[d]);
+                }
+            }
+        }
+    }
+    return load.bad;
+}
+
+template <int DP, int WR>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArgs f, int64_t per_xcd) {
+    constexpr int WK = 4 / WR, KT = tile_keys(DP, WR), DB = DP / 32, KS = DP / 16;
+    extern __shared__ __attribute__((aligned(1024))) char lds_mem[];
+    const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
+    const AttnArgs &a = f.a;
+    // consecutive workgroups go to the 8 dies in turn: each die takes a run of units, whose
+    // keys then meet in its cache
+    const int64_t u = (int64_t)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if (u >= f.p.p_units + f.p.s_units) return;
+    Work w;
+    if (!find_work<DP, WR>(f, u, w)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wr = wave / WK, wk = wave % WK, h = lane >> 5;
+    const int g = a.hq / a.hk, nch = a.d >> 3;
+    if (nch < DP / 8) {
+        for (int i = threadIdx.x; i < 2 * 2 * KT * DP / 8; i += 256)
+            ((uint4 *)lds_mem)[i] = make_uint4(0u, 0u, 0u, 0u);
+        __syncthreads();
+    }
+
+    // this lane's query row
+    const int64_t row = w.r0 + 32 * wr + (lane & 31);
+    const bool live = row < w.rows;
+    const int tok = (int)(min(row, w.rows - 1) / g);
+    const int head = w.kvh * g + (int)(min(row, w.rows - 1) - (int64_t)tok * g);
+    const int64_t t = w.s.q0 + tok;
+    bf16x8 q[KS];
+    {
+        const uint16_t *p = head_row(a.q, t, head);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = load_chunk(p, 2 * s + h, nch);
+    }
+    // suffix keys it sees, and the fewest that a row of this wavefront sees
+    const int seen = suffix_seen(w.s, tok);
+    const int least = suffix_seen(w.s, (int)(min(w.r0 + 32 * wr, w.rows - 1) / g));
+    floatx16 acc[DB];
+    float m, l;
+    bool off_table = key_loop<DP, WR, false>(a, w, lds, wk, seen, least, q, acc, m, l);
+    {
+        // A value that is not finite leaves a NaN also in rows that do not see its key: such
+        // a result is formed again with these rows' weights of it left out.
+        float s = 0.f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s = fmaf(acc[d][i], 0.f, s);
+        if (__syncthreads_or(!(s == 0.f)))
+            off_table = key_loop<DP, WR, true>(a, w, lds, wk, seen, least, q, acc, m, l);
+    }
+    l += __shfl_xor(l, 32);
+
+    const int64_t orow = t * a.hq + head;
+    const bool bad = __syncthreads_or(off_table) || w.s.bad;
+    // the registers (4 consecutive elements of the head each) that this wavefront writes
+    int g0 = 0;
+    if (WK > 1) {
+        // the row's wavefronts leave their parts in LDS and take a share of the elements each
+        float2 *ml = (float2 *)(lds_mem + 4 * DB * 4096);
+        float4 *po = (float4 *)lds_mem;
+        if (h == 0) ml[wave * 32 + lane] = make_float2(m, l);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                po[(wave * DB * 4 + d * 4 + j) * 64 + lane] =
+                    make_float4(acc[d][4 * j], acc[d][4 * j + 1], acc[d][4 * j + 2], acc[d][4 * j + 3]);
+        __syncthreads();
+        float pm[WK], pl[WK], top = kNegInf;
+#pragma unroll
+        for (int k = 0; k < WK; ++k) {
+            const float2 v = ml[(wr * WK + k) * 32 + (lane & 31)];
+            pm[k] = v.x;
+            pl[k] = v.y;
+            top = fmaxf(top, v.x);
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < WK; ++k) {
+            pm[k] = pm[k] == top ? 1.f : fast_exp2(pm[k] - top);
+            sum += pl[k] * pm[k];
+        }
+        m = top;
+        l = sum;
+        g0 = wk * (DB * 4 / WK);
+#pragma unroll
+        for (int i = 0; i < DB * 4 / WK; ++i) {
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < WK; ++k) {
+                const float4 v = po[((wr * WK + k) * DB * 4 + g0 + i) * 64 + lane];
+                o.x = fmaf(v.x, pm[k], o.x);
+                o.y = fmaf(v.y, pm[k], o.y);
+                o.z = fmaf(v.z, pm[k], o.z);
+                o.w = fmaf(v.w, pm[k], o.w);
+            }
+            acc[i / 4][4 * (i % 4)] = o.x;
+            acc[i / 4][4 * (i % 4) + 1] = o.y;
+            acc[i / 4][4 * (i % 4) + 2] = o.z;
+            acc[i / 4][4 * (i % 4) + 3] = o.w;
+        }
+    }
+    if (bad) l = __builtin_nanf("");
+    if (f.p.direct() && w.s.bad) {
+        // every row of the sequence, also those past max_q
+        for (int64_t i = threadIdx.x; i < w.rows * a.d; i += 256) {
+            const int64_t r = i / a.d, k = r / g;
+            ((uint16_t *)a.o.p)[(w.s.q0 + k) * a.o.st + (w.kvh * g + (r - k * g)) * a.o.sh + (i - r * a.d)] =
+                0x7fc0;
+        }
+        if (a.lse)
+            for (int64_t r = threadIdx.x; r < w.rows; r += 256)
+                a.lse[(w.s.q0 + r / g) * a.hq + w.kvh * g + r % g] = __builtin_nanf("");
+        return;
+    }
+    if (!live) return;
+    const bool first = wk == 0 && h == 0;
+    if (f.p.direct()) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        uint16_t *o = (uint16_t *)head_row(a.o, t, head);
+#pragma unroll
+        for (int i = 0; i < DB * 4 / WK; ++i) {
+            const int e = 8 * (g0 + i) + 4 * h;
+            if (e < a.d) {
+                uint2 v;
+                v.x = pack_bf16x2(acc[i / 4][4 * (i % 4)] * inv, acc[i / 4][4 * (i % 4) + 1] * inv);
+                v.y = pack_bf16x2(acc[i / 4][4 * (i % 4) + 2] * inv, acc[i / 4][4 * (i % 4) + 3] * inv);
+                *(uint2 *)(o + e) = v;
+            }
+        }
+        if (a.lse && first) a.lse[orow] = l == 0.f ? kNegInf : (m + fast_log2(l)) * kLn2;
+        return;
+    }
+    const int64_t slot = (int64_t)w.part * a.total_q * a.hq + orow;
+#pragma unroll
+    for (int i = 0; i < DB * 4 / WK; ++i) {
+        const int e = 8 * (g0 + i) + 4 * h;
+        if (e < a.d)
+            *(float4 *)(f.po + slot * a.d + e) =
+                make_float4(acc[i / 4][4 * (i % 4)], acc[i / 4][4 * (i % 4) + 1], acc[i / 4][4 * (i % 4) + 2],
+                            acc[i / 4][4 * (i % 4) + 3]);
+    }
+    if (first) f.pml[slot] = make_float2(m, l);
+}
+
+// Joins the parts of each row: a wavefront a row, 4 elements a lane and step.
+__global__ __launch_bounds__(256) void attn_join_kernel(FwdArgs f, int kt) {
+    const AttnArgs &a = f.a;
+    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (r >= a.total_q * a.hq) return;
+    const int lane = threadIdx.x & 63, g = a.hq / a.hk;
+    const int64_t t = r / a.hq;
+    const int head = (int)(r - t * a.hq);
+    const SeqView s = load_seq(a, seq_of(a, t));
+    if (s.skip || t < s.q0 || t >= s.q0 + s.n) return;
+    // the parts that have tiles: each begins where the one before ends
+    const int pt = (int)ceil_div(s.plen, kt);
+    const int tok = (int)(t - s.q0), bm = 32 * f.p.wr;
+    const int64_t rows = (int64_t)s.n * g, rt = ((int64_t)tok * g + head % g) / bm;
+    const int last = (int)((min(rows, (rt + 1) * bm) - 1) / g);
+    const int st = (int)ceil_div(suffix_seen(s, last), kt);
+    const auto has = [&](int i) {
+        int t0, t1;
+        if (f.p.shared && i < f.p.np) part_range(pt, f.p.np, i, t0, t1);
+        else part_range(f.p.shared ? st : pt + st, f.p.ns, i - f.p.np, t0, t1);
+        return t0 < t1;
+    };
+    const int64_t step = a.total_q * a.hq;
+    float top = kNegInf, sum = 0.f;
+    for (int i = lane; i < f.p.parts(); i += 64)
+        if (has(i)) top = fmaxf(top, f.pml[i * step + r].x);
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    for (int i = lane; i < f.p.parts(); i += 64)
+        if (has(i)) {
+            const float2 v = f.pml[i * step + r];
+            sum += v.y * (v.x == top ? 1.f : fast_exp2(v.x - top));
+        }
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if (s.bad) sum = __builtin_nanf("");
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    for (int e = lane * 4; e < a.d; e += 256) {
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < f.p.parts(); ++i) {
+            if (!has(i)) continue;
+            const float x = f.pml[i * step + r].x;
+            const float w = x == top ? 1.f : fast_exp2(x - top);
+            const float4 v = *(const float4 *)(f.po + (i * step + r) * a.d + e);
+            o.x = fmaf(v.x, w, o.x);
+            o.y = fmaf(v.y, w, o.y);
+            o.z = fmaf(v.z, w, o.z);
+            o.w = fmaf(v.w, w, o.w);
+        }
+        uint2 v;
+        v.x = pack_bf16x2(o.x * inv, o.y * inv);
+        v.y = pack_bf16x2(o.z * inv, o.w * inv);
+        *(uint2 *)((uint16_t *)head_row(a.o, t, head) + e) = v;
+    }
+    if (a.lse && lane == 0) a.lse[r] = sum == 0.f ? kNegInf : (top + fast_log2(sum)) * kLn2;
+}
+
+template <int DP, int WR>
+hipError_t go(const FwdArgs &f, hipStream_t st) {
+    constexpr int KT = tile_keys(DP, WR);
+    constexpr int stages = 2 * 2 * KT * DP * 2, join = WR < 4 ? 4 * (DP / 32) * 4096 + 1024 : 0;
+    const int64_t units = f.p.p_units + f.p.s_units, per = ceil_div(units, 8);
+    attn_fwd_kernel<DP, WR><<<(unsigned)(per * 8), 256, stages > join ? stages : join, st>>>(f, per);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && !f.p.direct()) {
+        attn_join_kernel<<<(unsigned)ceil_div(f.a.total_q * f.a.hq, 4), 256, 0, st>>>(f, KT);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+// Rows on 16 bytes, and the offsets of 128 of them in 32 bits.
+bool rows_on_16(const HeadsArg &h) {
+    return !h.p || ((((uintptr_t)h.p | (uint64_t)(h.st * 2) | (uint64_t)(h.sh * 2)) & 15) == 0 &&
+                    h.st >= 0 && h.st < (1 << 23));
+}
+
+}  // namespace
+
+bool attn_mfma_sizes(const AttnArgs &a, bool bf16) {
+    return bf16 && a.d % 8 == 0 && a.scale > 0.f;
+}
+bool attn_mfma_applies(const AttnArgs &a, bool bf16) {
+    if (!attn_mfma_sizes(a, bf16)) return false;
+    for (const HeadsArg *h : {&a.q, &a.kp, &a.vp, &a.ks, &a.vs, &a.o, &a.go, &a.gq, &a.gkp, &a.gvp, &a.gks,
+                              &a.gvs})
+        if (!rows_on_16(*h)) return false;
+    return true;
+}
+
+int64_t attn_forward_bytes(const AttnArgs &a, bool bf16) {
+    if (!attn_mfma_sizes(a, bf16)) return 0;
+    const FwdPlan p = make_plan(a);
+    if (p.direct()) return 0;
+    return (int64_t)p.parts() * a.total_q * a.hq * (a.d + 2) * (int64_t)sizeof(float);
+}
+
+hipError_t launch_attn_forward(const AttnArgs &a, bool bf16, hipStream_t st) {
+    if (!attn_mfma_applies(a, bf16)) return launch_attn_generic(a, bf16, st);
+    FwdArgs f{a, make_plan(a), nullptr, nullptr};
+    const int64_t rows = (int64_t)f.p.parts() * a.total_q * a.hq;
+    f.po = (float *)a.work;
+    f.pml = (float2 *)(f.po + rows * a.d);
+    switch (padded(a.d) + f.p.wr) {
+        case 64 + 1: return go<64, 1>(f, st);
+        case 64 + 2: return go<64, 2>(f, st);
+        case 64 + 4: return go<64, 4>(f, st);
+        case 128 + 1: return go<128, 1>(f, st);
+        case 128 + 2: return go<128, 2>(f, st);
+        case 128 + 4: return go<128, 4>(f, st);
+        case 256 + 2: return go<256, 2>(f, st);
+        default: return go<256, 4>(f, st);
+    }
+}
+
+}  // namespace olive

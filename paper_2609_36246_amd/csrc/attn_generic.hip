@@ -337,10 +337,9 @@ hipError_t backward(const AttnArgs &a, hipStream_t st) {
 
 }  // namespace
 
-int64_t attn_forward_bytes(const AttnArgs &, bool) { return 0; }
 int64_t attn_backward_bytes(const AttnArgs &a, bool) { return a.total_q * a.hq * (int64_t)sizeof(float); }
 
-hipError_t launch_attn_forward(const AttnArgs &a, bool bf16, hipStream_t st) {
+hipError_t launch_attn_generic(const AttnArgs &a, bool bf16, hipStream_t st) {
     return bf16 ? forward<uint16_t>(a, st) : forward<float>(a, st);
 }
 hipError_t launch_attn_backward(const AttnArgs &a, bool bf16, hipStream_t st) {

@@ -1,0 +1,97 @@
+// Pieces of the bf16 attention kernels on matrix instructions: the LDS tile of keys or query
+// rows with its swizzle, the asynchronous loads into it, and the operand reads out of it.
+//
+// A tile row holds one head of one token: DP elements (head_dim rounded up to 64, 128 or
+// 256) in 16-byte chunks. Chunk c of row r lies in slot c ^ swz(r). The two operand reads
+// are then free of bank conflicts: ds_read_b128 of one chunk of 16 consecutive rows, and
+// the transposing ds_read_b64_tr_b16 of 4 consecutive rows x 4 consecutive chunks.
+#pragma once
+
+#include "attn_seq.hpp"
+#include "mfma_pipe.hpp"
+#include "olive_device.hpp"
+
+namespace olive {
+
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef short shortx8 __attribute__((ext_vector_type(8)));
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+
+#define OLIVE_LDS(T, addr) (*(__attribute__((address_space(3))) T *)(uintptr_t)(uint32_t)(addr))
+
+template <int DP>
+struct TileRow {
+    static constexpr int CHUNKS = DP / 8;            // 16-byte chunks of a row
+    static constexpr int BYTES = DP * 2;
+    static constexpr int PER_DMA = 1024 / BYTES;     // rows of a wavefront's 1-KiB load
+    static __device__ __forceinline__ int swz(int r) {
+        return DP == 64 ? ((((r >> 1) & 1) << 2) | ((r >> 2) & 3))
+                        : (((r & 3) << 2) | ((r >> 2) & 3));
+    }
+};
+
+// Waits for this wavefront's loads into LDS, then for the workgroup's.
+__device__ __forceinline__ void tile_barrier() {
+    compiler_fence();
+    __builtin_amdgcn_s_waitcnt(vmcnt_lgkm0_imm(0));
+    __builtin_amdgcn_s_barrier();
+    compiler_fence();
+}
+
+// First operand (rows x K): row `r0 + lane % 32`, chunk 2 step + lane / 32.
+template <int DP>
+__device__ __forceinline__ uint32_t row_addr(int lane) {
+    const int r = lane & 31;
+    return (uint32_t)(r * TileRow<DP>::BYTES);
+}
+template <int DP>
+__device__ __forceinline__ bf16x8 read_row(uint32_t base, int lane, int step) {
+    const int r = lane & 31, c = 2 * step + (lane >> 5);
+    return OLIVE_LDS(bf16x8, base + r * TileRow<DP>::BYTES + ((c ^ TileRow<DP>::swz(r)) << 4));
+}
+
+// First operand transposed (elements x rows): lane % 32 is the element 32 db + lane % 32, the
+// 8 values are rows 4 (lane / 32) + 0..3 and 8 more: the rows whose results a lane of the same
+// half holds in registers 0..7 of a 32 x 32 product. `base` is row 16 m of the tile.
+template <int DP>
+__device__ __forceinline__ bf16x8 read_col(uint32_t base, int lane, int db) {
+    const int h = lane >> 5, r4 = (lane & 15) >> 2;
+    const int c = 4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    const int r0 = 4 * h + r4, r1 = r0 + 8;
+    const uint32_t a0 = base + r0 * TileRow<DP>::BYTES + ((c ^ TileRow<DP>::swz(r0)) << 4) + (lane & 1) * 8;
+    const uint32_t a1 = base + r1 * TileRow<DP>::BYTES + ((c ^ TileRow<DP>::swz(r1)) << 4) + (lane & 1) * 8;
+    const shortx4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(&OLIVE_LDS(shortx4, a0));
+    const shortx4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(&OLIVE_LDS(shortx4, a1));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Registers 8 m .. 8 m + 7 of a 32 x 32 product as the second operand of the next one.
+__device__ __forceinline__ bf16x8 pack8(const floatx16 &s, int m) {
+    uintx4 u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = pack_bf16x2(s[8 * m + 2 * j], s[8 * m + 2 * j + 1]);
+    return __builtin_bit_cast(bf16x8, u);
+}
+
+__device__ __forceinline__ floatx16 mfma(bf16x8 a, bf16x8 b, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx16 zero16() { return (floatx16)(0.f); }
+
+// Row of a 32 x 32 product that register i of a lane holds.
+__device__ __forceinline__ int acc_row(int i, int lane) { return 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3); }
+
+// A query row (one head of one token): rows are token major, the heads of a key head's group
+// within.
+__device__ __forceinline__ const uint16_t *head_row(const HeadsArg &h, int64_t t, int64_t head) {
+    return (const uint16_t *)h.p + t * h.st + head * h.sh;
+}
+
+// The same 8-element chunks of a row as read_row gives, from memory (zeros past d).
+__device__ __forceinline__ bf16x8 load_chunk(const uint16_t *row, int c, int nch) {
+    uintx4 u = {0u, 0u, 0u, 0u};
+    if (c < nch) u = *(const uintx4 *)(row + 8 * c);
+    return __builtin_bit_cast(bf16x8, u);
+}
+
+}  // namespace olive
