@@ -14,7 +14,7 @@ LIB = os.path.join(PKG, "libolive_score.so")
 SOURCES = ["olive_abi.hip", "prep.hip", "score_simple.hip", "score_mfma.hip", "combine.hip",
            "fixup.hip", "topk.hip", "gemm_mfma.hip", "backward.hip",
            "filter.hip", "argmax.hip", "score_wide.hip",
-           "layers_abi.hip", "qk_rope.hip", "attn_generic.hip", "attn_fwd.hip",
+           "layers_abi.hip", "qk_rope.hip", "attn_generic.hip", "attn_fwd.hip", "attn_bwd.hip",
            "grad_clip.hip"]
 ARCH = "gfx950"
 

@@ -1,0 +1,493 @@
+// Backward of the attention on shared prefixes, bf16 on matrix instructions (head_dim a
+// multiple of 8 up to 128, rows on 16 bytes).
+//
+//   p = exp(scale q k - lse),   dp = do v^T,   ds = p (dp - delta),   delta = sum of do * out
+//   dq = scale ds K,   dk = scale ds^T q,   dv = p^T do
+//
+// Two passes that each form p and ds again, so that every gradient is summed by one workgroup
+// in a fixed order (7 products for the 5 of a single pass with atomic additions):
+//   dq   32 query rows a wavefront; the keys and values pass through LDS. The products lie as
+//        keys x rows, so a lane holds one row and ds^T is the next product's operand as it is.
+//   dkv  32 keys a wavefront, held with their values in registers; the query rows and their
+//        output gradients pass through LDS. The products lie as rows x keys, a lane holds one
+//        key, and p and ds are the operands of dv^T = do^T p and dk^T = q^T ds as they are.
+// The transposed operands come out of LDS through the transposing read. p and ds are rounded
+// to bf16 as operands; all sums are fp32. A prefix's keys meet the rows of all its sequences;
+// where there are too few key tiles to fill the chip the rows are cut into parts, whose fp32
+// sums a last kernel adds in order.
+#include "attn_tile.hpp"
+
+namespace olive {
+namespace {
+
+constexpr int DQ_KEYS = 64;          // keys of a tile of the dq pass
+constexpr int KEYS = 128;            // keys of a workgroup of the dkv pass
+constexpr int ROWS = 32;             // query rows of a tile of the dkv pass
+
+struct BwdPlan {
+    int qtiles;                      // tiles of 128 rows of a sequence
+    int ptiles, stiles;              // tiles of KEYS keys of a prefix, of a suffix
+    int np, ns;                      // parts of the rows
+    int64_t q_units, p_units, s_units;   // workgroups of the dq pass, of the dkv pass
+};
+
+BwdPlan make_plan(const AttnArgs &a) {
+    BwdPlan p{};
+    const int64_t g = a.hq / a.hk, seq_rows = a.max_q * g;
+    p.qtiles = (int)ceil_div(seq_rows, 128);
+    p.q_units = (int64_t)a.seqs * p.qtiles * a.hk;
+    p.ptiles = (int)ceil_div(a.max_prefix, KEYS);
+    p.stiles = (int)ceil_div(a.max_suffix, KEYS);
+    const int64_t pu = (int64_t)a.groups * p.ptiles * a.hk, su = (int64_t)a.seqs * p.stiles * a.hk;
+    // two workgroups a compute unit; a part of at least four row tiles
+    const auto split = [&](int64_t units, int64_t rows) {
+        const int64_t most = ceil_div(rows, 4 * ROWS);
+        int64_t n = units > 0 ? 2 * kChipUnits / units : 1;
+        n = n < most ? n : most;
+        return (int)(n < 1 ? 1 : n);
+    };
+    p.np = split(pu, ceil_div(a.total_q * g, a.groups));
+    p.ns = split(pu * p.np + su, seq_rows);
+    p.p_units = pu * p.np;
+    p.s_units = su * p.ns;
+    return p;
+}
+
+struct BwdArgs {
+    AttnArgs a;
+    BwdPlan p;
+    float2 *stats;                   // [hk][total_q][g]: lse in log2 units (+inf where -inf), delta
+    float *part;                     // fp32 parts: prefix tiles, then suffix tiles
+};
+
+// lse and delta of a row: DP / 8 lanes a row.
+template <int DP>
+__global__ __launch_bounds__(256) void attn_stats_kernel(BwdArgs f) {
+    const AttnArgs &a = f.a;
+    constexpr int LPR = DP / 8;
+    const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPR;
+    const int c = threadIdx.x % LPR, nch = a.d / 8, g = a.hq / a.hk;
+    if (r >= a.total_q * a.hq) return;
+    const int64_t t = r / a.hq;
+    const int head = (int)(r - t * a.hq);
+    const uintx4 x = __builtin_bit_cast(uintx4, load_chunk(head_row(a.o, t, head), c, nch));
+    const uintx4 y = __builtin_bit_cast(uintx4, load_chunk(head_row(a.go, t, head), c, nch));
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        s = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), s);
+        s = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), s);
+    }
+#pragma unroll
+    for (int o = LPR / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    if (c == 0) {
+        const float lse = a.lse[r];
+        f.stats[((int64_t)(head / g) * a.total_q + t) * g + head % g] =
+            make_float2(lse == kNegInf ? __builtin_inff() : lse * kLog2e, s);
+    }
+}
+
+template <int DP>
+__global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f, int64_t per_xcd) {
+    constexpr int KT = DQ_KEYS, DB = DP / 32, KS = DP / 16;
+    using L = Loader<DP, KT>;
+    extern __shared__ __attribute__((aligned(1024))) char lds_mem[];
+    const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
+    const AttnArgs &a = f.a;
+    int64_t u = (int64_t)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if (u >= f.p.q_units) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = lane >> 5, g = a.hq / a.hk, nch = a.d >> 3;
+    // the last row tiles of a sequence, which see the most keys, come first
+    const int rt = f.p.qtiles - 1 - (int)(u % f.p.qtiles);
+    u /= f.p.qtiles;
+    Work w;
+    w.s = load_seq(a, (int)(u % a.seqs));
+    w.kvh = (int)(u / a.seqs);
+    w.part = 0;
+    w.rows = (int64_t)w.s.n * g;
+    w.r0 = (int64_t)rt * 128;
+    if (w.s.skip || w.r0 >= w.rows) return;
+    if (w.s.bad) {
+        for (int64_t i = threadIdx.x; rt == 0 && i < w.rows * a.d; i += 256) {
+            const int64_t r = i / a.d, k = r / g;
+            ((uint16_t *)a.gq.p)[(w.s.q0 + k) * a.gq.st + (w.kvh * g + (r - k * g)) * a.gq.sh + (i - r * a.d)] =
+                0x7fc0;
+        }
+        return;
+    }
+    w.pt = (int)ceil_div(w.s.plen, KT);
+    w.t0 = 0;
+    w.t1 = w.pt + (int)ceil_div(suffix_seen(w.s, (int)((min(w.rows, w.r0 + 128) - 1) / g)), KT);
+    if (nch < DP / 8) {
+        for (int i = threadIdx.x; i < 2 * 2 * KT * DP / 8; i += 256)
+            ((uint4 *)lds_mem)[i] = make_uint4(0u, 0u, 0u, 0u);
+        __syncthreads();
+    }
+    const int64_t row = w.r0 + 32 * wave + (lane & 31), crow = min(row, w.rows - 1);
+    const int tok = (int)(crow / g), head = w.kvh * g + (int)(crow - (int64_t)tok * g);
+    const int64_t t = w.s.q0 + tok;
+    bf16x8 q[KS], go[KS];
+    {
+        const uint16_t *p = head_row(a.q, t, head), *o = head_row(a.go, t, head);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            q[s] = load_chunk(p, 2 * s + h, nch);
+            go[s] = load_chunk(o, 2 * s + h, nch);
+        }
+    }
+    const float2 st = f.stats[(int64_t)w.kvh * a.total_q * g + w.s.q0 * g + crow];
+    const int seen = suffix_seen(w.s, tok);
+    const int least = suffix_seen(w.s, (int)(min(w.r0 + 32 * wave, w.rows - 1) / g));
+    const float c = a.scale * kLog2e;
+    floatx16 acc[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) acc[d] = zero16();
+
+    L load;
+    if (w.t0 < w.t1) {
+        load.open(a, w, w.t0 < w.pt);
+        load.issue(a, w, w.t0, lds);
+    }
+    for (int kt = w.t0; kt < w.t1; ++kt) {
+        const uint32_t kb = lds + ((kt - w.t0) & 1) * 2 * L::BYTES, vb = kb + L::BYTES;
+        tile_barrier();
+        if (kt + 1 < w.t1) load.issue(a, w, kt + 1, lds + ((kt + 1 - w.t0) & 1) * 2 * L::BYTES);
+        const bool pre = kt < w.pt;
+        const int limit = pre ? w.s.plen : seen, lowest = pre ? w.s.plen : least;
+#pragma unroll
+        for (int b = 0; b < KT / 32; ++b) {
+            const int j0 = (pre ? kt : kt - w.pt) * KT + 32 * b;
+            floatx16 z = zero16(), y = zero16();
+#pragma unroll
+            for (int s = 0; s < KS; ++s) z = mfma(read_row<DP>(kb + b * 32 * TileRow<DP>::BYTES, lane, s), q[s], z);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) y = mfma(read_row<DP>(vb + b * 32 * TileRow<DP>::BYTES, lane, s), go[s], y);
+            if (j0 + 32 > lowest) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] = j0 + acc_row(i, lane) < limit ? z[i] : kNegInf;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = fast_exp2(fmaf(z[i], c, -st.x)) * (y[i] - st.y);
+#pragma unroll
+            for (int mm = 0; mm < 2; ++mm) {
+                const bf16x8 p = pack8(z, mm);
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+                    acc[d] = mfma(read_col<DP>(kb + (32 * b + 16 * mm) * TileRow<DP>::BYTES, lane, d), p, acc[d]);
+            }
+        }
+    }
+    if (row >= w.rows) return;
+    uint16_t *o = (uint16_t *)head_row(a.gq, t, head);
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = 32 * d + 8 * i + 4 * h;
+            if (e < a.d) {
+                uint2 v;
+                v.x = pack_bf16x2(acc[d][4 * i] * a.scale, acc[d][4 * i + 1] * a.scale);
+                v.y = pack_bf16x2(acc[d][4 * i + 2] * a.scale, acc[d][4 * i + 3] * a.scale);
+                *(uint2 *)(o + e) = v;
+            }
+        }
+}
+
+// The keys of one workgroup of the dkv pass and the query rows that they meet.
+struct KeyWork {
+    bool prefix;
+    int keys, j0;                    // keys of the prefix or suffix, the first of this tile
+    int64_t krow;                    // row of its first key
+    int64_t q0, rows;                // the rows begin at token q0
+    int first;                       // suffix keys that query 0 sees, less one
+    int kvh, part, parts;
+    int64_t tile;                    // index of the tile among all of its kind (fp32 parts)
+};
+
+// v: tile x owner x key head x part (tiles of one owner and head first: they read the same rows)
+__device__ __forceinline__ bool find_keys(const BwdArgs &f, int64_t v, KeyWork &w) {
+    const AttnArgs &a = f.a;
+    w.prefix = v < f.p.p_units;
+    if (!w.prefix) v -= f.p.p_units;
+    const int tiles = w.prefix ? f.p.ptiles : f.p.stiles, owners = w.prefix ? a.groups : a.seqs;
+    w.parts = w.prefix ? f.p.np : f.p.ns;
+    const int64_t all = (int64_t)tiles * owners * a.hk;
+    w.part = (int)(v / all);
+    w.tile = v % all;
+    const int own = (int)(w.tile / tiles % owners);
+    w.j0 = (int)(w.tile % tiles) * KEYS;
+    w.kvh = (int)(w.tile / ((int64_t)tiles * owners));
+    const int g = a.hq / a.hk;
+    w.first = 0;
+    if (w.prefix) {
+        const int b0 = a.group_seqs[own], b1 = a.group_seqs[own + 1];
+        if (b0 < 0 || b1 < b0 || b1 > a.seqs || !prefix_ok(a, own)) return false;
+        const int64_t q0 = a.cu_q[b0], q1 = a.cu_q[b1];
+        if (q0 < 0 || q1 < q0 || q1 > a.total_q) return false;
+        w.keys = a.prefix_len[own];
+        w.krow = a.prefix_start[own];
+        w.q0 = q0;
+        w.rows = (q1 - q0) * g;
+    } else {
+        const SeqView s = load_seq(a, own);
+        if (s.skip || s.bad) return false;
+        w.keys = s.slen;
+        w.krow = s.sstart;
+        w.q0 = s.q0;
+        w.rows = (int64_t)s.n * g;
+        w.first = s.slen - s.n;
+    }
+    return w.j0 < w.keys;
+}
+
+// Tiles of ROWS query rows and their output gradients on their way into LDS, with the rows'
+// statistics: rows past the end are copies of the last one.
+template <int DP>
+struct RowLoader {
+    using R = TileRow<DP>;
+    static constexpr int N = ROWS / 4 / R::PER_DMA;
+    static constexpr int BYTES = ROWS * R::BYTES;
+    static constexpr int STAGE = 2 * BYTES + 1024;
+    int g, step_t, step_r;           // heads of a group; ROWS / g and ROWS % g
+    float inv_g;
+    int64_t tok;                     // token of the tile's first row, and its head in the group
+    int rem;
+    int64_t left;                    // rows from the tile's first to the end
+
+    __device__ __forceinline__ void open(const KeyWork &w, int g_, int64_t r0) {
+        g = g_;
+        step_t = ROWS / g;
+        step_r = ROWS % g;
+        inv_g = 1.f / (float)g;
+        tok = w.q0 + r0 / g;
+        rem = (int)(r0 % g);
+        left = w.rows - r0;
+    }
+    // (each call takes the next tile)
+    __device__ __forceinline__ void issue(const BwdArgs &f, const KeyWork &w, uint32_t lds) {
+        const AttnArgs &a = f.a;
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int nch = a.d / 8;
+        const int last = (int)min(left, (int64_t)ROWS) - 1;
+        const char *qb = a.q.p + (tok * a.q.st + (int64_t)w.kvh * g * a.q.sh) * 2;
+        const char *gb = a.go.p + (tok * a.go.st + (int64_t)w.kvh * g * a.go.sh) * 2;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int r = wave * (ROWS / 4) + n * R::PER_DMA + lane / R::CHUNKS;
+            const int x = rem + min(r, last);
+            // x / g: at most 4096 + 32, where this product is exact below the half
+            const int t = (int)(((float)x + 0.5f) * inv_g), j = x - t * g;
+            const int ch = (lane & (R::CHUNKS - 1)) ^ R::swz(r);
+            const uint32_t to = lds + (wave * (ROWS / 4) + n * R::PER_DMA) * R::BYTES;
+            if (ch < nch) {
+                dma16(qb + (t * a.q.st + j * a.q.sh) * 2 + ch * 16, to);
+                dma16(gb + (t * a.go.st + j * a.go.sh) * 2 + ch * 16, to + BYTES);
+            }
+        }
+        if (wave == 0) {
+            const char *sb = (const char *)(f.stats + ((int64_t)w.kvh * a.total_q + tok) * g + rem);
+            dma4(sb + min(lane >> 1, last) * 8 + (lane & 1) * 4, lds + 2 * BYTES);
+        }
+        tok += step_t;
+        rem += step_r;
+        if (rem >= g) {
+            rem -= g;
+            ++tok;
+        }
+        left -= ROWS;
+    }
+};
+
+template <int DP>
+__global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f, int64_t per_xcd) {
+    constexpr int DB = DP / 32, KS = DP / 16;
+    using L = RowLoader<DP>;
+    extern __shared__ __attribute__((aligned(1024))) char lds_mem[];
+    const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
+    const AttnArgs &a = f.a;
+    const int64_t u = (int64_t)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if (u >= f.p.p_units + f.p.s_units) return;
+    KeyWork w;
+    if (!find_keys(f, u, w)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = lane >> 5, g = a.hq / a.hk, nch = a.d >> 3;
+    if (nch < DP / 8) {
+        for (int i = threadIdx.x; i < 2 * L::STAGE / 16; i += 256)
+            ((uint4 *)lds_mem)[i] = make_uint4(0u, 0u, 0u, 0u);
+        __syncthreads();
+    }
+    const int key = w.j0 + 32 * wave + (lane & 31);
+    const int64_t krow = w.krow + min(key, w.keys - 1);
+    bf16x8 k[KS], v[KS];
+    {
+        const uint16_t *kp = head_row(w.prefix ? a.kp : a.ks, krow, w.kvh);
+        const uint16_t *vp = head_row(w.prefix ? a.vp : a.vs, krow, w.kvh);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            k[s] = load_chunk(kp, 2 * s + h, nch);
+            v[s] = load_chunk(vp, 2 * s + h, nch);
+        }
+    }
+    const float c = a.scale * kLog2e;
+    floatx16 dk[DB], dv[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) dk[d] = dv[d] = zero16();
+    // this part's tiles of the rows from the first that sees the tile's first key
+    int64_t r0 = w.prefix ? 0 : (int64_t)max(0, w.j0 - w.first) * g / ROWS * ROWS;
+    const int64_t all = w.rows > r0 ? ceil_div(w.rows - r0, ROWS) : 0;
+    const int64_t i0 = all * w.part / w.parts, i1 = all * (w.part + 1) / w.parts;
+    r0 += i0 * ROWS;
+    // the first rows that see this lane's key, and this wavefront's last and first one
+    const int64_t from = w.prefix ? 0 : (int64_t)max(0, key - w.first) * g;
+    const int64_t from_hi = w.prefix ? 0 : (int64_t)max(0, w.j0 + 32 * wave + 31 - w.first) * g;
+    const int64_t from_lo = w.prefix ? 0 : (int64_t)max(0, w.j0 + 32 * wave - w.first) * g;
+    L load;
+    if (i0 < i1) {
+        load.open(w, g, r0);
+        load.issue(f, w, lds);
+    }
+    for (int64_t i = i0; i < i1; ++i, r0 += ROWS) {
+        const uint32_t qb = lds + ((i - i0) & 1) * L::STAGE, gb = qb + L::BYTES, sb = gb + L::BYTES;
+        tile_barrier();
+        if (i + 1 < i1) load.issue(f, w, lds + ((i + 1 - i0) & 1) * L::STAGE);
+        if (r0 + ROWS <= from_lo) continue;          // no row of the tile sees this wavefront's keys
+        floatx16 p = zero16(), y = zero16();
+#pragma unroll
+        for (int s = 0; s < KS; ++s) p = mfma(read_row<DP>(qb, lane, s), k[s], p);
+        if (r0 + ROWS > w.rows || r0 < from_hi) {
+            const int lo = (int)min((int64_t)ROWS, max((int64_t)0, from - r0));
+            const int hi = (int)min((int64_t)ROWS, w.rows - r0);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int r = acc_row(e, lane);
+                p[e] = r >= lo && r < hi ? p[e] : kNegInf;
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < KS; ++s) y = mfma(read_row<DP>(gb, lane, s), v[s], y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            // rows 8 (e / 2) + 4 h + 2 (e % 2) and the next
+            const floatx4 st = OLIVE_LDS(floatx4, sb + (8 * (e >> 1) + 4 * h + 2 * (e & 1)) * 8);
+            p[2 * e] = fast_exp2(fmaf(p[2 * e], c, -st[0]));
+            p[2 * e + 1] = fast_exp2(fmaf(p[2 * e + 1], c, -st[2]));
+            y[2 * e] = p[2 * e] * (y[2 * e] - st[1]);
+            y[2 * e + 1] = p[2 * e + 1] * (y[2 * e + 1] - st[3]);
+        }
+#pragma unroll
+        for (int mm = 0; mm < 2; ++mm) {
+            const bf16x8 x = pack8(p, mm);
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+                dv[d] = mfma(read_col<DP>(gb + 16 * mm * TileRow<DP>::BYTES, lane, d), x, dv[d]);
+        }
+#pragma unroll
+        for (int mm = 0; mm < 2; ++mm) {
+            const bf16x8 x = pack8(y, mm);
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+                dk[d] = mfma(read_col<DP>(qb + 16 * mm * TileRow<DP>::BYTES, lane, d), x, dk[d]);
+        }
+    }
+    if (key >= w.keys) return;
+    if (w.parts == 1) {
+        uint16_t *ko = (uint16_t *)head_row(w.prefix ? a.gkp : a.gks, krow, w.kvh);
+        uint16_t *vo = (uint16_t *)head_row(w.prefix ? a.gvp : a.gvs, krow, w.kvh);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = 32 * d + 8 * i + 4 * h;
+                if (e >= a.d) continue;
+                uint2 x;
+                x.x = pack_bf16x2(dk[d][4 * i] * a.scale, dk[d][4 * i + 1] * a.scale);
+                x.y = pack_bf16x2(dk[d][4 * i + 2] * a.scale, dk[d][4 * i + 3] * a.scale);
+                *(uint2 *)(ko + e) = x;
+                x.x = pack_bf16x2(dv[d][4 * i], dv[d][4 * i + 1]);
+                x.y = pack_bf16x2(dv[d][4 * i + 2], dv[d][4 * i + 3]);
+                *(uint2 *)(vo + e) = x;
+            }
+        return;
+    }
+    // [part][tile][key][dk, dv][d], after the prefix's where both have parts
+    const int64_t tiles = (w.prefix ? f.p.p_units : f.p.s_units) / w.parts;
+    const int64_t before = w.prefix || f.p.np == 1 ? 0 : f.p.p_units * KEYS * 2 * a.d;
+    float *o = f.part + before + ((w.part * tiles + w.tile) * KEYS + (key - w.j0)) * 2 * a.d;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = 32 * d + 8 * i + 4 * h;
+            if (e >= a.d) continue;
+            *(float4 *)(o + e) = make_float4(dk[d][4 * i] * a.scale, dk[d][4 * i + 1] * a.scale,
+                                             dk[d][4 * i + 2] * a.scale, dk[d][4 * i + 3] * a.scale);
+            *(float4 *)(o + a.d + e) = make_float4(dv[d][4 * i], dv[d][4 * i + 1], dv[d][4 * i + 2], dv[d][4 * i + 3]);
+        }
+}
+
+// Adds the parts of a tile's gradients: a workgroup a tile.
+__global__ __launch_bounds__(256) void attn_dkv_join_kernel(BwdArgs f, int64_t first) {
+    const AttnArgs &a = f.a;
+    const int64_t pt = f.p.p_units / f.p.np;
+    const int64_t i = first + blockIdx.x;              // tiles of the prefixes, then of the suffixes
+    KeyWork w;
+    if (!find_keys(f, i < pt ? i : f.p.p_units + (i - pt), w) || w.parts == 1) return;
+    const int64_t tiles = (w.prefix ? f.p.p_units : f.p.s_units) / w.parts;
+    const int64_t before = w.prefix || f.p.np == 1 ? 0 : f.p.p_units * KEYS * 2 * a.d;
+    const int quads = a.d / 4;
+    const int n = min(KEYS, w.keys - w.j0) * 2 * quads;
+    for (int x = threadIdx.x; x < n; x += 256) {
+        const int e = 4 * (x % quads), kv = x / quads & 1, key = x / (2 * quads);
+        const float *p = f.part + before + (w.tile * KEYS + key) * 2 * a.d + kv * a.d + e;
+        float4 s = *(const float4 *)p;
+        for (int k = 1; k < w.parts; ++k) {
+            const float4 y = *(const float4 *)(p + (int64_t)k * tiles * KEYS * 2 * a.d);
+            s.x += y.x, s.y += y.y, s.z += y.z, s.w += y.w;
+        }
+        const HeadsArg &o = kv ? (w.prefix ? a.gvp : a.gvs) : (w.prefix ? a.gkp : a.gks);
+        uint2 v;
+        v.x = pack_bf16x2(s.x, s.y);
+        v.y = pack_bf16x2(s.z, s.w);
+        *(uint2 *)((uint16_t *)head_row(o, w.krow + w.j0 + key, w.kvh) + e) = v;
+    }
+}
+
+template <int DP>
+hipError_t go(const BwdArgs &f, hipStream_t st) {
+    const AttnArgs &a = f.a;
+    const BwdPlan &p = f.p;
+    if (a.total_q > 0) {
+        attn_stats_kernel<DP><<<(unsigned)ceil_div(a.total_q * a.hq, 256 / (DP / 8)), 256, 0, st>>>(f);
+        const int64_t per = ceil_div(p.q_units, 8);
+        attn_dq_kernel<DP><<<(unsigned)(per * 8), 256, 2 * 2 * DQ_KEYS * DP * 2, st>>>(f, per);
+    }
+    const int64_t units = p.p_units + p.s_units, per = ceil_div(units, 8);
+    if (units > 0) {
+        attn_dkv_kernel<DP><<<(unsigned)(per * 8), 256, 2 * RowLoader<DP>::STAGE, st>>>(f, per);
+        const int64_t pt = p.p_units / p.np, stl = p.s_units / p.ns;
+        const int64_t first = p.np > 1 ? 0 : pt, end = p.ns > 1 ? pt + stl : pt;
+        if (end > first) attn_dkv_join_kernel<<<(unsigned)(end - first), 256, 0, st>>>(f, first);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t attn_backward_bytes(const AttnArgs &a, bool bf16) {
+    const int64_t plain = a.total_q * a.hq * (int64_t)sizeof(float);   // the generic kernels' delta
+    if (!attn_mfma_sizes(a, bf16) || a.d > 128) return plain;
+    const BwdPlan p = make_plan(a);
+    const int64_t tiles = (p.np > 1 ? p.p_units : 0) + (p.ns > 1 ? p.s_units : 0);
+    return (a.total_q * a.hq * (int64_t)sizeof(float2) + 15) / 16 * 16 +
+           tiles * KEYS * 2 * a.d * (int64_t)sizeof(float);
+}
+
+hipError_t launch_attn_backward(const AttnArgs &a, bool bf16, hipStream_t st) {
+    if (a.d > 128 || !attn_mfma_applies(a, bf16)) return launch_attn_generic_backward(a, bf16, st);
+    BwdArgs f{a, make_plan(a), (float2 *)a.work, nullptr};
+    f.part = (float *)(a.work + (a.total_q * a.hq * (int64_t)sizeof(float2) + 15) / 16 * 16);
+    return a.d <= 64 ? go<64>(f, st) : go<128>(f, st);
+}
+
+}  // namespace olive

@@ -320,11 +320,13 @@ template <typename T>
 hipError_t backward(const AttnArgs &a, hipStream_t st) {
     float *delta = (float *)a.work;
     const int g = a.hq / a.hk;
-    attn_delta_kernel<T><<<(unsigned)tiles_of(a.total_q * a.hq, 4), THREADS, 0, st>>>(a, delta);
     const int tiles = (int)tiles_of((int64_t)a.max_q * g, R);
     const size_t bytes = sizeof(float) * ((2 * R + 2 * KT) * (a.d + 1) + 2 * R * KT);
-    attn_generic_dq_kernel<T><<<(unsigned)((int64_t)a.seqs * tiles * a.hk), THREADS, bytes, st>>>(
-        a, tiles, delta);
+    if (a.total_q > 0) {
+        attn_delta_kernel<T><<<(unsigned)tiles_of(a.total_q * a.hq, 4), THREADS, 0, st>>>(a, delta);
+        attn_generic_dq_kernel<T><<<(unsigned)((int64_t)a.seqs * tiles * a.hk), THREADS, bytes, st>>>(
+            a, tiles, delta);
+    }
     const int pt = (int)tiles_of(a.max_prefix, KT), sl = (int)tiles_of(a.max_suffix, KT);
     if (pt)
         attn_generic_dkv_kernel<T, true><<<(unsigned)((int64_t)a.groups * pt * a.hk), THREADS, bytes, st>>>(
@@ -337,12 +339,10 @@ hipError_t backward(const AttnArgs &a, hipStream_t st) {
 
 }  // namespace
 
-int64_t attn_backward_bytes(const AttnArgs &a, bool) { return a.total_q * a.hq * (int64_t)sizeof(float); }
-
 hipError_t launch_attn_generic(const AttnArgs &a, bool bf16, hipStream_t st) {
     return bf16 ? forward<uint16_t>(a, st) : forward<float>(a, st);
 }
-hipError_t launch_attn_backward(const AttnArgs &a, bool bf16, hipStream_t st) {
+hipError_t launch_attn_generic_backward(const AttnArgs &a, bool bf16, hipStream_t st) {
     return bf16 ? backward<uint16_t>(a, st) : backward<float>(a, st);
 }
 

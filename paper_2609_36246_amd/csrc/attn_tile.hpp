@@ -15,6 +15,7 @@ namespace olive {
 
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef short shortx8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 
 #define OLIVE_LDS(T, addr) (*(__attribute__((address_space(3))) T *)(uintptr_t)(uint32_t)(addr))
@@ -38,12 +39,16 @@ __device__ __forceinline__ void tile_barrier() {
     compiler_fence();
 }
 
-// First operand (rows x K): row `r0 + lane % 32`, chunk 2 step + lane / 32.
-template <int DP>
-__device__ __forceinline__ uint32_t row_addr(int lane) {
-    const int r = lane & 31;
-    return (uint32_t)(r * TileRow<DP>::BYTES);
+// dma16 (mfma_pipe.hpp) with 4 bytes a lane.
+__device__ __forceinline__ void dma4(const char *g, uint32_t la) {
+    la = __builtin_amdgcn_readfirstlane(la);
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(la), "v"(g) : "memory", "m0");
+#pragma clang diagnostic pop
 }
+
+// First operand (rows x K): row `r0 + lane % 32`, chunk 2 step + lane / 32.
 template <int DP>
 __device__ __forceinline__ bf16x8 read_row(uint32_t base, int lane, int step) {
     const int r = lane & 31, c = 2 * step + (lane >> 5);
@@ -93,5 +98,99 @@ __device__ __forceinline__ bf16x8 load_chunk(const uint16_t *row, int c, int nch
     if (c < nch) u = *(const uintx4 *)(row + 8 * c);
     return __builtin_bit_cast(bf16x8, u);
 }
+
+__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+inline int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+
+// Key tiles [t0, t1) of part i of n.
+__device__ __forceinline__ void part_range(int tiles, int n, int i, int &t0, int &t1) {
+    t0 = (int)((int64_t)tiles * i / n);
+    t1 = (int)((int64_t)tiles * (i + 1) / n);
+}
+
+// What one workgroup does.
+struct Work {
+    SeqView s;
+    int64_t rows;                    // query rows of the range that begins at token s.q0
+    int64_t r0;                      // first of this workgroup's
+    int kvh, part;
+    int pt;                          // prefix tiles come first
+    int t0, t1;
+};
+
+// Keys and values on their way into LDS. A wavefront loads KT / 4 rows of each of a tile; rows
+// past the end are copies of the last one (their scores are masked).
+template <int DP, int KT>
+struct Loader {
+    using R = TileRow<DP>;
+    static constexpr int N = KT / 4 / R::PER_DMA;    // loads of a wavefront, keys and values each
+    static constexpr int BYTES = KT * R::BYTES;      // of the tile's keys; the values follow
+    // the segment being read, prefix or suffix (wave-uniform)
+    const char *k, *v;                               // its first key's head
+    int64_t kst, vst;                                // bytes between keys
+    int len, tile0;                                  // its keys, its first tile's index
+    bool paged;
+    int shift;                                       // log2 of the page size, or -1
+    int32_t page[N];                                 // table entries of the next tile's rows
+    bool bad = false;
+
+    __device__ __forceinline__ void open(const AttnArgs &a, const Work &w, bool pre) {
+        const HeadsArg &kh = pre ? a.kp : a.ks, &vh = pre ? a.vp : a.vs;
+        const int64_t at = pre ? w.s.pstart : w.s.sstart;
+        kst = kh.st * 2;
+        vst = vh.st * 2;
+        k = kh.p + (int64_t)w.kvh * kh.sh * 2 + at * kst;
+        v = vh.p + (int64_t)w.kvh * vh.sh * 2 + at * vst;
+        len = pre ? w.s.plen : w.s.slen;
+        tile0 = pre ? 0 : w.pt;
+        paged = !pre && w.s.pages;
+        shift = (a.page_size & (a.page_size - 1)) == 0 ? 31 - __clz(a.page_size | 1) : -1;
+    }
+    static __device__ __forceinline__ int row(int n) {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        return wave * (KT / 4) + n * R::PER_DMA + lane / R::CHUNKS;
+    }
+    __device__ __forceinline__ int page_of(const AttnArgs &a, int j) const {
+        return shift >= 0 ? j >> shift : j / a.page_size;
+    }
+    // Asks for the table entries of tile t; they are there at the next barrier.
+    __device__ __forceinline__ void look_up(const AttnArgs &a, const Work &w, int t) {
+        if (!w.s.pages || t < w.pt || t >= w.t1) return;
+        const int j0 = (t - w.pt) * KT;
+#pragma unroll
+        for (int n = 0; n < N; ++n) page[n] = w.s.pages[page_of(a, min(j0 + row(n), w.s.slen - 1))];
+    }
+    __device__ __forceinline__ void issue(const AttnArgs &a, const Work &w, int t, uint32_t lds) {
+        if (t == w.pt && t != w.t0) open(a, w, false);
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int nch = a.d / 8;
+        const int j0 = (t - tile0) * KT, last = len - 1 - j0;
+        const char *kt = k + j0 * kst, *vt = v + j0 * vst;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int full = row(n), r = min(full, last);
+            const int ch = (lane & (R::CHUNKS - 1)) ^ R::swz(full), c = ch * 16;
+            if (ch >= nch) continue;      // the slots past head_dim keep their zeros
+            const uint32_t to = lds + (wave * (KT / 4) + n * R::PER_DMA) * R::BYTES;
+            if (paged) {
+                const int j = j0 + r;
+                int64_t at = (int64_t)page[n] * a.page_size;
+                if (at < 0 || at > a.suffix_rows - a.page_size) {
+                    bad = true;
+                    at = 0;
+                } else {
+                    at += j - page_of(a, j) * a.page_size;
+                }
+                dma16(k + at * kst + c, to);
+                dma16(v + at * vst + c, to + BYTES);
+            } else {
+                // the launcher takes strides for which a tile's offsets fit 32 bits
+                dma16_sv<0>(kt, (uint32_t)r * (uint32_t)kst + c, to);
+                dma16_sv<0>(vt, (uint32_t)r * (uint32_t)vst + c, to + BYTES);
+            }
+        }
+    }
+};
 
 }  // namespace olive

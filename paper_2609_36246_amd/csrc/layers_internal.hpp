@@ -79,6 +79,7 @@ int64_t attn_backward_bytes(const AttnArgs &a, bool bf16);
 bool attn_mfma_sizes(const AttnArgs &a, bool bf16);
 bool attn_mfma_applies(const AttnArgs &a, bool bf16);
 hipError_t launch_attn_generic(const AttnArgs &a, bool bf16, hipStream_t st);
+hipError_t launch_attn_generic_backward(const AttnArgs &a, bool bf16, hipStream_t st);
 hipError_t launch_attn_forward(const AttnArgs &a, bool bf16, hipStream_t st);
 hipError_t launch_attn_backward(const AttnArgs &a, bool bf16, hipStream_t st);
 

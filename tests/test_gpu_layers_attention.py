@@ -80,6 +80,13 @@ def test_backward(shape, hq, hk, d, dtype):
     a.check(a.run(grad=True), grad=True)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_no_queries(dtype):
+    """Nothing to do forward; the gradients of every key are zero."""
+    a = Attn(prefix=[40], seqs=[(0, 5, 0), (0, 0, 0)], dtype=dtype, grad=True)
+    a.check(a.run(grad=True), grad=True)
+
+
 @pytest.mark.parametrize("shape,n", [("update", 700), ("prompts", 1100)])
 def test_longer_runs(shape, n):
     """Several tiles of rows and keys in every direction."""
