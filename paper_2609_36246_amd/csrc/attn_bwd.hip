@@ -56,6 +56,7 @@ BwdPlan make_plan(const AttnArgs &a) {
 struct BwdArgs {
     AttnArgs a;
     BwdPlan p;
+    DieOrder qd, pd, sd;
     float2 *stats;                   // [hk][total_q][g]: lse in log2 units (+inf where -inf), delta
     float *part;                     // fp32 parts: prefix tiles, then suffix tiles
 };
@@ -88,14 +89,14 @@ __global__ __launch_bounds__(256) void attn_stats_kernel(BwdArgs f) {
 }
 
 template <int DP>
-__global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f, int64_t per_xcd) {
+__global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f) {
     constexpr int KT = DQ_KEYS, DB = DP / 32, KS = DP / 16;
     using L = Loader<DP, KT>;
     extern __shared__ __attribute__((aligned(1024))) char lds_mem[];
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
     const AttnArgs &a = f.a;
-    int64_t u = (int64_t)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if (u >= f.p.q_units) return;
+    int64_t u = f.qd.unit(blockIdx.x);
+    if (u >= f.qd.units) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, g = a.hq / a.hk, nch = a.d >> 3;
     // the last row tiles of a sequence, which see the most keys, come first
@@ -206,10 +207,9 @@ struct KeyWork {
 };
 
 // v: tile x owner x key head x part (tiles of one owner and head first: they read the same rows)
-__device__ __forceinline__ bool find_keys(const BwdArgs &f, int64_t v, KeyWork &w) {
+__device__ __forceinline__ bool find_keys(const BwdArgs &f, bool prefix, int64_t v, KeyWork &w) {
     const AttnArgs &a = f.a;
-    w.prefix = v < f.p.p_units;
-    if (!w.prefix) v -= f.p.p_units;
+    w.prefix = prefix;
     const int tiles = w.prefix ? f.p.ptiles : f.p.stiles, owners = w.prefix ? a.groups : a.seqs;
     w.parts = w.prefix ? f.p.np : f.p.ns;
     const int64_t all = (int64_t)tiles * owners * a.hk;
@@ -300,16 +300,16 @@ struct RowLoader {
 };
 
 template <int DP>
-__global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f, int64_t per_xcd) {
+__global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
     constexpr int DB = DP / 32, KS = DP / 16;
     using L = RowLoader<DP>;
     extern __shared__ __attribute__((aligned(1024))) char lds_mem[];
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
     const AttnArgs &a = f.a;
-    const int64_t u = (int64_t)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if (u >= f.p.p_units + f.p.s_units) return;
     KeyWork w;
-    if (!find_keys(f, u, w)) return;
+    const bool pre = blockIdx.x < f.pd.blocks();
+    const int64_t u = pre ? f.pd.unit(blockIdx.x) : f.sd.unit(blockIdx.x - f.pd.blocks());
+    if (u >= (pre ? f.pd.units : f.sd.units) || !find_keys(f, pre, u, w)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, g = a.hq / a.hk, nch = a.d >> 3;
     if (nch < DP / 8) {
@@ -319,13 +319,15 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f, int64_t per
     }
     const int key = w.j0 + 32 * wave + (lane & 31);
     const int64_t krow = w.krow + min(key, w.keys - 1);
-    bf16x8 k[KS], v[KS];
+    // the wavefront's keys in LDS, their values in registers
+    const uint32_t kl = lds + 2 * L::STAGE + wave * 32 * TileRow<DP>::BYTES;
+    bf16x8 v[KS];
     {
         const uint16_t *kp = head_row(w.prefix ? a.kp : a.ks, krow, w.kvh);
         const uint16_t *vp = head_row(w.prefix ? a.vp : a.vs, krow, w.kvh);
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            k[s] = load_chunk(kp, 2 * s + h, nch);
+            write_row<DP>(kl, lane, s, load_chunk(kp, 2 * s + h, nch));
             v[s] = load_chunk(vp, 2 * s + h, nch);
         }
     }
@@ -354,7 +356,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f, int64_t per
         if (r0 + ROWS <= from_lo) continue;          // no row of the tile sees this wavefront's keys
         floatx16 p = zero16(), y = zero16();
 #pragma unroll
-        for (int s = 0; s < KS; ++s) p = mfma(read_row<DP>(qb, lane, s), k[s], p);
+        for (int s = 0; s < KS; ++s) p = mfma(read_row<DP>(qb, lane, s), read_row<DP>(kl, lane, s), p);
         if (r0 + ROWS > w.rows || r0 < from_hi) {
             const int lo = (int)min((int64_t)ROWS, max((int64_t)0, from - r0));
             const int hi = (int)min((int64_t)ROWS, w.rows - r0);
@@ -432,7 +434,7 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(BwdArgs f, int64_t f
     const int64_t pt = f.p.p_units / f.p.np;
     const int64_t i = first + blockIdx.x;              // tiles of the prefixes, then of the suffixes
     KeyWork w;
-    if (!find_keys(f, i < pt ? i : f.p.p_units + (i - pt), w) || w.parts == 1) return;
+    if (!find_keys(f, i < pt, i < pt ? i : i - pt, w) || w.parts == 1) return;
     const int64_t tiles = (w.prefix ? f.p.p_units : f.p.s_units) / w.parts;
     const int64_t before = w.prefix || f.p.np == 1 ? 0 : f.p.p_units * KEYS * 2 * a.d;
     const int quads = a.d / 4;
@@ -459,12 +461,11 @@ hipError_t go(const BwdArgs &f, hipStream_t st) {
     const BwdPlan &p = f.p;
     if (a.total_q > 0) {
         attn_stats_kernel<DP><<<(unsigned)ceil_div(a.total_q * a.hq, 256 / (DP / 8)), 256, 0, st>>>(f);
-        const int64_t per = ceil_div(p.q_units, 8);
-        attn_dq_kernel<DP><<<(unsigned)(per * 8), 256, 2 * 2 * DQ_KEYS * DP * 2, st>>>(f, per);
+        attn_dq_kernel<DP><<<(unsigned)f.qd.blocks(), 256, 2 * 2 * DQ_KEYS * DP * 2, st>>>(f);
     }
-    const int64_t units = p.p_units + p.s_units, per = ceil_div(units, 8);
-    if (units > 0) {
-        attn_dkv_kernel<DP><<<(unsigned)(per * 8), 256, 2 * RowLoader<DP>::STAGE, st>>>(f, per);
+    if (p.p_units + p.s_units > 0) {
+        attn_dkv_kernel<DP><<<(unsigned)(f.pd.blocks() + f.sd.blocks()), 256,
+                              2 * RowLoader<DP>::STAGE + KEYS * DP * 2, st>>>(f);
         const int64_t pt = p.p_units / p.np, stl = p.s_units / p.ns;
         const int64_t first = p.np > 1 ? 0 : pt, end = p.ns > 1 ? pt + stl : pt;
         if (end > first) attn_dkv_join_kernel<<<(unsigned)(end - first), 256, 0, st>>>(f, first);
@@ -485,7 +486,13 @@ int64_t attn_backward_bytes(const AttnArgs &a, bool bf16) {
 
 hipError_t launch_attn_backward(const AttnArgs &a, bool bf16, hipStream_t st) {
     if (a.d > 128 || !attn_mfma_applies(a, bf16)) return launch_attn_generic_backward(a, bf16, st);
-    BwdArgs f{a, make_plan(a), (float2 *)a.work, nullptr};
+    BwdArgs f{};
+    f.a = a;
+    f.p = make_plan(a);
+    f.qd = DieOrder::of(f.p.q_units);
+    f.pd = DieOrder::of(f.p.p_units);
+    f.sd = DieOrder::of(f.p.s_units);
+    f.stats = (float2 *)a.work;
     f.part = (float *)(a.work + (a.total_q * a.hq * (int64_t)sizeof(float2) + 15) / 16 * 16);
     return a.d <= 64 ? go<64>(f, st) : go<128>(f, st);
 }

@@ -75,6 +75,7 @@ FwdPlan make_plan(const AttnArgs &a) {
 struct FwdArgs {
     AttnArgs a;
     FwdPlan p;
+    DieOrder pd, sd;
     float *po;                       // [part][total_q hq][d]
     float2 *pml;                     // [part][total_q hq]: maximum (log2 units), sum
 };
@@ -117,11 +118,13 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
 }
 
 template <int DP, int WR>
-__device__ __forceinline__ bool find_work(const FwdArgs &f, int64_t u, Work &w) {
+__device__ __forceinline__ bool find_work(const FwdArgs &f, int64_t block, Work &w) {
     const AttnArgs &a = f.a;
     constexpr int BM = 32 * WR, KT = tile_keys(DP, WR);
     const int g = a.hq / a.hk;
-    if (u < f.p.p_units) {
+    if (block < f.pd.blocks()) {
+        const int64_t u = f.pd.unit(block);
+        if (u >= f.pd.units) return false;
         const int64_t i = u % f.p.ptiles;
         int v = (int)(u / f.p.ptiles);
         w.kvh = v % a.hk;
@@ -139,14 +142,15 @@ __device__ __forceinline__ bool find_work(const FwdArgs &f, int64_t u, Work &w) 
         part_range(w.pt, f.p.np, w.part, w.t0, w.t1);
         return w.t0 < w.t1;
     }
-    u -= f.p.p_units;
+    int64_t u = f.sd.unit(block - f.pd.blocks());
+    if (u >= f.sd.units) return false;
     // the last row tiles of a sequence, which see the most keys, come first
     const int rt = f.p.stiles - 1 - (int)(u % f.p.stiles);
     u /= f.p.stiles;
+    w.s = load_seq(a, (int)(u % a.seqs));
+    u /= a.seqs;
     w.kvh = (int)(u % a.hk);
-    u /= a.hk;
-    w.part = (int)(u % f.p.ns);
-    w.s = load_seq(a, (int)(u / f.p.ns));
+    w.part = (int)(u / a.hk);
     w.rows = (int64_t)w.s.n * g;
     w.r0 = (int64_t)rt * BM;
     if (w.s.skip || w.r0 >= w.rows) return false;
@@ -283,17 +287,13 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
 }
 
 template <int DP, int WR>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArgs f, int64_t per_xcd) {
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArgs f) {
     constexpr int WK = 4 / WR, KT = tile_keys(DP, WR), DB = DP / 32, KS = DP / 16;
     extern __shared__ __attribute__((aligned(1024))) char lds_mem[];
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
     const AttnArgs &a = f.a;
-    // consecutive workgroups go to the 8 dies in turn: each die takes a run of units, whose
-    // keys then meet in its cache
-    const int64_t u = (int64_t)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if (u >= f.p.p_units + f.p.s_units) return;
     Work w;
-    if (!find_work<DP, WR>(f, u, w)) return;
+    if (!find_work<DP, WR>(f, blockIdx.x, w)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wr = wave / WK, wk = wave % WK, h = lane >> 5;
     const int g = a.hq / a.hk, nch = a.d >> 3;
@@ -486,8 +486,8 @@ template <int DP, int WR>
 hipError_t go(const FwdArgs &f, hipStream_t st) {
     constexpr int KT = tile_keys(DP, WR);
     constexpr int stages = 2 * 2 * KT * DP * 2, join = WR < 4 ? 4 * (DP / 32) * 4096 + 1024 : 0;
-    const int64_t units = f.p.p_units + f.p.s_units, per = ceil_div(units, 8);
-    attn_fwd_kernel<DP, WR><<<(unsigned)(per * 8), 256, stages > join ? stages : join, st>>>(f, per);
+    attn_fwd_kernel<DP, WR><<<(unsigned)(f.pd.blocks() + f.sd.blocks()), 256, stages > join ? stages : join,
+                              st>>>(f);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && !f.p.direct()) {
         attn_join_kernel<<<(unsigned)ceil_div(f.a.total_q * f.a.hq, 4), 256, 0, st>>>(f, KT);
@@ -524,7 +524,11 @@ int64_t attn_forward_bytes(const AttnArgs &a, bool bf16) {
 
 hipError_t launch_attn_forward(const AttnArgs &a, bool bf16, hipStream_t st) {
     if (!attn_mfma_applies(a, bf16)) return launch_attn_generic(a, bf16, st);
-    FwdArgs f{a, make_plan(a), nullptr, nullptr};
+    FwdArgs f{};
+    f.a = a;
+    f.p = make_plan(a);
+    f.pd = DieOrder::of(f.p.p_units);
+    f.sd = DieOrder::of(f.p.s_units);
     const int64_t rows = (int64_t)f.p.parts() * a.total_q * a.hq;
     f.po = (float *)a.work;
     f.pml = (float2 *)(f.po + rows * a.d);

@@ -55,6 +55,12 @@ __device__ __forceinline__ bf16x8 read_row(uint32_t base, int lane, int step) {
     return OLIVE_LDS(bf16x8, base + r * TileRow<DP>::BYTES + ((c ^ TileRow<DP>::swz(r)) << 4));
 }
 
+template <int DP>
+__device__ __forceinline__ void write_row(uint32_t base, int lane, int step, bf16x8 x) {
+    const int r = lane & 31, c = 2 * step + (lane >> 5);
+    OLIVE_LDS(bf16x8, base + r * TileRow<DP>::BYTES + ((c ^ TileRow<DP>::swz(r)) << 4)) = x;
+}
+
 // First operand transposed (elements x rows): lane % 32 is the element 32 db + lane % 32, the
 // 8 values are rows 4 (lane / 32) + 0..3 and 8 more: the rows whose results a lane of the same
 // half holds in registers 0..7 of a 32 x 32 product. `base` is row 16 m of the tile.
@@ -102,6 +108,24 @@ __device__ __forceinline__ bf16x8 load_chunk(const uint16_t *row, int c, int nch
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 inline int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+
+// Consecutive workgroups go to the 8 dies in turn, each with a cache of its own. Runs of `run`
+// consecutive units, which read the same keys or rows, go to one die, the runs to the dies in
+// turn: a die that got one long stretch of units would get all the long ones.
+struct DieOrder {
+    int64_t units;
+    int run;
+    __host__ static DieOrder of(int64_t units) {
+        const int64_t r = units / 64;
+        return DieOrder{units, (int)(r < 1 ? 1 : r > 16 ? 16 : r)};
+    }
+    __host__ __device__ int64_t blocks() const { return ceil_div(units, 8 * run) * 8 * run; }
+    // >= units: nothing to do
+    __device__ __forceinline__ int64_t unit(int64_t block) const {
+        const int64_t i = block >> 3;
+        return (i / run * 8 + (block & 7)) * run + i % run;
+    }
+};
 
 // Key tiles [t0, t1) of part i of n.
 __device__ __forceinline__ void part_range(int tiles, int n, int i, int &t0, int &t1) {
