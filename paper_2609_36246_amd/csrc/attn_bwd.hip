@@ -57,7 +57,10 @@ struct BwdArgs {
     AttnArgs a;
     BwdPlan p;
     DieOrder qd, pd, sd;
-    float2 *stats;                   // [hk][total_q][g]: lse in log2 units (+inf where -inf), delta
+    // [hk][total_q][g] each: what the products of a row begin at, so that z is scale^-1 (scale q
+    // k - lse) and y is dp - delta
+    float *nlse;                     // -lse / scale, -inf for a row that sees nothing
+    float *ndelta;                   // -delta
     float *part;                     // fp32 parts: prefix tiles, then suffix tiles
 };
 
@@ -83,8 +86,9 @@ __global__ __launch_bounds__(256) void attn_stats_kernel(BwdArgs f) {
     for (int o = LPR / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
     if (c == 0) {
         const float lse = a.lse[r];
-        f.stats[((int64_t)(head / g) * a.total_q + t) * g + head % g] =
-            make_float2(lse == kNegInf ? __builtin_inff() : lse * kLog2e, s);
+        const int64_t at = ((int64_t)(head / g) * a.total_q + t) * g + head % g;
+        f.nlse[at] = lse == kNegInf ? kNegInf : -lse / a.scale;
+        f.ndelta[at] = -s;
     }
 }
 
@@ -120,6 +124,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f) {
     w.pt = (int)ceil_div(w.s.plen, KT);
     w.t0 = 0;
     w.t1 = w.pt + (int)ceil_div(suffix_seen(w.s, (int)((min(w.rows, w.r0 + 128) - 1) / g)), KT);
+    make_uniform(w);
     if (nch < DP / 8) {
         for (int i = threadIdx.x; i < 2 * 2 * KT * DP / 8; i += 256)
             ((uint4 *)lds_mem)[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -137,7 +142,8 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f) {
             go[s] = load_chunk(o, 2 * s + h, nch);
         }
     }
-    const float2 st = f.stats[(int64_t)w.kvh * a.total_q * g + w.s.q0 * g + crow];
+    const int64_t at = (int64_t)w.kvh * a.total_q * g + w.s.q0 * g + crow;
+    const float ndelta = f.ndelta[at];
     const int seen = suffix_seen(w.s, tok);
     const int least = suffix_seen(w.s, (int)(min(w.r0 + 32 * wave, w.rows - 1) / g));
     const float c = a.scale * kLog2e;
@@ -145,39 +151,69 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f) {
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] = zero16();
 
+    const float nl = f.nlse[at] * c;
+    constexpr int RB = TileRow<DP>::BYTES, NB = KT / 32, FN = 2 * KS + 2 * DB;   // operands of a block
+    RowReader<DP> kr;
+    ColReader<DP> kc;
+    kr.open(lds, lane);
+    kc.open(lds, lane);
     L load;
     if (w.t0 < w.t1) {
         load.open(a, w, w.t0 < w.pt);
-        load.issue(a, w, w.t0, lds);
+        load.template issue<0>(a, w, w.t0, lds);
     }
-    for (int kt = w.t0; kt < w.t1; ++kt) {
-        const uint32_t kb = lds + ((kt - w.t0) & 1) * 2 * L::BYTES, vb = kb + L::BYTES;
+    const auto step = [&](auto stage, int kt) {
+        constexpr int AT = decltype(stage)::value * 2 * L::BYTES, NEXT = 2 * L::BYTES - AT;
         tile_barrier();
-        if (kt + 1 < w.t1) load.issue(a, w, kt + 1, lds + ((kt + 1 - w.t0) & 1) * 2 * L::BYTES);
+        if (kt + 1 < w.t1) load.template issue<NEXT>(a, w, kt + 1, lds);
         const bool pre = kt < w.pt;
         const int limit = pre ? w.s.plen : seen, lowest = pre ? w.s.plen : least;
+        // operands of block b: KS of its keys, KS of its values, 2 DB of its keys transposed
+        const auto at = [&](int x) {
+            const int b = x / FN, i = x % FN;
+            return i < KS       ? kr.read(i, AT + b * 32 * RB)
+                   : i < 2 * KS ? kr.read(i - KS, AT + L::BYTES + b * 32 * RB)
+                                : kc.read((i - 2 * KS) % DB, AT + (2 * b + (i - 2 * KS) / DB) * 16 * RB);
+        };
+        bf16x8 f[2][4], p;
+        floatx16 z, y;
 #pragma unroll
-        for (int b = 0; b < KT / 32; ++b) {
-            const int j0 = (pre ? kt : kt - w.pt) * KT + 32 * b;
-            floatx16 z = zero16(), y = zero16();
+        for (int i = 0; i < 4; ++i) f[0][i] = at(i);
 #pragma unroll
-            for (int s = 0; s < KS; ++s) z = mfma(read_row<DP>(kb + b * 32 * TileRow<DP>::BYTES, lane, s), q[s], z);
+        for (int n = 0; n < NB * FN / 4; ++n) {
+            if (n + 1 < NB * FN / 4) {
 #pragma unroll
-            for (int s = 0; s < KS; ++s) y = mfma(read_row<DP>(vb + b * 32 * TileRow<DP>::BYTES, lane, s), go[s], y);
-            if (j0 + 32 > lowest) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) z[i] = j0 + acc_row(i, lane) < limit ? z[i] : kNegInf;
+                for (int i = 0; i < 4; ++i) f[(n + 1) & 1][i] = at(4 * (n + 1) + i);
             }
+            keep_order();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = fast_exp2(fmaf(z[i], c, -st.x)) * (y[i] - st.y);
+            for (int i = 0; i < 4; ++i) {
+                const int b = (4 * n + i) / FN, x = (4 * n + i) % FN;
+                if (x < KS) {
+                    z = mfma(f[n & 1][i], q[x], x == 0 ? zero16() : z);
+                } else if (x < 2 * KS) {
+                    y = mfma(f[n & 1][i], go[x - KS], x == KS ? zero16() : y);
+                } else {
+                    const int mm = (x - 2 * KS) / DB, d = (x - 2 * KS) % DB;
+                    if (x == 2 * KS) {
+                        const int j0 = (pre ? kt : kt - w.pt) * KT + 32 * b;
+                        if (j0 + 32 > lowest) {
 #pragma unroll
-            for (int mm = 0; mm < 2; ++mm) {
-                const bf16x8 p = pack8(z, mm);
+                            for (int e = 0; e < 16; ++e) z[e] = j0 + acc_row(e, lane) < limit ? z[e] : kNegInf;
+                        }
 #pragma unroll
-                for (int d = 0; d < DB; ++d)
-                    acc[d] = mfma(read_col<DP>(kb + (32 * b + 16 * mm) * TileRow<DP>::BYTES, lane, d), p, acc[d]);
+                        for (int e = 0; e < 16; ++e) z[e] = fast_exp2(fmaf(z[e], c, nl)) * (y[e] + ndelta);
+                    }
+                    if (d == 0) p = pack8(z, mm);
+                    acc[d] = mfma(f[n & 1][i], p, acc[d]);
+                }
             }
+            keep_order();
         }
+    };
+    for (int kt = w.t0; kt < w.t1; kt += 2) {
+        step(Const<0>{}, kt);
+        if (kt + 1 < w.t1) step(Const<1>{}, kt + 1);
     }
     if (row >= w.rows) return;
     uint16_t *o = (uint16_t *)head_row(a.gq, t, head);
@@ -238,6 +274,12 @@ __device__ __forceinline__ bool find_keys(const BwdArgs &f, bool prefix, int64_t
         w.rows = (int64_t)s.n * g;
         w.first = s.slen - s.n;
     }
+    w.keys = uniform32(w.keys);
+    w.j0 = uniform32(w.j0);
+    w.krow = uniform64(w.krow);
+    w.q0 = uniform64(w.q0);
+    w.rows = uniform64(w.rows);
+    w.first = uniform32(w.first);
     return w.j0 < w.keys;
 }
 
@@ -280,14 +322,15 @@ struct RowLoader {
             const int t = (int)(((float)x + 0.5f) * inv_g), j = x - t * g;
             const int ch = (lane & (R::CHUNKS - 1)) ^ R::swz(r);
             const uint32_t to = lds + (wave * (ROWS / 4) + n * R::PER_DMA) * R::BYTES;
+            // the launcher takes strides for which these offsets fit 32 bits
             if (ch < nch) {
-                dma16(qb + (t * a.q.st + j * a.q.sh) * 2 + ch * 16, to);
-                dma16(gb + (t * a.go.st + j * a.go.sh) * 2 + ch * 16, to + BYTES);
+                dma16_from<0>(qb, (t * (uint32_t)a.q.st + j * (uint32_t)a.q.sh) * 2 + ch * 16, to);
+                dma16_from<BYTES>(gb, (t * (uint32_t)a.go.st + j * (uint32_t)a.go.sh) * 2 + ch * 16, to);
             }
         }
         if (wave == 0) {
-            const char *sb = (const char *)(f.stats + ((int64_t)w.kvh * a.total_q + tok) * g + rem);
-            dma4(sb + min(lane >> 1, last) * 8 + (lane & 1) * 4, lds + 2 * BYTES);
+            const int64_t at = ((int64_t)w.kvh * a.total_q + tok) * g + rem + min(lane & 31, last);
+            dma4((const char *)((lane < 32 ? f.nlse : f.ndelta) + at), lds + 2 * BYTES);
         }
         tok += step_t;
         rem += step_r;
@@ -319,15 +362,20 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
     }
     const int key = w.j0 + 32 * wave + (lane & 31);
     const int64_t krow = w.krow + min(key, w.keys - 1);
+    constexpr int RB = TileRow<DP>::BYTES;
+    RowReader<DP> rr;
+    ColReader<DP> rc;
+    rr.open(lds, lane);
+    rc.open(lds, lane);
     // the wavefront's keys in LDS, their values in registers
-    const uint32_t kl = lds + 2 * L::STAGE + wave * 32 * TileRow<DP>::BYTES;
+    const int kl = 2 * L::STAGE + wave * 32 * RB;
     bf16x8 v[KS];
     {
-        const uint16_t *kp = head_row(w.prefix ? a.kp : a.ks, krow, w.kvh);
-        const uint16_t *vp = head_row(w.prefix ? a.vp : a.vs, krow, w.kvh);
+        const uint16_t *kp = head_row(pick(w.prefix, a.kp, a.ks), krow, w.kvh);
+        const uint16_t *vp = head_row(pick(w.prefix, a.vp, a.vs), krow, w.kvh);
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            write_row<DP>(kl, lane, s, load_chunk(kp, 2 * s + h, nch));
+            rr.write(s, kl, load_chunk(kp, 2 * s + h, nch));
             v[s] = load_chunk(vp, 2 * s + h, nch);
         }
     }
@@ -349,17 +397,47 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
         load.open(w, g, r0);
         load.issue(f, w, lds);
     }
-    for (int64_t i = i0; i < i1; ++i, r0 += ROWS) {
-        const uint32_t qb = lds + ((i - i0) & 1) * L::STAGE, gb = qb + L::BYTES, sb = gb + L::BYTES;
+    const auto step = [&](auto stage, int64_t i) {
+        constexpr int AT = decltype(stage)::value * L::STAGE, NEXT = L::STAGE - AT;
         tile_barrier();
-        if (i + 1 < i1) load.issue(f, w, lds + ((i + 1 - i0) & 1) * L::STAGE);
-        if (r0 + ROWS <= from_lo) continue;          // no row of the tile sees this wavefront's keys
-        floatx16 p = zero16(), y = zero16();
+        if (i + 1 < i1) load.issue(f, w, lds + NEXT);
+        const int64_t row0 = r0;
+        r0 += ROWS;
+        if (r0 <= from_lo) return;                   // no row of the tile sees this wavefront's keys
+        floatx16 p, y;
+        // lane's registers are rows 8 j + 4 h + 0..3 of the tile
+        const uint32_t sb = lds + AT + 2 * L::BYTES + 16 * h;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) p = mfma(read_row<DP>(qb, lane, s), read_row<DP>(kl, lane, s), p);
-        if (r0 + ROWS > w.rows || r0 < from_hi) {
-            const int lo = (int)min((int64_t)ROWS, max((int64_t)0, from - r0));
-            const int hi = (int)min((int64_t)ROWS, w.rows - r0);
+        for (int j = 0; j < 4; ++j) {
+            const floatx4 x = OLIVE_LDS(floatx4, sb + 32 * j);
+            p[4 * j] = x[0], p[4 * j + 1] = x[1], p[4 * j + 2] = x[2], p[4 * j + 3] = x[3];
+        }
+        bf16x8 fa[2][2], fb[2][2], fr[2][2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) fa[0][x] = rr.read(x, AT), fb[0][x] = rr.read(x, kl);
+#pragma unroll
+        for (int n = 0; n < KS / 2; ++n) {
+            if (n + 1 < KS / 2) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    fa[(n + 1) & 1][x] = rr.read(2 * n + 2 + x, AT), fb[(n + 1) & 1][x] = rr.read(2 * n + 2 + x, kl);
+            } else {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) fr[0][x] = rr.read(x, AT + L::BYTES);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const floatx4 x = OLIVE_LDS(floatx4, sb + 128 + 32 * j);
+                    y[4 * j] = x[0], y[4 * j + 1] = x[1], y[4 * j + 2] = x[2], y[4 * j + 3] = x[3];
+                }
+            }
+            keep_order();
+#pragma unroll
+            for (int x = 0; x < 2; ++x) p = mfma(fa[n & 1][x], fb[n & 1][x], p);
+            keep_order();
+        }
+        if (r0 > w.rows || row0 < from_hi) {
+            const int lo = (int)min((int64_t)ROWS, max((int64_t)0, from - row0));
+            const int hi = (int)min((int64_t)ROWS, w.rows - row0);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int r = acc_row(e, lane);
@@ -367,35 +445,51 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
             }
         }
 #pragma unroll
-        for (int s = 0; s < KS; ++s) y = mfma(read_row<DP>(gb, lane, s), v[s], y);
+        for (int e = 0; e < 16; ++e) p[e] = fast_exp2(p[e] * c);
+        // KS output gradients, 2 DB of them transposed, 2 DB query rows transposed
+        constexpr int FN = KS + 4 * DB;
+        const auto at = [&](int x) {
+            const int i = x - KS;
+            return x < KS        ? rr.read(x, AT + L::BYTES)
+                   : i < 2 * DB ? rc.read(i % DB, AT + L::BYTES + i / DB * 16 * RB)
+                                : rc.read(i % DB, AT + (i / DB - 2) * 16 * RB);
+        };
+        bf16x8 o;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            // rows 8 (e / 2) + 4 h + 2 (e % 2) and the next
-            const floatx4 st = OLIVE_LDS(floatx4, sb + (8 * (e >> 1) + 4 * h + 2 * (e & 1)) * 8);
-            p[2 * e] = fast_exp2(fmaf(p[2 * e], c, -st[0]));
-            p[2 * e + 1] = fast_exp2(fmaf(p[2 * e + 1], c, -st[2]));
-            y[2 * e] = p[2 * e] * (y[2 * e] - st[1]);
-            y[2 * e + 1] = p[2 * e + 1] * (y[2 * e + 1] - st[3]);
+        for (int n = 0; n < FN / 2; ++n) {
+            if (n + 1 < FN / 2) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) fr[(n + 1) & 1][x] = at(2 * n + 2 + x);
+            }
+            keep_order();
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int x = 2 * n + j, d = (x - KS) % DB, mm = (x - KS) / DB;
+                if (x < KS) {
+                    y = mfma(fr[n & 1][j], v[x < KS ? x : 0], y);
+                } else if (mm < 2) {
+                    if (d == 0) o = pack8(p, mm);
+                    dv[d] = mfma(fr[n & 1][j], o, dv[d]);
+                } else {
+                    if (x == KS + 2 * DB) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) y[e] *= p[e];
+                    }
+                    if (d == 0) o = pack8(y, mm - 2);
+                    dk[d] = mfma(fr[n & 1][j], o, dk[d]);
+                }
+            }
+            keep_order();
         }
-#pragma unroll
-        for (int mm = 0; mm < 2; ++mm) {
-            const bf16x8 x = pack8(p, mm);
-#pragma unroll
-            for (int d = 0; d < DB; ++d)
-                dv[d] = mfma(read_col<DP>(gb + 16 * mm * TileRow<DP>::BYTES, lane, d), x, dv[d]);
-        }
-#pragma unroll
-        for (int mm = 0; mm < 2; ++mm) {
-            const bf16x8 x = pack8(y, mm);
-#pragma unroll
-            for (int d = 0; d < DB; ++d)
-                dk[d] = mfma(read_col<DP>(qb + 16 * mm * TileRow<DP>::BYTES, lane, d), x, dk[d]);
-        }
+    };
+    for (int64_t i = i0; i < i1; i += 2) {
+        step(Const<0>{}, i);
+        if (i + 1 < i1) step(Const<1>{}, i + 1);
     }
     if (key >= w.keys) return;
     if (w.parts == 1) {
-        uint16_t *ko = (uint16_t *)head_row(w.prefix ? a.gkp : a.gks, krow, w.kvh);
-        uint16_t *vo = (uint16_t *)head_row(w.prefix ? a.gvp : a.gvs, krow, w.kvh);
+        uint16_t *ko = (uint16_t *)head_row(pick(w.prefix, a.gkp, a.gks), krow, w.kvh);
+        uint16_t *vo = (uint16_t *)head_row(pick(w.prefix, a.gvp, a.gvs), krow, w.kvh);
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -447,7 +541,7 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(BwdArgs f, int64_t f
             const float4 y = *(const float4 *)(p + (int64_t)k * tiles * KEYS * 2 * a.d);
             s.x += y.x, s.y += y.y, s.z += y.z, s.w += y.w;
         }
-        const HeadsArg &o = kv ? (w.prefix ? a.gvp : a.gvs) : (w.prefix ? a.gkp : a.gks);
+        const HeadsArg o = pick(kv, pick(w.prefix, a.gvp, a.gvs), pick(w.prefix, a.gkp, a.gks));
         uint2 v;
         v.x = pack_bf16x2(s.x, s.y);
         v.y = pack_bf16x2(s.z, s.w);
@@ -480,7 +574,7 @@ int64_t attn_backward_bytes(const AttnArgs &a, bool bf16) {
     if (!attn_mfma_sizes(a, bf16) || a.d > 128) return plain;
     const BwdPlan p = make_plan(a);
     const int64_t tiles = (p.np > 1 ? p.p_units : 0) + (p.ns > 1 ? p.s_units : 0);
-    return (a.total_q * a.hq * (int64_t)sizeof(float2) + 15) / 16 * 16 +
+    return (a.total_q * a.hq * 2 * (int64_t)sizeof(float) + 15) / 16 * 16 +
            tiles * KEYS * 2 * a.d * (int64_t)sizeof(float);
 }
 
@@ -492,8 +586,9 @@ hipError_t launch_attn_backward(const AttnArgs &a, bool bf16, hipStream_t st) {
     f.qd = DieOrder::of(f.p.q_units);
     f.pd = DieOrder::of(f.p.p_units);
     f.sd = DieOrder::of(f.p.s_units);
-    f.stats = (float2 *)a.work;
-    f.part = (float *)(a.work + (a.total_q * a.hq * (int64_t)sizeof(float2) + 15) / 16 * 16);
+    f.nlse = (float *)a.work;
+    f.ndelta = f.nlse + a.total_q * a.hq;
+    f.part = (float *)(a.work + (a.total_q * a.hq * 2 * (int64_t)sizeof(float) + 15) / 16 * 16);
     return a.d <= 64 ? go<64>(f, st) : go<128>(f, st);
 }
 

@@ -111,12 +111,6 @@ __device__ __forceinline__ bool find_group(const AttnArgs &a, int g_heads, int b
     return false;
 }
 
-__device__ __forceinline__ int64_t uniform64(int64_t v) {
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
-    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)v >> 32));
-    return (int64_t)(((uint64_t)hi << 32) | lo);
-}
-
 template <int DP, int WR>
 __device__ __forceinline__ bool find_work(const FwdArgs &f, int64_t block, Work &w) {
     const AttnArgs &a = f.a;
@@ -166,31 +160,10 @@ __device__ __forceinline__ bool find_work(const FwdArgs &f, int64_t block, Work 
     return w.t0 < w.t1 || f.p.direct();
 }
 
-// acc + V^T p^T where some value is not finite and some row does not see its key: that row's
-// weight of it is 0, and the product would make a NaN of it. Rows that see such a value take
-// the product, the others the product without it. `seen` holds 1 where p's key is seen, and
-// `there` all bits where the key is one at all (past the end lie copies of the last one).
-__device__ __forceinline__ floatx16 mfma_special(bf16x8 v, bf16x8 p, uintx4 seen, uintx4 there, floatx16 acc) {
-    const uintx4 u = __builtin_bit_cast(uintx4, v) & there;
-    uintx4 fin, is;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const bool lo = (u[j] & 0x7f80u) == 0x7f80u, hi = (u[j] & 0x7f800000u) == 0x7f800000u;
-        fin[j] = u[j] & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
-        is[j] = (lo ? 0x3f80u : 0u) | (hi ? 0x3f800000u : 0u);
-    }
-    const floatx16 count = mfma(__builtin_bit_cast(bf16x8, is), __builtin_bit_cast(bf16x8, seen), zero16());
-    const floatx16 all = mfma(__builtin_bit_cast(bf16x8, u), p, acc);
-    floatx16 r = mfma(__builtin_bit_cast(bf16x8, fin), p, acc);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) r[i] = count[i] > 0.f ? all[i] : r[i];
-    return r;
-}
-
 // One pass along the key tiles [w.t0, w.t1): out^T (unscaled), the maximum in log2 units and
-// this half's share of the sum, of the query row `lane % 32` of a wavefront. SPECIAL: with
-// mfma_special where rows see different keys.
-template <int DP, int WR, bool SPECIAL>
+// this half's share of the sum, of the query row `lane % 32` of a wavefront. Returns whether a
+// page lay outside the cache.
+template <int DP, int WR>
 __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint32_t lds, int wk, int seen,
                                          int least, const bf16x8 (&q)[DP / 16], floatx16 (&acc)[DP / 32],
                                          float &m, float &l) {
@@ -198,32 +171,49 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
     using L = Loader<DP, KT>;
     const int lane = threadIdx.x & 63;
     const float c = a.scale * kLog2e;
+    constexpr int RB = TileRow<DP>::BYTES, KN = NB * KS, VN = NB * 2 * DB;
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] = zero16();
     m = kNegInf;
     l = 0.f;
+    RowReader<DP> kr;
+    ColReader<DP> vr;
+    kr.open(lds + wk * NB * 32 * RB, lane);
+    vr.open(lds + L::BYTES + wk * NB * 32 * RB, lane);
     L load;
     if (w.t0 < w.t1) {
         load.open(a, w, w.t0 < w.pt);
         load.look_up(a, w, w.t0);
-        load.issue(a, w, w.t0, lds);
+        load.template issue<0>(a, w, w.t0, lds);
         load.look_up(a, w, w.t0 + 1);
     }
-    for (int kt = w.t0; kt < w.t1; ++kt) {
-        const uint32_t kb = lds + ((kt - w.t0) & 1) * 2 * L::BYTES + wk * NB * 32 * TileRow<DP>::BYTES;
-        const uint32_t vb = kb + L::BYTES;
+    const auto step = [&](auto stage, int kt) {
+        constexpr int AT = decltype(stage)::value * 2 * L::BYTES, NEXT = 2 * L::BYTES - AT;
         tile_barrier();
         if (kt + 1 < w.t1) {
-            load.issue(a, w, kt + 1, lds + ((kt + 1 - w.t0) & 1) * 2 * L::BYTES);
+            load.template issue<NEXT>(a, w, kt + 1, lds);
             load.look_up(a, w, kt + 2);
         }
+        // operand i of the scores (block i / KS, step i % KS), then of the outputs (16 keys
+        // i / DB, elements i % DB)
+        bf16x8 f[2][4];
+        const auto k_at = [&](int i) { return kr.read(i % KS, AT + i / KS * 32 * RB); };
+        const auto v_at = [&](int i) { return vr.read(i % DB, AT + i / DB * 16 * RB); };
         floatx16 z[NB];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            z[b] = zero16();
+        for (int i = 0; i < 4; ++i) f[0][i] = k_at(i);
 #pragma unroll
-            for (int s = 0; s < KS; ++s)
-                z[b] = mfma(read_row<DP>(kb + b * 32 * TileRow<DP>::BYTES, lane, s), q[s], z[b]);
+        for (int n = 0; n < KN / 4; ++n) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                f[(n + 1) & 1][i] = 4 * (n + 1) < KN ? k_at(4 * (n + 1) + i) : v_at(i);
+            keep_order();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int x = 4 * n + i, b = x / KS, s = x % KS;
+                z[b] = mfma(f[n & 1][i], q[s], s == 0 ? zero16() : z[b]);
+            }
+            keep_order();
         }
         // masks: the end of the prefix, and the suffix keys that a row does not see
         const bool pre = kt < w.pt;
@@ -254,36 +244,108 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
             for (int d = 0; d < DB; ++d) acc[d] *= r;
         }
         const float m0 = m == kNegInf ? 0.f : m;
+        bf16x8 p;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            float sum = 0.f;
+        for (int n = 0; n < VN / 4; ++n) {
+            constexpr int V0 = KN / 4;               // where the values' first group lies in f
+            if (n + 1 < VN / 4) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                z[b][i] = fast_exp2(fmaf(z[b][i], c, -m0));
-                sum += z[b][i];
+                for (int i = 0; i < 4; ++i) f[(V0 + n + 1) & 1][i] = v_at(4 * (n + 1) + i);
             }
-            l += sum;
+            keep_order();
 #pragma unroll
-            for (int mm = 0; mm < 2; ++mm) {
-                const bf16x8 p = pack8(z[b], mm);
-                const uint32_t base = vb + (32 * b + 16 * mm) * TileRow<DP>::BYTES;
-                uintx4 on, there;
+            for (int i = 0; i < 4; ++i) {
+                const int x = 4 * n + i, d = x % DB, b = x / DB / 2, mm = x / DB % 2;
+                if (d == 0) {
+                    // the weights of the next 16 keys
+                    float sum = 0.f;
 #pragma unroll
-                for (int i = 0; SPECIAL && i < 4; ++i) {
-                    const int j = j0 + 32 * b + acc_row(8 * mm + 2 * i, lane), end = pre ? w.s.plen : w.s.slen;
-                    on[i] = (j < limit ? 0x3f80u : 0u) | (j + 1 < limit ? 0x3f800000u : 0u);
-                    there[i] = (j < end ? 0xffffu : 0u) | (j + 1 < end ? 0xffff0000u : 0u);
+                    for (int e = 8 * mm; e < 8 * mm + 8; ++e) {
+                        z[b][e] = fast_exp2(fmaf(z[b][e], c, -m0));
+                        sum += z[b][e];
+                    }
+                    l += sum;
+                    p = pack8(z[b], mm);
                 }
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const bf16x8 v = read_col<DP>(base, lane, d);
-                    acc[d] = SPECIAL ? mfma_special(v, p, on, there, acc[d])
-                                     : mfma(v, p, acc[d]);
-                }
+                acc[d] = mfma(f[(V0 + n) & 1][i], p, acc[d]);
             }
+            keep_order();
         }
+    };
+    for (int kt = w.t0; kt < w.t1; kt += 2) {
+        step(Const<0>{}, kt);
+        if (kt + 1 < w.t1) step(Const<1>{}, kt + 1);
     }
     return load.bad;
+}
+
+// A value that is not finite makes a NaN of the product also in rows that do not see its key
+// (their weight of it is 0). Where a unit's result is not finite and such a value lies among
+// the keys that not all its rows see, its rows are formed again one by one, each over the keys
+// that it sees. False: there is none.
+template <int KT>
+__device__ __forceinline__ bool row_by_row(const FwdArgs &f, const Work &w, int bm) {
+    const AttnArgs &a = f.a;
+    const int g = a.hq / a.hk, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (w.t0 >= w.t1) return false;
+    bool off_table = false;
+    const auto key_row = [&](bool pre, int j) { return pre ? w.s.pstart + j : suffix_row(a, w.s, j, off_table); };
+    {
+        bool found = false;
+        const auto look = [&](bool pre, int j) {
+            const uint16_t *v = head_row(pick(pre, a.vp, a.vs), key_row(pre, j), w.kvh);
+            for (int e = lane; e < a.d; e += 64) found |= (v[e] & 0x7f80) == 0x7f80;
+        };
+        const int s0 = suffix_seen(w.s, (int)(w.r0 / g));
+        for (int j = max(0, min(s0, w.s.slen - 1)) + wave; j < w.s.slen; j += 4) look(false, j);
+        if (w.s.plen > 0) look(true, w.s.plen - 1);   // (copies of it stand for keys past the end)
+        if (!__syncthreads_or(found)) return false;
+    }
+    for (int64_t row = w.r0 + wave; row < min(w.rows, w.r0 + bm); row += 4) {
+        const int tok = (int)(row / g), head = w.kvh * g + (int)(row - (int64_t)tok * g);
+        const int64_t t = w.s.q0 + tok;
+        const int seen = suffix_seen(w.s, tok);
+        const uint16_t *q = head_row(a.q, t, head);
+        float x[4], o[4] = {}, m = kNegInf, l = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = lane + 64 * i < a.d ? load_elem<uint16_t>(q, lane + 64 * i) : 0.f;
+        for (int kt = w.t0; kt < w.t1; ++kt) {
+            const bool pre = kt < w.pt;
+            const int j0 = (pre ? kt : kt - w.pt) * KT, end = min(j0 + KT, pre ? w.s.plen : seen);
+            for (int j = j0; j < end; ++j) {
+                const int64_t at = key_row(pre, j);
+                const uint16_t *k = head_row(pick(pre, a.kp, a.ks), at, w.kvh), *v = head_row(pick(pre, a.vp, a.vs), at, w.kvh);
+                float z = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (lane + 64 * i < a.d) z = fmaf(x[i], load_elem<uint16_t>(k, lane + 64 * i), z);
+                for (int s = 32; s > 0; s >>= 1) z += __shfl_xor(z, s);
+                z *= a.scale * kLog2e;
+                const float m2 = fmaxf(m, z), r = m2 == m ? 1.f : fast_exp2(m - m2);
+                const float p = z == kNegInf ? 0.f : fast_exp2(z - m2);
+                m = m2;
+                l = l * r + p;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (lane + 64 * i < a.d) o[i] = fmaf(p, load_elem<uint16_t>(v, lane + 64 * i), o[i] * r);
+            }
+        }
+        if (__any(off_table)) l = __builtin_nanf("");
+        const int64_t orow = t * a.hq + head, slot = (int64_t)w.part * a.total_q * a.hq + orow;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = lane + 64 * i;
+            if (e >= a.d) continue;
+            if (f.p.direct()) ((uint16_t *)head_row(a.o, t, head))[e] = (uint16_t)pack_bf16x2(o[i] * inv, 0.f);
+            else f.po[slot * a.d + e] = o[i];
+        }
+        if (lane == 0) {
+            if (!f.p.direct()) f.pml[slot] = make_float2(m, l);
+            else if (a.lse) a.lse[orow] = l == 0.f ? kNegInf : (m + fast_log2(l)) * kLn2;
+        }
+    }
+    return true;
 }
 
 template <int DP, int WR>
@@ -294,6 +356,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
     const AttnArgs &a = f.a;
     Work w;
     if (!find_work<DP, WR>(f, blockIdx.x, w)) return;
+    make_uniform(w);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wr = wave / WK, wk = wave % WK, h = lane >> 5;
     const int g = a.hq / a.hk, nch = a.d >> 3;
@@ -320,17 +383,14 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
     const int least = suffix_seen(w.s, (int)(min(w.r0 + 32 * wr, w.rows - 1) / g));
     floatx16 acc[DB];
     float m, l;
-    bool off_table = key_loop<DP, WR, false>(a, w, lds, wk, seen, least, q, acc, m, l);
+    const bool off_table = key_loop<DP, WR>(a, w, lds, wk, seen, least, q, acc, m, l);
     {
-        // A value that is not finite leaves a NaN also in rows that do not see its key: such
-        // a result is formed again with these rows' weights of it left out.
         float s = 0.f;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s = fmaf(acc[d][i], 0.f, s);
-        if (__syncthreads_or(!(s == 0.f)))
-            off_table = key_loop<DP, WR, true>(a, w, lds, wk, seen, least, q, acc, m, l);
+        if (__syncthreads_or(!(s == 0.f)) && row_by_row<KT>(f, w, 32 * WR)) return;
     }
     l += __shfl_xor(l, 32);
 
@@ -496,10 +556,10 @@ hipError_t go(const FwdArgs &f, hipStream_t st) {
     return e;
 }
 
-// Rows on 16 bytes, and the offsets of 128 of them in 32 bits.
-bool rows_on_16(const HeadsArg &h) {
+// Rows on 16 bytes, and the offsets of 128 of them, or of a group's heads, in 32 bits.
+bool rows_on_16(const HeadsArg &h, int g) {
     return !h.p || ((((uintptr_t)h.p | (uint64_t)(h.st * 2) | (uint64_t)(h.sh * 2)) & 15) == 0 &&
-                    h.st >= 0 && h.st < (1 << 23));
+                    h.st >= 0 && h.st < (1 << 23) && h.sh >= 0 && h.sh < (1 << 29) / g);
 }
 
 }  // namespace
@@ -511,7 +571,7 @@ bool attn_mfma_applies(const AttnArgs &a, bool bf16) {
     if (!attn_mfma_sizes(a, bf16)) return false;
     for (const HeadsArg *h : {&a.q, &a.kp, &a.vp, &a.ks, &a.vs, &a.o, &a.go, &a.gq, &a.gkp, &a.gvp, &a.gks,
                               &a.gvs})
-        if (!rows_on_16(*h)) return false;
+        if (!rows_on_16(*h, a.hq / a.hk)) return false;
     return true;
 }
 

@@ -39,6 +39,18 @@ __device__ __forceinline__ void tile_barrier() {
     compiler_fence();
 }
 
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)v >> 32));
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+// dma16_sv (mfma_pipe.hpp) from a base that is the same for every lane, wherever it is held.
+template <int OFF>
+__device__ __forceinline__ void dma16_from(const char *base, uint32_t voff, uint32_t la) {
+    dma16_sv<OFF>((const char *)uniform64((int64_t)base), voff, la);
+}
+
 // dma16 (mfma_pipe.hpp) with 4 bytes a lane.
 __device__ __forceinline__ void dma4(const char *g, uint32_t la) {
     la = __builtin_amdgcn_readfirstlane(la);
@@ -48,33 +60,55 @@ __device__ __forceinline__ void dma4(const char *g, uint32_t la) {
 #pragma clang diagnostic pop
 }
 
-// First operand (rows x K): row `r0 + lane % 32`, chunk 2 step + lane / 32.
-template <int DP>
-__device__ __forceinline__ bf16x8 read_row(uint32_t base, int lane, int step) {
-    const int r = lane & 31, c = 2 * step + (lane >> 5);
-    return OLIVE_LDS(bf16x8, base + r * TileRow<DP>::BYTES + ((c ^ TileRow<DP>::swz(r)) << 4));
+// Keeps an address in its register: the compiler would otherwise form it again at each use
+// rather than add a constant to it in the read.
+__device__ __forceinline__ uint32_t pinned(uint32_t x) {
+    asm("" : "+v"(x));
+    return x;
 }
 
+// First operand (rows x K) of a 32-row block: row lane % 32, chunk 2 step + lane / 32.
 template <int DP>
-__device__ __forceinline__ void write_row(uint32_t base, int lane, int step, bf16x8 x) {
-    const int r = lane & 31, c = 2 * step + (lane >> 5);
-    OLIVE_LDS(bf16x8, base + r * TileRow<DP>::BYTES + ((c ^ TileRow<DP>::swz(r)) << 4)) = x;
-}
+struct RowReader {
+    uint32_t at[DP / 16];
+    __device__ __forceinline__ void open(uint32_t base, int lane) {
+        const int r = lane & 31;
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s)
+            at[s] = pinned(base + r * TileRow<DP>::BYTES + (((2 * s + (lane >> 5)) ^ TileRow<DP>::swz(r)) << 4));
+    }
+    __device__ __forceinline__ bf16x8 read(int step, int offset) const { return OLIVE_LDS(bf16x8, at[step] + offset); }
+    __device__ __forceinline__ void write(int step, int offset, bf16x8 x) const { OLIVE_LDS(bf16x8, at[step] + offset) = x; }
+};
 
-// First operand transposed (elements x rows): lane % 32 is the element 32 db + lane % 32, the
-// 8 values are rows 4 (lane / 32) + 0..3 and 8 more: the rows whose results a lane of the same
-// half holds in registers 0..7 of a 32 x 32 product. `base` is row 16 m of the tile.
+// First operand transposed (elements x rows) of a 16-row block: lane % 32 is the element
+// 32 db + lane % 32, the 8 values are rows 4 (lane / 32) + 0..3 and 8 more: the rows whose
+// results a lane of the same half holds in 8 registers of a 32 x 32 product.
 template <int DP>
-__device__ __forceinline__ bf16x8 read_col(uint32_t base, int lane, int db) {
-    const int h = lane >> 5, r4 = (lane & 15) >> 2;
-    const int c = 4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    const int r0 = 4 * h + r4, r1 = r0 + 8;
-    const uint32_t a0 = base + r0 * TileRow<DP>::BYTES + ((c ^ TileRow<DP>::swz(r0)) << 4) + (lane & 1) * 8;
-    const uint32_t a1 = base + r1 * TileRow<DP>::BYTES + ((c ^ TileRow<DP>::swz(r1)) << 4) + (lane & 1) * 8;
-    const shortx4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(&OLIVE_LDS(shortx4, a0));
-    const shortx4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(&OLIVE_LDS(shortx4, a1));
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-}
+struct ColReader {
+    uint32_t at[DP / 32][2];
+    __device__ __forceinline__ void open(uint32_t base, int lane) {
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r = 8 * j + 4 * (lane >> 5) + ((lane & 15) >> 2);
+                const int c = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+                at[d][j] = pinned(base + r * TileRow<DP>::BYTES + ((c ^ TileRow<DP>::swz(r)) << 4) + (lane & 1) * 8);
+            }
+    }
+    __device__ __forceinline__ bf16x8 read(int db, int offset) const {
+        const shortx4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(&OLIVE_LDS(shortx4, at[db][0] + offset));
+        const shortx4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(&OLIVE_LDS(shortx4, at[db][1] + offset));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+// Operand reads run a group of four ahead of the products that use them: LDS reads and
+// products keep their order here, other instructions may move across.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x6); }
+
+template <int N> struct Const { static constexpr int value = N; };
 
 // Registers 8 m .. 8 m + 7 of a 32 x 32 product as the second operand of the next one.
 __device__ __forceinline__ bf16x8 pack8(const floatx16 &s, int m) {
@@ -133,6 +167,12 @@ __device__ __forceinline__ void part_range(int tiles, int n, int i, int &t0, int
     t1 = (int)((int64_t)tiles * (i + 1) / n);
 }
 
+// One of two views, field by field: a reference that is chosen at run time would put all of a
+// kernel's arguments into memory.
+__device__ __forceinline__ HeadsArg pick(bool first, HeadsArg x, HeadsArg y) {
+    return HeadsArg{first ? x.p : y.p, first ? x.st : y.st, first ? x.sh : y.sh};
+}
+
 // What one workgroup does.
 struct Work {
     SeqView s;
@@ -142,6 +182,26 @@ struct Work {
     int pt;                          // prefix tiles come first
     int t0, t1;
 };
+
+// The same for every lane, which the compiler cannot always tell from where it came from.
+__device__ __forceinline__ int uniform32(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ void make_uniform(Work &w) {
+    w.s.q0 = uniform64(w.s.q0);
+    w.s.n = uniform32(w.s.n);
+    w.s.plen = uniform32(w.s.plen);
+    w.s.slen = uniform32(w.s.slen);
+    w.s.pstart = uniform64(w.s.pstart);
+    w.s.sstart = uniform64(w.s.sstart);
+    w.s.pages = (const int32_t *)uniform64((int64_t)w.s.pages);
+    w.s.bad = uniform32(w.s.bad);
+    w.rows = uniform64(w.rows);
+    w.r0 = uniform64(w.r0);
+    w.kvh = uniform32(w.kvh);
+    w.part = uniform32(w.part);
+    w.pt = uniform32(w.pt);
+    w.t0 = uniform32(w.t0);
+    w.t1 = uniform32(w.t1);
+}
 
 // Keys and values on their way into LDS. A wavefront loads KT / 4 rows of each of a tile; rows
 // past the end are copies of the last one (their scores are masked).
@@ -160,7 +220,7 @@ struct Loader {
     bool bad = false;
 
     __device__ __forceinline__ void open(const AttnArgs &a, const Work &w, bool pre) {
-        const HeadsArg &kh = pre ? a.kp : a.ks, &vh = pre ? a.vp : a.vs;
+        const HeadsArg kh = pick(pre, a.kp, a.ks), vh = pick(pre, a.vp, a.vs);
         const int64_t at = pre ? w.s.pstart : w.s.sstart;
         kst = kh.st * 2;
         vst = vh.st * 2;
@@ -185,34 +245,61 @@ struct Loader {
 #pragma unroll
         for (int n = 0; n < N; ++n) page[n] = w.s.pages[page_of(a, min(j0 + row(n), w.s.slen - 1))];
     }
-    __device__ __forceinline__ void issue(const AttnArgs &a, const Work &w, int t, uint32_t lds) {
+    // Tile t to stage offset AT of the ring that begins at `ring`.
+    template <int AT>
+    __device__ __forceinline__ void issue(const AttnArgs &a, const Work &w, int t, uint32_t ring) {
         if (t == w.pt && t != w.t0) open(a, w, false);
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int nch = a.d / 8;
-        const int j0 = (t - tile0) * KT, last = len - 1 - j0;
-        const char *kt = k + j0 * kst, *vt = v + j0 * vst;
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int full = row(n), r = min(full, last);
-            const int ch = (lane & (R::CHUNKS - 1)) ^ R::swz(full), c = ch * 16;
-            if (ch >= nch) continue;      // the slots past head_dim keep their zeros
-            const uint32_t to = lds + (wave * (KT / 4) + n * R::PER_DMA) * R::BYTES;
-            if (paged) {
-                const int j = j0 + r;
-                int64_t at = (int64_t)page[n] * a.page_size;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int nch = a.d / 8, j0 = (t - tile0) * KT, last = len - 1 - j0;
+        ring += wave * (KT / 4) * R::BYTES;
+        if (paged) {
+            each<AT>([&](auto n, int ch) {
+                const int j = j0 + min(row(n.value), last);
+                int64_t at = (int64_t)page[n.value] * a.page_size;
                 if (at < 0 || at > a.suffix_rows - a.page_size) {
                     bad = true;
                     at = 0;
                 } else {
                     at += j - page_of(a, j) * a.page_size;
                 }
-                dma16(k + at * kst + c, to);
-                dma16(v + at * vst + c, to + BYTES);
-            } else {
-                // the launcher takes strides for which a tile's offsets fit 32 bits
-                dma16_sv<0>(kt, (uint32_t)r * (uint32_t)kst + c, to);
-                dma16_sv<0>(vt, (uint32_t)r * (uint32_t)vst + c, to + BYTES);
-            }
+                if (ch < nch) {
+                    dma16_at<n.to>(k + at * kst + ch * 16, ring);
+                    dma16_at<n.to + BYTES>(v + at * vst + ch * 16, ring);
+                }
+            });
+            return;
+        }
+        // the launcher takes strides for which a tile's offsets fit 32 bits
+        const char *kt = k + j0 * kst, *vt = v + j0 * vst;
+        if (last >= KT - 1) {
+            const uint32_t ro = row(0) * (uint32_t)kst, vo = row(0) * (uint32_t)vst;
+            each<AT>([&](auto n, int ch) {
+                if (ch < nch) {
+                    dma16_from<n.to>(kt + n.value * R::PER_DMA * kst, ro + ch * 16, ring);
+                    dma16_from<n.to + BYTES>(vt + n.value * R::PER_DMA * vst, vo + ch * 16, ring);
+                }
+            });
+        } else {
+            each<AT>([&](auto n, int ch) {
+                const uint32_t r = min(row(n.value), last);
+                if (ch < nch) {
+                    dma16_from<n.to>(kt, r * (uint32_t)kst + ch * 16, ring);
+                    dma16_from<n.to + BYTES>(vt, r * (uint32_t)vst + ch * 16, ring);
+                }
+            });
+        }
+    }
+
+  private:
+    template <int I, int TO>
+    struct Load { static constexpr int value = I, to = TO; };
+    // f(load, chunk of the row that this lane takes) for each of the wavefront's loads; the
+    // slots past head_dim keep their zeros
+    template <int AT, int I = 0, typename F>
+    static __device__ __forceinline__ void each(F f) {
+        if constexpr (I < N) {
+            f(Load<I, AT + I * 1024>{}, (threadIdx.x & (R::CHUNKS - 1)) ^ R::swz(row(I)));
+            each<AT, I + 1>(f);
         }
     }
 };
