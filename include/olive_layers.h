@@ -135,7 +135,8 @@ typedef struct {
     int32_t heads_kv;            /* >= 1 */
     int32_t head_dim;            /* in [1, 256] */
     int32_t max_q;               /* >= 1: most queries of a sequence */
-    int64_t total_q;             /* cu_q[B] (host copy of it), >= 0 (0: nothing is done) */
+    int64_t total_q;             /* cu_q[B] (host copy of it), >= 0 (0: nothing is done);
+                                    total_q * heads_q < 2^31 */
     int64_t max_prefix;          /* >= 0, < 2^31: longest prefix */
     int64_t max_suffix;          /* >= 0, < 2^31: longest suffix */
     int64_t prefix_rows;         /* rows of the prefix keys and values */

@@ -57,6 +57,7 @@ struct BwdArgs {
     AttnArgs a;
     BwdPlan p;
     DieOrder qd, pd, sd;
+    Div g, seqs, groups, qtiles, ptiles, stiles, pall, sall, np, ns;   // (pall, sall: tiles of a part)
     // [hk][total_q][g] each: what the products of a row begin at, so that z is scale^-1 (scale q
     // k - lse) and y is dp - delta
     float *nlse;                     // -lse / scale, -inf for a row that sees nothing
@@ -71,9 +72,8 @@ __global__ __launch_bounds__(256) void attn_stats_kernel(BwdArgs f) {
     constexpr int LPR = DP / 8;
     const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPR;
     const int c = threadIdx.x % LPR, nch = a.d / 8, g = a.hq / a.hk;
-    if (r >= a.total_q * a.hq) return;
-    const int64_t t = r / a.hq;
-    const int head = (int)(r - t * a.hq);
+    if (r >= (int64_t)a.total_q * a.hq) return;
+    const int t = (int)r / a.hq, head = (int)r - t * a.hq;
     const uintx4 x = __builtin_bit_cast(uintx4, load_chunk(head_row(a.o, t, head), c, nch));
     const uintx4 y = __builtin_bit_cast(uintx4, load_chunk(head_row(a.go, t, head), c, nch));
     float s = 0.f;
@@ -99,40 +99,42 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f) {
     extern __shared__ __attribute__((aligned(1024))) char lds_mem[];
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
     const AttnArgs &a = f.a;
-    int64_t u = f.qd.unit(blockIdx.x);
+    int u = f.qd.unit(blockIdx.x);
     if (u >= f.qd.units) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int h = lane >> 5, g = a.hq / a.hk, nch = a.d >> 3;
+    const int h = lane >> 5, g = f.g.d, nch = a.d >> 3;
+    int v = f.qtiles.quot(u);
     // the last row tiles of a sequence, which see the most keys, come first
-    const int rt = f.p.qtiles - 1 - (int)(u % f.p.qtiles);
-    u /= f.p.qtiles;
+    const int rt = f.p.qtiles - 1 - f.qtiles.rem(u, v);
+    u = v;
+    v = f.seqs.quot(u);
     Work w;
-    w.s = load_seq(a, (int)(u % a.seqs));
-    w.kvh = (int)(u / a.seqs);
+    w.s = load_seq(a, f.seqs.rem(u, v));
+    w.kvh = v;
     w.part = 0;
-    w.rows = (int64_t)w.s.n * g;
-    w.r0 = (int64_t)rt * 128;
+    w.rows = w.s.n * g;
+    w.r0 = rt * 128;
     if (w.s.skip || w.r0 >= w.rows) return;
     if (w.s.bad) {
-        for (int64_t i = threadIdx.x; rt == 0 && i < w.rows * a.d; i += 256) {
-            const int64_t r = i / a.d, k = r / g;
-            ((uint16_t *)a.gq.p)[(w.s.q0 + k) * a.gq.st + (w.kvh * g + (r - k * g)) * a.gq.sh + (i - r * a.d)] =
-                0x7fc0;
+        for (int r = threadIdx.x; rt == 0 && r < w.rows; r += 256) {
+            const int k = f.g.quot(r);
+            for (int e = 0; e < a.d; ++e)
+                ((uint16_t *)head_row(a.gq, w.s.q0 + k, w.kvh * g + f.g.rem(r, k)))[e] = 0x7fc0;
         }
         return;
     }
-    w.pt = (int)ceil_div(w.s.plen, KT);
+    w.pt = tiles_of<KT>(w.s.plen);
     w.t0 = 0;
-    w.t1 = w.pt + (int)ceil_div(suffix_seen(w.s, (int)((min(w.rows, w.r0 + 128) - 1) / g)), KT);
+    w.t1 = w.pt + tiles_of<KT>(suffix_seen(w.s, f.g.quot(min(w.rows, w.r0 + 128) - 1)));
     make_uniform(w);
     if (nch < DP / 8) {
         for (int i = threadIdx.x; i < 2 * 2 * KT * DP / 8; i += 256)
             ((uint4 *)lds_mem)[i] = make_uint4(0u, 0u, 0u, 0u);
         __syncthreads();
     }
-    const int64_t row = w.r0 + 32 * wave + (lane & 31), crow = min(row, w.rows - 1);
-    const int tok = (int)(crow / g), head = w.kvh * g + (int)(crow - (int64_t)tok * g);
-    const int64_t t = w.s.q0 + tok;
+    const int row = w.r0 + 32 * wave + (lane & 31), crow = min(row, w.rows - 1);
+    const int tok = f.g.quot(crow), head = w.kvh * g + f.g.rem(crow, tok);
+    const int t = w.s.q0 + tok;
     bf16x8 q[KS], go[KS];
     {
         const uint16_t *p = head_row(a.q, t, head), *o = head_row(a.go, t, head);
@@ -142,10 +144,10 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f) {
             go[s] = load_chunk(o, 2 * s + h, nch);
         }
     }
-    const int64_t at = (int64_t)w.kvh * a.total_q * g + w.s.q0 * g + crow;
+    const int64_t at = ((int64_t)w.kvh * a.total_q + w.s.q0) * g + crow;
     const float ndelta = f.ndelta[at];
     const int seen = suffix_seen(w.s, tok);
-    const int least = suffix_seen(w.s, (int)(min(w.r0 + 32 * wave, w.rows - 1) / g));
+    const int least = suffix_seen(w.s, f.g.quot(min(w.r0 + 32 * wave, w.rows - 1)));
     const float c = a.scale * kLog2e;
     floatx16 acc[DB];
 #pragma unroll
@@ -236,30 +238,29 @@ struct KeyWork {
     bool prefix;
     int keys, j0;                    // keys of the prefix or suffix, the first of this tile
     int64_t krow;                    // row of its first key
-    int64_t q0, rows;                // the rows begin at token q0
+    int q0, rows;                    // the rows begin at token q0
     int first;                       // suffix keys that query 0 sees, less one
     int kvh, part, parts;
-    int64_t tile;                    // index of the tile among all of its kind (fp32 parts)
+    int tile;                        // index of the tile among all of its kind (fp32 parts)
 };
 
 // v: tile x owner x key head x part (tiles of one owner and head first: they read the same rows)
-__device__ __forceinline__ bool find_keys(const BwdArgs &f, bool prefix, int64_t v, KeyWork &w) {
+__device__ __forceinline__ bool find_keys(const BwdArgs &f, bool prefix, int v, KeyWork &w) {
     const AttnArgs &a = f.a;
     w.prefix = prefix;
-    const int tiles = w.prefix ? f.p.ptiles : f.p.stiles, owners = w.prefix ? a.groups : a.seqs;
-    w.parts = w.prefix ? f.p.np : f.p.ns;
-    const int64_t all = (int64_t)tiles * owners * a.hk;
-    w.part = (int)(v / all);
-    w.tile = v % all;
-    const int own = (int)(w.tile / tiles % owners);
-    w.j0 = (int)(w.tile % tiles) * KEYS;
-    w.kvh = (int)(w.tile / ((int64_t)tiles * owners));
-    const int g = a.hq / a.hk;
+    const Div &tiles = prefix ? f.ptiles : f.stiles, &owners = prefix ? f.groups : f.seqs;
+    w.parts = prefix ? f.p.np : f.p.ns;
+    w.part = (prefix ? f.pall : f.sall).quot(v);
+    w.tile = (prefix ? f.pall : f.sall).rem(v, w.part);
+    const int x = tiles.quot(w.tile);
+    w.j0 = tiles.rem(w.tile, x) * KEYS;
+    w.kvh = owners.quot(x);
+    const int own = owners.rem(x, w.kvh), g = f.g.d;
     w.first = 0;
     if (w.prefix) {
         const int b0 = a.group_seqs[own], b1 = a.group_seqs[own + 1];
         if (b0 < 0 || b1 < b0 || b1 > a.seqs || !prefix_ok(a, own)) return false;
-        const int64_t q0 = a.cu_q[b0], q1 = a.cu_q[b1];
+        const int q0 = a.cu_q[b0], q1 = a.cu_q[b1];
         if (q0 < 0 || q1 < q0 || q1 > a.total_q) return false;
         w.keys = a.prefix_len[own];
         w.krow = a.prefix_start[own];
@@ -271,14 +272,14 @@ __device__ __forceinline__ bool find_keys(const BwdArgs &f, bool prefix, int64_t
         w.keys = s.slen;
         w.krow = s.sstart;
         w.q0 = s.q0;
-        w.rows = (int64_t)s.n * g;
+        w.rows = s.n * g;
         w.first = s.slen - s.n;
     }
     w.keys = uniform32(w.keys);
     w.j0 = uniform32(w.j0);
     w.krow = uniform64(w.krow);
-    w.q0 = uniform64(w.q0);
-    w.rows = uniform64(w.rows);
+    w.q0 = uniform32(w.q0);
+    w.rows = uniform32(w.rows);
     w.first = uniform32(w.first);
     return w.j0 < w.keys;
 }
@@ -293,17 +294,17 @@ struct RowLoader {
     static constexpr int STAGE = 2 * BYTES + 1024;
     int g, step_t, step_r;           // heads of a group; ROWS / g and ROWS % g
     float inv_g;
-    int64_t tok;                     // token of the tile's first row, and its head in the group
-    int rem;
-    int64_t left;                    // rows from the tile's first to the end
+    int tok, rem;                    // token of the tile's first row, and its head in the group
+    int left;                        // rows from the tile's first to the end
 
-    __device__ __forceinline__ void open(const KeyWork &w, int g_, int64_t r0) {
-        g = g_;
-        step_t = ROWS / g;
-        step_r = ROWS % g;
+    __device__ __forceinline__ void open(const BwdArgs &f, const KeyWork &w, int r0) {
+        g = f.g.d;
+        step_t = f.g.quot(ROWS);
+        step_r = f.g.rem(ROWS, step_t);
         inv_g = 1.f / (float)g;
-        tok = w.q0 + r0 / g;
-        rem = (int)(r0 % g);
+        const int k = f.g.quot(r0);
+        tok = w.q0 + k;
+        rem = f.g.rem(r0, k);
         left = w.rows - r0;
     }
     // (each call takes the next tile)
@@ -311,7 +312,7 @@ struct RowLoader {
         const AttnArgs &a = f.a;
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int nch = a.d / 8;
-        const int last = (int)min(left, (int64_t)ROWS) - 1;
+        const int last = min(left, ROWS) - 1;
         const char *qb = a.q.p + (tok * a.q.st + (int64_t)w.kvh * g * a.q.sh) * 2;
         const char *gb = a.go.p + (tok * a.go.st + (int64_t)w.kvh * g * a.go.sh) * 2;
 #pragma unroll
@@ -350,11 +351,11 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
     const AttnArgs &a = f.a;
     KeyWork w;
-    const bool pre = blockIdx.x < f.pd.blocks();
-    const int64_t u = pre ? f.pd.unit(blockIdx.x) : f.sd.unit(blockIdx.x - f.pd.blocks());
+    const bool pre = (int)blockIdx.x < f.pd.blocks;
+    const int u = pre ? f.pd.unit(blockIdx.x) : f.sd.unit(blockIdx.x - f.pd.blocks);
     if (u >= (pre ? f.pd.units : f.sd.units) || !find_keys(f, pre, u, w)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int h = lane >> 5, g = a.hq / a.hk, nch = a.d >> 3;
+    const int h = lane >> 5, g = f.g.d, nch = a.d >> 3;
     if (nch < DP / 8) {
         for (int i = threadIdx.x; i < 2 * L::STAGE / 16; i += 256)
             ((uint4 *)lds_mem)[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -384,24 +385,23 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
 #pragma unroll
     for (int d = 0; d < DB; ++d) dk[d] = dv[d] = zero16();
     // this part's tiles of the rows from the first that sees the tile's first key
-    int64_t r0 = w.prefix ? 0 : (int64_t)max(0, w.j0 - w.first) * g / ROWS * ROWS;
-    const int64_t all = w.rows > r0 ? ceil_div(w.rows - r0, ROWS) : 0;
-    const int64_t i0 = all * w.part / w.parts, i1 = all * (w.part + 1) / w.parts;
+    // (64 bits: max_suffix keys by g rows)
+    const auto row_of = [&](int j) { return w.prefix ? 0 : (int)min((int64_t)w.rows, (int64_t)max(0, j - w.first) * g); };
+    int r0 = row_of(w.j0) / ROWS * ROWS, i0, i1;
+    part_range(tiles_of<ROWS>(w.rows - r0), w.prefix ? f.np : f.ns, w.part, i0, i1);
     r0 += i0 * ROWS;
     // the first rows that see this lane's key, and this wavefront's last and first one
-    const int64_t from = w.prefix ? 0 : (int64_t)max(0, key - w.first) * g;
-    const int64_t from_hi = w.prefix ? 0 : (int64_t)max(0, w.j0 + 32 * wave + 31 - w.first) * g;
-    const int64_t from_lo = w.prefix ? 0 : (int64_t)max(0, w.j0 + 32 * wave - w.first) * g;
+    const int from = row_of(key), from_hi = row_of(w.j0 + 32 * wave + 31), from_lo = row_of(w.j0 + 32 * wave);
     L load;
     if (i0 < i1) {
-        load.open(w, g, r0);
+        load.open(f, w, r0);
         load.issue(f, w, lds);
     }
-    const auto step = [&](auto stage, int64_t i) {
+    const auto step = [&](auto stage, int i) {
         constexpr int AT = decltype(stage)::value * L::STAGE, NEXT = L::STAGE - AT;
         tile_barrier();
         if (i + 1 < i1) load.issue(f, w, lds + NEXT);
-        const int64_t row0 = r0;
+        const int row0 = r0;
         r0 += ROWS;
         if (r0 <= from_lo) return;                   // no row of the tile sees this wavefront's keys
         floatx16 p, y;
@@ -436,8 +436,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
             keep_order();
         }
         if (r0 > w.rows || row0 < from_hi) {
-            const int lo = (int)min((int64_t)ROWS, max((int64_t)0, from - row0));
-            const int hi = (int)min((int64_t)ROWS, w.rows - row0);
+            const int lo = max(0, from - row0), hi = w.rows - row0;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int r = acc_row(e, lane);
@@ -482,7 +481,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
             keep_order();
         }
     };
-    for (int64_t i = i0; i < i1; i += 2) {
+    for (int i = i0; i < i1; i += 2) {
         step(Const<0>{}, i);
         if (i + 1 < i1) step(Const<1>{}, i + 1);
     }
@@ -507,9 +506,9 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
         return;
     }
     // [part][tile][key][dk, dv][d], after the prefix's where both have parts
-    const int64_t tiles = (w.prefix ? f.p.p_units : f.p.s_units) / w.parts;
+    const int64_t tiles = w.prefix ? f.pall.d : f.sall.d;
     const int64_t before = w.prefix || f.p.np == 1 ? 0 : f.p.p_units * KEYS * 2 * a.d;
-    float *o = f.part + before + ((w.part * tiles + w.tile) * KEYS + (key - w.j0)) * 2 * a.d;
+    float *o = f.part + before + (((int64_t)w.part * tiles + w.tile) * KEYS + (key - w.j0)) * 2 * a.d;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -523,19 +522,19 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
 }
 
 // Adds the parts of a tile's gradients: a workgroup a tile.
-__global__ __launch_bounds__(256) void attn_dkv_join_kernel(BwdArgs f, int64_t first) {
+__global__ __launch_bounds__(256) void attn_dkv_join_kernel(BwdArgs f, int first) {
     const AttnArgs &a = f.a;
-    const int64_t pt = f.p.p_units / f.p.np;
-    const int64_t i = first + blockIdx.x;              // tiles of the prefixes, then of the suffixes
+    const int pt = (int)(f.p.p_units ? f.pall.d : 0);
+    const int i = first + blockIdx.x;              // tiles of the prefixes, then of the suffixes
     KeyWork w;
     if (!find_keys(f, i < pt, i < pt ? i : i - pt, w) || w.parts == 1) return;
-    const int64_t tiles = (w.prefix ? f.p.p_units : f.p.s_units) / w.parts;
+    const int64_t tiles = w.prefix ? f.pall.d : f.sall.d;
     const int64_t before = w.prefix || f.p.np == 1 ? 0 : f.p.p_units * KEYS * 2 * a.d;
     const int quads = a.d / 4;
     const int n = min(KEYS, w.keys - w.j0) * 2 * quads;
     for (int x = threadIdx.x; x < n; x += 256) {
         const int e = 4 * (x % quads), kv = x / quads & 1, key = x / (2 * quads);
-        const float *p = f.part + before + (w.tile * KEYS + key) * 2 * a.d + kv * a.d + e;
+        const float *p = f.part + before + ((int64_t)w.tile * KEYS + key) * 2 * a.d + kv * a.d + e;
         float4 s = *(const float4 *)p;
         for (int k = 1; k < w.parts; ++k) {
             const float4 y = *(const float4 *)(p + (int64_t)k * tiles * KEYS * 2 * a.d);
@@ -554,15 +553,15 @@ hipError_t go(const BwdArgs &f, hipStream_t st) {
     const AttnArgs &a = f.a;
     const BwdPlan &p = f.p;
     if (a.total_q > 0) {
-        attn_stats_kernel<DP><<<(unsigned)ceil_div(a.total_q * a.hq, 256 / (DP / 8)), 256, 0, st>>>(f);
-        attn_dq_kernel<DP><<<(unsigned)f.qd.blocks(), 256, 2 * 2 * DQ_KEYS * DP * 2, st>>>(f);
+        attn_stats_kernel<DP><<<(unsigned)ceil_div((int64_t)a.total_q * a.hq, 256 / (DP / 8)), 256, 0, st>>>(f);
+        attn_dq_kernel<DP><<<(unsigned)f.qd.blocks, 256, 2 * 2 * DQ_KEYS * DP * 2, st>>>(f);
     }
     if (p.p_units + p.s_units > 0) {
-        attn_dkv_kernel<DP><<<(unsigned)(f.pd.blocks() + f.sd.blocks()), 256,
+        attn_dkv_kernel<DP><<<(unsigned)(f.pd.blocks + f.sd.blocks), 256,
                               2 * RowLoader<DP>::STAGE + KEYS * DP * 2, st>>>(f);
         const int64_t pt = p.p_units / p.np, stl = p.s_units / p.ns;
         const int64_t first = p.np > 1 ? 0 : pt, end = p.ns > 1 ? pt + stl : pt;
-        if (end > first) attn_dkv_join_kernel<<<(unsigned)(end - first), 256, 0, st>>>(f, first);
+        if (end > first) attn_dkv_join_kernel<<<(unsigned)(end - first), 256, 0, st>>>(f, (int)first);
     }
     return hipGetLastError();
 }
@@ -570,11 +569,11 @@ hipError_t go(const BwdArgs &f, hipStream_t st) {
 }  // namespace
 
 int64_t attn_backward_bytes(const AttnArgs &a, bool bf16) {
-    const int64_t plain = a.total_q * a.hq * (int64_t)sizeof(float);   // the generic kernels' delta
+    const int64_t plain = (int64_t)a.total_q * a.hq * (int64_t)sizeof(float);   // the generic kernels' delta
     if (!attn_mfma_sizes(a, bf16) || a.d > 128) return plain;
     const BwdPlan p = make_plan(a);
     const int64_t tiles = (p.np > 1 ? p.p_units : 0) + (p.ns > 1 ? p.s_units : 0);
-    return (a.total_q * a.hq * 2 * (int64_t)sizeof(float) + 15) / 16 * 16 +
+    return ((int64_t)a.total_q * a.hq * 2 * (int64_t)sizeof(float) + 15) / 16 * 16 +
            tiles * KEYS * 2 * a.d * (int64_t)sizeof(float);
 }
 
@@ -586,9 +585,20 @@ hipError_t launch_attn_backward(const AttnArgs &a, bool bf16, hipStream_t st) {
     f.qd = DieOrder::of(f.p.q_units);
     f.pd = DieOrder::of(f.p.p_units);
     f.sd = DieOrder::of(f.p.s_units);
+    const auto div = [](int64_t d) { return Div::of(d > 0 ? d : 1); };
+    f.g = div(a.hq / a.hk);
+    f.seqs = div(a.seqs);
+    f.groups = div(a.groups);
+    f.qtiles = div(f.p.qtiles);
+    f.ptiles = div(f.p.ptiles);
+    f.stiles = div(f.p.stiles);
+    f.np = div(f.p.np);
+    f.ns = div(f.p.ns);
+    f.pall = div(f.p.p_units / f.p.np);
+    f.sall = div(f.p.s_units / f.p.ns);
     f.nlse = (float *)a.work;
-    f.ndelta = f.nlse + a.total_q * a.hq;
-    f.part = (float *)(a.work + (a.total_q * a.hq * 2 * (int64_t)sizeof(float) + 15) / 16 * 16);
+    f.ndelta = f.nlse + (int64_t)a.total_q * a.hq;
+    f.part = (float *)(a.work + ((int64_t)a.total_q * a.hq * 2 * (int64_t)sizeof(float) + 15) / 16 * 16);
     return a.d <= 64 ? go<64>(f, st) : go<128>(f, st);
 }
 

@@ -39,6 +39,7 @@ struct FwdPlan {
 __host__ __device__ constexpr int tile_keys(int dp, int wr) {
     return wr == 4 ? (dp == 256 ? 32 : 64) : wr == 2 ? 64 : 128;
 }
+
 FwdPlan make_plan(const AttnArgs &a) {
     FwdPlan p{};
     const int64_t g = a.hq / a.hk, dp = padded(a.d);
@@ -51,22 +52,22 @@ FwdPlan make_plan(const AttnArgs &a) {
     const int64_t kt = tile_keys((int)dp, p.wr), bm = 32 * p.wr;
     const int64_t pk = ceil_div(a.max_prefix, kt), sk = ceil_div(a.max_suffix, kt);
     p.stiles = (int)ceil_div(seq_rows, bm);
-    // two workgroups a compute unit; a part of at least two tiles
-    const auto split = [&](int64_t units, int64_t tiles, int64_t want) {
-        int64_t n = want / (units > 0 ? units : 1);
-        n = n < (tiles + 1) / 2 ? n : (tiles + 1) / 2;
+    // two workgroups a compute unit, parts of `least` tiles or more
+    const auto split = [&](int64_t units, int64_t tiles, int64_t least) {
+        int64_t n = 2 * kChipUnits / (units > 0 ? units : 1);
+        n = n < tiles / least ? n : tiles / least;
         return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
     };
     if (p.shared) {
         const int64_t likely = a.groups * ceil_div(group_rows, bm) * a.hk;
-        p.ptiles = (int)(ceil_div(a.total_q * g, bm) + a.groups);
-        p.np = split(likely, pk, 2 * kChipUnits);
-        p.ns = sk ? split((int64_t)a.seqs * p.stiles * a.hk, sk, 2 * kChipUnits) : 0;
+        p.ptiles = (int)(ceil_div(a.total_q * g, bm) + a.groups - 1);
+        p.np = split(likely, pk, 1);
+        p.ns = split((int64_t)a.seqs * p.stiles * a.hk, sk, 1);
         p.p_units = (int64_t)p.ptiles * a.hk * p.np;
         p.s_units = (int64_t)a.seqs * p.stiles * a.hk * p.ns;
     } else {
         const int64_t units = (int64_t)a.seqs * p.stiles * a.hk;
-        p.ns = split(units, pk + sk, 2 * kChipUnits);
+        p.ns = split(units, pk + sk, 2);
         p.s_units = units * p.ns;
     }
     return p;
@@ -76,88 +77,90 @@ struct FwdArgs {
     AttnArgs a;
     FwdPlan p;
     DieOrder pd, sd;
+    Div g, hk, seqs, ptiles, stiles, np, ns;
     float *po;                       // [part][total_q hq][d]
     float2 *pml;                     // [part][total_q hq]: maximum (log2 units), sum
 };
 
-// The row tile of flat index i over the groups: groups of 64 a step, by prefix sums.
-__device__ __forceinline__ bool find_group(const AttnArgs &a, int g_heads, int bm, int64_t i, int &grp,
-                                           int64_t &tile) {
+// The row tile of flat index i over the groups: groups of 64 a step, by prefix sums. A group's
+// first token, rows, and prefix go into w; false: no such tile.
+template <int BM>
+__device__ __forceinline__ bool find_group(const AttnArgs &a, int g_heads, int i, Work &w) {
     const int lane = threadIdx.x & 63;
     for (int g0 = 0; g0 < a.groups; g0 += 64) {
         const int g = g0 + lane;
-        int64_t n = 0;
+        int q0 = 0, rows = 0, plen = 0;
+        int64_t pstart = 0;
         if (g < a.groups) {
             const int b0 = a.group_seqs[g], b1 = a.group_seqs[g + 1];
+            const bool ok = prefix_ok(a, g);
+            plen = ok ? a.prefix_len[g] : 0;
+            pstart = a.prefix_start[g];
             if (b0 >= 0 && b0 <= b1 && b1 <= a.seqs) {
-                const int64_t q0 = a.cu_q[b0], q1 = a.cu_q[b1];
-                if (q0 >= 0 && q0 <= q1 && q1 <= a.total_q) n = ceil_div((q1 - q0) * g_heads, bm);
+                q0 = a.cu_q[b0];
+                const int q1 = a.cu_q[b1];
+                if (q0 >= 0 && q0 <= q1 && q1 <= a.total_q) rows = (q1 - q0) * g_heads;
             }
         }
-        int64_t sum = n;
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t v = __shfl_up(sum, o);
+        const int n = tiles_of<BM>(rows);
+        int sum = n;
+        for (int o = 1; a.groups > 1 && o < 64; o <<= 1) {
+            const int v = __shfl_up(sum, o);
             if (lane >= o) sum += v;
         }
         const uint64_t hit = __ballot(i < sum);
         if (hit) {
-            const int l = __ffsll((unsigned long long)hit) - 1;
-            grp = __builtin_amdgcn_readfirstlane(g0 + l);
-            tile = i - (__shfl(sum, l) - __shfl(n, l));
+            const int l = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)hit) - 1);
+            w.s.q0 = __builtin_amdgcn_readlane(q0, l);
+            w.rows = __builtin_amdgcn_readlane(rows, l);
+            w.s.plen = __builtin_amdgcn_readlane(plen, l);
+            w.s.pstart = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(pstart >> 32), l) << 32) |
+                                   (uint32_t)__builtin_amdgcn_readlane((int)pstart, l));
+            w.r0 = (i - __builtin_amdgcn_readlane(sum - n, l)) * BM;
             return true;
         }
-        i -= __shfl(sum, 63);
+        i -= __builtin_amdgcn_readlane(sum, 63);
     }
     return false;
 }
 
+// A part without tiles is written too: the second kernel reads every part of a row.
 template <int DP, int WR>
-__device__ __forceinline__ bool find_work(const FwdArgs &f, int64_t block, Work &w) {
+__device__ __forceinline__ bool find_work(const FwdArgs &f, int block, Work &w) {
     const AttnArgs &a = f.a;
     constexpr int BM = 32 * WR, KT = tile_keys(DP, WR);
-    const int g = a.hq / a.hk;
-    if (block < f.pd.blocks()) {
-        const int64_t u = f.pd.unit(block);
+    if (block < f.pd.blocks) {
+        const int u = f.pd.unit(block);
         if (u >= f.pd.units) return false;
-        const int64_t i = u % f.p.ptiles;
-        int v = (int)(u / f.p.ptiles);
-        w.kvh = v % a.hk;
-        w.part = v / a.hk;
-        int grp;
-        int64_t tile;
-        if (!find_group(a, g, BM, i, grp, tile) || !prefix_ok(a, grp)) return false;
+        const int v = f.ptiles.quot(u), i = f.ptiles.rem(u, v);
+        w.part = f.hk.quot(v);
+        w.kvh = f.hk.rem(v, w.part);
         w.s = SeqView{};
-        w.s.q0 = a.cu_q[a.group_seqs[grp]];
-        w.rows = (a.cu_q[a.group_seqs[grp + 1]] - w.s.q0) * g;
-        w.r0 = uniform64(tile) * BM;
-        w.s.plen = a.prefix_len[grp];
-        w.s.pstart = a.prefix_start[grp];
-        w.pt = (int)ceil_div(w.s.plen, KT);
-        part_range(w.pt, f.p.np, w.part, w.t0, w.t1);
-        return w.t0 < w.t1;
+        if (!find_group<BM>(a, f.g.d, i, w)) return false;
+        w.pt = tiles_of<KT>(w.s.plen);
+        part_range(w.pt, f.np, w.part, w.t0, w.t1);
+        return true;
     }
-    int64_t u = f.sd.unit(block - f.pd.blocks());
+    int u = f.sd.unit(block - f.pd.blocks);
     if (u >= f.sd.units) return false;
+    int v = f.stiles.quot(u);
     // the last row tiles of a sequence, which see the most keys, come first
-    const int rt = f.p.stiles - 1 - (int)(u % f.p.stiles);
-    u /= f.p.stiles;
-    w.s = load_seq(a, (int)(u % a.seqs));
-    u /= a.seqs;
-    w.kvh = (int)(u % a.hk);
-    w.part = (int)(u / a.hk);
-    w.rows = (int64_t)w.s.n * g;
-    w.r0 = (int64_t)rt * BM;
+    w.r0 = (f.p.stiles - 1 - f.stiles.rem(u, v)) * BM;
+    u = v;
+    v = f.seqs.quot(u);
+    w.s = load_seq(a, f.seqs.rem(u, v));
+    w.part = f.hk.quot(v);
+    w.kvh = f.hk.rem(v, w.part);
+    w.rows = w.s.n * (int)f.g.d;
     if (w.s.skip || w.r0 >= w.rows) return false;
-    if (w.s.bad) {
-        w.t0 = w.t1 = w.pt = 0;
-        return f.p.direct() && rt == 0;      // else the second kernel writes the NaN
-    }
-    const int last = (int)((min(w.rows, w.r0 + BM) - 1) / g);
-    const int st = (int)ceil_div(suffix_seen(w.s, last), KT);
-    w.pt = f.p.shared ? 0 : (int)ceil_div(w.s.plen, KT);
-    part_range(w.pt + st, f.p.ns, w.part, w.t0, w.t1);
+    // (a sequence that is out of range has no keys: its rows get NaN from the first row tile,
+    // which may have rows past max_q to mark)
+    if (w.s.bad && w.r0) return false;
+    const int st = tiles_of<KT>(suffix_seen(w.s, f.g.quot(min(w.rows, w.r0 + BM) - 1)));
+    w.pt = f.p.shared ? 0 : tiles_of<KT>(w.s.plen);
+    part_range(w.pt + st, f.ns, w.part, w.t0, w.t1);
     w.part += f.p.np;
-    return w.t0 < w.t1 || f.p.direct();
+    return true;
 }
 
 // One pass along the key tiles [w.t0, w.t1): out^T (unscaled), the maximum in log2 units and
@@ -286,7 +289,7 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
 template <int KT>
 __device__ __forceinline__ bool row_by_row(const FwdArgs &f, const Work &w, int bm) {
     const AttnArgs &a = f.a;
-    const int g = a.hq / a.hk, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (w.t0 >= w.t1) return false;
     bool off_table = false;
     const auto key_row = [&](bool pre, int j) { return pre ? w.s.pstart + j : suffix_row(a, w.s, j, off_table); };
@@ -296,14 +299,14 @@ __device__ __forceinline__ bool row_by_row(const FwdArgs &f, const Work &w, int 
             const uint16_t *v = head_row(pick(pre, a.vp, a.vs), key_row(pre, j), w.kvh);
             for (int e = lane; e < a.d; e += 64) found |= (v[e] & 0x7f80) == 0x7f80;
         };
-        const int s0 = suffix_seen(w.s, (int)(w.r0 / g));
+        const int s0 = suffix_seen(w.s, f.g.quot(w.r0));
         for (int j = max(0, min(s0, w.s.slen - 1)) + wave; j < w.s.slen; j += 4) look(false, j);
         if (w.s.plen > 0) look(true, w.s.plen - 1);   // (copies of it stand for keys past the end)
         if (!__syncthreads_or(found)) return false;
     }
-    for (int64_t row = w.r0 + wave; row < min(w.rows, w.r0 + bm); row += 4) {
-        const int tok = (int)(row / g), head = w.kvh * g + (int)(row - (int64_t)tok * g);
-        const int64_t t = w.s.q0 + tok;
+    for (int row = w.r0 + wave; row < min(w.rows, w.r0 + bm); row += 4) {
+        const int tok = f.g.quot(row), head = w.kvh * (int)f.g.d + f.g.rem(row, tok);
+        const int t = w.s.q0 + tok;
         const int seen = suffix_seen(w.s, tok);
         const uint16_t *q = head_row(a.q, t, head);
         float x[4], o[4] = {}, m = kNegInf, l = 0.f;
@@ -331,7 +334,7 @@ __device__ __forceinline__ bool row_by_row(const FwdArgs &f, const Work &w, int 
             }
         }
         if (__any(off_table)) l = __builtin_nanf("");
-        const int64_t orow = t * a.hq + head, slot = (int64_t)w.part * a.total_q * a.hq + orow;
+        const int64_t orow = (int64_t)t * a.hq + head, slot = (int64_t)w.part * a.total_q * a.hq + orow;
         const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -359,7 +362,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
     make_uniform(w);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wr = wave / WK, wk = wave % WK, h = lane >> 5;
-    const int g = a.hq / a.hk, nch = a.d >> 3;
+    const int g = f.g.d, nch = a.d >> 3;
     if (nch < DP / 8) {
         for (int i = threadIdx.x; i < 2 * 2 * KT * DP / 8; i += 256)
             ((uint4 *)lds_mem)[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -367,11 +370,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
     }
 
     // this lane's query row
-    const int64_t row = w.r0 + 32 * wr + (lane & 31);
+    const int row = w.r0 + 32 * wr + (lane & 31), crow = min(row, w.rows - 1);
     const bool live = row < w.rows;
-    const int tok = (int)(min(row, w.rows - 1) / g);
-    const int head = w.kvh * g + (int)(min(row, w.rows - 1) - (int64_t)tok * g);
-    const int64_t t = w.s.q0 + tok;
+    const int tok = f.g.quot(crow), head = w.kvh * g + f.g.rem(crow, tok);
+    const int t = w.s.q0 + tok;
     bf16x8 q[KS];
     {
         const uint16_t *p = head_row(a.q, t, head);
@@ -380,7 +382,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
     }
     // suffix keys it sees, and the fewest that a row of this wavefront sees
     const int seen = suffix_seen(w.s, tok);
-    const int least = suffix_seen(w.s, (int)(min(w.r0 + 32 * wr, w.rows - 1) / g));
+    const int least = suffix_seen(w.s, f.g.quot(min(w.r0 + 32 * wr, w.rows - 1)));
     floatx16 acc[DB];
     float m, l;
     const bool off_table = key_loop<DP, WR>(a, w, lds, wk, seen, least, q, acc, m, l);
@@ -394,7 +396,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
     }
     l += __shfl_xor(l, 32);
 
-    const int64_t orow = t * a.hq + head;
+    const int orow = t * a.hq + head;
     const bool bad = __syncthreads_or(off_table) || w.s.bad;
     // the registers (4 consecutive elements of the head each) that this wavefront writes
     int g0 = 0;
@@ -445,16 +447,19 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
         }
     }
     if (bad) l = __builtin_nanf("");
-    if (f.p.direct() && w.s.bad) {
-        // every row of the sequence, also those past max_q
-        for (int64_t i = threadIdx.x; i < w.rows * a.d; i += 256) {
-            const int64_t r = i / a.d, k = r / g;
-            ((uint16_t *)a.o.p)[(w.s.q0 + k) * a.o.st + (w.kvh * g + (r - k * g)) * a.o.sh + (i - r * a.d)] =
-                0x7fc0;
+    if (w.s.bad) {
+        // every row of the sequence, also those past max_q: the outputs, or sums for the second
+        // kernel to make them of
+        const int64_t part = (int64_t)w.part * a.total_q * a.hq;
+        for (int r = threadIdx.x; r < w.rows; r += 256) {
+            const int k = f.g.quot(r), tk = w.s.q0 + k, hd = w.kvh * g + f.g.rem(r, k);
+            if (!f.p.direct()) {
+                f.pml[part + (int64_t)tk * a.hq + hd] = make_float2(0.f, __builtin_nanf(""));
+                continue;
+            }
+            for (int e = 0; e < a.d; ++e) ((uint16_t *)head_row(a.o, tk, hd))[e] = 0x7fc0;
+            if (a.lse) a.lse[tk * a.hq + hd] = __builtin_nanf("");
         }
-        if (a.lse)
-            for (int64_t r = threadIdx.x; r < w.rows; r += 256)
-                a.lse[(w.s.q0 + r / g) * a.hq + w.kvh * g + r % g] = __builtin_nanf("");
         return;
     }
     if (!live) return;
@@ -476,6 +481,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
         return;
     }
     const int64_t slot = (int64_t)w.part * a.total_q * a.hq + orow;
+    if (first) f.pml[slot] = make_float2(m, l);
+    if (w.t0 == w.t1) return;
 #pragma unroll
     for (int i = 0; i < DB * 4 / WK; ++i) {
         const int e = 8 * (g0 + i) + 4 * h;
@@ -484,56 +491,60 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
                 make_float4(acc[i / 4][4 * (i % 4)], acc[i / 4][4 * (i % 4) + 1], acc[i / 4][4 * (i % 4) + 2],
                             acc[i / 4][4 * (i % 4) + 3]);
     }
-    if (first) f.pml[slot] = make_float2(m, l);
 }
 
-// Joins the parts of each row: a wavefront a row, 4 elements a lane and step.
-__global__ __launch_bounds__(256) void attn_join_kernel(FwdArgs f, int kt) {
+// Joins the parts of each row: a wavefront a row, 4 elements a lane; the lanes left over take
+// other parts of the same elements.
+__global__ __launch_bounds__(256) void attn_join_kernel(FwdArgs f) {
     const AttnArgs &a = f.a;
-    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), parts = f.p.parts();
     if (r >= a.total_q * a.hq) return;
-    const int lane = threadIdx.x & 63, g = a.hq / a.hk;
-    const int64_t t = r / a.hq;
-    const int head = (int)(r - t * a.hq);
-    const SeqView s = load_seq(a, seq_of(a, t));
-    if (s.skip || t < s.q0 || t >= s.q0 + s.n) return;
-    // the parts that have tiles: each begins where the one before ends
-    const int pt = (int)ceil_div(s.plen, kt);
-    const int tok = (int)(t - s.q0), bm = 32 * f.p.wr;
-    const int64_t rows = (int64_t)s.n * g, rt = ((int64_t)tok * g + head % g) / bm;
-    const int last = (int)((min(rows, (rt + 1) * bm) - 1) / g);
-    const int st = (int)ceil_div(suffix_seen(s, last), kt);
-    const auto has = [&](int i) {
-        int t0, t1;
-        if (f.p.shared && i < f.p.np) part_range(pt, f.p.np, i, t0, t1);
-        else part_range(f.p.shared ? st : pt + st, f.p.ns, i - f.p.np, t0, t1);
-        return t0 < t1;
-    };
-    const int64_t step = a.total_q * a.hq;
-    float top = kNegInf, sum = 0.f;
-    for (int i = lane; i < f.p.parts(); i += 64)
-        if (has(i)) top = fmaxf(top, f.pml[i * step + r].x);
+    const int lane = threadIdx.x & 63;
+    const int64_t step = (int64_t)a.total_q * a.hq;
+    // (at most 128 parts)
+    float2 x = make_float2(kNegInf, 0.f), y = x;
+    if (lane < parts) x = f.pml[lane * step + r];
+    if (lane + 64 < parts) y = f.pml[(lane + 64) * step + r];
+    const int t = r / a.hq, head = r - t * a.hq;
+    const int b = seq_of(a, t);
+    if (a.cu_q[b] < 0 || t < a.cu_q[b] || t >= a.cu_q[b + 1] || a.cu_q[b + 1] > a.total_q) return;
+    float top = fmaxf(x.x, y.x);
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    for (int i = lane; i < f.p.parts(); i += 64)
-        if (has(i)) {
-            const float2 v = f.pml[i * step + r];
-            sum += v.y * (v.x == top ? 1.f : fast_exp2(v.x - top));
-        }
+    const float wx = x.x == top ? 1.f : fast_exp2(x.x - top), wy = y.x == top ? 1.f : fast_exp2(y.x - top);
+    float sum = x.y * wx + y.y * wy;
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    if (s.bad) sum = __builtin_nanf("");
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    for (int e = lane * 4; e < a.d; e += 256) {
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int i = 0; i < f.p.parts(); ++i) {
-            if (!has(i)) continue;
-            const float x = f.pml[i * step + r].x;
-            const float w = x == top ? 1.f : fast_exp2(x - top);
-            const float4 v = *(const float4 *)(f.po + (i * step + r) * a.d + e);
-            o.x = fmaf(v.x, w, o.x);
-            o.y = fmaf(v.y, w, o.y);
-            o.z = fmaf(v.z, w, o.z);
-            o.w = fmaf(v.w, w, o.w);
+    const int lpr = a.d <= 64 ? 16 : a.d <= 128 ? 32 : 64, e = 4 * (lane & (lpr - 1)), first = lane / lpr;
+    const int every = 64 / lpr;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = first; i < parts + first; i += 4 * every) {
+        float4 v[4];
+        float w[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const int k = i + n * every;
+            // a part that has nothing of the row holds no outputs
+            const float l = __shfl(k < 64 ? x.y : y.y, k & 63);
+            w[n] = __shfl(k < 64 ? wx : wy, k & 63);
+            const bool in = k < parts && e < a.d && !(l == 0.f);
+            v[n] = in ? *(const float4 *)(f.po + (k * step + r) * a.d + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+            w[n] = in ? w[n] : 0.f;
         }
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            o.x = fmaf(v[n].x, w[n], o.x);
+            o.y = fmaf(v[n].y, w[n], o.y);
+            o.z = fmaf(v[n].z, w[n], o.z);
+            o.w = fmaf(v[n].w, w[n], o.w);
+        }
+    }
+    for (int s = lpr; s < 64; s <<= 1) {
+        o.x += __shfl_xor(o.x, s);
+        o.y += __shfl_xor(o.y, s);
+        o.z += __shfl_xor(o.z, s);
+        o.w += __shfl_xor(o.w, s);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    if (lane < lpr && e < a.d) {
         uint2 v;
         v.x = pack_bf16x2(o.x * inv, o.y * inv);
         v.y = pack_bf16x2(o.z * inv, o.w * inv);
@@ -546,11 +557,11 @@ template <int DP, int WR>
 hipError_t go(const FwdArgs &f, hipStream_t st) {
     constexpr int KT = tile_keys(DP, WR);
     constexpr int stages = 2 * 2 * KT * DP * 2, join = WR < 4 ? 4 * (DP / 32) * 4096 + 1024 : 0;
-    attn_fwd_kernel<DP, WR><<<(unsigned)(f.pd.blocks() + f.sd.blocks()), 256, stages > join ? stages : join,
+    attn_fwd_kernel<DP, WR><<<(unsigned)(f.pd.blocks + f.sd.blocks), 256, stages > join ? stages : join,
                               st>>>(f);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && !f.p.direct()) {
-        attn_join_kernel<<<(unsigned)ceil_div(f.a.total_q * f.a.hq, 4), 256, 0, st>>>(f, KT);
+        attn_join_kernel<<<(unsigned)ceil_div(f.a.total_q * f.a.hq, 4), 256, 0, st>>>(f);
         e = hipGetLastError();
     }
     return e;
@@ -589,6 +600,13 @@ hipError_t launch_attn_forward(const AttnArgs &a, bool bf16, hipStream_t st) {
     f.p = make_plan(a);
     f.pd = DieOrder::of(f.p.p_units);
     f.sd = DieOrder::of(f.p.s_units);
+    f.g = Div::of(a.hq / a.hk);
+    f.hk = Div::of(a.hk);
+    f.seqs = Div::of(a.seqs);
+    f.ptiles = Div::of(f.p.ptiles > 0 ? f.p.ptiles : 1);
+    f.stiles = Div::of(f.p.stiles);
+    f.np = Div::of(f.p.np > 0 ? f.p.np : 1);
+    f.ns = Div::of(f.p.ns);
     const int64_t rows = (int64_t)f.p.parts() * a.total_q * a.hq;
     f.po = (float *)a.work;
     f.pml = (float2 *)(f.po + rows * a.d);

@@ -8,7 +8,7 @@ namespace olive {
 
 // The keys that a range of query tokens reads.
 struct SeqView {
-    int64_t q0;          // first query token
+    int32_t q0;          // first query token
     int32_t n;           // query tokens
     int32_t plen, slen;  // keys of the prefix and of the suffix
     int64_t pstart;      // row of the prefix's first key
@@ -18,27 +18,27 @@ struct SeqView {
     bool bad;            // something else is out of range: the rows get NaN
 };
 
-// The last group that begins at or before sequence b (empty groups lie before it).
+// The last i in [0, n) with a[i] <= x, or 0: `a` does not decrease, and if it does the result is
+// still in range. 64 entries a step, for a whole wavefront that asks for the same x.
+__device__ __forceinline__ int last_at_most(const int32_t *a, int n, int x) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0;
+    while (n > 1) {
+        const int step = (n + 63) >> 6, i = lo + lane * step;
+        const int k = __popcll(__ballot(lane * step < n && a[i] <= x)) - 1;
+        if (k > 0) {
+            lo += k * step;
+            n -= k * step;
+        }
+        n = n < step ? n : step;
+    }
+    return lo;
+}
+// The group of sequence b (empty groups lie before it), and the sequence of query token t.
 __device__ __forceinline__ int group_of(const AttnArgs &a, int b) {
-    int lo = 0, hi = a.groups - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.group_seqs[mid] <= b) lo = mid;
-        else hi = mid - 1;
-    }
-    return lo;
+    return last_at_most(a.group_seqs, a.groups, b);
 }
-
-// The sequence that query token t belongs to: the last one that begins at or before t.
-__device__ __forceinline__ int seq_of(const AttnArgs &a, int64_t t) {
-    int lo = 0, hi = a.seqs - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.cu_q[mid] <= t) lo = mid;
-        else hi = mid - 1;
-    }
-    return lo;
-}
+__device__ __forceinline__ int seq_of(const AttnArgs &a, int t) { return last_at_most(a.cu_q, a.seqs, t); }
 
 __device__ __forceinline__ bool prefix_ok(const AttnArgs &a, int g) {
     const int64_t len = a.prefix_len[g], start = a.prefix_start[g];
@@ -47,10 +47,10 @@ __device__ __forceinline__ bool prefix_ok(const AttnArgs &a, int g) {
 
 __device__ __forceinline__ SeqView load_seq(const AttnArgs &a, int b) {
     SeqView s;
-    const int64_t q0 = a.cu_q[b], q1 = a.cu_q[b + 1];
+    const int32_t q0 = a.cu_q[b], q1 = a.cu_q[b + 1];
     s.skip = q0 < 0 || q1 < q0 || q1 > a.total_q;
     s.q0 = s.skip ? 0 : q0;
-    s.n = s.skip ? 0 : (int32_t)(q1 - q0);
+    s.n = s.skip ? 0 : q1 - q0;
     const int g = group_of(a, b);
     s.bad = s.n > a.max_q || a.group_seqs[g] > b || a.group_seqs[g + 1] <= b || !prefix_ok(a, g);
     s.plen = s.bad ? 0 : a.prefix_len[g];

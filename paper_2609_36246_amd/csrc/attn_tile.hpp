@@ -139,7 +139,10 @@ __device__ __forceinline__ bf16x8 load_chunk(const uint16_t *row, int c, int nch
     return __builtin_bit_cast(bf16x8, u);
 }
 
-__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Tiles of n >= 0 keys or rows (the tile is a power of two known at compile time).
+template <int TILE>
+__device__ __forceinline__ int tiles_of(int n) { return (int)(((unsigned)n + TILE - 1) / TILE); }
 
 inline int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
@@ -147,24 +150,24 @@ inline int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 // consecutive units, which read the same keys or rows, go to one die, the runs to the dies in
 // turn: a die that got one long stretch of units would get all the long ones.
 struct DieOrder {
-    int64_t units;
-    int run;
-    __host__ static DieOrder of(int64_t units) {
-        const int64_t r = units / 64;
-        return DieOrder{units, (int)(r < 1 ? 1 : r > 16 ? 16 : r)};
+    int32_t units, blocks;
+    Div run;
+    static DieOrder of(int64_t units) {
+        const int64_t r = units / 64, run = r < 1 ? 1 : r > 16 ? 16 : r;
+        return DieOrder{(int32_t)units, (int32_t)(ceil_div(units, 8 * run) * 8 * run), Div::of(run)};
     }
-    __host__ __device__ int64_t blocks() const { return ceil_div(units, 8 * run) * 8 * run; }
     // >= units: nothing to do
-    __device__ __forceinline__ int64_t unit(int64_t block) const {
-        const int64_t i = block >> 3;
-        return (i / run * 8 + (block & 7)) * run + i % run;
+    __device__ __forceinline__ int unit(int block) const {
+        const int i = block >> 3, q = run.quot(i);
+        return (q * 8 + (block & 7)) * (int)run.d + run.rem(i, q);
     }
 };
 
-// Key tiles [t0, t1) of part i of n.
-__device__ __forceinline__ void part_range(int tiles, int n, int i, int &t0, int &t1) {
-    t0 = (int)((int64_t)tiles * i / n);
-    t1 = (int)((int64_t)tiles * (i + 1) / n);
+// Tiles [t0, t1) of part i of n.
+__device__ __forceinline__ void part_range(int tiles, const Div &n, int i, int &t0, int &t1) {
+    const int q = n.quot(tiles), r = n.rem(tiles, q);
+    t0 = i * q + min(i, r);
+    t1 = t0 + q + (i < r);
 }
 
 // One of two views, field by field: a reference that is chosen at run time would put all of a
@@ -176,8 +179,8 @@ __device__ __forceinline__ HeadsArg pick(bool first, HeadsArg x, HeadsArg y) {
 // What one workgroup does.
 struct Work {
     SeqView s;
-    int64_t rows;                    // query rows of the range that begins at token s.q0
-    int64_t r0;                      // first of this workgroup's
+    int rows;                        // query rows of the range that begins at token s.q0
+    int r0;                          // first of this workgroup's
     int kvh, part;
     int pt;                          // prefix tiles come first
     int t0, t1;
@@ -186,7 +189,7 @@ struct Work {
 // The same for every lane, which the compiler cannot always tell from where it came from.
 __device__ __forceinline__ int uniform32(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ void make_uniform(Work &w) {
-    w.s.q0 = uniform64(w.s.q0);
+    w.s.q0 = uniform32(w.s.q0);
     w.s.n = uniform32(w.s.n);
     w.s.plen = uniform32(w.s.plen);
     w.s.slen = uniform32(w.s.slen);
@@ -194,8 +197,8 @@ __device__ __forceinline__ void make_uniform(Work &w) {
     w.s.sstart = uniform64(w.s.sstart);
     w.s.pages = (const int32_t *)uniform64((int64_t)w.s.pages);
     w.s.bad = uniform32(w.s.bad);
-    w.rows = uniform64(w.rows);
-    w.r0 = uniform64(w.r0);
+    w.rows = uniform32(w.rows);
+    w.r0 = uniform32(w.r0);
     w.kvh = uniform32(w.kvh);
     w.part = uniform32(w.part);
     w.pt = uniform32(w.pt);

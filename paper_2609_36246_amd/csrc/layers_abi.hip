@@ -76,7 +76,7 @@ olive_status check_attn(const olive_attn_desc *d) {
     if (d->num_groups < 1 || d->num_seqs < d->num_groups || d->num_seqs >= (1 << 20) ||
         d->heads_kv < 1 || d->heads_q < d->heads_kv || d->heads_q > 4096 ||
         d->heads_q % d->heads_kv || d->head_dim < 1 || d->max_q < 1 || d->total_q < 0 ||
-        d->total_q > kMaxInt || d->max_prefix < 0 || d->max_prefix > kMaxInt || d->max_suffix < 0 ||
+        d->total_q > kMaxInt / d->heads_q || d->max_prefix < 0 || d->max_prefix > kMaxInt || d->max_suffix < 0 ||
         d->max_suffix > kMaxInt - d->max_prefix || d->prefix_rows < 0 || d->suffix_rows < 0)
         return OLIVE_E_SHAPE;
     if (d->head_dim > 256) return OLIVE_E_UNSUPPORTED;
@@ -107,7 +107,7 @@ AttnArgs attn_args(const olive_attn_desc *d) {
     a.hk = d->heads_kv;
     a.d = d->head_dim;
     a.max_q = (int32_t)(d->max_q < d->total_q ? d->max_q : d->total_q);
-    a.total_q = d->total_q;
+    a.total_q = (int32_t)d->total_q;
     a.max_prefix = d->max_prefix;
     a.max_suffix = d->max_suffix;
     a.prefix_rows = d->prefix_rows;

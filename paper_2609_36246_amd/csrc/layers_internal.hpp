@@ -11,6 +11,26 @@ namespace olive {
 
 constexpr int kChipUnits = 256;      // compute units of an MI355X
 
+// Division of 0 <= n < 2^31 by a d that is known on the host: with k = 31 + ceil(log2 d) and
+// m = ceil(2^k / d), n m / 2^k is off by less than n / 2^k < 1 / d, so its floor is the quotient.
+struct Div {
+    uint32_t d, mul, shift;
+    static Div of(int64_t d) {
+        Div r{(uint32_t)d, 0, 0};
+        uint32_t bits = 0;
+        while (((int64_t)1 << bits) < d) ++bits;
+        if (d > 1) {
+            r.mul = (uint32_t)((((unsigned __int128)1 << (31 + bits)) + d - 1) / d);
+            r.shift = bits - 1;
+        }
+        return r;
+    }
+    __device__ __forceinline__ int quot(int n) const {
+        return d == 1 ? n : (int)(__umulhi((uint32_t)n, mul) >> shift);
+    }
+    __device__ __forceinline__ int rem(int n, int q) const { return n - q * (int)d; }
+};
+
 struct HeadsArg {                    // olive_heads with a typed use in the kernels
     char *p;
     int64_t st, sh;                  // elements between tokens and heads
@@ -61,7 +81,8 @@ struct AttnArgs {
     float *lse;                      // [total_q][hq], forward: or NULL
     HeadsArg go, gq, gkp, gvp, gks, gvs;   // backward
     int32_t groups, seqs, hq, hk, d, max_q;
-    int64_t total_q, max_prefix, max_suffix, prefix_rows, suffix_rows;
+    int32_t total_q;                 // total_q * hq < 2^31
+    int64_t max_prefix, max_suffix, prefix_rows, suffix_rows;
     const int32_t *group_seqs, *cu_q;
     const int64_t *prefix_start;
     const int32_t *prefix_len, *suffix_len;
