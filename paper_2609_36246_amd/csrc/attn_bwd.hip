@@ -168,6 +168,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f) {
         constexpr int AT = decltype(stage)::value * 2 * L::BYTES, NEXT = 2 * L::BYTES - AT;
         tile_barrier();
         if (kt + 1 < w.t1) load.template issue<NEXT>(a, w, kt + 1, lds);
+        scalar_loads_done();
         const bool pre = kt < w.pt;
         const int limit = pre ? w.s.plen : seen, lowest = pre ? w.s.plen : least;
         // operands of block b: KS of its keys, KS of its values, 2 DB of its keys transposed
@@ -187,7 +188,6 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) f[(n + 1) & 1][i] = at(4 * (n + 1) + i);
             }
-            keep_order();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int b = (4 * n + i) / FN, x = (4 * n + i) % FN;
@@ -210,7 +210,6 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f) {
                     acc[d] = mfma(f[n & 1][i], p, acc[d]);
                 }
             }
-            keep_order();
         }
     };
     for (int kt = w.t0; kt < w.t1; kt += 2) {
@@ -403,6 +402,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
         if (i + 1 < i1) load.issue(f, w, lds + NEXT);
         const int row0 = r0;
         r0 += ROWS;
+        scalar_loads_done();
         if (r0 <= from_lo) return;                   // no row of the tile sees this wavefront's keys
         floatx16 p, y;
         // lane's registers are rows 8 j + 4 h + 0..3 of the tile
@@ -430,10 +430,8 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
                     y[4 * j] = x[0], y[4 * j + 1] = x[1], y[4 * j + 2] = x[2], y[4 * j + 3] = x[3];
                 }
             }
-            keep_order();
 #pragma unroll
             for (int x = 0; x < 2; ++x) p = mfma(fa[n & 1][x], fb[n & 1][x], p);
-            keep_order();
         }
         if (r0 > w.rows || row0 < from_hi) {
             const int lo = max(0, from - row0), hi = w.rows - row0;
@@ -460,7 +458,6 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
 #pragma unroll
                 for (int x = 0; x < 2; ++x) fr[(n + 1) & 1][x] = at(2 * n + 2 + x);
             }
-            keep_order();
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int x = 2 * n + j, d = (x - KS) % DB, mm = (x - KS) / DB;
@@ -478,7 +475,6 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
                     dk[d] = mfma(fr[n & 1][j], o, dk[d]);
                 }
             }
-            keep_order();
         }
     };
     for (int i = i0; i < i1; i += 2) {

@@ -52,23 +52,26 @@ FwdPlan make_plan(const AttnArgs &a) {
     const int64_t kt = tile_keys((int)dp, p.wr), bm = 32 * p.wr;
     const int64_t pk = ceil_div(a.max_prefix, kt), sk = ceil_div(a.max_suffix, kt);
     p.stiles = (int)ceil_div(seq_rows, bm);
-    // two workgroups a compute unit, parts of `least` tiles or more
-    const auto split = [&](int64_t units, int64_t tiles, int64_t least) {
-        int64_t n = 2 * kChipUnits / (units > 0 ? units : 1);
-        n = n < tiles / least ? n : tiles / least;
+    // Parts of as many key tiles each as fill the places on the chip (one workgroup a compute
+    // unit where it takes over half of the LDS, else two).
+    const int64_t places = kChipUnits * ((dp >= 128 && p.wr == 1) || dp == 256 ? 1 : 2);
+    const auto parts = [&](int64_t tiles, int64_t len) {
+        const int64_t n = len > 0 ? ceil_div(tiles, len) : 1;
         return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
     };
+    const int64_t s_tiles = (int64_t)a.seqs * p.stiles * a.hk;
     if (p.shared) {
         const int64_t likely = a.groups * ceil_div(group_rows, bm) * a.hk;
+        const int64_t len = ceil_div(likely * pk + s_tiles * sk, places);
         p.ptiles = (int)(ceil_div(a.total_q * g, bm) + a.groups - 1);
-        p.np = split(likely, pk, 1);
-        p.ns = split((int64_t)a.seqs * p.stiles * a.hk, sk, 1);
+        p.np = parts(pk, len);
+        p.ns = parts(sk, len);
         p.p_units = (int64_t)p.ptiles * a.hk * p.np;
-        p.s_units = (int64_t)a.seqs * p.stiles * a.hk * p.ns;
+        p.s_units = s_tiles * p.ns;
     } else {
-        const int64_t units = (int64_t)a.seqs * p.stiles * a.hk;
-        p.ns = split(units, pk + sk, 2);
-        p.s_units = units * p.ns;
+        const int64_t len = ceil_div(s_tiles * (pk + sk), places);
+        p.ns = s_tiles >= places ? 1 : parts(pk + sk, len < 2 ? 2 : len);
+        p.s_units = s_tiles * p.ns;
     }
     return p;
 }
@@ -197,6 +200,7 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
             load.template issue<NEXT>(a, w, kt + 1, lds);
             load.look_up(a, w, kt + 2);
         }
+        scalar_loads_done();
         // operand i of the scores (block i / KS, step i % KS), then of the outputs (16 keys
         // i / DB, elements i % DB)
         bf16x8 f[2][4];
@@ -210,13 +214,11 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 f[(n + 1) & 1][i] = 4 * (n + 1) < KN ? k_at(4 * (n + 1) + i) : v_at(i);
-            keep_order();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int x = 4 * n + i, b = x / KS, s = x % KS;
                 z[b] = mfma(f[n & 1][i], q[s], s == 0 ? zero16() : z[b]);
             }
-            keep_order();
         }
         // masks: the end of the prefix, and the suffix keys that a row does not see
         const bool pre = kt < w.pt;
@@ -235,7 +237,7 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, z[b][i]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * c;
+        top = max_of_halves(top) * c;
         // The maximum that the weights refer to follows the running one only when it falls
         // more than 2^8 behind: fp32 sums have the room, and the outputs are seldom rescaled.
         if (__any(top > m + kRescale)) {
@@ -255,7 +257,6 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
 #pragma unroll
                 for (int i = 0; i < 4; ++i) f[(V0 + n + 1) & 1][i] = v_at(4 * (n + 1) + i);
             }
-            keep_order();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int x = 4 * n + i, d = x % DB, b = x / DB / 2, mm = x / DB % 2;
@@ -272,7 +273,6 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
                 }
                 acc[d] = mfma(f[(V0 + n) & 1][i], p, acc[d]);
             }
-            keep_order();
         }
     };
     for (int kt = w.t0; kt < w.t1; kt += 2) {

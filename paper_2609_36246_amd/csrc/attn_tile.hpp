@@ -60,6 +60,16 @@ __device__ __forceinline__ void dma4(const char *g, uint32_t la) {
 #pragma clang diagnostic pop
 }
 
+// No scalar load is pending from here on: beside one, every wait for an LDS read would have to
+// be a wait for all of them.
+__device__ __forceinline__ void scalar_loads_done() { __builtin_amdgcn_s_waitcnt(0xC07F); }
+
+// The larger of the two halves' values of a lane pair l, l + 32.
+__device__ __forceinline__ float max_of_halves(float x) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
 // Keeps an address in its register: the compiler would otherwise form it again at each use
 // rather than add a constant to it in the read.
 __device__ __forceinline__ uint32_t pinned(uint32_t x) {
@@ -103,10 +113,6 @@ struct ColReader {
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
-
-// Operand reads run a group of four ahead of the products that use them: LDS reads and
-// products keep their order here, other instructions may move across.
-__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x6); }
 
 template <int N> struct Const { static constexpr int value = N; };
 
@@ -174,6 +180,12 @@ __device__ __forceinline__ void part_range(int tiles, const Div &n, int i, int &
 // kernel's arguments into memory.
 __device__ __forceinline__ HeadsArg pick(bool first, HeadsArg x, HeadsArg y) {
     return HeadsArg{first ? x.p : y.p, first ? x.st : y.st, first ? x.sh : y.sh};
+}
+
+// (a pointer that went through integers would be read as one that might point into LDS, and
+// every wait for an LDS read beside such a load is a wait for all)
+__device__ __forceinline__ const __attribute__((address_space(1))) int32_t *global_int(const int32_t *p) {
+    return (const __attribute__((address_space(1))) int32_t *)p;
 }
 
 // What one workgroup does.
@@ -246,7 +258,7 @@ struct Loader {
         if (!w.s.pages || t < w.pt || t >= w.t1) return;
         const int j0 = (t - w.pt) * KT;
 #pragma unroll
-        for (int n = 0; n < N; ++n) page[n] = w.s.pages[page_of(a, min(j0 + row(n), w.s.slen - 1))];
+        for (int n = 0; n < N; ++n) page[n] = global_int(w.s.pages)[page_of(a, min(j0 + row(n), w.s.slen - 1))];
     }
     // Tile t to stage offset AT of the ring that begins at `ring`.
     template <int AT>
