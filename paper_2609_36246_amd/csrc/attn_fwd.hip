@@ -46,9 +46,14 @@ FwdPlan make_plan(const AttnArgs &a) {
     const int64_t seq_rows = a.max_q * g;
     // rows of a group, if the groups are alike
     const int64_t group_rows = ceil_div(a.total_q * g, a.groups);
-    p.shared = a.max_prefix > 0 && a.seqs > a.groups && seq_rows <= 64;
+    // Up to two tiles of rows a sequence, the group's rows fill the tiles better than each
+    // sequence's own: runs of up to 97 tokens of 3 heads 34 us for 43, of up to 128 tokens of 4
+    // heads 82 us for 105.
+    p.shared = a.max_prefix > 0 && a.seqs > a.groups && a.total_q * g <= 256 * (int64_t)a.seqs;
     const auto pick = [&](int64_t rows) { return rows <= 32 && dp < 256 ? 1 : rows <= 64 ? 2 : 4; };
-    p.wr = pick(p.shared ? group_rows : seq_rows);
+    // (with a block of rows a sequence or less, four blocks would leave the suffixes to one
+    // wavefront of each workgroup: 64 single tokens on one prefix of 8192 80 us, with two 74)
+    p.wr = pick(!p.shared ? seq_rows : seq_rows <= 32 && group_rows > 64 ? 64 : group_rows);
     const int64_t kt = tile_keys((int)dp, p.wr), bm = 32 * p.wr;
     const int64_t pk = ceil_div(a.max_prefix, kt), sk = ceil_div(a.max_suffix, kt);
     p.stiles = (int)ceil_div(seq_rows, bm);
@@ -170,7 +175,7 @@ __device__ __forceinline__ bool find_work(const FwdArgs &f, int block, Work &w) 
 // this half's share of the sum, of the query row `lane % 32` of a wavefront. Returns whether a
 // page lay outside the cache.
 template <int DP, int WR>
-__device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint32_t lds, int wk, int seen,
+__device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint32_t lds, int wk, bool idle, int seen,
                                          int least, const bf16x8 (&q)[DP / 16], floatx16 (&acc)[DP / 32],
                                          float &m, float &l) {
     constexpr int WK = 4 / WR, KT = tile_keys(DP, WR), NB = KT / 32 / WK, DB = DP / 32, KS = DP / 16;
@@ -201,6 +206,7 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
             load.look_up(a, w, kt + 2);
         }
         scalar_loads_done();
+        if (idle) return;                            // (it has loaded its share of the tile)
         // operand i of the scores (block i / KS, step i % KS), then of the outputs (16 keys
         // i / DB, elements i % DB)
         bf16x8 f[2][4];
@@ -385,7 +391,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
     const int least = suffix_seen(w.s, f.g.quot(min(w.r0 + 32 * wr, w.rows - 1)));
     floatx16 acc[DB];
     float m, l;
-    const bool off_table = key_loop<DP, WR>(a, w, lds, wk, seen, least, q, acc, m, l);
+    const bool off_table = key_loop<DP, WR>(a, w, lds, wk, w.r0 + 32 * wr >= w.rows, seen, least, q, acc, m, l);
     {
         float s = 0.f;
 #pragma unroll
@@ -557,8 +563,7 @@ template <int DP, int WR>
 hipError_t go(const FwdArgs &f, hipStream_t st) {
     constexpr int KT = tile_keys(DP, WR);
     constexpr int stages = 2 * 2 * KT * DP * 2, join = WR < 4 ? 4 * (DP / 32) * 4096 + 1024 : 0;
-    attn_fwd_kernel<DP, WR><<<(unsigned)(f.pd.blocks + f.sd.blocks), 256, stages > join ? stages : join,
-                              st>>>(f);
+    attn_fwd_kernel<DP, WR><<<(unsigned)(f.pd.blocks + f.sd.blocks), 256, stages > join ? stages : join, st>>>(f);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && !f.p.direct()) {
         attn_join_kernel<<<(unsigned)ceil_div(f.a.total_q * f.a.hq, 4), 256, 0, st>>>(f);

@@ -40,23 +40,53 @@ __device__ __forceinline__ int group_of(const AttnArgs &a, int b) {
 }
 __device__ __forceinline__ int seq_of(const AttnArgs &a, int t) { return last_at_most(a.cu_q, a.seqs, t); }
 
-__device__ __forceinline__ bool prefix_ok(const AttnArgs &a, int g) {
-    const int64_t len = a.prefix_len[g], start = a.prefix_start[g];
+__device__ __forceinline__ bool prefix_ok(const AttnArgs &a, int64_t len, int64_t start) {
     return len >= 0 && len <= a.max_prefix && (len == 0 || (start >= 0 && start <= a.prefix_rows - len));
+}
+__device__ __forceinline__ bool prefix_ok(const AttnArgs &a, int g) {
+    return prefix_ok(a, a.prefix_len[g], a.prefix_start[g]);
+}
+
+// The group of sequence b: where it lies among the sequences, and its prefix.
+struct GroupView {
+    int32_t first, end, plen;
+    int64_t pstart;
+};
+__device__ __forceinline__ GroupView load_group(const AttnArgs &a, int b) {
+    GroupView v;
+    if (a.groups < 64) {
+        // one round of loads instead of three that wait for each other
+        const int lane = threadIdx.x & 63, g = min(lane, a.groups - 1);
+        const int at = a.group_seqs[min(lane, a.groups)], plen = a.prefix_len[g];
+        const int64_t pstart = a.prefix_start[g];
+        const int k = max(0, __popcll(__ballot(lane < a.groups && at <= b)) - 1);
+        v.first = __builtin_amdgcn_readlane(at, k);
+        v.end = __builtin_amdgcn_readlane(at, k + 1);
+        v.plen = __builtin_amdgcn_readlane(plen, k);
+        v.pstart = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(pstart >> 32), k) << 32) |
+                             (uint32_t)__builtin_amdgcn_readlane((int)pstart, k));
+        return v;
+    }
+    const int g = group_of(a, b);
+    v.first = a.group_seqs[g];
+    v.end = a.group_seqs[g + 1];
+    v.plen = a.prefix_len[g];
+    v.pstart = a.prefix_start[g];
+    return v;
 }
 
 __device__ __forceinline__ SeqView load_seq(const AttnArgs &a, int b) {
     SeqView s;
     const int32_t q0 = a.cu_q[b], q1 = a.cu_q[b + 1];
+    s.slen = a.suffix_len[b];
+    s.sstart = a.pages || !a.suffix_start ? 0 : a.suffix_start[b];
+    const GroupView g = load_group(a, b);
     s.skip = q0 < 0 || q1 < q0 || q1 > a.total_q;
     s.q0 = s.skip ? 0 : q0;
     s.n = s.skip ? 0 : q1 - q0;
-    const int g = group_of(a, b);
-    s.bad = s.n > a.max_q || a.group_seqs[g] > b || a.group_seqs[g + 1] <= b || !prefix_ok(a, g);
-    s.plen = s.bad ? 0 : a.prefix_len[g];
-    s.pstart = s.bad ? 0 : a.prefix_start[g];
-    s.slen = a.suffix_len[b];
-    s.sstart = 0;
+    s.bad = s.n > a.max_q || g.first > b || g.end <= b || !prefix_ok(a, g.plen, g.pstart);
+    s.plen = g.plen;
+    s.pstart = g.pstart;
     s.pages = nullptr;
     if (s.slen < 0 || s.slen > a.max_suffix) {
         s.bad = true;
@@ -65,7 +95,6 @@ __device__ __forceinline__ SeqView load_seq(const AttnArgs &a, int b) {
             s.pages = a.pages + (int64_t)b * a.table_stride;
             s.bad |= a.suffix_rows < a.page_size;
         } else {
-            s.sstart = a.suffix_start[b];
             s.bad |= s.sstart < 0 || s.sstart > a.suffix_rows - s.slen;
         }
     }
