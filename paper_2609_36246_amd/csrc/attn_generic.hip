@@ -1,252 +1,355 @@
 // Attention on shared prefixes and its backward for every type, head size and stride: 32-bit
-// products on the vector units. 16 query rows (a row is one query head of one token) against
-// tiles of 16 keys, a thread for each pair; the running maximum and sum of the softmax and
-// the output stay in registers over the one pass along the keys.
+// products on the matrix units (v_mfma_f32_16x16x4_f32), operands straight from memory.
+//
+// A workgroup takes 16 query rows (a row is one query head of one token), or 16 keys in the
+// pass for the keys' gradients; its 4 wavefronts take different tiles of 16 along the other
+// axis and join their sums through LDS at the end. The first product is formed so that its
+// result is the second one's operand where it lies: a lane holds 4 values of one column, and
+// product i of the next sum takes the i-th of them from every lane, with rows of the other
+// operand to match.
 #include "attn_seq.hpp"
 #include "olive_device.hpp"
 
 namespace olive {
 namespace {
 
-constexpr int R = 16, KT = 16, THREADS = 256, MAXC = 16;   // MAXC * 16 >= head_dim
+constexpr int R = 16, THREADS = 256;
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+struct GenArgs {
+    AttnArgs a;
+    Div g, tiles;
+    float *delta;                    // backward: [total_q][hq] sums of grad_out * out
+};
+
+__device__ __forceinline__ floatx4 mfma4(float x, float y, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(x, y, c, 0, 0, 0);
+}
 
 template <typename T>
 __device__ __forceinline__ const T *row_ptr(const HeadsArg &h, int64_t t, int64_t head) {
     return (const T *)h.p + t * h.st + head * h.sh;
 }
 template <typename T>
-__device__ __forceinline__ void put(const HeadsArg &h, int64_t t, int64_t head, int e, float v) {
-    T *p = (T *)h.p + t * h.st + head * h.sh + e;
+__device__ __forceinline__ void put(T *p, float v) {
     if constexpr (sizeof(T) == 2) *p = (T)(pack_bf16x2(v, v) & 0xffffu);
     else *p = v;
 }
 
-__device__ __forceinline__ float max16(float v) {
-    for (int o = 8; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
-}
-__device__ __forceinline__ float sum16(float v) {
-    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
-}
-
-// Rows r0 .. r0 + 15 of a token range into LDS (zeros past its end): row r is token r / g.
-template <typename T>
-__device__ __forceinline__ void load_rows(const HeadsArg &h, int64_t q0, int64_t r0, int64_t rows,
-                                          int g, int kvh, int d, int ld, float *dst) {
-    for (int i = threadIdx.x; i < R * d; i += THREADS) {
-        const int r = i / d, e = i - r * d;
-        float v = 0.f;
-        if (r0 + r < rows) {
-            const int64_t tok = (r0 + r) / g;
-            v = load_elem<T>(row_ptr<T>(h, q0 + tok, kvh * g + (r0 + r - tok * g)), e);
+// NT 16-element blocks cover the head. Block n of a row as a first or second operand: elements
+// 16 n + 4 q + 0..3 (q = lane / 16), zeros past d.
+template <typename T, int NT>
+__device__ __forceinline__ void load_row(const T *p, int d, floatx4 (&x)[NT]) {
+    const int q = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = 16 * n + 4 * q + e;
+            x[n][e] = i < d ? load_elem<T>(p, i) : 0.f;
         }
-        dst[r * ld + e] = v;
+}
+// Rows 4 q + 0..3 (their pointers) as a transposed first operand: element 16 n + lane % 16.
+template <typename T, int NT>
+__device__ __forceinline__ void load_cols(const T *const (&p)[4], int d, floatx4 (&x)[NT]) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int i = 16 * n + (threadIdx.x & 15);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[n][e] = i < d ? load_elem<T>(p[e], i) : 0.f;
+    }
+}
+// Sum over the head of two rows' products: 16 x 16 results.
+template <int NT>
+__device__ __forceinline__ floatx4 product(const floatx4 (&x)[NT], const floatx4 (&y)[NT]) {
+    floatx4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = mfma4(x[n][e], y[n][e], c);
+    return c;
+}
+template <int NT>
+__device__ __forceinline__ void add_outer(const floatx4 (&x)[NT], floatx4 p, floatx4 (&acc)[NT]) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[n] = mfma4(x[n][e], p[e], acc[n]);
+}
+__device__ __forceinline__ float max_of_quarters(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float sum_of_quarters(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// 16 query rows of a sequence; this lane's is row lane % 16 (a copy of the last one past the end).
+struct Rows {
+    SeqView s;
+    int kvh, r0, rows;
+    int tok, t, head;                // of this lane's row
+    bool live, any;
+};
+__device__ __forceinline__ Rows find_rows(const GenArgs &f) {
+    const AttnArgs &a = f.a;
+    Rows w;
+    w.kvh = blockIdx.x % a.hk;
+    const int v = blockIdx.x / a.hk, b = f.tiles.quot(v);
+    w.r0 = f.tiles.rem(v, b) * R;
+    w.s = load_seq(a, b);
+    w.rows = w.s.n * (int)f.g.d;
+    w.any = !w.s.skip && w.r0 < w.rows;
+    const int r = w.r0 + (threadIdx.x & 15), c = max(0, min(r, w.rows - 1));
+    w.live = r < w.rows;
+    w.tok = f.g.quot(c);
+    w.head = w.kvh * (int)f.g.d + f.g.rem(c, w.tok);
+    w.t = w.s.q0 + w.tok;
+    return w;
+}
+// Every row of a sequence that is out of range.
+template <typename T>
+__device__ __forceinline__ void put_nan(const GenArgs &f, const Rows &w, const HeadsArg &o, float *lse) {
+    if (w.r0) return;
+    for (int r = threadIdx.x; r < w.rows; r += THREADS) {
+        const int k = f.g.quot(r), t = w.s.q0 + k, head = w.kvh * (int)f.g.d + f.g.rem(r, k);
+        T *p = (T *)row_ptr<T>(o, t, head);
+        for (int e = 0; e < f.a.d; ++e) put<T>(p + e, __builtin_nanf(""));
+        if (lse) lse[(int64_t)t * f.a.hq + head] = __builtin_nanf("");
     }
 }
 
-// Keys j0 .. j0 + 15 of a sequence's prefix and suffix (zeros past `end`).
+// Key j of the prefix and suffix together (a copy of key `end` - 1 from there on).
 template <typename T>
-__device__ __forceinline__ void load_keys(const AttnArgs &a, const SeqView &s, const HeadsArg &p,
-                                          const HeadsArg &u, int j0, int end, int kvh, int ld,
-                                          float *dst, bool &bad) {
-    for (int i = threadIdx.x; i < KT * a.d; i += THREADS) {
-        const int r = i / a.d, e = i - r * a.d, j = j0 + r;
-        float v = 0.f;
-        if (j < end)
-            v = load_elem<T>(j < s.plen ? row_ptr<T>(p, s.pstart + j, kvh)
-                                        : row_ptr<T>(u, suffix_row(a, s, j - s.plen, bad), kvh), e);
-        dst[r * ld + e] = v;
+__device__ __forceinline__ void key_ptrs(const AttnArgs &a, const SeqView &s, int kvh, int j, int end, bool &bad,
+                                         const T *&k, const T *&v) {
+    j = min(j, end - 1);
+    if (j < s.plen) {
+        k = row_ptr<T>(a.kp, s.pstart + j, kvh);
+        v = row_ptr<T>(a.vp, s.pstart + j, kvh);
+    } else {
+        const int64_t row = suffix_row(a, s, j - s.plen, bad);
+        k = row_ptr<T>(a.ks, row, kvh);
+        v = row_ptr<T>(a.vs, row, kvh);
     }
 }
 
-__device__ __forceinline__ float dot(const float *x, const float *y, int d) {
-    float s = 0.f;
-    for (int e = 0; e < d; ++e) s = fmaf(x[e], y[e], s);
-    return s;
-}
-
-struct Unit { int b, kvh; int64_t r0; };
-__device__ __forceinline__ Unit unit_of(const AttnArgs &a, int tiles) {
-    Unit u;
-    u.kvh = blockIdx.x % a.hk;
-    const int v = blockIdx.x / a.hk;
-    u.r0 = (int64_t)(v % tiles) * R;
-    u.b = v / tiles;
-    return u;
-}
-
-template <typename T>
-__global__ __launch_bounds__(THREADS) void attn_generic_kernel(AttnArgs a, int tiles) {
+template <typename T, int NT>
+__global__ __launch_bounds__(THREADS, NT > 8 ? 1 : 2) void attn_generic_kernel(GenArgs f) {
     extern __shared__ float lds[];
-    const int ld = a.d + 1, g = a.hq / a.hk;
-    float *qs = lds, *ks = qs + R * ld, *vs = ks + KT * ld, *ps = vs + KT * ld;
-    const Unit u = unit_of(a, tiles);
-    const SeqView s = load_seq(a, u.b);
-    const int64_t rows = (int64_t)s.n * g;
-    const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
-    if (s.skip || u.r0 >= rows) return;
-    if (s.bad) {
-        if (u.r0) return;
-        for (int64_t i = threadIdx.x; i < rows * a.d; i += THREADS) {
-            const int64_t row = i / a.d, tok = row / g;
-            put<T>(a.o, s.q0 + tok, u.kvh * g + (row - tok * g), (int)(i - row * a.d), __builtin_nanf(""));
-        }
-        if (a.lse)
-            for (int64_t row = threadIdx.x; row < rows; row += THREADS)
-                a.lse[(s.q0 + row / g) * a.hq + u.kvh * g + row % g] = __builtin_nanf("");
+    const AttnArgs &a = f.a;
+    const Rows w = find_rows(f);
+    if (!w.any) return;
+    if (w.s.bad) {
+        put_nan<T>(f, w, a.o, a.lse);
         return;
     }
-    load_rows<T>(a.q, s.q0, u.r0, rows, g, u.kvh, a.d, ld, qs);
-    const int64_t row = u.r0 + r;
-    const int tok = (int)(row / g);
-    const int seen = row < rows ? s.plen + suffix_seen(s, tok) : 0;
-    const int last = (int)(min(rows, u.r0 + R) - 1) / g;
-    const int end = s.plen + suffix_seen(s, last);
-    float m = kNegInf, l = 0.f, acc[MAXC] = {};
-    bool bad = false;
-    for (int j0 = 0; j0 < end; j0 += KT) {
-        __syncthreads();
-        load_keys<T>(a, s, a.kp, a.ks, j0, end, u.kvh, ld, ks, bad);
-        load_keys<T>(a, s, a.vp, a.vs, j0, end, u.kvh, ld, vs, bad);
-        __syncthreads();
-        float z = j0 + c < seen ? dot(qs + r * ld, ks + c * ld, a.d) * a.scale : kNegInf;
-        const float m2 = fmaxf(m, max16(z));
-        const float p = m2 == kNegInf && z == kNegInf ? 0.f : expf(z - m2);
-        const float f = m == m2 ? 1.f : expf(m - m2);
-        m = m2;
-        l = l * f + sum16(p);
-        ps[r * KT + c] = p;
-        __syncthreads();
-        // a key that a row does not see adds nothing to it, whatever its value holds
-        const int keys = min(KT, seen - j0);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = lane >> 4;
+    floatx4 q[NT], acc[NT];
+    load_row<T, NT>(row_ptr<T>(a.q, w.t, w.head), a.d, q);
 #pragma unroll
-        for (int i = 0; i < MAXC; ++i) {
-            const int e = c + 16 * i;
-            if (e >= a.d) continue;
-            float v = acc[i] * f;
-            for (int k = 0; k < keys; ++k) v = fmaf(ps[r * KT + k], vs[k * ld + e], v);
-            acc[i] = v;
+    for (int n = 0; n < NT; ++n) acc[n] = (floatx4)(0.f);
+    const int seen = w.live ? w.s.plen + suffix_seen(w.s, w.tok) : 0;
+    const int least = w.s.plen + suffix_seen(w.s, f.g.quot(w.r0));
+    const int end = w.s.plen + suffix_seen(w.s, f.g.quot(min(w.rows, w.r0 + R) - 1));
+    float m = kNegInf, l = 0.f;
+    bool bad = false;
+    for (int j0 = wave * R; j0 < end; j0 += 4 * R) {
+        const T *kp, *vp, *col[4], *unused;
+        key_ptrs<T>(a, w.s, w.kvh, j0 + (lane & 15), end, bad, kp, vp);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) key_ptrs<T>(a, w.s, w.kvh, j0 + 4 * quarter + e, end, bad, unused, col[e]);
+        floatx4 x[NT];
+        load_row<T, NT>(kp, a.d, x);
+        floatx4 z = product<NT>(x, q), p;
+        float top = kNegInf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            z[e] = j0 + 4 * quarter + e < seen ? z[e] * a.scale : kNegInf;
+            top = fmaxf(top, z[e]);
+        }
+        const float m2 = fmaxf(m, max_of_quarters(top));
+        const float r = m == m2 ? 1.f : expf(m - m2), m0 = m2 == kNegInf ? 0.f : m2;
+        m = m2;
+        l *= r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            p[e] = expf(z[e] - m0);
+            l += p[e];
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[n] *= r;
+        load_cols<T, NT>(col, a.d, x);
+        bool special = false;
+        if (j0 + R > least) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) special |= !(fabsf(x[n][e]) < __builtin_inff());
+        }
+        if (!__any(special)) {
+            add_outer<NT>(x, p, acc);
+            continue;
+        }
+        // A value that is not finite, and rows that do not see its key: key by key, without the
+        // rows that do not see it.
+        for (int k = 0; k < R; ++k) {
+            const T *v;
+            key_ptrs<T>(a, w.s, w.kvh, j0 + k, end, bad, unused, v);
+            const int e = k & 3;
+            const float pk = __shfl(e == 0 ? p[0] : e == 1 ? p[1] : e == 2 ? p[2] : p[3],
+                                    (k >> 2) * 16 + (lane & 15));
+            if (j0 + k >= seen) continue;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = 16 * n + 4 * quarter + i;
+                    if (at < a.d) acc[n][i] = fmaf(pk, load_elem<T>(v, at), acc[n][i]);
+                }
         }
     }
-    if (__syncthreads_or(bad)) l = __builtin_nanf("");
-    if (row >= rows) return;
-    const int64_t t = s.q0 + tok;
-    const int head = u.kvh * g + (int)(row - (int64_t)tok * g);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    l = sum_of_quarters(l);
+    bad = __syncthreads_or(bad);
+    // [wave][row]: maximum, sum; [wave][row][element]
+    float2 *ml = (float2 *)lds;
+    float *o = lds + 2 * 4 * R;
+    const int ld = a.d + 1, row = lane & 15;
+    if (quarter == 0) ml[wave * R + row] = make_float2(m, l);
 #pragma unroll
-    for (int i = 0; i < MAXC; ++i) {
-        const int e = c + 16 * i;
-        if (e >= a.d) continue;
-        put<T>(a.o, t, head, e, acc[i] * inv);
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = 16 * n + 4 * quarter + i;
+            if (at < a.d) o[(wave * R + row) * ld + at] = acc[n][i];
+        }
+    __syncthreads();
+    // 16 threads a row, whose row is the one of their lane % 16 found above
+    float wt[4], top = kNegInf, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, ml[k * R + row].x);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float2 x = ml[k * R + row];
+        wt[k] = x.x == top ? 1.f : expf(x.x - top);
+        sum += x.y * wt[k];
     }
-    if (a.lse && c == 0) a.lse[t * a.hq + head] = l == 0.f ? kNegInf : m + logf(l);
+    if (bad) sum = __builtin_nanf("");
+    if (!w.live) return;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    T *out = (T *)row_ptr<T>(a.o, w.t, w.head);
+    for (int e = threadIdx.x >> 4; e < a.d; e += 16) {
+        float x = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x = fmaf(o[(k * R + row) * ld + e], wt[k], x);
+        put<T>(out + e, x * inv);
+    }
+    if (a.lse && threadIdx.x < R) a.lse[(int64_t)w.t * a.hq + w.head] = sum == 0.f ? kNegInf : top + logf(sum);
 }
 
 // delta = sum of grad_out * out of a row: 64 lanes a row.
 template <typename T>
-__global__ __launch_bounds__(THREADS) void attn_delta_kernel(AttnArgs a, float *delta) {
+__global__ __launch_bounds__(THREADS) void attn_delta_kernel(GenArgs f) {
+    const AttnArgs &a = f.a;
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (w >= a.total_q * a.hq) return;
-    const int64_t t = w / a.hq;
-    const int head = (int)(w - t * a.hq);
+    if (w >= (int64_t)a.total_q * a.hq) return;
+    const int t = (int)w / a.hq, head = (int)w - t * a.hq;
     const T *x = row_ptr<T>(a.o, t, head), *y = row_ptr<T>(a.go, t, head);
     float s = 0.f;
     for (int e = threadIdx.x & 63; e < a.d; e += 64) s = fmaf(load_elem<T>(x, e), load_elem<T>(y, e), s);
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
-    if ((threadIdx.x & 63) == 0) delta[w] = s;
+    if ((threadIdx.x & 63) == 0) f.delta[w] = s;
 }
 
-// p and dz of a pair from its two products; lse and delta are the row's.
-__device__ __forceinline__ float pair_p(float z, float lse) {
-    return lse == kNegInf ? 0.f : expf(z - lse);
-}
+// p of a pair from its scaled score and the row's log-normaliser.
+__device__ __forceinline__ float pair_p(float z, float lse) { return lse == kNegInf ? 0.f : expf(z - lse); }
 
-template <typename T>
-__global__ __launch_bounds__(THREADS) void attn_generic_dq_kernel(AttnArgs a, int tiles,
-                                                                  const float *delta) {
-    extern __shared__ float lds[];
-    const int ld = a.d + 1, g = a.hq / a.hk;
-    float *qs = lds, *gs = qs + R * ld, *ks = gs + R * ld, *vs = ks + KT * ld, *ps = vs + KT * ld;
-    const Unit u = unit_of(a, tiles);
-    const SeqView s = load_seq(a, u.b);
-    const int64_t rows = (int64_t)s.n * g;
-    const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
-    if (s.skip || u.r0 >= rows) return;
-    if (s.bad) {
-        if (u.r0) return;
-        for (int64_t i = threadIdx.x; i < rows * a.d; i += THREADS) {
-            const int64_t row = i / a.d, tok = row / g;
-            put<T>(a.gq, s.q0 + tok, u.kvh * g + (row - tok * g), (int)(i - row * a.d), __builtin_nanf(""));
+// Adds the four wavefronts' sums of 16 columns (lane % 16) and writes them, scaled: column c of
+// the first `cols` to out(c).
+template <typename T, int NT, typename F>
+__device__ __forceinline__ void join_and_put(float *o, const floatx4 (&acc)[NT], int d, int cols, float scale, F out) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, ld = d + 1;
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = 16 * n + 4 * (lane >> 4) + i;
+            if (at < d) o[(wave * R + c) * ld + at] = acc[n][i];
         }
+    __syncthreads();
+    if (c >= cols) return;
+    T *p = out(c);
+    for (int e = threadIdx.x >> 4; e < d; e += 16)
+        put<T>(p + e, ((o[c * ld + e] + o[(R + c) * ld + e]) + (o[(2 * R + c) * ld + e] + o[(3 * R + c) * ld + e])) * scale);
+}
+
+template <typename T, int NT>
+__global__ __launch_bounds__(THREADS, NT > 8 ? 1 : 2) void attn_generic_dq_kernel(GenArgs f) {
+    extern __shared__ float lds[];
+    const AttnArgs &a = f.a;
+    const Rows w = find_rows(f);
+    if (!w.any) return;
+    if (w.s.bad) {
+        put_nan<T>(f, w, a.gq, nullptr);
         return;
     }
-    load_rows<T>(a.q, s.q0, u.r0, rows, g, u.kvh, a.d, ld, qs);
-    load_rows<T>(a.go, s.q0, u.r0, rows, g, u.kvh, a.d, ld, gs);
-    const int64_t row = u.r0 + r;
-    const int tok = (int)(row / g);
-    const int64_t t = s.q0 + tok;
-    const int head = u.kvh * g + (int)(row - (int64_t)tok * g);
-    const bool live = row < rows;
-    const float lse = live ? a.lse[t * a.hq + head] : kNegInf;
-    const float del = live ? delta[t * a.hq + head] : 0.f;
-    const int seen = live ? s.plen + suffix_seen(s, tok) : 0;
-    const int end = s.plen + suffix_seen(s, (int)(min(rows, u.r0 + R) - 1) / g);
-    float acc[MAXC] = {};
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = lane >> 4;
+    floatx4 q[NT], go[NT], acc[NT];
+    load_row<T, NT>(row_ptr<T>(a.q, w.t, w.head), a.d, q);
+    load_row<T, NT>(row_ptr<T>(a.go, w.t, w.head), a.d, go);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n] = (floatx4)(0.f);
+    const int64_t at = (int64_t)w.t * a.hq + w.head;
+    const float lse = a.lse[at], delta = f.delta[at];
+    const int seen = w.live ? w.s.plen + suffix_seen(w.s, w.tok) : 0;
+    const int end = w.s.plen + suffix_seen(w.s, f.g.quot(min(w.rows, w.r0 + R) - 1));
     bool bad = false;
-    for (int j0 = 0; j0 < end; j0 += KT) {
-        __syncthreads();
-        load_keys<T>(a, s, a.kp, a.ks, j0, end, u.kvh, ld, ks, bad);
-        load_keys<T>(a, s, a.vp, a.vs, j0, end, u.kvh, ld, vs, bad);
-        __syncthreads();
-        float dz = 0.f;
-        if (j0 + c < seen) {
-            const float p = pair_p(dot(qs + r * ld, ks + c * ld, a.d) * a.scale, lse);
-            dz = p * (dot(gs + r * ld, vs + c * ld, a.d) - del) * a.scale;
-        }
-        ps[r * KT + c] = dz;
-        __syncthreads();
-        const int keys = min(KT, seen - j0);
+    for (int j0 = wave * R; j0 < end; j0 += 4 * R) {
+        const T *kp, *vp, *col[4], *unused;
+        key_ptrs<T>(a, w.s, w.kvh, j0 + (lane & 15), end, bad, kp, vp);
 #pragma unroll
-        for (int i = 0; i < MAXC; ++i) {
-            const int e = c + 16 * i;
-            if (e >= a.d) continue;
-            float v = acc[i];
-            for (int k = 0; k < keys; ++k) v = fmaf(ps[r * KT + k], ks[k * ld + e], v);
-            acc[i] = v;
-        }
-    }
-    if (!live) return;
+        for (int e = 0; e < 4; ++e) key_ptrs<T>(a, w.s, w.kvh, j0 + 4 * quarter + e, end, bad, col[e], unused);
+        floatx4 x[NT];
+        load_row<T, NT>(kp, a.d, x);
+        floatx4 z = product<NT>(x, q);
+        load_row<T, NT>(vp, a.d, x);
+        const floatx4 y = product<NT>(x, go);
 #pragma unroll
-    for (int i = 0; i < MAXC; ++i) {
-        const int e = c + 16 * i;
-        if (e >= a.d) continue;
-        put<T>(a.gq, t, head, e, acc[i]);
+        for (int e = 0; e < 4; ++e)
+            z[e] = j0 + 4 * quarter + e < seen ? pair_p(z[e] * a.scale, lse) * (y[e] - delta) : 0.f;
+        load_cols<T, NT>(col, a.d, x);
+        add_outer<NT>(x, z, acc);
     }
+    const int g = f.g.d;
+    join_and_put<T, NT>(lds, acc, a.d, min(R, w.rows - w.r0), a.scale, [&](int c) {
+        const int k = f.g.quot(w.r0 + c);
+        return (T *)row_ptr<T>(a.gq, w.s.q0 + k, w.kvh * g + f.g.rem(w.r0 + c, k));
+    });
 }
 
 // 16 keys of a prefix (seen by every row of its group) or of a suffix against all the rows
 // that see them.
-template <typename T, bool PREFIX>
-__global__ __launch_bounds__(THREADS) void attn_generic_dkv_kernel(AttnArgs a, int tiles,
-                                                                   const float *delta) {
+template <typename T, int NT, bool PREFIX>
+__global__ __launch_bounds__(THREADS, NT > 4 ? 1 : 2) void attn_generic_dkv_kernel(GenArgs f) {
     extern __shared__ float lds[];
-    const int ld = a.d + 1, g = a.hq / a.hk;
-    float *qs = lds, *gs = qs + R * ld, *ks = gs + R * ld, *vs = ks + KT * ld, *ps = vs + KT * ld,
-          *ds = ps + R * KT;
-    const int kvh = blockIdx.x % a.hk;
-    const int v = blockIdx.x / a.hk, own = v / tiles, j0 = (v - own * tiles) * KT;
+    const AttnArgs &a = f.a;
+    const int kvh = blockIdx.x % a.hk, g = f.g.d;
+    const int u = blockIdx.x / a.hk, own = f.tiles.quot(u), j0 = f.tiles.rem(u, own) * R;
     const HeadsArg &kh = PREFIX ? a.kp : a.ks, &vh = PREFIX ? a.vp : a.vs;
     const HeadsArg &gk = PREFIX ? a.gkp : a.gks, &gv = PREFIX ? a.gvp : a.gvs;
-    int64_t q0, toks, krow;
-    int keys, first = 0;            // first: suffix keys that query 0 sees, less one
+    int q0, toks, keys, first = 0;  // first: suffix keys that query 0 sees, less one
+    int64_t krow;
     if (PREFIX) {
         const int b0 = a.group_seqs[own], b1 = a.group_seqs[own + 1];
         if (b0 < 0 || b1 < b0 || b1 > a.seqs || !prefix_ok(a, own)) return;
         keys = a.prefix_len[own];
         krow = a.prefix_start[own];
         q0 = a.cu_q[b0];
-        toks = a.cu_q[b1] - q0;
+        const int q1 = a.cu_q[b1];
+        if (q0 < 0 || q1 < q0 || q1 > a.total_q) return;
+        toks = q1 - q0;
     } else {
         const SeqView s = load_seq(a, own);
         if (s.skip || s.bad) return;
@@ -256,94 +359,98 @@ __global__ __launch_bounds__(THREADS) void attn_generic_dkv_kernel(AttnArgs a, i
         toks = s.n;
         first = s.slen - s.n;
     }
-    if (j0 >= keys || q0 < 0 || toks < 0 || q0 + toks > a.total_q) return;
-    for (int i = threadIdx.x; i < KT * a.d; i += THREADS) {
-        const int k = i / a.d, e = i - k * a.d;
-        const bool in = j0 + k < keys;
-        ks[k * ld + e] = in ? load_elem<T>(row_ptr<T>(kh, krow + j0 + k, kvh), e) : 0.f;
-        vs[k * ld + e] = in ? load_elem<T>(row_ptr<T>(vh, krow + j0 + k, kvh), e) : 0.f;
-    }
-    const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
-    float dk[MAXC] = {}, dv[MAXC] = {};
-    const int64_t rows = toks * g;
-    // the first row that sees the tile's first key
-    const int64_t from = PREFIX ? 0 : (int64_t)max(0, j0 - first) * g / R * R;
-    for (int64_t r0 = from; r0 < rows; r0 += R) {
-        __syncthreads();
-        load_rows<T>(a.q, q0, r0, rows, g, kvh, a.d, ld, qs);
-        load_rows<T>(a.go, q0, r0, rows, g, kvh, a.d, ld, gs);
-        __syncthreads();
-        const int64_t row = r0 + r, tok = row / g;
-        float p = 0.f, dz = 0.f;
-        if (row < rows && j0 + c < keys && (PREFIX || j0 + c <= first + tok)) {
-            const int64_t at = (q0 + tok) * a.hq + kvh * g + (row - tok * g);
-            p = pair_p(dot(qs + r * ld, ks + c * ld, a.d) * a.scale, a.lse[at]);
-            dz = p * (dot(gs + r * ld, vs + c * ld, a.d) - delta[at]) * a.scale;
-        }
-        ps[c * R + r] = p;
-        ds[c * R + r] = dz;
-        __syncthreads();
+    if (j0 >= keys) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = lane >> 4;
+    const int key = j0 + (lane & 15), rows = toks * g;
+    floatx4 k[NT], v[NT], dk[NT], dv[NT];
+    load_row<T, NT>(row_ptr<T>(kh, krow + min(key, keys - 1), kvh), a.d, k);
+    load_row<T, NT>(row_ptr<T>(vh, krow + min(key, keys - 1), kvh), a.d, v);
 #pragma unroll
-        for (int i = 0; i < MAXC; ++i) {
-            const int e = c + 16 * i;
-            if (e >= a.d) continue;
-            float x = dk[i], y = dv[i];
-            for (int k = 0; k < R; ++k) {
-                x = fmaf(ds[r * R + k], qs[k * ld + e], x);
-                y = fmaf(ps[r * R + k], gs[k * ld + e], y);
-            }
-            dk[i] = x;
-            dv[i] = y;
-        }
-    }
-    if (j0 + r >= keys) return;
+    for (int n = 0; n < NT; ++n) dk[n] = dv[n] = (floatx4)(0.f);
+    // the first row that sees this lane's key, and the tile's first one
+    const auto row_of = [&](int j) { return PREFIX ? 0 : (int)min((int64_t)rows, (int64_t)max(0, j - first) * g); };
+    const int from = row_of(key);
+    for (int r0 = row_of(j0) / R * R + wave * R; r0 < rows; r0 += 4 * R) {
+        const T *qc[4], *gc[4];
+        float lse[4], delta[4];
 #pragma unroll
-    for (int i = 0; i < MAXC; ++i) {
-        const int e = c + 16 * i;
-        if (e >= a.d) continue;
-        put<T>(gk, krow + j0 + r, kvh, e, dk[i]);
-        put<T>(gv, krow + j0 + r, kvh, e, dv[i]);
+        for (int e = 0; e < 4; ++e) {
+            const int r = min(r0 + 4 * quarter + e, rows - 1), tok = f.g.quot(r);
+            const int t = q0 + tok, head = kvh * g + f.g.rem(r, tok);
+            qc[e] = row_ptr<T>(a.q, t, head);
+            gc[e] = row_ptr<T>(a.go, t, head);
+            lse[e] = a.lse[(int64_t)t * a.hq + head];
+            delta[e] = f.delta[(int64_t)t * a.hq + head];
+        }
+        const int r = min(r0 + (lane & 15), rows - 1), tok = f.g.quot(r);
+        const int t = q0 + tok, head = kvh * g + f.g.rem(r, tok);
+        floatx4 x[NT], p, z;
+        load_row<T, NT>(row_ptr<T>(a.q, t, head), a.d, x);
+        z = product<NT>(x, k);
+        load_row<T, NT>(row_ptr<T>(a.go, t, head), a.d, x);
+        const floatx4 y = product<NT>(x, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int row = r0 + 4 * quarter + e;
+            p[e] = row >= from && row < rows ? pair_p(z[e] * a.scale, lse[e]) : 0.f;
+            z[e] = p[e] == 0.f ? 0.f : p[e] * (y[e] - delta[e]);
+        }
+        load_cols<T, NT>(gc, a.d, x);
+        add_outer<NT>(x, p, dv);
+        load_cols<T, NT>(qc, a.d, x);
+        add_outer<NT>(x, z, dk);
     }
+    const int cols = min(R, keys - j0);
+    join_and_put<T, NT>(lds, dk, a.d, cols, a.scale, [&](int c) { return (T *)row_ptr<T>(gk, krow + j0 + c, kvh); });
+    join_and_put<T, NT>(lds, dv, a.d, cols, 1.f, [&](int c) { return (T *)row_ptr<T>(gv, krow + j0 + c, kvh); });
 }
 
-int64_t tiles_of(int64_t n, int tile) { return (n + tile - 1) / tile; }
+int64_t tiles_of(int64_t n) { return (n + R - 1) / R; }
 
-template <typename T>
+template <typename T, int NT>
 hipError_t forward(const AttnArgs &a, hipStream_t st) {
-    const int tiles = (int)tiles_of((int64_t)a.max_q * (a.hq / a.hk), R);
-    const size_t bytes = sizeof(float) * ((R + 2 * KT) * (a.d + 1) + R * KT);
-    attn_generic_kernel<T><<<(unsigned)((int64_t)a.seqs * tiles * a.hk), THREADS, bytes, st>>>(a, tiles);
+    const int64_t tiles = tiles_of((int64_t)a.max_q * (a.hq / a.hk));
+    const GenArgs f{a, Div::of(a.hq / a.hk), Div::of(tiles), nullptr};
+    attn_generic_kernel<T, NT><<<(unsigned)(a.seqs * tiles * a.hk), THREADS,
+                                 sizeof(float) * (2 * 4 * R + 4 * R * (a.d + 1)), st>>>(f);
+    return hipGetLastError();
+}
+
+template <typename T, int NT>
+hipError_t backward(const AttnArgs &a, hipStream_t st) {
+    const int64_t g = a.hq / a.hk, tiles = tiles_of(a.max_q * g);
+    const size_t bytes = sizeof(float) * 4 * R * (a.d + 1);
+    GenArgs f{a, Div::of(g), Div::of(tiles > 0 ? tiles : 1), (float *)a.work};
+    if (a.total_q > 0) {
+        attn_delta_kernel<T><<<(unsigned)(((int64_t)a.total_q * a.hq + 3) / 4), THREADS, 0, st>>>(f);
+        attn_generic_dq_kernel<T, NT><<<(unsigned)(a.seqs * tiles * a.hk), THREADS, bytes, st>>>(f);
+    }
+    const int64_t pt = tiles_of(a.max_prefix), sl = tiles_of(a.max_suffix);
+    if (pt) {
+        f.tiles = Div::of(pt);
+        attn_generic_dkv_kernel<T, NT, true><<<(unsigned)(a.groups * pt * a.hk), THREADS, bytes, st>>>(f);
+    }
+    if (sl) {
+        f.tiles = Div::of(sl);
+        attn_generic_dkv_kernel<T, NT, false><<<(unsigned)(a.seqs * sl * a.hk), THREADS, bytes, st>>>(f);
+    }
     return hipGetLastError();
 }
 
 template <typename T>
-hipError_t backward(const AttnArgs &a, hipStream_t st) {
-    float *delta = (float *)a.work;
-    const int g = a.hq / a.hk;
-    const int tiles = (int)tiles_of((int64_t)a.max_q * g, R);
-    const size_t bytes = sizeof(float) * ((2 * R + 2 * KT) * (a.d + 1) + 2 * R * KT);
-    if (a.total_q > 0) {
-        attn_delta_kernel<T><<<(unsigned)tiles_of(a.total_q * a.hq, 4), THREADS, 0, st>>>(a, delta);
-        attn_generic_dq_kernel<T><<<(unsigned)((int64_t)a.seqs * tiles * a.hk), THREADS, bytes, st>>>(
-            a, tiles, delta);
-    }
-    const int pt = (int)tiles_of(a.max_prefix, KT), sl = (int)tiles_of(a.max_suffix, KT);
-    if (pt)
-        attn_generic_dkv_kernel<T, true><<<(unsigned)((int64_t)a.groups * pt * a.hk), THREADS, bytes, st>>>(
-            a, pt, delta);
-    if (sl)
-        attn_generic_dkv_kernel<T, false><<<(unsigned)((int64_t)a.seqs * sl * a.hk), THREADS, bytes, st>>>(
-            a, sl, delta);
-    return hipGetLastError();
+hipError_t by_size(const AttnArgs &a, bool back, hipStream_t st) {
+    if (a.d <= 64) return back ? backward<T, 4>(a, st) : forward<T, 4>(a, st);
+    if (a.d <= 128) return back ? backward<T, 8>(a, st) : forward<T, 8>(a, st);
+    return back ? backward<T, 16>(a, st) : forward<T, 16>(a, st);
 }
 
 }  // namespace
 
 hipError_t launch_attn_generic(const AttnArgs &a, bool bf16, hipStream_t st) {
-    return bf16 ? forward<uint16_t>(a, st) : forward<float>(a, st);
+    return bf16 ? by_size<uint16_t>(a, false, st) : by_size<float>(a, false, st);
 }
 hipError_t launch_attn_generic_backward(const AttnArgs &a, bool bf16, hipStream_t st) {
-    return bf16 ? backward<uint16_t>(a, st) : backward<float>(a, st);
+    return bf16 ? by_size<uint16_t>(a, true, st) : by_size<float>(a, true, st);
 }
 
 }  // namespace olive
