@@ -6,6 +6,8 @@
 // it walks over heads: the angles and weights of its elements stay in registers.
 //
 // Bound by memory: 7 (backward 14) operations an element for 4 (6) bytes in bf16.
+#include <type_traits>
+
 #include "layers_internal.hpp"
 #include "olive_device.hpp"
 
@@ -41,9 +43,37 @@ __device__ __forceinline__ void store_vec(T *p, const float (&x)[VEC]) {
     *(Pack<T, VEC> *)p = u;
 }
 
+// A value from another lane of the same 16, without LDS: CTRL is the DPP pattern.
+template <int CTRL, int BANKS = 0xf>
+__device__ __forceinline__ float dpp(float old, float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(v), CTRL, 0xf, BANKS, false));
+}
+constexpr int kRor = 0x120, kShl = 0x100, kShr = 0x110, kHalfMirror = 0x141;
+constexpr int quad(int a, int b, int c, int d) { return a | b << 2 | c << 4 | d << 6; }
+
+// Sum over the LPR lanes of a row (LPR 0: `lpr` of them).
+template <int LPR>
 __device__ __forceinline__ float row_sum(float v, int lpr) {
-    for (int o = lpr >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    if constexpr (LPR == 16) {
+        v += dpp<kRor + 8>(v, v);
+        v += dpp<kRor + 4>(v, v);
+        v += dpp<kRor + 2>(v, v);
+        v += dpp<kRor + 1>(v, v);
+    } else if constexpr (LPR == 8) {
+        v += dpp<kHalfMirror>(v, v);
+        v += dpp<quad(2, 3, 0, 1)>(v, v);
+        v += dpp<quad(1, 0, 3, 2)>(v, v);
+    } else {
+        for (int o = lpr >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    }
     return v;
+}
+// The value of the lane LPR / 2 away in the same row.
+template <int LPR>
+__device__ __forceinline__ float across(float v) {
+    if constexpr (LPR == 16) return dpp<kRor + 8>(v, v);
+    const float lo = dpp<kShl + 4, 0x5>(v, v);       // lanes 0..3 of 8 take 4..7
+    return dpp<kShr + 4, 0xa>(lo, v);                // and the other way round
 }
 
 // What a lane keeps of a token: for each of its elements the cosine and the signed sine of
@@ -88,10 +118,16 @@ __device__ __forceinline__ void load_angles(const QkArgs &a, int t, int li, int 
     }
 }
 
-// x cos + partner * sin of a row; SIGN -1 is the transposed rotation.
-template <int VEC, int NV, int SIGN>
-__device__ __forceinline__ void rotate(const Angles<VEC, NV> &g, int rot, int layout, int li,
-                                       int lpr, float (&x)[NV][VEC]) {
+// x cos + partner * sin of a row; SIGN -1 is the transposed rotation. LPR: the whole head turns
+// by halves that lie LPR / 2 lanes apart (0: any rotation).
+template <int VEC, int NV, int LPR, int SIGN>
+__device__ __forceinline__ void rotate(const Angles<VEC, NV> &g, int rot, int layout, int li, int lpr,
+                                       float (&x)[NV][VEC]) {
+    if constexpr (LPR > 0) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[0][j] = fmaf(across<LPR>(x[0][j]), SIGN * g.s[0][j], x[0][j] * g.c[0][j]);
+        return;
+    }
     float p[NV][VEC];
     if (VEC > 1 && layout == OLIVE_ROPE_PAIRS) {
 #pragma unroll
@@ -119,7 +155,7 @@ __device__ __forceinline__ void rotate(const Angles<VEC, NV> &g, int rot, int la
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
             const bool turned = (li + 64 * v) * VEC + j < rot;
-            x[v][j] = x[v][j] * g.c[v][j] + (turned ? p[v][j] : 0.f) * (SIGN * g.s[v][j]);
+            x[v][j] = fmaf(turned ? p[v][j] : 0.f, SIGN * g.s[v][j], x[v][j] * g.c[v][j]);
         }
 }
 
@@ -135,89 +171,89 @@ __device__ __forceinline__ void load_weight(const void *w, int li, int nvec,
     }
 }
 
+// 1 / root of the mean square (v_rsq_f32 is off by one unit at most).
+__device__ __forceinline__ float inv_root(float ss, float inv_d, float eps) {
+    return __builtin_amdgcn_rsqf(fmaf(ss, inv_d, eps));
+}
+
 // Wavefront w of the grid: token w / chunks, rows (w % chunks) * per ... of its q, k and v.
-template <typename T, int VEC, int NV>
-__global__ __launch_bounds__(256) void qk_forward_kernel(QkArgs a, int lpr, int chunks, int per) {
+template <typename T, int VEC, int NV, int LPR>
+__global__ __launch_bounds__(256) void qk_forward_kernel(QkArgs a, int lpr_, int chunks, int per) {
+    const int lpr = LPR ? LPR : lpr_;
     const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t = (int)(w / chunks);
     if (t >= a.tokens) return;
     const int li = lane & (lpr - 1), sub = lane / lpr, rpw = 64 / lpr;
     const int nvec = a.d / VEC;
-    const int rows = a.hq + a.hk + a.hv;
-    const int h0 = (int)(w % chunks) * per, h1 = min(rows, h0 + per);
+    const int h0 = (int)(w % chunks) * per, h1 = h0 + per;
+    const float inv_d = 1.f / (float)a.d;
 
     Angles<VEC, NV> g;
     load_angles<VEC, NV>(a, t, li, nvec, g);
-    float wq[NV][VEC], wk[NV][VEC];
-    load_weight<T, VEC, NV>(a.wq, li, nvec, wq);
-    load_weight<T, VEC, NV>(a.wk, li, nvec, wk);
     const int64_t slot = a.slots ? (int64_t)a.slots[t] : t;
     const bool put = !a.slots || (slot >= 0 && slot < a.slot_rows);
 
-    for (int h = h0; h < h1; h += rpw) {
-        const int r = h + sub;
-        const bool live = r < h1;
-        const bool is_q = r < a.hq, is_v = r >= a.hq + a.hk;
-        const T *src;
-        T *dst;
-        if (is_q) {
-            src = (const T *)a.q.p + t * a.q.st + r * a.q.sh;
-            dst = (T *)a.qo.p + t * a.qo.st + r * a.qo.sh;
-        } else if (!is_v) {
-            src = (const T *)a.k.p + t * a.k.st + (r - a.hq) * a.k.sh;
-            dst = (T *)a.ko.p + slot * a.ko.st + (r - a.hq) * a.ko.sh;
-        } else {
-            src = (const T *)a.v.p + t * a.v.st + (r - a.hq - a.hk) * a.v.sh;
-            dst = (T *)a.vo.p + slot * a.vo.st + (r - a.hq - a.hk) * a.vo.sh;
-        }
-        float x[NV][VEC];
-        float ss = 0.f;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int i = li + 64 * v;
-            if (live && i < nvec) {
-                load_vec<T, VEC>(src + i * VEC, x[v]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) x[v][j] = 0.f;
-            }
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) ss = fmaf(x[v][j], x[v][j], ss);
-        }
-        ss = row_sum(ss, lpr);
-        if (!is_v) {
-            const float r_ = (is_q ? a.wq : a.wk) ? 1.f / sqrtf(ss / (float)a.d + a.eps) : 1.f;
-#pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) x[v][j] *= r_ * (is_q ? wq[v][j] : wk[v][j]);
-        }
-        float y[NV][VEC];
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) y[v][j] = x[v][j];
-        rotate<VEC, NV, 1>(g, a.rot, a.layout, li, lpr, y);
-        if (live && (is_q || put)) {
+    // heads [first, first + n) of this wavefront's rows are those of one view
+    const auto heads = [&](auto kind, int first, int n, const HeadsArg &from, const HeadsArg &to, const void *weight,
+                           int64_t row, bool keep) {
+        constexpr bool COPY = decltype(kind)::value;
+        const T *src = (const T *)from.p + t * from.st;
+        T *dst = (T *)to.p + row * to.st;
+        float wt[NV][VEC];
+        load_weight<T, VEC, NV>(weight, li, nvec, wt);
+        for (int h = max(h0 - first, 0); h < min(h1 - first, n); h += rpw) {
+            const int r = h + sub;
+            const bool live = r < min(h1 - first, n);
+            float x[NV][VEC], ss = 0.f;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int i = li + 64 * v;
-                if (i < nvec) store_vec<T, VEC>(dst + i * VEC, is_v ? x[v] : y[v]);
+                if (live && i < nvec) {
+                    load_vec<T, VEC>(src + r * from.sh + i * VEC, x[v]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) x[v][j] = 0.f;
+                }
+            }
+            if (!COPY) {
+                if (weight) {
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) ss = fmaf(x[v][j], x[v][j], ss);
+                    const float rr = inv_root(row_sum<LPR>(ss, lpr), inv_d, a.eps);
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) x[v][j] = x[v][j] * rr * wt[v][j];
+                }
+                rotate<VEC, NV, LPR, 1>(g, a.rot, a.layout, li, lpr, x);
+            }
+            if (live && keep) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const int i = li + 64 * v;
+                    if (i < nvec) store_vec<T, VEC>(dst + r * to.sh + i * VEC, x[v]);
+                }
             }
         }
-    }
+    };
+    heads(std::false_type{}, 0, a.hq, a.q, a.qo, a.wq, t, true);
+    heads(std::false_type{}, a.hq, a.hk, a.k, a.ko, a.wk, slot, put);
+    if (a.hv) heads(std::true_type{}, a.hq + a.hk, a.hv, a.v, a.vo, nullptr, slot, put);
 }
 
 // Persistent wavefronts over tokens; a lane sums its elements' weight gradients over all its
 // rows, the workgroup joins them in a fixed order and writes one partial row.
-template <typename T, int VEC, int NV>
-__global__ __launch_bounds__(256) void qk_backward_kernel(QkArgs a, int lpr) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+template <typename T, int VEC, int NV, int LPR>
+__global__ __launch_bounds__(256) void qk_backward_kernel(QkArgs a, int lpr_) {
+    const int lpr = LPR ? LPR : lpr_;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int li = lane & (lpr - 1), sub = lane / lpr, rpw = 64 / lpr;
     const int nvec = a.d / VEC;
-    const int rows = a.hq + a.hk;
     const int stride = gridDim.x * 4;
+    const float inv_d = 1.f / (float)a.d;
     float wq[NV][VEC], wk[NV][VEC], sq[NV][VEC] = {}, sk[NV][VEC] = {};
     load_weight<T, VEC, NV>(a.wq, li, nvec, wq);
     load_weight<T, VEC, NV>(a.wk, li, nvec, wk);
@@ -225,64 +261,58 @@ __global__ __launch_bounds__(256) void qk_backward_kernel(QkArgs a, int lpr) {
     for (int t = blockIdx.x * 4 + wave; t < a.tokens; t += stride) {
         Angles<VEC, NV> g;
         load_angles<VEC, NV>(a, t, li, nvec, g);
-        for (int h = 0; h < rows; h += rpw) {
-            const int r = h + sub;
-            const bool live = r < rows, is_q = r < a.hq;
-            const T *src, *grd;
-            T *dst;
-            if (is_q) {
-                src = (const T *)a.q.p + t * a.q.st + r * a.q.sh;
-                grd = (const T *)a.qo.p + t * a.qo.st + r * a.qo.sh;
-                dst = (T *)a.gq.p + t * a.gq.st + r * a.gq.sh;
-            } else {
-                src = (const T *)a.k.p + t * a.k.st + (r - a.hq) * a.k.sh;
-                grd = (const T *)a.ko.p + t * a.ko.st + (r - a.hq) * a.ko.sh;
-                dst = (T *)a.gk.p + t * a.gk.st + (r - a.hq) * a.gk.sh;
-            }
-            float x[NV][VEC], y[NV][VEC];
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int i = li + 64 * v;
-                if (live && i < nvec) {
-                    load_vec<T, VEC>(src + i * VEC, x[v]);
-                    load_vec<T, VEC>(grd + i * VEC, y[v]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) x[v][j] = y[v][j] = 0.f;
-                }
-            }
-            rotate<VEC, NV, -1>(g, a.rot, a.layout, li, lpr, y);
-            if ((is_q ? a.wq : a.wk)) {
-                float ss = 0.f, sh = 0.f;
-#pragma unroll
-                for (int v = 0; v < NV; ++v)
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        ss = fmaf(x[v][j], x[v][j], ss);
-                        sh = fmaf(y[v][j] * (is_q ? wq[v][j] : wk[v][j]), x[v][j], sh);
-                    }
-                ss = row_sum(ss, lpr);
-                sh = row_sum(sh, lpr);
-                const float r_ = 1.f / sqrtf(ss / (float)a.d + a.eps);
-                const float m = r_ * r_ * (sh / (float)a.d);
-#pragma unroll
-                for (int v = 0; v < NV; ++v)
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        // (rows that are not there have x = y = 0)
-                        const float gw = live && (li + 64 * v) < nvec ? y[v][j] * (x[v][j] * r_) : 0.f;
-                        if (is_q) sq[v][j] += gw; else sk[v][j] += gw;
-                        y[v][j] = r_ * (y[v][j] * (is_q ? wq[v][j] : wk[v][j]) - x[v][j] * m);
-                    }
-            }
-            if (live) {
+        const auto heads = [&](int n, const HeadsArg &from, const HeadsArg &grad, const HeadsArg &to, bool normed,
+                               const float (&wt)[NV][VEC], float (&sum)[NV][VEC]) {
+            const T *src = (const T *)from.p + t * from.st, *grd = (const T *)grad.p + t * grad.st;
+            T *dst = (T *)to.p + t * to.st;
+            for (int h = 0; h < n; h += rpw) {
+                const int r = h + sub;
+                const bool live = r < n;
+                float x[NV][VEC], y[NV][VEC];
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {
                     const int i = li + 64 * v;
-                    if (i < nvec) store_vec<T, VEC>(dst + i * VEC, y[v]);
+                    if (live && i < nvec) {
+                        load_vec<T, VEC>(src + r * from.sh + i * VEC, x[v]);
+                        load_vec<T, VEC>(grd + r * grad.sh + i * VEC, y[v]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) x[v][j] = y[v][j] = 0.f;
+                    }
+                }
+                rotate<VEC, NV, LPR, -1>(g, a.rot, a.layout, li, lpr, y);
+                if (normed) {
+                    float ss = 0.f, sh = 0.f;
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) {
+                            ss = fmaf(x[v][j], x[v][j], ss);
+                            sh = fmaf(y[v][j] * wt[v][j], x[v][j], sh);
+                        }
+                    ss = row_sum<LPR>(ss, lpr);
+                    sh = row_sum<LPR>(sh, lpr);
+                    const float rr = inv_root(ss, inv_d, a.eps), m = rr * rr * (sh * inv_d);
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) {
+                            // (a row that is not there has x = y = 0, and eps may be 0)
+                            if (live && li + 64 * v < nvec) sum[v][j] = fmaf(y[v][j], x[v][j] * rr, sum[v][j]);
+                            y[v][j] = rr * (y[v][j] * wt[v][j] - x[v][j] * m);
+                        }
+                }
+                if (live) {
+#pragma unroll
+                    for (int v = 0; v < NV; ++v) {
+                        const int i = li + 64 * v;
+                        if (i < nvec) store_vec<T, VEC>(dst + r * to.sh + i * VEC, y[v]);
+                    }
                 }
             }
-        }
+        };
+        heads(a.hq, a.q, a.qo, a.gq, a.wq != nullptr, wq, sq);
+        heads(a.hk, a.k, a.ko, a.gk, a.wk != nullptr, wk, sk);
     }
     if (!a.gwq && !a.gwk) return;
     __shared__ float join[4][2][256];
@@ -309,28 +339,32 @@ __global__ __launch_bounds__(256) void qk_backward_kernel(QkArgs a, int lpr) {
     }
 }
 
-// Sums the partial rows: 16 columns a workgroup, 16 threads a column.
+// Sums the partial rows: 16 columns a workgroup, 4 of them and every 64th row a thread.
 __global__ __launch_bounds__(256) void qk_weight_grad_kernel(QkArgs a, int blocks) {
-    const int col = blockIdx.x * 16 + (threadIdx.x & 15), part = threadIdx.x >> 4;
-    float s = 0.f;
-    if (col < 2 * a.d)
-        for (int b = part; b < blocks; b += 16) s += a.part[(int64_t)b * 2 * a.d + col];
-    __shared__ float join[16][17];
-    join[part][threadIdx.x & 15] = s;
+    const int cols = 2 * a.d, quad = threadIdx.x & 3, part = threadIdx.x >> 2, c0 = blockIdx.x * 16 + 4 * quad;
+    float s[4] = {};
+#pragma unroll 4
+    for (int b = part; b < blocks; b += 64)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c0 + i < cols) s[i] += a.part[(int64_t)b * cols + c0 + i];
+    __shared__ float join[64][17];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) join[part][4 * quad + i] = s[i];
     __syncthreads();
-    if (part == 0 && col < 2 * a.d) {
-        float u = 0.f;
-        for (int i = 0; i < 16; ++i) u += join[i][threadIdx.x & 15];
-        float *out = col < a.d ? a.gwq : a.gwk;
-        if (out) out[col < a.d ? col : col - a.d] = u;
+    // 16 threads a column, then their sums
+    const int col = threadIdx.x >> 4, k = threadIdx.x & 15;
+    float u = (join[k][col] + join[k + 16][col]) + (join[k + 32][col] + join[k + 48][col]);
+    for (int o = 8; o > 0; o >>= 1) u += __shfl_xor(u, o);
+    const int c = blockIdx.x * 16 + col;
+    if (k == 0 && c < cols) {
+        float *out = c < a.d ? a.gwq : a.gwk;
+        if (out) out[c < a.d ? c : c - a.d] = u;
     }
 }
 
-template <typename T, int VEC, int NV>
-hipError_t go(const QkArgs &a, bool backward, hipStream_t st) {
-    const int nvec = a.d / VEC;
-    int lpr = 1;
-    while (lpr < nvec && lpr < 64) lpr <<= 1;
+template <typename T, int VEC, int NV, int LPR>
+hipError_t launch(const QkArgs &a, int lpr, bool backward, hipStream_t st) {
     if (!backward) {
         const int rpw = 64 / lpr, rows = a.hq + a.hk + a.hv;
         // a wavefront walks over all heads of its token where there are tokens enough to
@@ -341,14 +375,27 @@ hipError_t go(const QkArgs &a, bool backward, hipStream_t st) {
         per = (per + rpw - 1) / rpw * rpw;
         const int chunks = (rows + per - 1) / per;
         const int64_t waves = (int64_t)a.tokens * chunks;
-        qk_forward_kernel<T, VEC, NV><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(a, lpr, chunks,
-                                                                                   per);
+        qk_forward_kernel<T, VEC, NV, LPR><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(a, lpr, chunks, per);
         return hipGetLastError();
     }
     const int blocks = max(1, min(kQkBwdBlocks, (a.tokens + 3) / 4));
-    qk_backward_kernel<T, VEC, NV><<<blocks, 256, 0, st>>>(a, lpr);
+    qk_backward_kernel<T, VEC, NV, LPR><<<blocks, 256, 0, st>>>(a, lpr);
     if (a.gwq || a.gwk) qk_weight_grad_kernel<<<(2 * a.d + 15) / 16, 256, 0, st>>>(a, blocks);
     return hipGetLastError();
+}
+
+template <typename T, int VEC, int NV>
+hipError_t go(const QkArgs &a, bool backward, hipStream_t st) {
+    const int nvec = a.d / VEC;
+    int lpr = 1;
+    while (lpr < nvec && lpr < 64) lpr <<= 1;
+    // whole heads that turn by halves, on 16 or 8 lanes: sums and partners without LDS
+    if constexpr (NV == 1 && VEC * sizeof(T) == 16) {
+        const bool halves = a.layout == OLIVE_ROPE_HALF && a.rot == a.d && nvec == lpr;
+        if (halves && lpr == 16) return launch<T, VEC, NV, 16>(a, lpr, backward, st);
+        if (halves && lpr == 8) return launch<T, VEC, NV, 8>(a, lpr, backward, st);
+    }
+    return launch<T, VEC, NV, 0>(a, lpr, backward, st);
 }
 
 bool aligned(const HeadsArg &h, int bytes, int esz) {
