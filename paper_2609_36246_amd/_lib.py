@@ -11,6 +11,8 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
+import threading
 from typing import Optional
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -129,6 +131,7 @@ class OliveError(RuntimeError):
 
 
 _lib: Optional[ctypes.CDLL] = None
+_calls = {}              # the layer operators' entries with addresses for every pointer
 
 
 def load() -> ctypes.CDLL:
@@ -181,6 +184,12 @@ def load() -> ctypes.CDLL:
     lib.olive_score_last_stats.restype = st
     lib.olive_score_kernel_times.argtypes = [vp, ctypes.POINTER(ctypes.c_float), ctypes.c_int]
     lib.olive_score_kernel_times.restype = st
+    for name, args in (("olive_qk_norm_rope", "p" * 8), ("olive_qk_norm_rope_backward", "p" * 10 + "lp"),
+                       ("olive_prefix_attention", "p" * 9 + "lp"),
+                       ("olive_prefix_attention_backward", "p" * 15 + "lp"),
+                       ("olive_grad_clip", "pfpp")):
+        kinds = {"p": vp, "l": ctypes.c_int64, "f": ctypes.c_float}
+        _calls[name] = ctypes.CFUNCTYPE(st, *(kinds[a] for a in args))((name, lib))
     hp, qp = ctypes.POINTER(olive_heads), ctypes.POINTER(olive_qk_desc)
     ap, i64 = ctypes.POINTER(olive_attn_desc), ctypes.c_int64
     lib.olive_qk_norm_rope.argtypes = [qp] + [hp] * 6 + [vp]
@@ -218,7 +227,7 @@ def _ptr(x) -> Optional[int]:
 def _stream(stream) -> Optional[int]:
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -417,18 +426,51 @@ def make_heads(x) -> Optional[olive_heads]:
     contiguous (None stays None; the caller keeps the tensor alive)."""
     if x is None or isinstance(x, olive_heads):
         return x
-    if x.dim() != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
+    return olive_heads(*_view(x))
+
+
+def _view(x):
+    s = x.stride()
+    if len(s) != 3 or (s[2] != 1 and x.shape[2] > 1):
         raise ValueError("expected [tokens, heads, head_dim] with contiguous heads")
-    return olive_heads(_ptr(x), x.stride(0), x.stride(1))
+    return x.data_ptr(), s[0], s[1]
 
 
-def _heads(x):
-    h = make_heads(x)
-    return None if h is None else ctypes.byref(h)
+class _Views(threading.local):
+    """A thread's olive_heads of one call: written before it, read by it before it returns."""
+
+    def __init__(self):
+        self.buffer = ctypes.create_string_buffer(16 * ctypes.sizeof(olive_heads))
+        self.at = [ctypes.addressof(self.buffer) + i * ctypes.sizeof(olive_heads) for i in range(16)]
+
+
+_views = _Views()
+_packers = [struct.Struct("=%dq" % (3 * i)) for i in range(17)]
+
+
+def _heads(*xs):
+    """Addresses of the views' olive_heads (one object made for each would cost more time than
+    a small call on the GPU)."""
+    values, at = [], []
+    for x, place in zip(xs, _views.at):
+        if x is None:
+            values += (0, 0, 0)
+            at.append(None)
+        else:
+            values += (x.data or 0, x.stride_token, x.stride_head) if isinstance(x, olive_heads) else _view(x)
+            at.append(place)
+    _packers[len(at)].pack_into(_views.buffer, 0, *values)
+    return at
+
+
+def _call(name):
+    if _lib is None:
+        load()
+    return _calls[name]
 
 
 def _workspace(w):
-    return _ptr(w), (0 if w is None else w.numel() * w.element_size())
+    return (None, 0) if w is None else (w.data_ptr(), w.numel() * w.element_size())
 
 
 def make_qk_desc(tokens, heads_q, heads_k, head_dim, positions=None, cos=None, sin=None,
@@ -451,8 +493,8 @@ def make_qk_desc(tokens, heads_q, heads_k, head_dim, positions=None, cos=None, s
 
 def olive_qk_norm_rope(desc: olive_qk_desc, q, k, q_out, k_out, v=None, v_out=None, stream=None,
                        check: bool = True) -> int:
-    s = load().olive_qk_norm_rope(ctypes.byref(desc), _heads(q), _heads(k), _heads(v),
-                                  _heads(q_out), _heads(k_out), _heads(v_out), _stream(stream))
+    s = _call("olive_qk_norm_rope")(ctypes.addressof(desc), *_heads(q, k, v, q_out, k_out, v_out),
+                                    _stream(stream))
     if check:
         _check(s, "olive_qk_norm_rope")
     return s
@@ -469,10 +511,9 @@ def olive_qk_norm_rope_workspace(desc: olive_qk_desc) -> int:
 def olive_qk_norm_rope_backward(desc: olive_qk_desc, q, k, grad_q_out, grad_k_out, grad_q, grad_k,
                                 grad_weight_q=None, grad_weight_k=None, workspace=None,
                                 stream=None, check: bool = True) -> int:
-    s = load().olive_qk_norm_rope_backward(
-        ctypes.byref(desc), _heads(q), _heads(k), _heads(grad_q_out), _heads(grad_k_out),
-        _heads(grad_q), _heads(grad_k), _ptr(grad_weight_q), _ptr(grad_weight_k),
-        *_workspace(workspace), _stream(stream))
+    s = _call("olive_qk_norm_rope_backward")(
+        ctypes.addressof(desc), *_heads(q, k, grad_q_out, grad_k_out, grad_q, grad_k),
+        _ptr(grad_weight_q), _ptr(grad_weight_k), *_workspace(workspace), _stream(stream))
     if check:
         _check(s, "olive_qk_norm_rope_backward")
     return s
@@ -517,9 +558,9 @@ def olive_prefix_attention_workspace(desc: olive_attn_desc, backward: bool = Fal
 
 def olive_prefix_attention(desc: olive_attn_desc, q, k_prefix, v_prefix, k_suffix, v_suffix, out,
                            lse=None, workspace=None, stream=None, check: bool = True) -> int:
-    s = load().olive_prefix_attention(
-        ctypes.byref(desc), _heads(q), _heads(k_prefix), _heads(v_prefix), _heads(k_suffix),
-        _heads(v_suffix), _heads(out), _ptr(lse), *_workspace(workspace), _stream(stream))
+    s = _call("olive_prefix_attention")(
+        ctypes.addressof(desc), *_heads(q, k_prefix, v_prefix, k_suffix, v_suffix, out), _ptr(lse),
+        *_workspace(workspace), _stream(stream))
     if check:
         _check(s, "olive_prefix_attention")
     return s
@@ -529,11 +570,10 @@ def olive_prefix_attention_backward(desc: olive_attn_desc, q, k_prefix, v_prefix
                                     v_suffix, out, lse, grad_out, grad_q, grad_k_prefix,
                                     grad_v_prefix, grad_k_suffix, grad_v_suffix, workspace=None,
                                     stream=None, check: bool = True) -> int:
-    s = load().olive_prefix_attention_backward(
-        ctypes.byref(desc), _heads(q), _heads(k_prefix), _heads(v_prefix), _heads(k_suffix),
-        _heads(v_suffix), _heads(out), _ptr(lse), _heads(grad_out), _heads(grad_q),
-        _heads(grad_k_prefix), _heads(grad_v_prefix), _heads(grad_k_suffix),
-        _heads(grad_v_suffix), *_workspace(workspace), _stream(stream))
+    at = _heads(q, k_prefix, v_prefix, k_suffix, v_suffix, out, grad_out, grad_q, grad_k_prefix,
+                grad_v_prefix, grad_k_suffix, grad_v_suffix)
+    s = _call("olive_prefix_attention_backward")(
+        ctypes.addressof(desc), *at[:6], _ptr(lse), *at[6:], *_workspace(workspace), _stream(stream))
     if check:
         _check(s, "olive_prefix_attention_backward")
     return s
@@ -566,7 +606,7 @@ def olive_grad_clip_init(grads, outs=None, stream=None) -> int:
 
 
 def olive_grad_clip(ctx, max_norm: float, norm=None, stream=None, check: bool = True) -> int:
-    s = load().olive_grad_clip(ctx, float(max_norm), _ptr(norm), _stream(stream))
+    s = _call("olive_grad_clip")(ctx, max_norm, _ptr(norm), _stream(stream))
     if check:
         _check(s, "olive_grad_clip")
     return s

@@ -183,7 +183,12 @@ def test_attention_pages_and_views():
 
 def test_attention_workspace():
     d = attn_desc()
-    need = L.olive_prefix_attention_workspace(d, backward=True)
+    n = [ctypes.c_int64(), ctypes.c_int64()]
+    for i in (0, 1):
+        assert L.load().olive_prefix_attention_workspace(ctypes.byref(d), i, ctypes.byref(n[i])) == E.OLIVE_OK
+    assert L.olive_prefix_attention_workspace(d) == n[0].value
+    assert L.olive_prefix_attention_workspace(d, backward=True) == max(n[0].value, n[1].value)
+    need = n[1].value
     assert attn_backward(d, size=need - 1) == E.OLIVE_E_SHAPE
     assert attn_backward(d, work=None) == E.OLIVE_E_NULL
     assert attn_backward(d, work=P + 4) == E.OLIVE_E_UNSUPPORTED
