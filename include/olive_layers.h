@@ -153,8 +153,10 @@ typedef struct {
     float scale;                 /* finite */
 } olive_attn_desc;
 
-/* Bytes of the forward's workspace (backward: 0) or of the backward's (1). Host only; a
- * workspace of one description serves every description with sizes that are not larger. */
+/* Bytes of the forward's workspace (backward: 0) or of the backward's (1). Host only. They
+ * grow with total_q, heads_q and head_dim alone (two times min(64 r, 65536 + r) (head_dim + 2)
+ * values for r = total_q heads_q rows; 8 r bytes and 1024 tiles of 128 keys for the backward):
+ * the workspace of the largest call of a dtype serves the others. */
 olive_status olive_prefix_attention_workspace(const olive_attn_desc *desc, int32_t backward,
                                               int64_t *bytes);
 

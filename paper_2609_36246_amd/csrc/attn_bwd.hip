@@ -564,13 +564,13 @@ hipError_t go(const BwdArgs &f, hipStream_t st) {
 
 }  // namespace
 
+// A bound that grows with total_q, the heads and their size alone: parts of the rows are made
+// where the key tiles times the parts are at most two a compute unit.
 int64_t attn_backward_bytes(const AttnArgs &a, bool bf16) {
-    const int64_t plain = (int64_t)a.total_q * a.hq * (int64_t)sizeof(float);   // the generic kernels' delta
-    if (!attn_mfma_sizes(a, bf16) || a.d > 128) return plain;
-    const BwdPlan p = make_plan(a);
-    const int64_t tiles = (p.np > 1 ? p.p_units : 0) + (p.ns > 1 ? p.s_units : 0);
-    return ((int64_t)a.total_q * a.hq * 2 * (int64_t)sizeof(float) + 15) / 16 * 16 +
-           tiles * KEYS * 2 * a.d * (int64_t)sizeof(float);
+    const int64_t rows = (int64_t)a.total_q * a.hq;
+    if (!attn_mfma_sizes(a, bf16) || a.d > 128) return rows * (int64_t)sizeof(float);   // (the generic kernels' delta)
+    return (rows * 2 * (int64_t)sizeof(float) + 15) / 16 * 16 +
+           (int64_t)2 * 2 * kChipUnits * KEYS * 2 * a.d * (int64_t)sizeof(float);
 }
 
 hipError_t launch_attn_backward(const AttnArgs &a, bool bf16, hipStream_t st) {

@@ -591,11 +591,14 @@ bool attn_mfma_applies(const AttnArgs &a, bool bf16) {
     return true;
 }
 
+// A bound that grows with total_q, the heads and their size alone, so that the workspace of the
+// largest call serves the others: along an axis there are at most 64 parts, and at most
+// places / (row tiles) + 1 of them, whose rows together are at most places row tiles and the
+// rows once more.
 int64_t attn_forward_bytes(const AttnArgs &a, bool bf16) {
     if (!attn_mfma_sizes(a, bf16)) return 0;
-    const FwdPlan p = make_plan(a);
-    if (p.direct()) return 0;
-    return (int64_t)p.parts() * a.total_q * a.hq * (a.d + 2) * (int64_t)sizeof(float);
+    const int64_t rows = (int64_t)a.total_q * a.hq, some = 64 * rows, many = 2 * kChipUnits * 128 + rows;
+    return 2 * (some < many ? some : many) * (a.d + 2) * (int64_t)sizeof(float);
 }
 
 hipError_t launch_attn_forward(const AttnArgs &a, bool bf16, hipStream_t st) {

@@ -25,10 +25,10 @@ struct Div {
         }
         return r;
     }
-    __device__ __forceinline__ int quot(int n) const {
-        return d == 1 ? n : (int)(__umulhi((uint32_t)n, mul) >> shift);
+    __host__ __device__ int quot(int n) const {
+        return d == 1 ? n : (int)((uint32_t)((uint64_t)(uint32_t)n * mul >> 32) >> shift);
     }
-    __device__ __forceinline__ int rem(int n, int q) const { return n - q * (int)d; }
+    __host__ __device__ int rem(int n, int q) const { return n - q * (int)d; }
 };
 
 struct HeadsArg {                    // olive_heads with a typed use in the kernels

@@ -165,6 +165,46 @@ def test_out_of_range_arrays(dtype):
     assert nan_rows(p, page_table=table) == [False, False, True]
 
 
+@pytest.mark.parametrize("seqs,max_q", [([(0, 9, 1), (0, 30, 3), (0, 4, 1)], 1),
+                                        ([(0, 400, 300), (0, 300, 200)], 250)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_more_queries_than_stated(seqs, max_q, dtype):
+    """A sequence with more than max_q queries gets NaN in all of them, the others what is theirs."""
+    a = Attn(hq=4, hk=2, d=64, dtype=dtype, prefix=[50], seqs=seqs, grad=True)
+    good, bad = a.run(), a.run(grad=True, desc=a.desc(max_q=max_q))
+    for b, (_, _, n) in enumerate(seqs):
+        s = slice(a.cu[b], a.cu[b + 1])
+        for k in ("out", "lse") + (("dq",) if n > max_q else ()):
+            if n > max_q:
+                assert bool(torch.isnan(bad[k][s]).all()), (b, k)
+        if n <= max_q:
+            ref = a.reference()[b]
+            assert np.all(np.abs(f64(bad["out"][s]) - ref["out"]) <= 0.05 * ref["out_abs"] + 1e-3)
+            assert torch.allclose(bad["lse"][s], good["lse"][s], rtol=1e-5)
+
+
+@pytest.mark.parametrize("groups,dtype", [(64, BF16), (131, BF16), (64, F32)])
+def test_many_groups(groups, dtype):
+    """More groups and sequences than a wavefront looks through at once."""
+    r = np.random.RandomState(1)
+    seqs = [(g, int(r.randint(1, 9)), 1) for g in range(groups) for _ in range(r.randint(0, 5))]
+    a = Attn(hq=2, hk=1, d=64, dtype=dtype, prefix=[int(x) for x in r.randint(0, 40, groups)], seqs=seqs)
+    a.check(a.run())
+
+
+def test_many_sequences():
+    a = Attn(hq=1, hk=1, d=64, prefix=[3, 5], seqs=[(i // 2600, 1 + i % 3, 1) for i in range(5200)], spare=0)
+    a.check(a.run())
+    a = Attn(hq=1, hk=1, d=64, prefix=[0] * 4200, seqs=[(i, 1 + i % 3, 1) for i in range(4200)], spare=0)
+    a.check(a.run())
+
+
+def test_workspace_of_the_largest_call_serves_the_others():
+    need = lambda **k: L.olive_prefix_attention_workspace(Attn(hq=8, hk=2, d=128, **k).desc(), backward=True)  # noqa: E731
+    most = need(prefix=[400], seqs=[(0, 64, 64)] * 4)
+    assert all(need(**SHAPES[s]) <= most for s in ("one_key", "decode", "decode_long", "decode_groups", "extend"))
+
+
 def test_query_offsets_out_of_order():
     """A sequence whose query rows are not in [0, total_q] is left out."""
     a = Attn(hq=2, hk=1, d=64, prefix=[30], seqs=[(0, 8, 4), (0, 9, 3), (0, 5, 5)])
