@@ -476,7 +476,8 @@ def _workspace(w):
 def make_qk_desc(tokens, heads_q, heads_k, head_dim, positions=None, cos=None, sin=None,
                  weight_q=None, weight_k=None, dtype=OLIVE_BF16, eps=1e-6, layout=OLIVE_ROPE_HALF,
                  rot_dim=None, num_positions=None, slots=None, slot_rows=0) -> olive_qk_desc:
-    """cos and sin: fp32 [num_positions, rot_dim / 2], which give the default sizes."""
+    """cos and sin: fp32 [num_positions, rot_dim / 2], which give the default sizes. The
+    descriptor keeps its tensors alive."""
     d = olive_qk_desc()
     d.size = ctypes.sizeof(olive_qk_desc)
     d.dtype, d.tokens = int(dtype), int(tokens)
@@ -488,6 +489,7 @@ def make_qk_desc(tokens, heads_q, heads_k, head_dim, positions=None, cos=None, s
     d.positions, d.cos, d.sin = _ptr(positions), _ptr(cos), _ptr(sin)
     d.weight_q, d.weight_k = _ptr(weight_q), _ptr(weight_k)
     d.slots, d.slot_rows = _ptr(slots), int(slot_rows)
+    d.tensors = (positions, cos, sin, weight_q, weight_k, slots)
     return d
 
 
@@ -524,7 +526,8 @@ def make_attn_desc(heads_q, heads_kv, head_dim, group_seqs, cu_q, prefix_start, 
                    suffix_start=None, page_table=None, page_size=0, dtype=OLIVE_BF16,
                    scale=None, num_groups=None, num_seqs=None) -> olive_attn_desc:
     """Device tensors: group_seqs [G + 1], cu_q [B + 1], prefix_len [G], suffix_len [B] int32,
-    prefix_start [G], suffix_start [B] int64, page_table [B, pages] int32."""
+    prefix_start [G], suffix_start [B] int64, page_table [B, pages] int32. The descriptor
+    keeps them alive."""
     d = olive_attn_desc()
     d.size = ctypes.sizeof(olive_attn_desc)
     d.dtype = int(dtype)
@@ -541,6 +544,7 @@ def make_attn_desc(heads_q, heads_kv, head_dim, group_seqs, cu_q, prefix_start, 
     d.table_stride = 0 if page_table is None or isinstance(page_table, int) \
         else page_table.stride(0)
     d.scale = float(scale if scale is not None else head_dim ** -0.5)
+    d.tensors = (group_seqs, cu_q, prefix_start, prefix_len, suffix_len, suffix_start, page_table)
     return d
 
 
