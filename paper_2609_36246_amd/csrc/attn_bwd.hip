@@ -92,9 +92,10 @@ __global__ __launch_bounds__(256) void attn_stats_kernel(BwdArgs f) {
     }
 }
 
-template <int DP>
+// DB 32-element blocks of the padded head are formed.
+template <int DP, int DB>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f) {
-    constexpr int KT = DQ_KEYS, DB = DP / 32, KS = DP / 16;
+    constexpr int KT = DQ_KEYS, KS = 2 * DB;
     using L = Loader<DP, KT>;
     extern __shared__ __attribute__((aligned(1024))) char lds_mem[];
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
@@ -342,9 +343,9 @@ struct RowLoader {
     }
 };
 
-template <int DP>
+template <int DP, int DB>
 __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
-    constexpr int DB = DP / 32, KS = DP / 16;
+    constexpr int KS = 2 * DB;
     using L = RowLoader<DP>;
     extern __shared__ __attribute__((aligned(1024))) char lds_mem[];
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
@@ -544,16 +545,16 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(BwdArgs f, int first
     }
 }
 
-template <int DP>
+template <int DP, int DB>
 hipError_t go(const BwdArgs &f, hipStream_t st) {
     const AttnArgs &a = f.a;
     const BwdPlan &p = f.p;
     if (a.total_q > 0) {
         attn_stats_kernel<DP><<<(unsigned)ceil_div((int64_t)a.total_q * a.hq, 256 / (DP / 8)), 256, 0, st>>>(f);
-        attn_dq_kernel<DP><<<(unsigned)f.qd.blocks, 256, 2 * 2 * DQ_KEYS * DP * 2, st>>>(f);
+        attn_dq_kernel<DP, DB><<<(unsigned)f.qd.blocks, 256, 2 * 2 * DQ_KEYS * DP * 2, st>>>(f);
     }
     if (p.p_units + p.s_units > 0) {
-        attn_dkv_kernel<DP><<<(unsigned)(f.pd.blocks + f.sd.blocks), 256,
+        attn_dkv_kernel<DP, DB><<<(unsigned)(f.pd.blocks + f.sd.blocks), 256,
                               2 * RowLoader<DP>::STAGE + KEYS * DP * 2, st>>>(f);
         const int64_t pt = p.p_units / p.np, stl = p.s_units / p.ns;
         const int64_t first = p.np > 1 ? 0 : pt, end = p.ns > 1 ? pt + stl : pt;
@@ -595,7 +596,9 @@ hipError_t launch_attn_backward(const AttnArgs &a, bool bf16, hipStream_t st) {
     f.nlse = (float *)a.work;
     f.ndelta = f.nlse + (int64_t)a.total_q * a.hq;
     f.part = (float *)(a.work + ((int64_t)a.total_q * a.hq * 2 * (int64_t)sizeof(float) + 15) / 16 * 16);
-    return a.d <= 64 ? go<64>(f, st) : go<128>(f, st);
+    if (a.d <= 32) return go<64, 1>(f, st);
+    if (a.d <= 64) return go<64, 2>(f, st);
+    return a.d <= 96 ? go<128, 3>(f, st) : go<128, 4>(f, st);
 }
 
 }  // namespace olive

@@ -174,15 +174,16 @@ __device__ __forceinline__ bool find_work(const FwdArgs &f, int block, Work &w) 
 // One pass along the key tiles [w.t0, w.t1): out^T (unscaled), the maximum in log2 units and
 // this half's share of the sum, of the query row `lane % 32` of a wavefront. Returns whether a
 // page lay outside the cache.
-template <int DP, int WR>
+template <int DP, int DB, int WR>
 __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint32_t lds, int wk, bool idle, int seen,
-                                         int least, const bf16x8 (&q)[DP / 16], floatx16 (&acc)[DP / 32],
+                                         int least, const bf16x8 (&q)[2 * DB], floatx16 (&acc)[DB],
                                          float &m, float &l) {
-    constexpr int WK = 4 / WR, KT = tile_keys(DP, WR), NB = KT / 32 / WK, DB = DP / 32, KS = DP / 16;
+    constexpr int WK = 4 / WR, KT = tile_keys(DP, WR), NB = KT / 32 / WK, KS = 2 * DB;
     using L = Loader<DP, KT>;
     const int lane = threadIdx.x & 63;
     const float c = a.scale * kLog2e;
     constexpr int RB = TileRow<DP>::BYTES, KN = NB * KS, VN = NB * 2 * DB;
+    constexpr int GS = KN % 4 ? 2 : 4;               // operands that are read ahead together
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] = zero16();
     m = kNegInf;
@@ -209,20 +210,20 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
         if (idle) return;                            // (it has loaded its share of the tile)
         // operand i of the scores (block i / KS, step i % KS), then of the outputs (16 keys
         // i / DB, elements i % DB)
-        bf16x8 f[2][4];
+        bf16x8 f[2][GS];
         const auto k_at = [&](int i) { return kr.read(i % KS, AT + i / KS * 32 * RB); };
         const auto v_at = [&](int i) { return vr.read(i % DB, AT + i / DB * 16 * RB); };
         floatx16 z[NB];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[0][i] = k_at(i);
+        for (int i = 0; i < GS; ++i) f[0][i] = k_at(i);
 #pragma unroll
-        for (int n = 0; n < KN / 4; ++n) {
+        for (int n = 0; n < KN / GS; ++n) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                f[(n + 1) & 1][i] = 4 * (n + 1) < KN ? k_at(4 * (n + 1) + i) : v_at(i);
+            for (int i = 0; i < GS; ++i)
+                f[(n + 1) & 1][i] = GS * (n + 1) < KN ? k_at(GS * (n + 1) + i) : v_at(i);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int x = 4 * n + i, b = x / KS, s = x % KS;
+            for (int i = 0; i < GS; ++i) {
+                const int x = GS * n + i, b = x / KS, s = x % KS;
                 z[b] = mfma(f[n & 1][i], q[s], s == 0 ? zero16() : z[b]);
             }
         }
@@ -257,15 +258,15 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
         const float m0 = m == kNegInf ? 0.f : m;
         bf16x8 p;
 #pragma unroll
-        for (int n = 0; n < VN / 4; ++n) {
-            constexpr int V0 = KN / 4;               // where the values' first group lies in f
-            if (n + 1 < VN / 4) {
+        for (int n = 0; n < VN / GS; ++n) {
+            constexpr int V0 = KN / GS;               // where the values' first group lies in f
+            if (n + 1 < VN / GS) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) f[(V0 + n + 1) & 1][i] = v_at(4 * (n + 1) + i);
+                for (int i = 0; i < GS; ++i) f[(V0 + n + 1) & 1][i] = v_at(GS * (n + 1) + i);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int x = 4 * n + i, d = x % DB, b = x / DB / 2, mm = x / DB % 2;
+            for (int i = 0; i < GS; ++i) {
+                const int x = GS * n + i, d = x % DB, b = x / DB / 2, mm = x / DB % 2;
                 if (d == 0) {
                     // the weights of the next 16 keys
                     float sum = 0.f;
@@ -357,9 +358,10 @@ __device__ __forceinline__ bool row_by_row(const FwdArgs &f, const Work &w, int 
     return true;
 }
 
-template <int DP, int WR>
+// DB 32-element blocks of the padded head are formed.
+template <int DP, int DB, int WR>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArgs f) {
-    constexpr int WK = 4 / WR, KT = tile_keys(DP, WR), DB = DP / 32, KS = DP / 16;
+    constexpr int WK = 4 / WR, KT = tile_keys(DP, WR), KS = 2 * DB;
     extern __shared__ __attribute__((aligned(1024))) char lds_mem[];
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
     const AttnArgs &a = f.a;
@@ -391,7 +393,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
     const int least = suffix_seen(w.s, f.g.quot(min(w.r0 + 32 * wr, w.rows - 1)));
     floatx16 acc[DB];
     float m, l;
-    const bool off_table = key_loop<DP, WR>(a, w, lds, wk, w.r0 + 32 * wr >= w.rows, seen, least, q, acc, m, l);
+    const bool off_table = key_loop<DP, DB, WR>(a, w, lds, wk, w.r0 + 32 * wr >= w.rows, seen, least, q, acc, m, l);
     {
         float s = 0.f;
 #pragma unroll
@@ -559,11 +561,11 @@ __global__ __launch_bounds__(256) void attn_join_kernel(FwdArgs f) {
     if (a.lse && lane == 0) a.lse[r] = sum == 0.f ? kNegInf : (top + fast_log2(sum)) * kLn2;
 }
 
-template <int DP, int WR>
+template <int DP, int DB, int WR>
 hipError_t go(const FwdArgs &f, hipStream_t st) {
     constexpr int KT = tile_keys(DP, WR);
     constexpr int stages = 2 * 2 * KT * DP * 2, join = WR < 4 ? 4 * (DP / 32) * 4096 + 1024 : 0;
-    attn_fwd_kernel<DP, WR><<<(unsigned)(f.pd.blocks + f.sd.blocks), 256, stages > join ? stages : join, st>>>(f);
+    attn_fwd_kernel<DP, DB, WR><<<(unsigned)(f.pd.blocks + f.sd.blocks), 256, stages > join ? stages : join, st>>>(f);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && !f.p.direct()) {
         attn_join_kernel<<<(unsigned)ceil_div(f.a.total_q * f.a.hq, 4), 256, 0, st>>>(f);
@@ -618,16 +620,18 @@ hipError_t launch_attn_forward(const AttnArgs &a, bool bf16, hipStream_t st) {
     const int64_t rows = (int64_t)f.p.parts() * a.total_q * a.hq;
     f.po = (float *)a.work;
     f.pml = (float2 *)(f.po + rows * a.d);
-    switch (padded(a.d) + f.p.wr) {
-        case 64 + 1: return go<64, 1>(f, st);
-        case 64 + 2: return go<64, 2>(f, st);
-        case 64 + 4: return go<64, 4>(f, st);
-        case 128 + 1: return go<128, 1>(f, st);
-        case 128 + 2: return go<128, 2>(f, st);
-        case 128 + 4: return go<128, 4>(f, st);
-        case 256 + 2: return go<256, 2>(f, st);
-        default: return go<256, 4>(f, st);
-    }
+    const auto by_rows = [&](auto dp, auto db) {
+        constexpr int DP = decltype(dp)::value, DB = decltype(db)::value;
+        if (f.p.wr == 4) return go<DP, DB, 4>(f, st);
+        if constexpr (DP < 256)
+            if (f.p.wr == 1) return go<DP, DB, 1>(f, st);
+        return go<DP, DB, 2>(f, st);
+    };
+    if (a.d <= 32) return by_rows(Const<64>{}, Const<1>{});
+    if (a.d <= 64) return by_rows(Const<64>{}, Const<2>{});
+    if (a.d <= 96) return by_rows(Const<128>{}, Const<3>{});
+    if (a.d <= 128) return by_rows(Const<128>{}, Const<4>{});
+    return by_rows(Const<256>{}, Const<8>{});
 }
 
 }  // namespace olive

@@ -46,7 +46,7 @@ SHAPES = {
     "tall": dict(prefix=[3], seqs=[(0, 2, 2)] * 70),
 }
 HEADS = [(4, 2, 64, BF16), (2, 2, 128, BF16), (7, 1, 128, BF16), (6, 2, 80, BF16), (4, 1, 112, BF16),
-         (3, 3, 40, BF16), (4, 2, 256, BF16), (2, 1, 100, BF16), (2, 1, 1, BF16), (4, 2, 64, F32),
+         (3, 3, 40, BF16), (4, 2, 96, BF16), (4, 2, 24, BF16), (2, 1, 8, BF16), (4, 2, 256, BF16), (2, 1, 100, BF16), (2, 1, 1, BF16), (4, 2, 64, F32),
          (7, 1, 36, F32), (2, 2, 256, F32)]
 
 
