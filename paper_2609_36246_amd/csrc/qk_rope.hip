@@ -339,28 +339,29 @@ __global__ __launch_bounds__(256) void qk_backward_kernel(QkArgs a, int lpr_) {
     }
 }
 
-// Sums the partial rows: 16 columns a workgroup, 4 of them and every 64th row a thread.
+// Sums the partial rows: 4 columns a workgroup, every 256th row a thread (at most 4 of them, all
+// loads in flight together: the pass is a chain of waits, and few rows a thread keep it short).
 __global__ __launch_bounds__(256) void qk_weight_grad_kernel(QkArgs a, int blocks) {
-    const int cols = 2 * a.d, quad = threadIdx.x & 3, part = threadIdx.x >> 2, c0 = blockIdx.x * 16 + 4 * quad;
+    const int cols = 2 * a.d, c0 = blockIdx.x * 4;
     float s[4] = {};
-#pragma unroll 4
-    for (int b = part; b < blocks; b += 64)
+#pragma unroll
+    for (int k = 0; k < kQkBwdBlocks / 256; ++k) {
+        const int b = threadIdx.x + 256 * k;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (c0 + i < cols) s[i] += a.part[(int64_t)b * cols + c0 + i];
-    __shared__ float join[64][17];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) join[part][4 * quad + i] = s[i];
-    __syncthreads();
-    // 16 threads a column, then their sums
-    const int col = threadIdx.x >> 4, k = threadIdx.x & 15;
-    float u = (join[k][col] + join[k + 16][col]) + (join[k + 32][col] + join[k + 48][col]);
-    for (int o = 8; o > 0; o >>= 1) u += __shfl_xor(u, o);
-    const int c = blockIdx.x * 16 + col;
-    if (k == 0 && c < cols) {
-        float *out = c < a.d ? a.gwq : a.gwk;
-        if (out) out[c < a.d ? c : c - a.d] = u;
+            if (b < blocks && c0 + i < cols) s[i] += a.part[(int64_t)b * cols + c0 + i];
     }
+    __shared__ float join[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        for (int o = 32; o > 0; o >>= 1) s[i] += __shfl_xor(s[i], o);
+        if ((threadIdx.x & 63) == 0) join[threadIdx.x >> 6][i] = s[i];
+    }
+    __syncthreads();
+    const int i = threadIdx.x, c = c0 + i;
+    if (i >= 4 || c >= cols) return;
+    float *out = c < a.d ? a.gwq : a.gwk;
+    if (out) out[c < a.d ? c : c - a.d] = (join[0][i] + join[1][i]) + (join[2][i] + join[3][i]);
 }
 
 template <typename T, int VEC, int NV, int LPR>
@@ -380,7 +381,7 @@ hipError_t launch(const QkArgs &a, int lpr, bool backward, hipStream_t st) {
     }
     const int blocks = max(1, min(kQkBwdBlocks, (a.tokens + 3) / 4));
     qk_backward_kernel<T, VEC, NV, LPR><<<blocks, 256, 0, st>>>(a, lpr);
-    if (a.gwq || a.gwk) qk_weight_grad_kernel<<<(2 * a.d + 15) / 16, 256, 0, st>>>(a, blocks);
+    if (a.gwq || a.gwk) qk_weight_grad_kernel<<<(2 * a.d + 3) / 4, 256, 0, st>>>(a, blocks);
     return hipGetLastError();
 }
 
