@@ -40,6 +40,15 @@ __host__ __device__ constexpr int tile_keys(int dp, int wr) {
     return wr == 4 ? (dp == 256 ? 32 : 64) : wr == 2 ? 64 : 128;
 }
 
+// Rows of partial outputs that the workspace holds for the parts along one axis. They grow with
+// the rows alone, so that the workspace of the largest call serves the others: along an axis
+// there are at most 64 parts, and at most places / (row tiles) + 1 of them, whose rows together
+// are at most places row tiles and the rows once more.
+int64_t kept_rows(const AttnArgs &a) {
+    const int64_t rows = (int64_t)a.total_q * a.hq, some = 64 * rows, many = 2 * kChipUnits * 128 + rows;
+    return some < many ? some : many;
+}
+
 FwdPlan make_plan(const AttnArgs &a) {
     FwdPlan p{};
     const int64_t g = a.hq / a.hk, dp = padded(a.d);
@@ -57,12 +66,14 @@ FwdPlan make_plan(const AttnArgs &a) {
     const int64_t kt = tile_keys((int)dp, p.wr), bm = 32 * p.wr;
     const int64_t pk = ceil_div(a.max_prefix, kt), sk = ceil_div(a.max_suffix, kt);
     p.stiles = (int)ceil_div(seq_rows, bm);
+    // What the workspace holds (attn_forward_bytes) also where more queries come than max_q says.
+    const int64_t most = kept_rows(a) / ((int64_t)a.total_q * a.hq);
     // Parts of as many key tiles each as fill the places on the chip (one workgroup a compute
     // unit where it takes over half of the LDS, else two).
     const int64_t places = kChipUnits * ((dp >= 128 && p.wr == 1) || dp == 256 ? 1 : 2);
     const auto parts = [&](int64_t tiles, int64_t len) {
         const int64_t n = len > 0 ? ceil_div(tiles, len) : 1;
-        return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+        return (int)(n < 1 ? 1 : n < most ? n : most);
     };
     const int64_t s_tiles = (int64_t)a.seqs * p.stiles * a.hk;
     if (p.shared) {
@@ -593,14 +604,9 @@ bool attn_mfma_applies(const AttnArgs &a, bool bf16) {
     return true;
 }
 
-// A bound that grows with total_q, the heads and their size alone, so that the workspace of the
-// largest call serves the others: along an axis there are at most 64 parts, and at most
-// places / (row tiles) + 1 of them, whose rows together are at most places row tiles and the
-// rows once more.
 int64_t attn_forward_bytes(const AttnArgs &a, bool bf16) {
     if (!attn_mfma_sizes(a, bf16)) return 0;
-    const int64_t rows = (int64_t)a.total_q * a.hq, some = 64 * rows, many = 2 * kChipUnits * 128 + rows;
-    return 2 * (some < many ? some : many) * (a.d + 2) * (int64_t)sizeof(float);
+    return 2 * kept_rows(a) * (a.d + 2) * (int64_t)sizeof(float);
 }
 
 hipError_t launch_attn_forward(const AttnArgs &a, bool bf16, hipStream_t st) {

@@ -205,6 +205,18 @@ def test_workspace_of_the_largest_call_serves_the_others():
     assert all(need(**SHAPES[s]) <= most for s in ("one_key", "decode", "decode_long", "decode_groups", "extend"))
 
 
+def test_workspace_holds_more_queries_than_stated():
+    """Nothing is written past the workspace where a sequence has more queries than max_q."""
+    a = Attn(hq=4, hk=2, d=64, prefix=[20000], seqs=[(0, 5, 3000)], seed=11)
+    desc = a.desc(max_q=1)
+    need = L.olive_prefix_attention_workspace(desc)
+    room = torch.full((need + (64 << 20),), 0xa5, dtype=torch.uint8, device="cuda")
+    o = a.run(desc=desc, workspace=room[:need])
+    torch.cuda.synchronize()
+    assert bool((room[need:] == 0xa5).all())
+    assert bool(torch.isnan(o["out"]).all()) and bool(torch.isnan(o["lse"]).all())
+
+
 def test_query_offsets_out_of_order():
     """A sequence whose query rows are not in [0, total_q] is left out."""
     a = Attn(hq=2, hk=1, d=64, prefix=[30], seqs=[(0, 8, 4), (0, 9, 3), (0, 5, 5)])
