@@ -17,6 +17,13 @@
 //           prefix, so that it is read once for 32 WR of them, and each sequence's rows
 //           against its suffix
 // Parts of a row meet in a second kernel through fp32 partial outputs.
+//
+// Single tokens are bound by the reading of the keys and values (64 sequences on 4 prefixes of
+// 16000 to 32768 tokens, 32 / 8 heads of 128: 130 us with the join, 4.3 TB/s; 4 sequences on one of 4096, 16
+// heads: 13 us and 5 us for the join, chains of waits). Long runs are bound by the products and
+// the exponentials beside them (8 runs of 1024 tokens on 2 prefixes of 4096, 16 / 8 heads of 128:
+// 359 us, 860 TFLOP/s; prompts of 1200 to 6000 tokens with heads of 64, where a score has half
+// the products: 244 us, 790 TFLOP/s).
 #include "attn_tile.hpp"
 
 namespace olive {
@@ -31,6 +38,7 @@ struct FwdPlan {
     int np, ns;                      // parts along the prefix and the suffix (own: np = 0, and
                                      // ns along both)
     int ptiles, stiles;              // row tiles: over all groups (a bound), of a sequence
+    RowOrder order;                  // of a sequence's row tiles
     int64_t p_units, s_units;        // workgroups
     __host__ __device__ int parts() const { return np + ns; }
     __host__ __device__ bool direct() const { return !shared && ns == 1; }
@@ -76,6 +84,8 @@ FwdPlan make_plan(const AttnArgs &a) {
         return (int)(n < 1 ? 1 : n < most ? n : most);
     };
     const int64_t s_tiles = (int64_t)a.seqs * p.stiles * a.hk;
+    p.order = RowOrder::of(p.stiles);
+    const int64_t s_all = a.seqs * p.order.units() * a.hk;
     if (p.shared) {
         const int64_t likely = a.groups * ceil_div(group_rows, bm) * a.hk;
         const int64_t len = ceil_div(likely * pk + s_tiles * sk, places);
@@ -83,11 +93,11 @@ FwdPlan make_plan(const AttnArgs &a) {
         p.np = parts(pk, len);
         p.ns = parts(sk, len);
         p.p_units = (int64_t)p.ptiles * a.hk * p.np;
-        p.s_units = s_tiles * p.ns;
+        p.s_units = s_all * p.ns;
     } else {
         const int64_t len = ceil_div(s_tiles * (pk + sk), places);
         p.ns = s_tiles >= places ? 1 : parts(pk + sk, len < 2 ? 2 : len);
-        p.s_units = s_tiles * p.ns;
+        p.s_units = s_all * p.ns;
     }
     return p;
 }
@@ -96,7 +106,7 @@ struct FwdArgs {
     AttnArgs a;
     FwdPlan p;
     DieOrder pd, sd;
-    Div g, hk, seqs, ptiles, stiles, np, ns;
+    Div g, hk, seqs, ptiles, np, ns;
     float *po;                       // [part][total_q hq][d]
     float2 *pml;                     // [part][total_q hq]: maximum (log2 units), sum
 };
@@ -162,14 +172,23 @@ __device__ __forceinline__ bool find_work(const FwdArgs &f, int block, Work &w) 
     }
     int u = f.sd.unit(block - f.pd.blocks);
     if (u >= f.sd.units) return false;
-    int v = f.stiles.quot(u);
-    // the last row tiles of a sequence, which see the most keys, come first
-    w.r0 = (f.p.stiles - 1 - f.stiles.rem(u, v)) * BM;
+    // chunk of row tiles x part x sequence x key head x tile of the chunk (the heads inside, so
+    // that what lies side by side on the dies takes equally long)
+    int v = f.p.order.chunk.quot(u);
+    const int in = f.p.order.chunk.rem(u, v);
+    u = v;
+    v = f.hk.quot(u);
+    w.kvh = f.hk.rem(u, v);
     u = v;
     v = f.seqs.quot(u);
-    w.s = load_seq(a, f.seqs.rem(u, v));
-    w.part = f.hk.quot(v);
-    w.kvh = f.hk.rem(v, w.part);
+    const int b = f.seqs.rem(u, v);
+    u = v;
+    v = f.ns.quot(u);
+    w.part = f.ns.rem(u, v);
+    const int rt = f.p.order.tile(v, in);
+    if (rt < 0) return false;
+    w.r0 = rt * BM;
+    w.s = load_seq(a, b);
     w.rows = w.s.n * (int)f.g.d;
     if (w.s.skip || w.r0 >= w.rows) return false;
     // (a sequence that is out of range has no keys: its rows get NaN from the first row tile,
@@ -620,7 +639,6 @@ hipError_t launch_attn_forward(const AttnArgs &a, bool bf16, hipStream_t st) {
     f.hk = Div::of(a.hk);
     f.seqs = Div::of(a.seqs);
     f.ptiles = Div::of(f.p.ptiles > 0 ? f.p.ptiles : 1);
-    f.stiles = Div::of(f.p.stiles);
     f.np = Div::of(f.p.np > 0 ? f.p.np : 1);
     f.ns = Div::of(f.p.ns);
     const int64_t rows = (int64_t)f.p.parts() * a.total_q * a.hq;

@@ -169,6 +169,26 @@ struct DieOrder {
     }
 };
 
+// The row tiles of a sequence in chunks of a die's run, the last chunk of all sequences and heads
+// first: under a causal mask the last rows see the most keys, and what starts late is short.
+// (Sequence by sequence a fifth of the chip waited for the last ones: ragged prompts of 1200 to
+// 6000 tokens, 16 heads of 64, 269 us, in this order 244.)
+constexpr int kRowChunk = 16;
+struct RowOrder {
+    int tiles, chunks;
+    Div chunk;
+    static RowOrder of(int64_t tiles) {
+        const int64_t c = tiles < 1 ? 1 : tiles < kRowChunk ? tiles : kRowChunk;
+        return RowOrder{(int)tiles, (int)ceil_div(tiles, c), Div::of(c)};
+    }
+    int64_t units() const { return (int64_t)chunks * chunk.d; }   // of a sequence, absent ones among them
+    // Tile `in` of the i-th chunk in that order; -1: there is none.
+    __device__ __forceinline__ int tile(int i, int in) const {
+        const int t = (chunks - 1 - i) * (int)chunk.d + (int)chunk.d - 1 - in;
+        return t < tiles ? t : -1;
+    }
+};
+
 // Tiles [t0, t1) of part i of n.
 __device__ __forceinline__ void part_range(int tiles, const Div &n, int i, int &t0, int &t1) {
     const int q = n.quot(tiles), r = n.rem(tiles, q);
