@@ -31,6 +31,7 @@ struct BwdPlan {
     RowOrder order;                  // of a sequence's tiles of 128 rows
     int ptiles, stiles;              // tiles of KEYS keys of a prefix, of a suffix
     int np, ns;                      // parts of the rows
+    RowOrder porder, sorder;         // of the key tiles of a prefix, of a suffix
     int64_t q_units, p_units, s_units;   // workgroups of the dq pass, of the dkv pass
 };
 
@@ -51,6 +52,8 @@ BwdPlan make_plan(const AttnArgs &a) {
     };
     p.np = split(pu, ceil_div(a.total_q * g, a.groups));
     p.ns = split(pu * p.np + su, seq_rows);
+    p.porder = RowOrder::of(p.ptiles);
+    p.sorder = RowOrder::of(p.stiles);
     p.p_units = pu * p.np;
     p.s_units = su * p.ns;
     return p;
@@ -292,6 +295,25 @@ __device__ __forceinline__ bool find_keys(const BwdArgs &f, bool prefix, int v, 
     return w.j0 < w.keys;
 }
 
+// The v of find_keys that is the u-th to run: chunk of tiles x part x owner x key head x tile of
+// the chunk. The first keys meet the most rows under a causal mask; -1: there is none.
+__device__ __forceinline__ int key_unit(const BwdArgs &f, const RowOrder &order, const Div &owners, const Div &parts,
+                                        const Div &all, int u) {
+    int v = order.chunk.quot(u);
+    const int in = order.chunk.rem(u, v);
+    u = v;
+    v = f.hk.quot(u);
+    const int kvh = f.hk.rem(u, v);
+    u = v;
+    v = owners.quot(u);
+    const int own = owners.rem(u, v);
+    u = v;
+    v = parts.quot(u);
+    const int part = parts.rem(u, v), t = v * (int)order.chunk.d + in;
+    if (t >= order.tiles) return -1;
+    return part * (int)all.d + (kvh * (int)owners.d + own) * order.tiles + t;
+}
+
 // Tiles of ROWS query rows and their output gradients on their way into LDS, with the rows'
 // statistics: rows past the end are copies of the last one.
 template <int DP>
@@ -360,8 +382,10 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
     const AttnArgs &a = f.a;
     KeyWork w;
     const bool pre = (int)blockIdx.x < f.pd.blocks;
-    const int u = pre ? f.pd.unit(blockIdx.x) : f.sd.unit(blockIdx.x - f.pd.blocks);
-    if (u >= (pre ? f.pd.units : f.sd.units) || !find_keys(f, pre, u, w)) return;
+    int u = pre ? f.pd.unit(blockIdx.x) : f.sd.unit(blockIdx.x - f.pd.blocks);
+    if (u >= (pre ? f.pd.units : f.sd.units)) return;
+    u = pre ? key_unit(f, f.p.porder, f.groups, f.np, f.pall, u) : key_unit(f, f.p.sorder, f.seqs, f.ns, f.sall, u);
+    if (u < 0 || !find_keys(f, pre, u, w)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, g = f.g.d, nch = a.d >> 3;
     if (nch < DP / 8) {
@@ -588,8 +612,8 @@ hipError_t launch_attn_backward(const AttnArgs &a, bool bf16, hipStream_t st) {
     f.a = a;
     f.p = make_plan(a);
     f.qd = DieOrder::of(f.p.q_units);
-    f.pd = DieOrder::of(f.p.p_units);
-    f.sd = DieOrder::of(f.p.s_units);
+    f.pd = DieOrder::of(a.groups * f.p.porder.units() * a.hk * f.p.np);
+    f.sd = DieOrder::of(a.seqs * f.p.sorder.units() * a.hk * f.p.ns);
     const auto div = [](int64_t d) { return Div::of(d > 0 ? d : 1); };
     f.g = div(a.hq / a.hk);
     f.seqs = div(a.seqs);

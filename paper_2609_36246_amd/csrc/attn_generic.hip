@@ -7,6 +7,9 @@
 // result is the second one's operand where it lies: a lane holds 4 values of one column, and
 // product i of the next sum takes the i-th of them from every lane, with rows of the other
 // operand to match.
+//
+// Bound by the waits for the operands: forward and backward of 3 runs of 30 to 90 tokens on a
+// prefix of 150, fp32, 4 / 2 heads of 64: 100 us in five launches of 5 to 35 us.
 #include "attn_seq.hpp"
 #include "olive_device.hpp"
 

@@ -5,7 +5,9 @@
 // rotation come from another lane or the same vector. A wavefront keeps to one token while
 // it walks over heads: the angles and weights of its elements stay in registers.
 //
-// Bound by memory: 7 (backward 14) operations an element for 4 (6) bytes in bf16.
+// Bound by memory: 7 (backward 14) operations an element for 4 (6) bytes in bf16. 32768 tokens
+// of 40 heads of 128: 160 us, 4.2 TB/s (a large copy: 4.75); the backward of 24 heads 136 us,
+// 4.45 TB/s, of which 5 us the weight gradients' second pass; 8 tokens into a cache 5 us.
 #include <type_traits>
 
 #include "layers_internal.hpp"

@@ -96,6 +96,14 @@ def test_longer_runs(shape, n):
     a.check(a.run(grad=True), grad=True)
 
 
+@pytest.mark.parametrize("hq,hk", [(3, 3), (4, 2), (4, 1)])
+def test_ragged_runs_of_many_tiles(hq, hk):
+    """More tiles of rows and of keys than are taken in one go, and sequences that lack most of them."""
+    a = Attn(hq=hq, hk=hk, d=64, prefix=[0, 2200, 0], seqs=[(0, 2300, 2300), (1, 129, 129), (1, 1, 1), (2, 700, 700)],
+             grad=True, seed=12)
+    a.check(a.run(grad=True), grad=True)
+
+
 def test_peaked_rows():
     """Weights that underflow beside ones near 1, and a maximum that grows along the keys."""
     a = Attn(hq=4, hk=2, d=64, prefix=[400], seqs=[(0, 200, 200), (0, 90, 1)], std=4.0, grad=True, seed=5)
