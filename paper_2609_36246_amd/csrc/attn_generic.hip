@@ -9,7 +9,7 @@
 // operand to match.
 //
 // Bound by the waits for the operands: forward and backward of 3 runs of 30 to 90 tokens on a
-// prefix of 150, fp32, 4 / 2 heads of 64: 100 us in five launches of 5 to 35 us.
+// prefix of 150, fp32, 4 / 2 heads of 64: 39 us (13 forward, 4 delta, 24 gradients).
 #include "attn_seq.hpp"
 #include "olive_device.hpp"
 
@@ -21,7 +21,9 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 struct GenArgs {
     AttnArgs a;
-    Div g, tiles;
+    Div g, tiles, ptiles, stiles;    // (tiles: of a sequence's rows; of a prefix's and a suffix's keys)
+    int dq_blocks, prefix_blocks;    // backward: workgroups of the pass for dq, of the prefixes' keys
+    bool quads;                      // 4 elements of a row can be read at once
     float *delta;                    // backward: [total_q][hq] sums of grad_out * out
 };
 
@@ -42,8 +44,20 @@ __device__ __forceinline__ void put(T *p, float v) {
 // NT 16-element blocks cover the head. Block n of a row as a first or second operand: elements
 // 16 n + 4 q + 0..3 (q = lane / 16), zeros past d.
 template <typename T, int NT>
-__device__ __forceinline__ void load_row(const T *p, int d, floatx4 (&x)[NT]) {
+__device__ __forceinline__ void load_row(const T *p, int d, bool quads, floatx4 (&x)[NT]) {
     const int q = (threadIdx.x & 63) >> 4;
+    if (quads) {
+        struct alignas(4 * sizeof(T)) Quad { T v[4]; };
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int i = 16 * n + 4 * q;
+            Quad u{};
+            if (i < d) u = *(const Quad *)(p + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[n][e] = load_elem<T>(u.v, e);
+        }
+        return;
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -150,7 +164,7 @@ __global__ __launch_bounds__(THREADS, NT > 8 ? 1 : 2) void attn_generic_kernel(G
     }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = lane >> 4;
     floatx4 q[NT], acc[NT];
-    load_row<T, NT>(row_ptr<T>(a.q, w.t, w.head), a.d, q);
+    load_row<T, NT>(row_ptr<T>(a.q, w.t, w.head), a.d, f.quads, q);
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[n] = (floatx4)(0.f);
     const int seen = w.live ? w.s.plen + suffix_seen(w.s, w.tok) : 0;
@@ -164,7 +178,7 @@ __global__ __launch_bounds__(THREADS, NT > 8 ? 1 : 2) void attn_generic_kernel(G
 #pragma unroll
         for (int e = 0; e < 4; ++e) key_ptrs<T>(a, w.s, w.kvh, j0 + 4 * quarter + e, end, bad, unused, col[e]);
         floatx4 x[NT];
-        load_row<T, NT>(kp, a.d, x);
+        load_row<T, NT>(kp, a.d, f.quads, x);
         floatx4 z = product<NT>(x, q), p;
         float top = kNegInf;
 #pragma unroll
@@ -289,8 +303,7 @@ __device__ __forceinline__ void join_and_put(float *o, const floatx4 (&acc)[NT],
 }
 
 template <typename T, int NT>
-__global__ __launch_bounds__(THREADS, NT > 8 ? 1 : 2) void attn_generic_dq_kernel(GenArgs f) {
-    extern __shared__ float lds[];
+__device__ __forceinline__ void dq_tile(const GenArgs &f, float *lds) {
     const AttnArgs &a = f.a;
     const Rows w = find_rows(f);
     if (!w.any) return;
@@ -300,8 +313,8 @@ __global__ __launch_bounds__(THREADS, NT > 8 ? 1 : 2) void attn_generic_dq_kerne
     }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = lane >> 4;
     floatx4 q[NT], go[NT], acc[NT];
-    load_row<T, NT>(row_ptr<T>(a.q, w.t, w.head), a.d, q);
-    load_row<T, NT>(row_ptr<T>(a.go, w.t, w.head), a.d, go);
+    load_row<T, NT>(row_ptr<T>(a.q, w.t, w.head), a.d, f.quads, q);
+    load_row<T, NT>(row_ptr<T>(a.go, w.t, w.head), a.d, f.quads, go);
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[n] = (floatx4)(0.f);
     const int64_t at = (int64_t)w.t * a.hq + w.head;
@@ -315,9 +328,9 @@ __global__ __launch_bounds__(THREADS, NT > 8 ? 1 : 2) void attn_generic_dq_kerne
 #pragma unroll
         for (int e = 0; e < 4; ++e) key_ptrs<T>(a, w.s, w.kvh, j0 + 4 * quarter + e, end, bad, col[e], unused);
         floatx4 x[NT];
-        load_row<T, NT>(kp, a.d, x);
+        load_row<T, NT>(kp, a.d, f.quads, x);
         floatx4 z = product<NT>(x, q);
-        load_row<T, NT>(vp, a.d, x);
+        load_row<T, NT>(vp, a.d, f.quads, x);
         const floatx4 y = product<NT>(x, go);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -335,11 +348,11 @@ __global__ __launch_bounds__(THREADS, NT > 8 ? 1 : 2) void attn_generic_dq_kerne
 // 16 keys of a prefix (seen by every row of its group) or of a suffix against all the rows
 // that see them.
 template <typename T, int NT, bool PREFIX>
-__global__ __launch_bounds__(THREADS, NT > 4 ? 1 : 2) void attn_generic_dkv_kernel(GenArgs f) {
-    extern __shared__ float lds[];
+__device__ __forceinline__ void dkv_tile(const GenArgs &f, int block, float *lds) {
     const AttnArgs &a = f.a;
-    const int kvh = blockIdx.x % a.hk, g = f.g.d;
-    const int u = blockIdx.x / a.hk, own = f.tiles.quot(u), j0 = f.tiles.rem(u, own) * R;
+    const Div &tiles = PREFIX ? f.ptiles : f.stiles;
+    const int kvh = block % a.hk, g = f.g.d;
+    const int u = block / a.hk, own = tiles.quot(u), j0 = tiles.rem(u, own) * R;
     const HeadsArg &kh = PREFIX ? a.kp : a.ks, &vh = PREFIX ? a.vp : a.vs;
     const HeadsArg &gk = PREFIX ? a.gkp : a.gks, &gv = PREFIX ? a.gvp : a.gvs;
     int q0, toks, keys, first = 0;  // first: suffix keys that query 0 sees, less one
@@ -366,8 +379,8 @@ __global__ __launch_bounds__(THREADS, NT > 4 ? 1 : 2) void attn_generic_dkv_kern
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = lane >> 4;
     const int key = j0 + (lane & 15), rows = toks * g;
     floatx4 k[NT], v[NT], dk[NT], dv[NT];
-    load_row<T, NT>(row_ptr<T>(kh, krow + min(key, keys - 1), kvh), a.d, k);
-    load_row<T, NT>(row_ptr<T>(vh, krow + min(key, keys - 1), kvh), a.d, v);
+    load_row<T, NT>(row_ptr<T>(kh, krow + min(key, keys - 1), kvh), a.d, f.quads, k);
+    load_row<T, NT>(row_ptr<T>(vh, krow + min(key, keys - 1), kvh), a.d, f.quads, v);
 #pragma unroll
     for (int n = 0; n < NT; ++n) dk[n] = dv[n] = (floatx4)(0.f);
     // the first row that sees this lane's key, and the tile's first one
@@ -388,9 +401,9 @@ __global__ __launch_bounds__(THREADS, NT > 4 ? 1 : 2) void attn_generic_dkv_kern
         const int r = min(r0 + (lane & 15), rows - 1), tok = f.g.quot(r);
         const int t = q0 + tok, head = kvh * g + f.g.rem(r, tok);
         floatx4 x[NT], p, z;
-        load_row<T, NT>(row_ptr<T>(a.q, t, head), a.d, x);
+        load_row<T, NT>(row_ptr<T>(a.q, t, head), a.d, f.quads, x);
         z = product<NT>(x, k);
-        load_row<T, NT>(row_ptr<T>(a.go, t, head), a.d, x);
+        load_row<T, NT>(row_ptr<T>(a.go, t, head), a.d, f.quads, x);
         const floatx4 y = product<NT>(x, v);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -408,12 +421,44 @@ __global__ __launch_bounds__(THREADS, NT > 4 ? 1 : 2) void attn_generic_dkv_kern
     join_and_put<T, NT>(lds, dv, a.d, cols, 1.f, [&](int c) { return (T *)row_ptr<T>(gv, krow + j0 + c, kvh); });
 }
 
+// The passes for dq and for the keys' gradients need nothing of each other: small heads run
+// them in one launch (few workgroups that wait for loads: side by side they hide each other),
+// large ones, whose registers differ, in two.
+template <typename T, int NT, bool DQ, bool DKV>
+__global__ __launch_bounds__(THREADS, NT > (DKV ? 4 : 8) ? 1 : 2) void attn_generic_backward_kernel(GenArgs f) {
+    extern __shared__ float lds[];
+    int block = blockIdx.x;
+    if constexpr (DQ) {
+        if (!DKV || block < f.dq_blocks) {
+            dq_tile<T, NT>(f, lds);
+            return;
+        }
+        block -= f.dq_blocks;
+    }
+    if constexpr (DKV) {
+        if (block < f.prefix_blocks) dkv_tile<T, NT, true>(f, block, lds);
+        else dkv_tile<T, NT, false>(f, block - f.prefix_blocks, lds);
+    }
+}
+
 int64_t tiles_of(int64_t n) { return (n + R - 1) / R; }
+
+// Whether rows of every operand lie on 4 elements.
+bool in_quads(const AttnArgs &a, int esz) {
+    if (a.d % 4) return false;
+    for (const HeadsArg *h : {&a.q, &a.kp, &a.vp, &a.ks, &a.vs, &a.go})
+        if (h->p && (((uintptr_t)h->p | (uint64_t)(h->st * esz) | (uint64_t)(h->sh * esz)) & (4 * esz - 1))) return false;
+    return true;
+}
 
 template <typename T, int NT>
 hipError_t forward(const AttnArgs &a, hipStream_t st) {
     const int64_t tiles = tiles_of((int64_t)a.max_q * (a.hq / a.hk));
-    const GenArgs f{a, Div::of(a.hq / a.hk), Div::of(tiles), nullptr};
+    GenArgs f{};
+    f.a = a;
+    f.g = Div::of(a.hq / a.hk);
+    f.tiles = Div::of(tiles);
+    f.quads = in_quads(a, sizeof(T));
     attn_generic_kernel<T, NT><<<(unsigned)(a.seqs * tiles * a.hk), THREADS,
                                  sizeof(float) * (2 * 4 * R + 4 * R * (a.d + 1)), st>>>(f);
     return hipGetLastError();
@@ -423,20 +468,30 @@ template <typename T, int NT>
 hipError_t backward(const AttnArgs &a, hipStream_t st) {
     const int64_t g = a.hq / a.hk, tiles = tiles_of(a.max_q * g);
     const size_t bytes = sizeof(float) * 4 * R * (a.d + 1);
-    GenArgs f{a, Div::of(g), Div::of(tiles > 0 ? tiles : 1), (float *)a.work};
-    if (a.total_q > 0) {
-        attn_delta_kernel<T><<<(unsigned)(((int64_t)a.total_q * a.hq + 3) / 4), THREADS, 0, st>>>(f);
-        attn_generic_dq_kernel<T, NT><<<(unsigned)(a.seqs * tiles * a.hk), THREADS, bytes, st>>>(f);
-    }
     const int64_t pt = tiles_of(a.max_prefix), sl = tiles_of(a.max_suffix);
-    if (pt) {
-        f.tiles = Div::of(pt);
-        attn_generic_dkv_kernel<T, NT, true><<<(unsigned)(a.groups * pt * a.hk), THREADS, bytes, st>>>(f);
+    const auto div = [](int64_t d) { return Div::of(d > 0 ? d : 1); };
+    GenArgs f{};
+    f.a = a;
+    f.g = Div::of(g);
+    f.tiles = div(tiles);
+    f.ptiles = div(pt);
+    f.stiles = div(sl);
+    f.quads = in_quads(a, sizeof(T));
+    f.delta = (float *)a.work;
+    const int64_t rows = a.total_q > 0 ? a.seqs * tiles * a.hk : 0;
+    const int64_t prefix = a.groups * pt * a.hk, keys = prefix + a.seqs * sl * a.hk;
+    f.prefix_blocks = (int)prefix;
+    if (rows) attn_delta_kernel<T><<<(unsigned)(((int64_t)a.total_q * a.hq + 3) / 4), THREADS, 0, st>>>(f);
+    if constexpr (NT <= 4) {
+        if (rows + keys <= 0x7fffffff) {
+            f.dq_blocks = (int)rows;
+            if (rows + keys)
+                attn_generic_backward_kernel<T, NT, true, true><<<(unsigned)(rows + keys), THREADS, bytes, st>>>(f);
+            return hipGetLastError();
+        }
     }
-    if (sl) {
-        f.tiles = Div::of(sl);
-        attn_generic_dkv_kernel<T, NT, false><<<(unsigned)(a.seqs * sl * a.hk), THREADS, bytes, st>>>(f);
-    }
+    if (rows) attn_generic_backward_kernel<T, NT, true, false><<<(unsigned)rows, THREADS, bytes, st>>>(f);
+    if (keys) attn_generic_backward_kernel<T, NT, false, true><<<(unsigned)keys, THREADS, bytes, st>>>(f);
     return hipGetLastError();
 }
 
