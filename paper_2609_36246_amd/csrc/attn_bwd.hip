@@ -17,7 +17,7 @@
 // sums a last kernel adds in order.
 //
 // Bound by the products: 8 runs of 1024 tokens on 2 prefixes of 4096, 16 / 8 heads of 128: dq
-// 450 us and dkv 630 us (matrix units 54 and 49 % busy at 1.8 to 1.9 GHz), lse and delta 15 us.
+// 434 us and dkv 606 us (matrix units 54 and 49 % busy at 1.9 to 2.0 GHz), lse and delta 15 us.
 #include "attn_tile.hpp"
 
 namespace olive {

@@ -22,7 +22,7 @@
 // 16000 to 32768 tokens, 32 / 8 heads of 128: 130 us with the join, 4.3 TB/s; 4 sequences on one of 4096, 16
 // heads: 13 us and 5 us for the join, chains of waits). Long runs are bound by the products and
 // the exponentials beside them (8 runs of 1024 tokens on 2 prefixes of 4096, 16 / 8 heads of 128:
-// 359 us, 860 TFLOP/s; prompts of 1200 to 6000 tokens with heads of 64, where a score has half
+// 348 us, 890 TFLOP/s; prompts of 1200 to 6000 tokens with heads of 64, where a score has half
 // the products: 244 us, 790 TFLOP/s).
 #include "attn_tile.hpp"
 
