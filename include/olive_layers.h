@@ -122,8 +122,11 @@ olive_status olive_qk_norm_rope_backward(const olive_qk_desc *desc, const olive_
  * The suffix rows are packed, suffix_start[b] + j, or pages: token j of sequence b is row
  * page_table[b * table_stride + j / page_size] * page_size + j % page_size.
  * max_q, max_prefix and max_suffix bound what the device arrays hold and choose how the
- * work is split; a sequence beyond them, or with rows outside the buffers, gets NaN (one
- * whose cu_q entries are not in order within [0, total_q] is left out).
+ * work is split; a sequence beyond them, or with rows outside the buffers, gets NaN (with
+ * pages: at least the queries that see a token of such a page). One whose cu_q entries are
+ * not in order within [0, total_q] is left out; others of a call with such entries, or with
+ * group_seqs out of order, get NaN where their rows do not lie between the first and the last
+ * entry of their group. Rows that two sequences or groups have get no defined value.
  * Rows of keys and values that no sequence has are never read into a result.
  */
 typedef struct {

@@ -112,26 +112,41 @@ struct FwdArgs {
 };
 
 // The row tile of flat index i over the groups: groups of 64 a step, by prefix sums. A group's
-// first token, rows, and prefix go into w; false: no such tile.
+// first token, rows, and prefix go into w; false: no such tile. Where cu_q is not in order, a group
+// has the rows that no earlier one has: the tiles of all are then no more than the plan's.
 template <int BM>
 __device__ __forceinline__ bool find_group(const AttnArgs &a, int g_heads, int i, Work &w) {
     const int lane = threadIdx.x & 63;
+    int end = 0;                                     // of the groups before these 64
+    bool broken = false;
     for (int g0 = 0; g0 < a.groups; g0 += 64) {
         const int g = g0 + lane;
-        int q0 = 0, rows = 0, plen = 0;
+        int q0 = end, q1 = end, plen = 0;
         int64_t pstart = 0;
+        bool ordered = true;
         if (g < a.groups) {
-            const int b0 = a.group_seqs[g], b1 = a.group_seqs[g + 1];
             const bool ok = prefix_ok(a, g);
             plen = ok ? a.prefix_len[g] : 0;
             pstart = a.prefix_start[g];
-            if (b0 >= 0 && b0 <= b1 && b1 <= a.seqs) {
-                q0 = a.cu_q[b0];
-                const int q1 = a.cu_q[b1];
-                if (q0 >= 0 && q0 <= q1 && q1 <= a.total_q) rows = (q1 - q0) * g_heads;
-            }
+            ordered = group_tokens(a, a.group_seqs[g], a.group_seqs[g + 1], q0, q1);
         }
-        const int n = tiles_of<BM>(rows);
+        // (a group begins at the entry that the one before it ends at)
+        broken |= __any(!ordered);
+        if (broken) {
+            int most = ordered ? q1 : 0;
+            for (int o = 1; o < 64; o <<= 1) {
+                const int v = __shfl_up(most, o);
+                if (lane >= o) most = max(most, v);
+            }
+            const int m = __shfl_up(most, 1);
+            q0 = max(q0, max(end, lane ? m : 0));
+            q1 = ordered ? max(q0, q1) : q0;
+            most = max(end, most);
+            end = __builtin_amdgcn_readlane(most, 63);
+        } else {
+            end = __builtin_amdgcn_readlane(q1, 63);
+        }
+        const int rows = (q1 - q0) * g_heads, n = tiles_of<BM>(rows);
         int sum = n;
         for (int o = 1; a.groups > 1 && o < 64; o <<= 1) {
             const int v = __shfl_up(sum, o);
@@ -324,7 +339,7 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
 // the keys that not all its rows see, its rows are formed again one by one, each over the keys
 // that it sees. False: there is none.
 template <int KT>
-__device__ __forceinline__ bool row_by_row(const FwdArgs &f, const Work &w, int bm) {
+__device__ __forceinline__ bool row_by_row(const FwdArgs &f, const Work &w, int bm, bool alone) {
     const AttnArgs &a = f.a;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (w.t0 >= w.t1) return false;
@@ -370,7 +385,7 @@ __device__ __forceinline__ bool row_by_row(const FwdArgs &f, const Work &w, int 
                     if (lane + 64 * i < a.d) o[i] = fmaf(p, load_elem<uint16_t>(v, lane + 64 * i), o[i] * r);
             }
         }
-        if (__any(off_table)) l = __builtin_nanf("");
+        if (__any(off_table) || alone) l = __builtin_nanf("");
         const int64_t orow = (int64_t)t * a.hq + head, slot = (int64_t)w.part * a.total_q * a.hq + orow;
         const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -398,6 +413,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
     Work w;
     if (!find_work<DP, WR>(f, blockIdx.x, w)) return;
     make_uniform(w);
+    // (asked for here, looked at after the keys)
+    const bool suffix_rows = f.p.shared && (int)blockIdx.x >= f.pd.blocks;
+    const int32_t entry = suffix_rows && !w.s.bad ? group_entry(a, w.s) : 0;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wr = wave / WK, wk = wave % WK, h = lane >> 5;
     const int g = f.g.d, nch = a.d >> 3;
@@ -424,18 +442,20 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
     floatx16 acc[DB];
     float m, l;
     const bool off_table = key_loop<DP, DB, WR>(a, w, lds, wk, w.r0 + 32 * wr >= w.rows, seen, least, q, acc, m, l);
+    // a sequence whose rows do not lie among its group's: they against the prefix are nobody's work
+    const bool alone = suffix_rows && !w.s.bad && __any(!entry_holds(a, w.s, entry));
     {
         float s = 0.f;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s = fmaf(acc[d][i], 0.f, s);
-        if (__syncthreads_or(!(s == 0.f)) && row_by_row<KT>(f, w, 32 * WR)) return;
+        if (__syncthreads_or(!(s == 0.f)) && row_by_row<KT>(f, w, 32 * WR, alone)) return;
     }
     l += __shfl_xor(l, 32);
 
     const int orow = t * a.hq + head;
-    const bool bad = __syncthreads_or(off_table) || w.s.bad;
+    const bool bad = __syncthreads_or(off_table) || w.s.bad || alone;
     // the registers (4 consecutive elements of the head each) that this wavefront writes
     int g0 = 0;
     if (WK > 1) {
@@ -544,8 +564,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(FwdArgs f) {
     if (lane < parts) x = f.pml[lane * step + r];
     if (lane + 64 < parts) y = f.pml[(lane + 64) * step + r];
     const int t = r / a.hq, head = r - t * a.hq;
-    const int b = seq_of(a, t);
-    if (a.cu_q[b] < 0 || t < a.cu_q[b] || t >= a.cu_q[b + 1] || a.cu_q[b + 1] > a.total_q) return;
+    if (!any_has_token(a, t)) return;
     float top = fmaxf(x.x, y.x);
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     const float wx = x.x == top ? 1.f : fast_exp2(x.x - top), wy = y.x == top ? 1.f : fast_exp2(y.x - top);

@@ -14,6 +14,7 @@ struct SeqView {
     int64_t pstart;      // row of the prefix's first key
     int64_t sstart;      // packed suffixes: row of the first key
     const int32_t *pages;
+    int32_t group, group_end;   // the sequences of its group
     bool skip;           // the query rows themselves are out of order: nothing is written
     bool bad;            // something else is out of range: the rows get NaN
 };
@@ -85,6 +86,8 @@ __device__ __forceinline__ SeqView load_seq(const AttnArgs &a, int b) {
     s.q0 = s.skip ? 0 : q0;
     s.n = s.skip ? 0 : q1 - q0;
     s.bad = s.n > a.max_q || g.first > b || g.end <= b || !prefix_ok(a, g.plen, g.pstart);
+    s.group = g.first;
+    s.group_end = g.end;
     s.plen = g.plen;
     s.pstart = g.pstart;
     s.pages = nullptr;
@@ -100,6 +103,38 @@ __device__ __forceinline__ SeqView load_seq(const AttnArgs &a, int b) {
     }
     if (s.bad) s.plen = s.slen = 0;
     return s;
+}
+
+// Whether sequence b is not left out and has query token t.
+__device__ __forceinline__ bool has_token(const AttnArgs &a, int b, int t) {
+    const int32_t q0 = a.cu_q[b], q1 = a.cu_q[b + 1];
+    return q0 >= 0 && q0 <= t && t < q1 && q1 <= a.total_q;
+}
+// Whether any sequence has (for a whole wavefront that asks for the same t). All of them are
+// looked through where the one that the order of cu_q leads to has not.
+__device__ __forceinline__ bool any_has_token(const AttnArgs &a, int t) {
+    if (has_token(a, seq_of(a, t), t)) return true;
+    bool any = false;
+    for (int b = threadIdx.x & 63; b < a.seqs; b += 64) any |= has_token(a, b, t);
+    return __any(any);
+}
+
+// The query tokens [q0, q1) of the sequences [b0, b1): whether these entries are in order.
+__device__ __forceinline__ bool group_tokens(const AttnArgs &a, int b0, int b1, int &q0, int &q1) {
+    q0 = q1 = 0;
+    if (b0 < 0 || b1 < b0 || b1 > a.seqs) return false;
+    q0 = a.cu_q[b0];
+    q1 = a.cu_q[b1];
+    return q0 >= 0 && q0 <= q1 && q1 <= a.total_q;
+}
+// Whether the tokens of a sequence lie among those of its group (group_tokens): the first lane of
+// a pair holds the group's first entry, the second its last one, and each says what its own says.
+__device__ __forceinline__ int32_t group_entry(const AttnArgs &a, const SeqView &s) {
+    if (s.group < 0 || s.group_end > a.seqs) return -1;
+    return a.cu_q[threadIdx.x & 1 ? s.group_end : s.group];
+}
+__device__ __forceinline__ bool entry_holds(const AttnArgs &a, const SeqView &s, int32_t entry) {
+    return threadIdx.x & 1 ? s.q0 + s.n <= entry && entry <= a.total_q : 0 <= entry && entry <= s.q0;
 }
 
 // Row of suffix token j (0 <= j < slen). A page outside the buffer sets `bad` and gives row 0.

@@ -1,0 +1,76 @@
+"""The layer operators where the device arrays are not in order, at the ends of the documented
+ranges, and where values are not finite."""
+import pytest
+import torch
+
+from paper_2609_36246_amd import _lib as L
+from tests.layers_harness import Attn
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def gpu():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    L.load()
+
+
+def filled(a, value):
+    """Output buffers that hold `value` throughout."""
+    o = a.outputs()
+    for t in o.values():
+        t.fill_(value)
+    return o
+
+
+def in_order(cu, b, total):
+    return 0 <= cu[b] <= cu[b + 1] <= total
+
+
+# (sequences, cu_q, group_seqs) with 12 query tokens: the entries of some are out of order
+BROKEN = {
+    "last_entry": ([0, 0, 0], [0, 4, 7, 40], [0, 3]),
+    "end_of_a_group": ([0, 0, 1], [0, 4, 40, 12], [0, 2, 3]),
+    "begin_of_a_group": ([0, 1, 1], [0, -3, 7, 12], [0, 1, 3]),
+    "inside": ([0, 0, 0], [0, 40, 7, 12], [0, 3]),
+    "more_sequences_than_there_are": ([0, 0, 1], [0, 4, 7, 12], [0, 2, 7]),
+    "outside_its_group": ([0, 0, 0], [0, 4, 9, 2], [0, 3]),
+}
+
+
+@pytest.mark.parametrize("fill", [0x00, 0x3f, 0xff])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("case", list(BROKEN))
+def test_offsets_out_of_order(case, dtype, fill):
+    """A sequence whose own offsets are out of order is left out. The others get what is theirs,
+    or NaN, and nothing that the workspace held before."""
+    groups, cu, group_seqs = BROKEN[case]
+    a = Attn(hq=2, hk=1, d=64, dtype=dtype, prefix=[300, 200][:max(groups) + 1],
+             seqs=list(zip(groups, (8, 9, 7), (4, 3, 5))))
+    a.dev["cu_q"] = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    a.dev["group_seqs"] = torch.tensor(group_seqs, dtype=torch.int32, device="cuda")
+    desc = a.desc()
+    need = L.olive_prefix_attention_workspace(desc)
+    o = a.run(desc=desc, outputs=filled(a, 7.0),
+              workspace=torch.full((need,), fill, dtype=torch.uint8, device="cuda"))
+    # each sequence with as many queries as its offsets say, by itself
+    mine = torch.zeros(12, dtype=torch.bool)
+    for b in range(3):
+        if not in_order(cu, b, 12) or cu[b] == cu[b + 1]:
+            continue
+        n = cu[b + 1] - cu[b]
+        rows = slice(cu[b], cu[b + 1])
+        mine[rows] = True
+        got, lse = o["out"][rows], o["lse"][rows]
+        if bool(torch.isnan(got).all()) and bool(torch.isnan(lse).all()):
+            continue
+        g = groups[b]
+        s = Attn(hq=2, hk=1, d=64, dtype=dtype, prefix=[a.prefix[g]], seqs=[(0, a.seqs[b][1], n)])
+        s.t["q"] = a.t["q"][rows]
+        for p, at, m in (("kp", a.pstart[g], a.prefix[g]), ("vp", a.pstart[g], a.prefix[g]),
+                         ("ks", a.sstart[b], a.seqs[b][1]), ("vs", a.sstart[b], a.seqs[b][1])):
+            s.t[p][5:5 + m] = a.t[p][at:at + m]
+        s.check({"out": got, "lse": lse})
+    for t in ("out", "lse"):
+        assert bool((o[t][~mine.cuda()] == 7.0).all()), t
