@@ -180,7 +180,9 @@ olive_status olive_prefix_attention(const olive_attn_desc *desc, const olive_hea
  * The gradients of q and of the keys and values from out's, with out and lse of the
  * forward. The gradient of a prefix row is the sum over its group's sequences; rows that
  * belong to no prefix or suffix are not written, and no two prefixes or suffixes overlap.
- * Packed suffixes only (E_UNSUPPORTED with a page table). A value that is not finite may reach
+ * Packed suffixes only (E_UNSUPPORTED with a page table). A sequence that is out of range
+ * or left out makes NaN of the gradients of its suffix and of its group's prefix; where
+ * these rows themselves are out of range they are not written. A value that is not finite may reach
  * the gradients of other rows and keys of its sequence and group, also of queries that do not
  * see it (the forward keeps it from them).
  */

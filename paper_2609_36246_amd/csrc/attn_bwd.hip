@@ -253,6 +253,7 @@ struct KeyWork {
     int first;                       // suffix keys that query 0 sees, less one
     int kvh, part, parts;
     int tile;                        // index of the tile among all of its kind (fp32 parts)
+    bool nan;                        // a sequence that has these keys is out of range: no rows, the sums are NaN
 };
 
 // v: tile x owner x key head x part (tiles of one owner and head first: they read the same rows)
@@ -269,21 +270,20 @@ __device__ __forceinline__ bool find_keys(const BwdArgs &f, bool prefix, int v, 
     const int own = owners.rem(x, w.kvh), g = f.g.d;
     w.first = 0;
     if (w.prefix) {
-        const int b0 = a.group_seqs[own], b1 = a.group_seqs[own + 1];
-        if (b0 < 0 || b1 < b0 || b1 > a.seqs || !prefix_ok(a, own)) return false;
-        const int q0 = a.cu_q[b0], q1 = a.cu_q[b1];
-        if (q0 < 0 || q1 < q0 || q1 > a.total_q) return false;
+        int q0, q1;
+        w.nan = !group_in_order(a, a.group_seqs[own], a.group_seqs[own + 1], q0, q1);
+        if (!prefix_ok(a, own)) return false;
         w.keys = a.prefix_len[own];
         w.krow = a.prefix_start[own];
         w.q0 = q0;
-        w.rows = (q1 - q0) * g;
+        w.rows = w.nan ? 0 : (q1 - q0) * g;
     } else {
         const SeqView s = load_seq(a, own);
-        if (s.skip || s.bad) return false;
-        w.keys = s.slen;
+        w.nan = s.skip || s.bad;
+        w.keys = s.keys;
         w.krow = s.sstart;
         w.q0 = s.q0;
-        w.rows = s.n * g;
+        w.rows = w.nan ? 0 : s.n * g;
         w.first = s.slen - s.n;
     }
     w.keys = uniform32(w.keys);
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
     const float c = a.scale * kLog2e;
     floatx16 dk[DB], dv[DB];
 #pragma unroll
-    for (int d = 0; d < DB; ++d) dk[d] = dv[d] = zero16();
+    for (int d = 0; d < DB; ++d) dk[d] = dv[d] = w.nan ? (floatx16)(__builtin_nanf("")) : zero16();
     // this part's tiles of the rows from the first that sees the tile's first key
     // (64 bits: max_suffix keys by g rows)
     const auto row_of = [&](int j) { return w.prefix ? 0 : (int)min((int64_t)w.rows, (int64_t)max(0, j - w.first) * g); };

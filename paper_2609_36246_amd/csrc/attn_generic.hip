@@ -357,19 +357,18 @@ __device__ __forceinline__ void dkv_tile(const GenArgs &f, int block, float *lds
     const HeadsArg &gk = PREFIX ? a.gkp : a.gks, &gv = PREFIX ? a.gvp : a.gvs;
     int q0, toks, keys, first = 0;  // first: suffix keys that query 0 sees, less one
     int64_t krow;
+    bool nan;                        // a sequence that has these keys is out of range: the sums are NaN
     if (PREFIX) {
-        const int b0 = a.group_seqs[own], b1 = a.group_seqs[own + 1];
-        if (b0 < 0 || b1 < b0 || b1 > a.seqs || !prefix_ok(a, own)) return;
+        int q1;
+        nan = !group_in_order(a, a.group_seqs[own], a.group_seqs[own + 1], q0, q1);
+        if (!prefix_ok(a, own)) return;
         keys = a.prefix_len[own];
         krow = a.prefix_start[own];
-        q0 = a.cu_q[b0];
-        const int q1 = a.cu_q[b1];
-        if (q0 < 0 || q1 < q0 || q1 > a.total_q) return;
         toks = q1 - q0;
     } else {
         const SeqView s = load_seq(a, own);
-        if (s.skip || s.bad) return;
-        keys = s.slen;
+        nan = s.skip || s.bad;
+        keys = s.keys;
         krow = s.sstart;
         q0 = s.q0;
         toks = s.n;
@@ -377,12 +376,12 @@ __device__ __forceinline__ void dkv_tile(const GenArgs &f, int block, float *lds
     }
     if (j0 >= keys) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = lane >> 4;
-    const int key = j0 + (lane & 15), rows = toks * g;
+    const int key = j0 + (lane & 15), rows = nan ? 0 : toks * g;
     floatx4 k[NT], v[NT], dk[NT], dv[NT];
     load_row<T, NT>(row_ptr<T>(kh, krow + min(key, keys - 1), kvh), a.d, f.quads, k);
     load_row<T, NT>(row_ptr<T>(vh, krow + min(key, keys - 1), kvh), a.d, f.quads, v);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) dk[n] = dv[n] = (floatx4)(0.f);
+    for (int n = 0; n < NT; ++n) dk[n] = dv[n] = (floatx4)(nan ? __builtin_nanf("") : 0.f);
     // the first row that sees this lane's key, and the tile's first one
     const auto row_of = [&](int j) { return PREFIX ? 0 : (int)min((int64_t)rows, (int64_t)max(0, j - first) * g); };
     const int from = row_of(key);

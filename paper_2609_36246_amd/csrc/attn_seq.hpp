@@ -15,6 +15,7 @@ struct SeqView {
     int64_t sstart;      // packed suffixes: row of the first key
     const int32_t *pages;
     int32_t group, group_end;   // the sequences of its group
+    int32_t keys;        // keys of the suffix where it lies in the buffers, whatever else is wrong
     bool skip;           // the query rows themselves are out of order: nothing is written
     bool bad;            // something else is out of range: the rows get NaN
 };
@@ -91,16 +92,17 @@ __device__ __forceinline__ SeqView load_seq(const AttnArgs &a, int b) {
     s.plen = g.plen;
     s.pstart = g.pstart;
     s.pages = nullptr;
-    if (s.slen < 0 || s.slen > a.max_suffix) {
-        s.bad = true;
-    } else if (s.slen > 0) {
+    bool inside = s.slen >= 0 && s.slen <= a.max_suffix;
+    if (inside && s.slen > 0) {
         if (a.pages) {
             s.pages = a.pages + (int64_t)b * a.table_stride;
-            s.bad |= a.suffix_rows < a.page_size;
+            inside = a.suffix_rows >= a.page_size;
         } else {
-            s.bad |= s.sstart < 0 || s.sstart > a.suffix_rows - s.slen;
+            inside = s.sstart >= 0 && s.sstart <= a.suffix_rows - s.slen;
         }
     }
+    s.keys = inside ? s.slen : 0;
+    s.bad |= !inside;
     if (s.bad) s.plen = s.slen = 0;
     return s;
 }
@@ -126,6 +128,13 @@ __device__ __forceinline__ bool group_tokens(const AttnArgs &a, int b0, int b1, 
     q0 = a.cu_q[b0];
     q1 = a.cu_q[b1];
     return q0 >= 0 && q0 <= q1 && q1 <= a.total_q;
+}
+// The same, and whether all entries between are in order (a whole wavefront asks).
+__device__ __forceinline__ bool group_in_order(const AttnArgs &a, int b0, int b1, int &q0, int &q1) {
+    if (!group_tokens(a, b0, b1, q0, q1)) return false;
+    bool ok = true;
+    for (int b = b0 + (threadIdx.x & 63); b < b1; b += 64) ok &= a.cu_q[b] <= a.cu_q[b + 1];
+    return __all(ok);
 }
 // Whether the tokens of a sequence lie among those of its group (group_tokens): the first lane of
 // a pair holds the group's first entry, the second its last one, and each says what its own says.

@@ -16,9 +16,9 @@ def gpu():
     L.load()
 
 
-def filled(a, value):
+def filled(a, value, grad=False):
     """Output buffers that hold `value` throughout."""
-    o = a.outputs()
+    o = a.outputs(grad)
     for t in o.values():
         t.fill_(value)
     return o
@@ -74,3 +74,55 @@ def test_offsets_out_of_order(case, dtype, fill):
         s.check({"out": got, "lse": lse})
     for t in ("out", "lse"):
         assert bool((o[t][~mine.cuda()] == 7.0).all()), t
+
+
+# what the device arrays hold; of 3 sequences, the first two of one group: whose suffix rows' and
+# which prefixes' gradients are NaN, whose and which are not written (their rows are unknown)
+WRONG = {
+    "nothing": (dict(), {}, [], [], [], []),
+    "queries_over_max_q": (dict(), dict(max_q=0.9), [0], [0], [], []),
+    "suffix_too_long": (dict(suffix_len=(1, 1 << 20)), {}, [], [0], [1], []),
+    "suffix_outside": (dict(suffix_start=(0, 1 << 40)), {}, [], [0], [0], []),
+    "prefix_outside": (dict(prefix_start=(0, -5)), {}, [0, 1], [], [], [0]),
+    "prefix_too_long": (dict(prefix_len=(1, 1 << 20)), {}, [2], [], [], [1]),
+    "offset_inside_a_group": (dict(cu_q=(1, 1 << 20)), {}, [0, 1], [0], [], []),
+    "offset_between_groups": (dict(cu_q=(2, -4)), {}, [1, 2], [0, 1], [], []),
+}
+
+
+@pytest.mark.parametrize("n", [(5, 3, 7), (220, 130, 150)])
+@pytest.mark.parametrize("dtype,how", [(BF16, "plain"), (BF16, "odd"), (F32, "plain")])
+@pytest.mark.parametrize("case", list(WRONG))
+def test_gradients_of_what_is_out_of_range(case, dtype, how, n):
+    """NaN in the gradients of the keys that it concerns, where their rows are known, in no others."""
+    change, stated, nan_suffix, nan_prefix, no_suffix, no_prefix = WRONG[case]
+    a = Attn(hq=4, hk=1, d=64, dtype=dtype, how=how, prefix=[40, 300], grad=True,
+             seqs=[(0, n[0] + 2, n[0]), (0, n[1], n[1]), (1, n[2], n[2])])
+    good = a.run(grad=True)
+    for k, (i, v) in change.items():
+        a.dev[k][i] = v
+    desc = a.desc(**{k: int(max(n) * v) for k, v in stated.items()})
+    if "max_q" in stated:
+        nan_suffix = [b for b in range(3) if n[b] > desc.max_q]
+        nan_prefix = sorted({a.seqs[b][0] for b in nan_suffix})
+    bad = a.run(grad=True, desc=desc, outputs=filled(a, 7.0, grad=True))
+    rows = [("ks", b, torch.from_numpy(a.rows[b]).cuda(), nan_suffix, no_suffix) for b in range(3)]
+    rows += [("kp", g, torch.arange(a.pstart[g], a.pstart[g] + a.prefix[g], device="cuda"), nan_prefix, no_prefix)
+             for g in range(2)]
+    for name, i, at, nans, none in rows:
+        for x in ("d" + name, "dv" + name[1]):
+            got = bad[x][at]
+            if i in nans:
+                assert bool(torch.isnan(got).all()), (x, i)
+            elif i in none:
+                assert bool((got == 7.0).all()), (x, i)
+            elif not (case == "offset_between_groups" and (name, i) == ("ks", 0) and bool(torch.isnan(got).all())):
+                # (a sequence whose group's entries do not enclose it may get NaN)
+                # the same sums, cut into other parts where max_q differs
+                assert torch.allclose(got.float(), good[x][at].float(), rtol=2.0 ** -6, atol=1e-2), (x, i)
+    for x, used in (("ks", rows[:3]), ("kp", rows[3:])):
+        keep = torch.ones(bad["d" + x].shape[0], dtype=torch.bool, device="cuda")
+        for r in used:
+            keep[r[2]] = False
+        for y in ("d" + x, "dv" + x[1]):
+            assert bool((bad[y][keep] == 7.0).all()), y
