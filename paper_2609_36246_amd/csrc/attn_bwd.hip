@@ -76,7 +76,7 @@ template <int DP>
 __global__ __launch_bounds__(256) void attn_stats_kernel(BwdArgs f) {
     const AttnArgs &a = f.a;
     constexpr int LPR = DP / 8;
-    const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPR;
+    const int64_t r = ((int64_t)block_index() * 256 + threadIdx.x) / LPR;
     const int c = threadIdx.x % LPR, nch = a.d / 8, g = a.hq / a.hk;
     if (r >= (int64_t)a.total_q * a.hq) return;
     const int t = (int)r / a.hq, head = (int)r - t * a.hq;
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f) {
     extern __shared__ __attribute__((aligned(1024))) char lds_mem[];
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
     const AttnArgs &a = f.a;
-    int u = f.qd.unit(blockIdx.x);
+    int u = f.qd.unit(block_index());
     if (u >= f.qd.units) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5, g = f.g.d, nch = a.d >> 3;
@@ -381,8 +381,9 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
     const AttnArgs &a = f.a;
     KeyWork w;
-    const bool pre = (int)blockIdx.x < f.pd.blocks;
-    int u = pre ? f.pd.unit(blockIdx.x) : f.sd.unit(blockIdx.x - f.pd.blocks);
+    const int block = block_index();
+    const bool pre = block < f.pd.blocks;
+    int u = pre ? f.pd.unit(block) : f.sd.unit(block - f.pd.blocks);
     if (u >= (pre ? f.pd.units : f.sd.units)) return;
     u = pre ? key_unit(f, f.p.porder, f.groups, f.np, f.pall, u) : key_unit(f, f.p.sorder, f.seqs, f.ns, f.sall, u);
     if (u < 0 || !find_keys(f, pre, u, w)) return;
@@ -581,17 +582,24 @@ template <int DP, int DB>
 hipError_t go(const BwdArgs &f, hipStream_t st) {
     const AttnArgs &a = f.a;
     const BwdPlan &p = f.p;
+    hipError_t e = hipSuccess;
     if (a.total_q > 0) {
-        attn_stats_kernel<DP><<<(unsigned)ceil_div((int64_t)a.total_q * a.hq, 256 / (DP / 8)), 256, 0, st>>>(f);
-        attn_dq_kernel<DP, DB><<<(unsigned)f.qd.blocks, 256, 2 * 2 * DQ_KEYS * DP * 2, st>>>(f);
+        attn_stats_kernel<DP><<<grid_of(ceil_div((int64_t)a.total_q * a.hq, 256 / (DP / 8))), 256, 0, st>>>(f);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        attn_dq_kernel<DP, DB><<<grid_of(f.qd.blocks), 256, 2 * 2 * DQ_KEYS * DP * 2, st>>>(f);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
     }
-    if (p.p_units + p.s_units > 0) {
-        attn_dkv_kernel<DP, DB><<<(unsigned)(f.pd.blocks + f.sd.blocks), 256,
+    if (p.p_units + p.s_units == 0) return e;
+    attn_dkv_kernel<DP, DB><<<grid_of((int64_t)f.pd.blocks + f.sd.blocks), 256,
                               2 * RowLoader<DP>::STAGE + KEYS * DP * 2, st>>>(f);
-        const int64_t pt = p.p_units / p.np, stl = p.s_units / p.ns;
-        const int64_t first = p.np > 1 ? 0 : pt, end = p.ns > 1 ? pt + stl : pt;
-        if (end > first) attn_dkv_join_kernel<<<(unsigned)(end - first), 256, 0, st>>>(f, (int)first);
-    }
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    // (of a kind that has parts there are at most two tiles a compute unit)
+    const int64_t pt = p.p_units / p.np, stl = p.s_units / p.ns;
+    const int64_t first = p.np > 1 ? 0 : pt, end = p.ns > 1 ? pt + stl : pt;
+    if (end > first) attn_dkv_join_kernel<<<(unsigned)(end - first), 256, 0, st>>>(f, (int)first);
     return hipGetLastError();
 }
 

@@ -411,10 +411,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void *)lds_mem;
     const AttnArgs &a = f.a;
     Work w;
-    if (!find_work<DP, WR>(f, blockIdx.x, w)) return;
+    const int block = block_index();
+    if (!find_work<DP, WR>(f, block, w)) return;
     make_uniform(w);
     // (asked for here, looked at after the keys)
-    const bool suffix_rows = f.p.shared && (int)blockIdx.x >= f.pd.blocks;
+    const bool suffix_rows = f.p.shared && block >= f.pd.blocks;
     const int32_t entry = suffix_rows && !w.s.bad ? group_entry(a, w.s) : 0;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wr = wave / WK, wk = wave % WK, h = lane >> 5;
@@ -555,8 +556,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attn_fwd_kernel(FwdArg
 // other parts of the same elements.
 __global__ __launch_bounds__(256) void attn_join_kernel(FwdArgs f) {
     const AttnArgs &a = f.a;
-    const int r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), parts = f.p.parts();
-    if (r >= a.total_q * a.hq) return;
+    const uint32_t row = (uint32_t)block_index() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (row >= (uint32_t)(a.total_q * a.hq)) return;
+    const int r = (int)row, parts = f.p.parts();
     const int lane = threadIdx.x & 63;
     const int64_t step = (int64_t)a.total_q * a.hq;
     // (at most 128 parts)
@@ -614,13 +616,12 @@ template <int DP, int DB, int WR>
 hipError_t go(const FwdArgs &f, hipStream_t st) {
     constexpr int KT = tile_keys(DP, WR);
     constexpr int stages = 2 * 2 * KT * DP * 2, join = WR < 4 ? 4 * (DP / 32) * 4096 + 1024 : 0;
-    attn_fwd_kernel<DP, DB, WR><<<(unsigned)(f.pd.blocks + f.sd.blocks), 256, stages > join ? stages : join, st>>>(f);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && !f.p.direct()) {
-        attn_join_kernel<<<(unsigned)ceil_div(f.a.total_q * f.a.hq, 4), 256, 0, st>>>(f);
-        e = hipGetLastError();
-    }
-    return e;
+    const dim3 grid = grid_of((int64_t)f.pd.blocks + f.sd.blocks);
+    attn_fwd_kernel<DP, DB, WR><<<grid, 256, stages > join ? stages : join, st>>>(f);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || f.p.direct()) return e;
+    attn_join_kernel<<<grid_of(ceil_div((int64_t)f.a.total_q * f.a.hq, 4)), 256, 0, st>>>(f);
+    return hipGetLastError();
 }
 
 // Rows on 16 bytes, and the offsets of 128 of them, or of a group's heads, in 32 bits.

@@ -109,15 +109,15 @@ struct Rows {
     int tok, t, head;                // of this lane's row
     bool live, any;
 };
-__device__ __forceinline__ Rows find_rows(const GenArgs &f) {
+__device__ __forceinline__ Rows find_rows(const GenArgs &f, int block) {
     const AttnArgs &a = f.a;
     Rows w;
-    w.kvh = blockIdx.x % a.hk;
-    const int v = blockIdx.x / a.hk, b = f.tiles.quot(v);
+    const int v = (uint32_t)block / (uint32_t)a.hk, b = f.tiles.quot(v);
+    w.kvh = block - v * a.hk;
     w.r0 = f.tiles.rem(v, b) * R;
-    w.s = load_seq(a, b);
+    w.s = load_seq(a, min(b, a.seqs - 1));
     w.rows = w.s.n * (int)f.g.d;
-    w.any = !w.s.skip && w.r0 < w.rows;
+    w.any = b < a.seqs && !w.s.skip && w.r0 < w.rows;
     const int r = w.r0 + (threadIdx.x & 15), c = max(0, min(r, w.rows - 1));
     w.live = r < w.rows;
     w.tok = f.g.quot(c);
@@ -156,7 +156,7 @@ template <typename T, int NT>
 __global__ __launch_bounds__(THREADS, NT > 8 ? 1 : 2) void attn_generic_kernel(GenArgs f) {
     extern __shared__ float lds[];
     const AttnArgs &a = f.a;
-    const Rows w = find_rows(f);
+    const Rows w = find_rows(f, block_index());
     if (!w.any) return;
     if (w.s.bad) {
         put_nan<T>(f, w, a.o, a.lse);
@@ -269,7 +269,7 @@ __global__ __launch_bounds__(THREADS, NT > 8 ? 1 : 2) void attn_generic_kernel(G
 template <typename T>
 __global__ __launch_bounds__(THREADS) void attn_delta_kernel(GenArgs f) {
     const AttnArgs &a = f.a;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t w = (int64_t)block_index() * 4 + (threadIdx.x >> 6);
     if (w >= (int64_t)a.total_q * a.hq) return;
     const int t = (int)w / a.hq, head = (int)w - t * a.hq;
     const T *x = row_ptr<T>(a.o, t, head), *y = row_ptr<T>(a.go, t, head);
@@ -303,9 +303,9 @@ __device__ __forceinline__ void join_and_put(float *o, const floatx4 (&acc)[NT],
 }
 
 template <typename T, int NT>
-__device__ __forceinline__ void dq_tile(const GenArgs &f, float *lds) {
+__device__ __forceinline__ void dq_tile(const GenArgs &f, int block, float *lds) {
     const AttnArgs &a = f.a;
-    const Rows w = find_rows(f);
+    const Rows w = find_rows(f, block);
     if (!w.any) return;
     if (w.s.bad) {
         put_nan<T>(f, w, a.gq, nullptr);
@@ -351,8 +351,9 @@ template <typename T, int NT, bool PREFIX>
 __device__ __forceinline__ void dkv_tile(const GenArgs &f, int block, float *lds) {
     const AttnArgs &a = f.a;
     const Div &tiles = PREFIX ? f.ptiles : f.stiles;
-    const int kvh = block % a.hk, g = f.g.d;
-    const int u = block / a.hk, own = tiles.quot(u), j0 = tiles.rem(u, own) * R;
+    const int u = (uint32_t)block / (uint32_t)a.hk, kvh = block - u * a.hk, g = f.g.d;
+    const int own = tiles.quot(u), j0 = tiles.rem(u, own) * R;
+    if (own >= (PREFIX ? a.groups : a.seqs)) return;
     const HeadsArg &kh = PREFIX ? a.kp : a.ks, &vh = PREFIX ? a.vp : a.vs;
     const HeadsArg &gk = PREFIX ? a.gkp : a.gks, &gv = PREFIX ? a.gvp : a.gvs;
     int q0, toks, keys, first = 0;  // first: suffix keys that query 0 sees, less one
@@ -426,10 +427,10 @@ __device__ __forceinline__ void dkv_tile(const GenArgs &f, int block, float *lds
 template <typename T, int NT, bool DQ, bool DKV>
 __global__ __launch_bounds__(THREADS, NT > (DKV ? 4 : 8) ? 1 : 2) void attn_generic_backward_kernel(GenArgs f) {
     extern __shared__ float lds[];
-    int block = blockIdx.x;
+    int block = block_index();
     if constexpr (DQ) {
         if (!DKV || block < f.dq_blocks) {
-            dq_tile<T, NT>(f, lds);
+            dq_tile<T, NT>(f, block, lds);
             return;
         }
         block -= f.dq_blocks;
@@ -458,7 +459,7 @@ hipError_t forward(const AttnArgs &a, hipStream_t st) {
     f.g = Div::of(a.hq / a.hk);
     f.tiles = Div::of(tiles);
     f.quads = in_quads(a, sizeof(T));
-    attn_generic_kernel<T, NT><<<(unsigned)(a.seqs * tiles * a.hk), THREADS,
+    attn_generic_kernel<T, NT><<<grid_of(a.seqs * tiles * a.hk), THREADS,
                                  sizeof(float) * (2 * 4 * R + 4 * R * (a.d + 1)), st>>>(f);
     return hipGetLastError();
 }
@@ -480,17 +481,23 @@ hipError_t backward(const AttnArgs &a, hipStream_t st) {
     const int64_t rows = a.total_q > 0 ? a.seqs * tiles * a.hk : 0;
     const int64_t prefix = a.groups * pt * a.hk, keys = prefix + a.seqs * sl * a.hk;
     f.prefix_blocks = (int)prefix;
-    if (rows) attn_delta_kernel<T><<<(unsigned)(((int64_t)a.total_q * a.hq + 3) / 4), THREADS, 0, st>>>(f);
+    hipError_t e = hipSuccess;
+    if (rows) {
+        attn_delta_kernel<T><<<grid_of(((int64_t)a.total_q * a.hq + 3) / 4), THREADS, 0, st>>>(f);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     if constexpr (NT <= 4) {
-        if (rows + keys <= 0x7fffffff) {
+        if (rows + keys <= kMostBlocks) {
             f.dq_blocks = (int)rows;
-            if (rows + keys)
-                attn_generic_backward_kernel<T, NT, true, true><<<(unsigned)(rows + keys), THREADS, bytes, st>>>(f);
+            if (rows + keys) attn_generic_backward_kernel<T, NT, true, true><<<grid_of(rows + keys), THREADS, bytes, st>>>(f);
             return hipGetLastError();
         }
     }
-    if (rows) attn_generic_backward_kernel<T, NT, true, false><<<(unsigned)rows, THREADS, bytes, st>>>(f);
-    if (keys) attn_generic_backward_kernel<T, NT, false, true><<<(unsigned)keys, THREADS, bytes, st>>>(f);
+    if (rows) attn_generic_backward_kernel<T, NT, true, false><<<grid_of(rows), THREADS, bytes, st>>>(f);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (keys) attn_generic_backward_kernel<T, NT, false, true><<<grid_of(keys), THREADS, bytes, st>>>(f);
     return hipGetLastError();
 }
 

@@ -153,6 +153,8 @@ hipError_t launch_clip(const ClipTensor *tensors, const ClipChunk *chunks, int64
                        double *part, float max_norm, float *norm, hipStream_t st) {
     const int grid = (int)(n_chunks < kClipBlocks ? (n_chunks > 0 ? n_chunks : 1) : kClipBlocks);
     clip_norm_kernel<<<grid, kThreads, 0, st>>>(tensors, chunks, n_chunks, part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     clip_scale_kernel<<<grid, kThreads, 0, st>>>(tensors, chunks, n_chunks, part, grid, max_norm,
                                                  norm);
     return hipGetLastError();

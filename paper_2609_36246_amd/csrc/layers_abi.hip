@@ -91,11 +91,13 @@ olive_status check_attn(const olive_attn_desc *d) {
                 return OLIVE_E_SHAPE;
         }
     }
-    // workgroups of a launch (16 rows or keys each in the kernels with the smallest tiles)
+    // workgroups of a launch (16 rows or keys each in the kernels with the smallest tiles): of the
+    // sequences' and the groups' rows, of the keys
     const int64_t g = d->heads_q / d->heads_kv;
     const int64_t rows = tiles((int64_t)d->max_q * g, 16) * d->num_seqs;
     const int64_t keys = tiles(d->max_prefix, 16) * d->num_groups + tiles(d->max_suffix, 16) * d->num_seqs;
-    if (rows > kMaxInt / d->heads_kv || keys > kMaxInt / d->heads_kv) return OLIVE_E_SHAPE;
+    const int64_t shared = tiles(d->total_q * g, 16) + d->num_groups;
+    if (rows + shared > kMostBlocks / d->heads_kv || keys > kMostBlocks / d->heads_kv) return OLIVE_E_SHAPE;
     return OLIVE_OK;
 }
 

@@ -11,6 +11,19 @@ namespace olive {
 
 constexpr int kChipUnits = 256;      // compute units of an MI355X
 
+// A grid has fewer than 2^32 threads along a dimension (of a launch with more, some workgroups
+// never run, without an error), so workgroups of 256 threads past the first 2^23 go to further
+// rows of it. The last row is a whole one: a kernel finds nothing to do at an index past its work.
+constexpr int64_t kGridRow = 1 << 23;
+constexpr int64_t kMostBlocks = 0x7fffffff - 2 * kGridRow;   // (with whole rows indexes fit an int)
+inline dim3 grid_of(int64_t blocks) {
+    if (blocks <= kGridRow) return dim3((uint32_t)blocks);
+    return dim3((uint32_t)kGridRow, (uint32_t)((blocks + kGridRow - 1) / kGridRow));
+}
+#ifdef __HIPCC__
+__device__ __forceinline__ int block_index() { return (int)(blockIdx.y * (uint32_t)kGridRow + blockIdx.x); }
+#endif
+
 // Division of 0 <= n < 2^31 by a d that is known on the host: with k = 31 + ceil(log2 d) and
 // m = ceil(2^k / d), n m / 2^k is off by less than n / 2^k < 1 / d, so its floor is the quotient.
 struct Div {

@@ -183,9 +183,9 @@ template <typename T, int VEC, int NV, int LPR>
 __global__ __launch_bounds__(256) void qk_forward_kernel(QkArgs a, int lpr_, int chunks, int per) {
     const int lpr = LPR ? LPR : lpr_;
     const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int t = (int)(w / chunks);
-    if (t >= a.tokens) return;
+    const int64_t w = (int64_t)block_index() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t t = (uint32_t)(w / chunks);
+    if (t >= (uint32_t)a.tokens) return;
     const int li = lane & (lpr - 1), sub = lane / lpr, rpw = 64 / lpr;
     const int nvec = a.d / VEC;
     const int h0 = (int)(w % chunks) * per, h1 = h0 + per;
@@ -378,11 +378,13 @@ hipError_t launch(const QkArgs &a, int lpr, bool backward, hipStream_t st) {
         per = (per + rpw - 1) / rpw * rpw;
         const int chunks = (rows + per - 1) / per;
         const int64_t waves = (int64_t)a.tokens * chunks;
-        qk_forward_kernel<T, VEC, NV, LPR><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(a, lpr, chunks, per);
+        qk_forward_kernel<T, VEC, NV, LPR><<<grid_of((waves + 3) / 4), 256, 0, st>>>(a, lpr, chunks, per);
         return hipGetLastError();
     }
     const int blocks = max(1, min(kQkBwdBlocks, (a.tokens + 3) / 4));
     qk_backward_kernel<T, VEC, NV, LPR><<<blocks, 256, 0, st>>>(a, lpr);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     if (a.gwq || a.gwk) qk_weight_grad_kernel<<<(2 * a.d + 3) / 4, 256, 0, st>>>(a, blocks);
     return hipGetLastError();
 }

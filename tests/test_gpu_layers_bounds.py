@@ -126,3 +126,79 @@ def test_gradients_of_what_is_out_of_range(case, dtype, how, n):
             keep[r[2]] = False
         for y in ("d" + x, "dv" + x[1]):
             assert bool((bad[y][keep] == 7.0).all()), y
+
+
+def arrays(total, prefix=0, suffix=1):
+    """`total` sequences of one group with one query and `suffix` tokens each."""
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    return dict(group_seqs=i32([0, total]), cu_q=torch.arange(total + 1, dtype=torch.int32, device="cuda"),
+                prefix_start=torch.zeros(1, dtype=torch.int64, device="cuda"), prefix_len=i32([prefix]),
+                suffix_len=torch.full((total,), suffix, dtype=torch.int32, device="cuda"),
+                suffix_start=torch.arange(total, device="cuda"), total_q=total, max_q=1, max_prefix=prefix,
+                max_suffix=suffix, prefix_rows=prefix, suffix_rows=total)
+
+
+def test_tokens_past_a_row_of_the_grid():
+    """A wavefront a token: more of them than a dimension of a grid has threads for."""
+    T = (1 << 26) + 5
+    x = torch.randn(T, 1, 1, device="cuda").to(BF16)
+    w = torch.full((1,), 1.5, dtype=BF16, device="cuda")
+    y = torch.full_like(x, float("nan"))
+    L.olive_qk_norm_rope(L.make_qk_desc(T, 1, 0, 1, weight_q=w, eps=0.25), x, None, y, None)
+    f = x.float()
+    want = f * torch.rsqrt(f * f + 0.25) * 1.5
+    assert bool(((y.float() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-30).all())
+
+
+def test_rows_past_a_row_of_the_grid():
+    """So many sequences and heads that the pass, and the join of its parts, take more
+    workgroups than that: single tokens with one key of their own and 3 that all share."""
+    B, H, D = (1 << 20) - 1, 65, 8
+    rnd = lambda n: torch.randn(n, H, D, device="cuda").to(BF16)  # noqa: E731
+    q, ks, vs, kp, vp = rnd(B), rnd(B), rnd(B), rnd(3), rnd(3)
+    out, lse = torch.full_like(q, float("nan")), torch.full((B, H), float("nan"), device="cuda")
+    desc = L.make_attn_desc(H, H, D, scale=0.5, **arrays(B, prefix=3))
+    work = torch.empty(L.olive_prefix_attention_workspace(desc), dtype=torch.uint8, device="cuda")
+    L.olive_prefix_attention(desc, q, kp, vp, ks, vs, out, lse, workspace=work)
+    torch.cuda.synchronize()
+    del work
+    for at in (slice(0, 1000), slice(B // 2, B // 2 + 1000), slice(B - 1000, B)):
+        k, v = (torch.cat([p[None].expand(1000, 3, H, D), s[at][:, None]], 1).double()
+                for p, s in ((kp, ks), (vp, vs)))
+        z = 0.5 * (q[at].double()[:, None] * k).sum(-1)
+        want = (torch.softmax(z, 1)[..., None] * v).sum(1)
+        # weights and outputs are rounded to bf16
+        assert bool(((out[at].double() - want).abs() <= 2.0 ** -7 * v.abs().amax(1)).all())
+        assert bool(((lse[at].double() - torch.logsumexp(z, 1)).abs() <= 1e-5).all())
+    for part in range(0, B, 1 << 17):
+        assert bool(torch.isfinite(out[part:part + (1 << 17)]).all())
+
+
+@pytest.mark.parametrize("dtype,most", [(BF16, 1 << 29), (F32, 1 << 26)])
+def test_keys_past_a_row_of_the_grid(dtype, most):
+    """The key tiles of the longest suffixes that the sizes allow, of which few are there."""
+    a = Attn(hq=4, hk=2, d=64, dtype=dtype, prefix=[30], grad=True,
+             seqs=[(0, 40, 40), (0, 5, 3), (0, 1, 1), (0, 300, 200), (0, 9, 9)])
+    a.check(a.run(grad=True, desc=a.desc(max_suffix=most)), grad=True)
+
+
+def test_backward_rows_past_a_row_of_the_grid():
+    """fp32 rows, one wavefront each in the pass before the gradients: every query sees one key,
+    so dq and dk are 0 and dv is the sum of the heads' output gradients."""
+    B, H = (1 << 16) + 1, 1 << 10
+    rnd = lambda h: torch.randn(B, h, 1, device="cuda")  # noqa: E731
+    q, do, k, v = rnd(H), rnd(H), rnd(1), rnd(1)
+    desc = L.make_attn_desc(H, 1, 1, dtype=L.OLIVE_F32, scale=1.0, **arrays(B))
+    out, dq = torch.full_like(q, 7.0), torch.full_like(q, 7.0)
+    dk, dv = torch.full_like(k, 7.0), torch.full_like(k, 7.0)
+    lse = torch.full((B, H), 7.0, device="cuda")
+    work = torch.full((L.olive_prefix_attention_workspace(desc, backward=True),), 0x3f, dtype=torch.uint8,
+                      device="cuda")
+    L.olive_prefix_attention(desc, q, None, None, k, v, out, lse, workspace=work)
+    L.olive_prefix_attention_backward(desc, q, None, None, k, v, out, lse, do, dq, None, None, dk, dv,
+                                      workspace=work)
+    assert bool((out == v).all()) and bool((lse - (q * k)[..., 0]).abs().amax() <= 1e-5)
+    # (lse is rounded, so p is off by one unit of it at most; |do v| stays below 40)
+    assert bool((dq.abs() <= 1e-4 * k.abs() + 1e-30).all())
+    assert bool((dk.abs() <= 1e-4 * q.abs().sum(1, keepdim=True)).all())
+    assert bool(((dv - do.sum(1, keepdim=True)).abs() <= 1e-5 * do.abs().sum(1, keepdim=True)).all())
