@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f) {
     }
     w.pt = tiles_of<KT>(w.s.plen);
     w.t0 = 0;
-    w.t1 = w.pt + tiles_of<KT>(suffix_seen(w.s, f.g.quot(min(w.rows, w.r0 + 128) - 1)));
+    w.t1 = w.pt + tiles_of<KT>(suffix_seen(w.s, f.g.quot(upto(w.r0, 128, w.rows) - 1)));
     make_uniform(w);
     if (nch < DP / 8) {
         for (int i = threadIdx.x; i < 2 * 2 * KT * DP / 8; i += 256)
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(BwdArgs f) {
                     const int mm = (x - 2 * KS) / DB, d = (x - 2 * KS) % DB;
                     if (x == 2 * KS) {
                         const int j0 = (pre ? kt : kt - w.pt) * KT + 32 * b;
-                        if (j0 + 32 > lowest) {
+                        if (j0 > lowest - 32) {
 #pragma unroll
                             for (int e = 0; e < 16; ++e) z[e] = j0 + acc_row(e, lane) < limit ? z[e] : kNegInf;
                         }
@@ -435,9 +435,9 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
         tile_barrier();
         if (i + 1 < i1) load.issue(f, w, lds + NEXT);
         const int row0 = r0;
-        r0 += ROWS;
+        r0 = (int)((uint32_t)r0 + ROWS);
         scalar_loads_done();
-        if (r0 <= from_lo) return;                   // no row of the tile sees this wavefront's keys
+        if (row0 <= from_lo - ROWS) return;                   // no row of the tile sees this wavefront's keys
         floatx16 p, y;
         // lane's registers are rows 8 j + 4 h + 0..3 of the tile
         const uint32_t sb = lds + AT + 2 * L::BYTES + 16 * h;
@@ -467,7 +467,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
 #pragma unroll
             for (int x = 0; x < 2; ++x) p = mfma(fa[n & 1][x], fb[n & 1][x], p);
         }
-        if (r0 > w.rows || row0 < from_hi) {
+        if (row0 > w.rows - ROWS || row0 < from_hi) {
             const int lo = max(0, from - row0), hi = w.rows - row0;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {

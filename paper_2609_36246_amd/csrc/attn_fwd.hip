@@ -209,7 +209,7 @@ __device__ __forceinline__ bool find_work(const FwdArgs &f, int block, Work &w) 
     // (a sequence that is out of range has no keys: its rows get NaN from the first row tile,
     // which may have rows past max_q to mark)
     if (w.s.bad && w.r0) return false;
-    const int st = tiles_of<KT>(suffix_seen(w.s, f.g.quot(min(w.rows, w.r0 + BM) - 1)));
+    const int st = tiles_of<KT>(suffix_seen(w.s, f.g.quot(upto(w.r0, BM, w.rows) - 1)));
     w.pt = f.p.shared ? 0 : tiles_of<KT>(w.s.plen);
     part_range(w.pt + st, f.ns, w.part, w.t0, w.t1);
     w.part += f.p.np;
@@ -276,7 +276,7 @@ __device__ __forceinline__ bool key_loop(const AttnArgs &a, const Work &w, uint3
         const bool pre = kt < w.pt;
         const int j0 = (pre ? kt : kt - w.pt) * KT + wk * NB * 32;
         const int limit = pre ? w.s.plen : seen;
-        const bool masked = j0 + NB * 32 > (pre ? w.s.plen : least);
+        const bool masked = j0 > (pre ? w.s.plen : least) - NB * 32;
         if (masked) {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -352,12 +352,13 @@ __device__ __forceinline__ bool row_by_row(const FwdArgs &f, const Work &w, int 
             for (int e = lane; e < a.d; e += 64) found |= (v[e] & 0x7f80) == 0x7f80;
         };
         const int s0 = suffix_seen(w.s, f.g.quot(w.r0));
-        for (int j = max(0, min(s0, w.s.slen - 1)) + wave; j < w.s.slen; j += 4) look(false, j);
+        const int j0 = max(0, min(s0, w.s.slen - 1));
+        for (int i = wave; i < w.s.slen - j0; i += 4) look(false, j0 + i);
         if (w.s.plen > 0) look(true, w.s.plen - 1);   // (copies of it stand for keys past the end)
         if (!__syncthreads_or(found)) return false;
     }
-    for (int row = w.r0 + wave; row < min(w.rows, w.r0 + bm); row += 4) {
-        const int tok = f.g.quot(row), head = w.kvh * (int)f.g.d + f.g.rem(row, tok);
+    for (int i = wave; i < min(bm, w.rows - w.r0); i += 4) {
+        const int row = w.r0 + i, tok = f.g.quot(row), head = w.kvh * (int)f.g.d + f.g.rem(row, tok);
         const int t = w.s.q0 + tok;
         const int seen = suffix_seen(w.s, tok);
         const uint16_t *q = head_row(a.q, t, head);
@@ -366,7 +367,7 @@ __device__ __forceinline__ bool row_by_row(const FwdArgs &f, const Work &w, int 
         for (int i = 0; i < 4; ++i) x[i] = lane + 64 * i < a.d ? load_elem<uint16_t>(q, lane + 64 * i) : 0.f;
         for (int kt = w.t0; kt < w.t1; ++kt) {
             const bool pre = kt < w.pt;
-            const int j0 = (pre ? kt : kt - w.pt) * KT, end = min(j0 + KT, pre ? w.s.plen : seen);
+            const int j0 = (pre ? kt : kt - w.pt) * KT, end = upto(j0, KT, pre ? w.s.plen : seen);
             for (int j = j0; j < end; ++j) {
                 const int64_t at = key_row(pre, j);
                 const uint16_t *k = head_row(pick(pre, a.kp, a.ks), at, w.kvh), *v = head_row(pick(pre, a.vp, a.vs), at, w.kvh);

@@ -169,10 +169,10 @@ __global__ __launch_bounds__(THREADS, NT > 8 ? 1 : 2) void attn_generic_kernel(G
     for (int n = 0; n < NT; ++n) acc[n] = (floatx4)(0.f);
     const int seen = w.live ? w.s.plen + suffix_seen(w.s, w.tok) : 0;
     const int least = w.s.plen + suffix_seen(w.s, f.g.quot(w.r0));
-    const int end = w.s.plen + suffix_seen(w.s, f.g.quot(min(w.rows, w.r0 + R) - 1));
+    const int end = w.s.plen + suffix_seen(w.s, f.g.quot(upto(w.r0, R, w.rows) - 1));
     float m = kNegInf, l = 0.f;
     bool bad = false;
-    for (int j0 = wave * R; j0 < end; j0 += 4 * R) {
+    for (int j0 = wave * R; j0 < end; j0 = upto(j0, 4 * R, end)) {
         const T *kp, *vp, *col[4], *unused;
         key_ptrs<T>(a, w.s, w.kvh, j0 + (lane & 15), end, bad, kp, vp);
 #pragma unroll
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(THREADS, NT > 8 ? 1 : 2) void attn_generic_kernel(G
         for (int n = 0; n < NT; ++n) acc[n] *= r;
         load_cols<T, NT>(col, a.d, x);
         bool special = false;
-        if (j0 + R > least) {
+        if (j0 > least - R) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -320,9 +320,9 @@ __device__ __forceinline__ void dq_tile(const GenArgs &f, int block, float *lds)
     const int64_t at = (int64_t)w.t * a.hq + w.head;
     const float lse = a.lse[at], delta = f.delta[at];
     const int seen = w.live ? w.s.plen + suffix_seen(w.s, w.tok) : 0;
-    const int end = w.s.plen + suffix_seen(w.s, f.g.quot(min(w.rows, w.r0 + R) - 1));
+    const int end = w.s.plen + suffix_seen(w.s, f.g.quot(upto(w.r0, R, w.rows) - 1));
     bool bad = false;
-    for (int j0 = wave * R; j0 < end; j0 += 4 * R) {
+    for (int j0 = wave * R; j0 < end; j0 = upto(j0, 4 * R, end)) {
         const T *kp, *vp, *col[4], *unused;
         key_ptrs<T>(a, w.s, w.kvh, j0 + (lane & 15), end, bad, kp, vp);
 #pragma unroll
@@ -386,7 +386,7 @@ __device__ __forceinline__ void dkv_tile(const GenArgs &f, int block, float *lds
     // the first row that sees this lane's key, and the tile's first one
     const auto row_of = [&](int j) { return PREFIX ? 0 : (int)min((int64_t)rows, (int64_t)max(0, j - first) * g); };
     const int from = row_of(key);
-    for (int r0 = row_of(j0) / R * R + wave * R; r0 < rows; r0 += 4 * R) {
+    for (int r0 = upto(row_of(j0) / R * R, wave * R, rows); r0 < rows; r0 = upto(r0, 4 * R, rows)) {
         const T *qc[4], *gc[4];
         float lse[4], delta[4];
 #pragma unroll

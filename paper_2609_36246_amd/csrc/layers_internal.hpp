@@ -44,6 +44,9 @@ struct Div {
     __host__ __device__ int rem(int n, int q) const { return n - q * (int)d; }
 };
 
+// at + n, no further than end (rows, tokens and keys go up to 2^31 - 1, where the sum passes 32 bits).
+__host__ __device__ inline int upto(int at, int n, int end) { return n < (int64_t)end - at ? at + n : end; }
+
 struct HeadsArg {                    // olive_heads with a typed use in the kernels
     char *p;
     int64_t st, sh;                  // elements between tokens and heads

@@ -254,13 +254,13 @@ __global__ __launch_bounds__(256) void qk_backward_kernel(QkArgs a, int lpr_) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int li = lane & (lpr - 1), sub = lane / lpr, rpw = 64 / lpr;
     const int nvec = a.d / VEC;
-    const int stride = gridDim.x * 4;
+    const uint32_t stride = gridDim.x * 4;
     const float inv_d = 1.f / (float)a.d;
     float wq[NV][VEC], wk[NV][VEC], sq[NV][VEC] = {}, sk[NV][VEC] = {};
     load_weight<T, VEC, NV>(a.wq, li, nvec, wq);
     load_weight<T, VEC, NV>(a.wk, li, nvec, wk);
 
-    for (int t = blockIdx.x * 4 + wave; t < a.tokens; t += stride) {
+    for (uint32_t t = blockIdx.x * 4 + wave; t < (uint32_t)a.tokens; t += stride) {
         Angles<VEC, NV> g;
         load_angles<VEC, NV>(a, t, li, nvec, g);
         const auto heads = [&](int n, const HeadsArg &from, const HeadsArg &grad, const HeadsArg &to, bool normed,
@@ -381,7 +381,7 @@ hipError_t launch(const QkArgs &a, int lpr, bool backward, hipStream_t st) {
         qk_forward_kernel<T, VEC, NV, LPR><<<grid_of((waves + 3) / 4), 256, 0, st>>>(a, lpr, chunks, per);
         return hipGetLastError();
     }
-    const int blocks = max(1, min(kQkBwdBlocks, (a.tokens + 3) / 4));
+    const int blocks = min(kQkBwdBlocks, (a.tokens - 1) / 4 + 1);   // (one without tokens)
     qk_backward_kernel<T, VEC, NV, LPR><<<blocks, 256, 0, st>>>(a, lpr);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -202,3 +202,38 @@ def test_backward_rows_past_a_row_of_the_grid():
     assert bool((dq.abs() <= 1e-4 * k.abs() + 1e-30).all())
     assert bool((dk.abs() <= 1e-4 * q.abs().sum(1, keepdim=True)).all())
     assert bool(((dv - do.sum(1, keepdim=True)).abs() <= 1e-5 * do.abs().sum(1, keepdim=True)).all())
+
+
+def test_the_most_tokens_backward():
+    """2^31 - 1 tokens of one element: dx = r (g w - x^2 r^2 g w)."""
+    T = (1 << 31) - 1
+    x, g, dx = (torch.empty(T, 1, 1, dtype=BF16, device="cuda") for _ in range(3))
+    x.normal_()
+    g.normal_()
+    w = torch.full((1,), 1.5, dtype=BF16, device="cuda")
+    desc = L.make_qk_desc(T, 1, 0, 1, weight_q=w, eps=0.25)
+    L.olive_qk_norm_rope_backward(desc, x, None, g, None, dx, None)
+    for at in list(range(0, T, 1 << 28)) + [T - (1 << 20)]:
+        s = slice(at, min(T, at + (1 << 20)))
+        y, f = x[s].double(), g[s].double() * 1.5
+        r = (y * y + 0.25).rsqrt()
+        # a difference of two terms of up to r |g w| in 32 bits, rounded to bf16
+        want, size = r * (f - y * y * r * r * f), r * f.abs()
+        assert bool(((dx[s].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -20 * size).all()), at
+
+
+def test_the_longest_prefix():
+    """2^31 - 1 keys: the last one, in a tile with one key less, counts once."""
+    n, d = (1 << 31) - 1, 8
+    k, v = (torch.zeros(n, 1, d, dtype=BF16, device="cuda") for _ in range(2))
+    k[n - 1], v[n - 1] = 8.0, 1.0
+    q = torch.ones(1, 1, d, dtype=BF16, device="cuda")
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    desc = L.make_attn_desc(1, 1, d, i32([0, 1]), i32([0, 1]), torch.zeros(1, dtype=torch.int64, device="cuda"),
+                            i32([n]), i32([0]), total_q=1, max_q=1, max_prefix=n, max_suffix=0, prefix_rows=n,
+                            suffix_rows=0, scale=1.0)
+    work = torch.empty(L.olive_prefix_attention_workspace(desc), dtype=torch.uint8, device="cuda")
+    out, lse = torch.full_like(q, 7.0), torch.full((1, 1), 7.0, device="cuda")
+    L.olive_prefix_attention(desc, q, k, v, None, None, out, lse, workspace=work)
+    # e^64 beside 2^31 times e^0
+    assert abs(float(lse) - 64.0) <= 1e-4 and bool((out == 1.0).all())
