@@ -223,8 +223,8 @@ olive_status olive_grad_clip_init(olive_clip_ctx **out, const olive_grad_tensor 
  *   norm = (sum over all gradients of their squares)^1/2      (summed in 64 bits)
  *   out  = grad * min(1, max_norm / (norm + 1e-6))
  * norm: device fp32 [1] or NULL. max_norm >= 0; +inf: out gets the gradients unscaled
- * (nothing is written in place). A norm that is not finite leaves the gradients unscaled
- * too, and the caller skips the step by it. A context takes one call at a time.
+ * (nothing is written in place). A norm that is not finite in fp32 leaves the gradients
+ * unscaled too, and the caller skips the step by it. A context takes one call at a time.
  * Errors: E_NULL, E_RANGE (max_norm negative or NaN), E_HIP.
  */
 olive_status olive_grad_clip(olive_clip_ctx *ctx, float max_norm, float *norm,

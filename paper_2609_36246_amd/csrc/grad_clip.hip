@@ -124,9 +124,9 @@ __global__ __launch_bounds__(kThreads) void clip_scale_kernel(const ClipTensor *
     double s = 0.0;
     for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
     const double n = sqrt(block_sum(s));
-    // 1 for a norm that is not finite: the values are left as they are
+    // 1 for a norm that is not finite as the caller gets it: the values are left as they are
     float f = 1.f;
-    if (n < __builtin_inf()) {
+    if ((float)n < __builtin_inff()) {
         const double g = (double)max_norm / (n + 1e-6);
         f = g < 1.0 ? (float)g : 1.f;
     }

@@ -237,3 +237,20 @@ def test_the_longest_prefix():
     L.olive_prefix_attention(desc, q, k, v, None, None, out, lse, workspace=work)
     # e^64 beside 2^31 times e^0
     assert abs(float(lse) - 64.0) <= 1e-4 and bool((out == 1.0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("max_norm", [1.0, 1e38])
+def test_norm_past_the_largest_fp32(dtype, in_place, max_norm):
+    """Finite gradients whose norm is none in fp32: it is reported as infinite, and nothing is scaled."""
+    g = [torch.full((n,), 3e38, device="cuda").to(dtype) for n in (5, 4000)]
+    before = [x.clone() for x in g]
+    outs = g if in_place else [torch.full_like(x, 7.0) for x in g]
+    norm = torch.zeros(1, device="cuda")
+    ctx = L.olive_grad_clip_init(g, outs)
+    L.olive_grad_clip(ctx, max_norm, norm)
+    torch.cuda.synchronize()
+    L.olive_grad_clip_free(ctx)
+    assert float(norm) == float("inf")
+    assert all(torch.equal(x, y) for x, y in zip(outs, before))
