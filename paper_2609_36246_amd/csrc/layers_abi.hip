@@ -304,12 +304,12 @@ olive_status olive_grad_clip_init(olive_clip_ctx **out, const olive_grad_tensor 
         if ((uintptr_t)t.grad % (t.dtype == OLIVE_BF16 ? 2 : 4) ||
             (t.out && (uintptr_t)t.out % (t.dtype_out == OLIVE_BF16 ? 2 : 4)))
             return OLIVE_E_UNSUPPORTED;
-        const int64_t c = tiles(t.n, kClipChunk);
+        const int64_t c = t.n / kClipChunk + (t.n % kClipChunk > 0);
         if (c > kMaxInt - n_chunks) return OLIVE_E_SHAPE;
         n_chunks += c;
     }
     olive_clip_ctx *ctx = new (std::nothrow) olive_clip_ctx;
-    ClipTensor *ht = new (std::nothrow) ClipTensor[count + 1];
+    ClipTensor *ht = new (std::nothrow) ClipTensor[(size_t)count + 1];
     ClipChunk *hc = new (std::nothrow) ClipChunk[n_chunks + 1];
     olive_status s = ctx && ht && hc ? OLIVE_OK : OLIVE_E_NOMEM;
     if (s == OLIVE_OK) {
@@ -322,7 +322,7 @@ olive_status olive_grad_clip_init(olive_clip_ctx **out, const olive_grad_tensor 
         }
         ctx->n_chunks = n_chunks;
         hipStream_t st = (hipStream_t)hip_stream;
-        if (hipMalloc((void **)&ctx->tensors, sizeof(ClipTensor) * (count + 1)) != hipSuccess ||
+        if (hipMalloc((void **)&ctx->tensors, sizeof(ClipTensor) * ((size_t)count + 1)) != hipSuccess ||
             hipMalloc((void **)&ctx->chunks, sizeof(ClipChunk) * (n_chunks + 1)) != hipSuccess ||
             hipMalloc((void **)&ctx->part, sizeof(double) * kClipBlocks) != hipSuccess)
             s = OLIVE_E_NOMEM;
