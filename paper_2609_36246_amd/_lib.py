@@ -4,6 +4,8 @@ include/olive_layers.h).
 Argument marshalling only: every function has the C name and forwards plain
 pointers, sizes and the HIP stream. Torch tensors are accepted wherever the C
 function takes a device pointer (their data_ptr() is passed); None maps to NULL.
+The layer operators' functions refuse tensors of another type or layout than the
+library would read (ValueError); the sizes of the heads' views are the caller's.
 The library must have been built (python -m paper_2609_36246_amd.build); loading
 fails loudly otherwise -- there is no fallback path.
 """
@@ -426,14 +428,31 @@ def make_heads(x) -> Optional[olive_heads]:
     contiguous (None stays None; the caller keeps the tensor alive)."""
     if x is None or isinstance(x, olive_heads):
         return x
-    return olive_heads(*_view(x))
-
-
-def _view(x):
     s = x.stride()
     if len(s) != 3 or (s[2] != 1 and x.shape[2] > 1):
         raise ValueError("expected [tokens, heads, head_dim] with contiguous heads")
-    return x.data_ptr(), s[0], s[1]
+    return olive_heads(x.data_ptr(), s[0], s[1])
+
+
+_dtypes = {}             # torch's types by olive_dtype or name, at the first call
+
+
+def _dtype(kind):
+    if not _dtypes:
+        import torch
+        _dtypes.update({OLIVE_F32: torch.float32, OLIVE_BF16: torch.bfloat16, "int32": torch.int32,
+                        "int64": torch.int64})
+    return _dtypes.get(kind)
+
+
+def _array(x, kind, least: int, what: str) -> Optional[int]:
+    """Address of a contiguous tensor of a type (_dtype) with at least so many elements (None
+    and an address are taken as they are)."""
+    if x is None or isinstance(x, int):
+        return x
+    if x.dtype is not _dtype(kind) or not x.is_contiguous() or x.numel() < least:
+        raise ValueError("%s: expected a contiguous tensor of %s, %d elements at least" % (what, _dtype(kind), least))
+    return x.data_ptr()
 
 
 class _Views(threading.local):
@@ -448,17 +467,24 @@ _views = _Views()
 _packers = [struct.Struct("=%dq" % (3 * i)) for i in range(17)]
 
 
-def _heads(*xs):
+def _heads(desc, *xs):
     """Addresses of the views' olive_heads (one object made for each would cost more time than
     a small call on the GPU)."""
-    values, at = [], []
+    values, at, dtype = [], [], _dtype(desc.dtype)
     for x, place in zip(xs, _views.at):
         if x is None:
             values += (0, 0, 0)
             at.append(None)
-        else:
-            values += (x.data or 0, x.stride_token, x.stride_head) if isinstance(x, olive_heads) else _view(x)
-            at.append(place)
+            continue
+        at.append(place)
+        if isinstance(x, olive_heads):
+            values += (x.data or 0, x.stride_token, x.stride_head)
+            continue
+        s = x.stride()
+        if len(s) != 3 or x.dtype is not dtype or (s[2] != 1 and x.shape[2] > 1):
+            raise ValueError("expected [tokens, heads, head_dim] of the descriptor's dtype (%s) with contiguous heads"
+                             % dtype)
+        values += (x.data_ptr(), s[0], s[1])
     _packers[len(at)].pack_into(_views.buffer, 0, *values)
     return at
 
@@ -470,14 +496,19 @@ def _call(name):
 
 
 def _workspace(w):
-    return (None, 0) if w is None else (w.data_ptr(), w.numel() * w.element_size())
+    if w is None:
+        return None, 0
+    if not w.is_contiguous():
+        raise ValueError("a workspace is a contiguous tensor")
+    return w.data_ptr(), w.numel() * w.element_size()
 
 
 def make_qk_desc(tokens, heads_q, heads_k, head_dim, positions=None, cos=None, sin=None,
                  weight_q=None, weight_k=None, dtype=OLIVE_BF16, eps=1e-6, layout=OLIVE_ROPE_HALF,
                  rot_dim=None, num_positions=None, slots=None, slot_rows=0) -> olive_qk_desc:
-    """cos and sin: fp32 [num_positions, rot_dim / 2], which give the default sizes. The
-    descriptor keeps its tensors alive."""
+    """cos and sin: fp32 [num_positions, rot_dim / 2], which give the default sizes; positions
+    and slots int32, the weights of the heads' dtype, all contiguous. The descriptor keeps its
+    tensors alive."""
     d = olive_qk_desc()
     d.size = ctypes.sizeof(olive_qk_desc)
     d.dtype, d.tokens = int(dtype), int(tokens)
@@ -486,16 +517,22 @@ def make_qk_desc(tokens, heads_q, heads_k, head_dim, positions=None, cos=None, s
     d.num_positions = int(num_positions if num_positions is not None
                           else 0 if cos is None else cos.shape[0])
     d.layout, d.eps = int(layout), float(eps)
-    d.positions, d.cos, d.sin = _ptr(positions), _ptr(cos), _ptr(sin)
-    d.weight_q, d.weight_k = _ptr(weight_q), _ptr(weight_k)
-    d.slots, d.slot_rows = _ptr(slots), int(slot_rows)
+    for table in (cos, sin) if d.rot_dim else ():
+        if not (table is None or isinstance(table, int)) and 2 * table.shape[-1] != d.rot_dim:
+            raise ValueError("cos and sin have rot_dim / 2 columns")
+    d.positions = _array(positions, "int32", d.tokens, "positions")
+    angles = d.num_positions * d.rot_dim // 2
+    d.cos, d.sin = _array(cos, OLIVE_F32, angles, "cos"), _array(sin, OLIVE_F32, angles, "sin")
+    d.weight_q = _array(weight_q, d.dtype, d.head_dim, "weight_q")
+    d.weight_k = _array(weight_k, d.dtype, d.head_dim, "weight_k")
+    d.slots, d.slot_rows = _array(slots, "int32", d.tokens, "slots"), int(slot_rows)
     d.tensors = (positions, cos, sin, weight_q, weight_k, slots)
     return d
 
 
 def olive_qk_norm_rope(desc: olive_qk_desc, q, k, q_out, k_out, v=None, v_out=None, stream=None,
                        check: bool = True) -> int:
-    s = _call("olive_qk_norm_rope")(ctypes.addressof(desc), *_heads(q, k, v, q_out, k_out, v_out),
+    s = _call("olive_qk_norm_rope")(ctypes.addressof(desc), *_heads(desc, q, k, v, q_out, k_out, v_out),
                                     _stream(stream))
     if check:
         _check(s, "olive_qk_norm_rope")
@@ -514,8 +551,9 @@ def olive_qk_norm_rope_backward(desc: olive_qk_desc, q, k, grad_q_out, grad_k_ou
                                 grad_weight_q=None, grad_weight_k=None, workspace=None,
                                 stream=None, check: bool = True) -> int:
     s = _call("olive_qk_norm_rope_backward")(
-        ctypes.addressof(desc), *_heads(q, k, grad_q_out, grad_k_out, grad_q, grad_k),
-        _ptr(grad_weight_q), _ptr(grad_weight_k), *_workspace(workspace), _stream(stream))
+        ctypes.addressof(desc), *_heads(desc, q, k, grad_q_out, grad_k_out, grad_q, grad_k),
+        _array(grad_weight_q, OLIVE_F32, desc.head_dim, "grad_weight_q"),
+        _array(grad_weight_k, OLIVE_F32, desc.head_dim, "grad_weight_k"), *_workspace(workspace), _stream(stream))
     if check:
         _check(s, "olive_qk_norm_rope_backward")
     return s
@@ -526,8 +564,8 @@ def make_attn_desc(heads_q, heads_kv, head_dim, group_seqs, cu_q, prefix_start, 
                    suffix_start=None, page_table=None, page_size=0, dtype=OLIVE_BF16,
                    scale=None, num_groups=None, num_seqs=None) -> olive_attn_desc:
     """Device tensors: group_seqs [G + 1], cu_q [B + 1], prefix_len [G], suffix_len [B] int32,
-    prefix_start [G], suffix_start [B] int64, page_table [B, pages] int32. The descriptor
-    keeps them alive."""
+    prefix_start [G], suffix_start [B] int64, page_table [B, pages] int32 (its rows at any
+    distance, the others contiguous). The descriptor keeps them alive."""
     d = olive_attn_desc()
     d.size = ctypes.sizeof(olive_attn_desc)
     d.dtype = int(dtype)
@@ -537,12 +575,18 @@ def make_attn_desc(heads_q, heads_kv, head_dim, group_seqs, cu_q, prefix_start, 
     d.max_q, d.total_q = int(max_q), int(total_q)
     d.max_prefix, d.max_suffix = int(max_prefix), int(max_suffix)
     d.prefix_rows, d.suffix_rows = int(prefix_rows), int(suffix_rows)
-    d.group_seqs, d.cu_q = _ptr(group_seqs), _ptr(cu_q)
-    d.prefix_start, d.prefix_len = _ptr(prefix_start), _ptr(prefix_len)
-    d.suffix_len, d.suffix_start = _ptr(suffix_len), _ptr(suffix_start)
+    G, B = d.num_groups, d.num_seqs
+    d.group_seqs, d.cu_q = _array(group_seqs, "int32", G + 1, "group_seqs"), _array(cu_q, "int32", B + 1, "cu_q")
+    d.prefix_start = _array(prefix_start, "int64", G, "prefix_start")
+    d.prefix_len = _array(prefix_len, "int32", G, "prefix_len")
+    d.suffix_len = _array(suffix_len, "int32", B, "suffix_len")
+    d.suffix_start = _array(suffix_start, "int64", B, "suffix_start")
     d.page_table, d.page_size = _ptr(page_table), int(page_size)
-    d.table_stride = 0 if page_table is None or isinstance(page_table, int) \
-        else page_table.stride(0)
+    if page_table is not None and not isinstance(page_table, int):
+        if page_table.dtype is not _dtype("int32") or page_table.dim() != 2 or page_table.shape[0] < B or \
+                (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError("page_table: expected int32 [%d, pages] with contiguous rows" % B)
+        d.table_stride = page_table.stride(0)
     d.scale = float(scale if scale is not None else head_dim ** -0.5)
     d.tensors = (group_seqs, cu_q, prefix_start, prefix_len, suffix_len, suffix_start, page_table)
     return d
@@ -563,8 +607,8 @@ def olive_prefix_attention_workspace(desc: olive_attn_desc, backward: bool = Fal
 def olive_prefix_attention(desc: olive_attn_desc, q, k_prefix, v_prefix, k_suffix, v_suffix, out,
                            lse=None, workspace=None, stream=None, check: bool = True) -> int:
     s = _call("olive_prefix_attention")(
-        ctypes.addressof(desc), *_heads(q, k_prefix, v_prefix, k_suffix, v_suffix, out), _ptr(lse),
-        *_workspace(workspace), _stream(stream))
+        ctypes.addressof(desc), *_heads(desc, q, k_prefix, v_prefix, k_suffix, v_suffix, out),
+        _array(lse, OLIVE_F32, desc.total_q * desc.heads_q, "lse"), *_workspace(workspace), _stream(stream))
     if check:
         _check(s, "olive_prefix_attention")
     return s
@@ -574,10 +618,11 @@ def olive_prefix_attention_backward(desc: olive_attn_desc, q, k_prefix, v_prefix
                                     v_suffix, out, lse, grad_out, grad_q, grad_k_prefix,
                                     grad_v_prefix, grad_k_suffix, grad_v_suffix, workspace=None,
                                     stream=None, check: bool = True) -> int:
-    at = _heads(q, k_prefix, v_prefix, k_suffix, v_suffix, out, grad_out, grad_q, grad_k_prefix,
+    at = _heads(desc, q, k_prefix, v_prefix, k_suffix, v_suffix, out, grad_out, grad_q, grad_k_prefix,
                 grad_v_prefix, grad_k_suffix, grad_v_suffix)
     s = _call("olive_prefix_attention_backward")(
-        ctypes.addressof(desc), *at[:6], _ptr(lse), *at[6:], *_workspace(workspace), _stream(stream))
+        ctypes.addressof(desc), *at[:6], _array(lse, OLIVE_F32, desc.total_q * desc.heads_q, "lse"), *at[6:],
+        *_workspace(workspace), _stream(stream))
     if check:
         _check(s, "olive_prefix_attention_backward")
     return s
@@ -610,7 +655,7 @@ def olive_grad_clip_init(grads, outs=None, stream=None) -> int:
 
 
 def olive_grad_clip(ctx, max_norm: float, norm=None, stream=None, check: bool = True) -> int:
-    s = _call("olive_grad_clip")(ctx, max_norm, _ptr(norm), _stream(stream))
+    s = _call("olive_grad_clip")(ctx, max_norm, _array(norm, OLIVE_F32, 1, "norm"), _stream(stream))
     if check:
         _check(s, "olive_grad_clip")
     return s
