@@ -254,3 +254,11 @@ def test_norm_past_the_largest_fp32(dtype, in_place, max_norm):
     L.olive_grad_clip_free(ctx)
     assert float(norm) == float("inf")
     assert all(torch.equal(x, y) for x, y in zip(outs, before))
+
+
+def test_the_current_stream():
+    """Where no stream is given it is torch's current one, on which the call runs."""
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        assert L._stream(None) == side.cuda_stream == torch.cuda.current_stream().cuda_stream
+    assert L._stream(None) == torch.cuda.current_stream().cuda_stream != side.cuda_stream

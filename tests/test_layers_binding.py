@@ -109,3 +109,10 @@ def test_calls_of_other_tensors(lib, monkeypatch):
             call()
     # what is an address or a view already is the caller's
     assert isinstance(L.make_heads(h(F32)), L.olive_heads) and ctypes.sizeof(L.olive_heads) == 24
+
+
+def test_the_current_stream_without_the_bare_handle(monkeypatch):
+    """A torch that lacks the entry for a stream's bare handle is asked by its public one."""
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: type("S", (), {"cuda_stream": 77}))
+    assert L._stream(None) == 77 and L._stream(5) == 5
