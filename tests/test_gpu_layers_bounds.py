@@ -262,3 +262,38 @@ def test_the_current_stream():
     with torch.cuda.stream(side):
         assert L._stream(None) == side.cuda_stream == torch.cuda.current_stream().cuda_stream
     assert L._stream(None) == torch.cuda.current_stream().cuda_stream != side.cuda_stream
+
+
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("dtype,how,d", [(BF16, "plain", 64), (BF16, "plain", 256), (BF16, "odd", 64),
+                                         (BF16, "plain", 100), (F32, "plain", 64), (F32, "odd", 40),
+                                         (F32, "plain", 256)])
+@pytest.mark.parametrize("prefix,seqs", [([37], [(0, 70, 70), (0, 40, 9), (0, 5, 1)]),
+                                         ([0, 200], [(0, 300, 300), (1, 40, 9)])])
+def test_values_that_not_every_query_sees(prefix, seqs, dtype, how, d, page):
+    """NaN and infinities inside a tile of keys that some rows see, and in a prefix's last row."""
+    a = Attn(hq=4, hk=2, d=d, dtype=dtype, how=how, page=page, prefix=prefix, seqs=seqs, seed=13)
+    for j, h, e, x in ((45, 0, 3, float("inf")), (50, 1, slice(0, d), float("nan")), (69, 0, 5, -float("inf"))):
+        a.t["vs"][int(a.rows[0][j]), h, e] = x
+    a.t["vp"][a.pstart[-1] + prefix[-1] - 1, 1, 2] = -float("inf")
+    a.check(a.run())
+    # a key: its queries get NaN, the others what they get without it
+    b, j = 1, 38
+    key, first = int(a.rows[b][j]), j - (seqs[b][1] - seqs[b][2])
+    rows = slice(a.cu[b], a.cu[b] + first)
+    a.t["ks"][key] = 0.0
+    want = a.run()
+    a.t["ks"][key] = float("nan")
+    got = a.run()
+    assert bool(torch.isnan(got["out"][a.cu[b] + first:a.cu[b + 1]]).all())
+    assert bool(torch.isnan(got["lse"][a.cu[b] + first:a.cu[b + 1]]).all())
+    unit = 2.0 ** -7 if dtype == BF16 else 1e-4      # (rows formed one by one round otherwise)
+    x, y = got["out"][rows].double(), want["out"][rows].double()
+    both = torch.isfinite(y)
+    assert torch.equal(torch.isfinite(x), both) and torch.equal(x.isnan(), y.isnan())
+    assert bool(((x - y).abs()[both] <= 2 * unit * (1 + y.abs()[both])).all())
+    assert torch.allclose(got["lse"][rows], want["lse"][rows], rtol=1e-4, atol=1e-4)
+    for c in range(len(seqs)):
+        if c != b:
+            s = slice(a.cu[c], a.cu[c + 1])
+            assert torch.equal(torch.nan_to_num(got["out"][s], 9.0), torch.nan_to_num(want["out"][s], 9.0))
