@@ -17,6 +17,7 @@ namespace olive {
 namespace {
 
 constexpr int R = 16, THREADS = 256;
+constexpr int kSideBySide = 4 * kChipUnits;   // workgroups of the backward's passes that one launch takes
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 struct GenArgs {
@@ -421,9 +422,12 @@ __device__ __forceinline__ void dkv_tile(const GenArgs &f, int block, float *lds
     join_and_put<T, NT>(lds, dv, a.d, cols, 1.f, [&](int c) { return (T *)row_ptr<T>(gv, krow + j0 + c, kvh); });
 }
 
-// The passes for dq and for the keys' gradients need nothing of each other: small heads run
-// them in one launch (few workgroups that wait for loads: side by side 24 us at the size above,
-// one after the other 23, 35 and 21 with scalar loads), large ones, whose registers differ, in two.
+// The passes for dq and for the keys' gradients need nothing of each other. Up to four workgroups
+// a compute unit of both together they run side by side in one launch: few workgroups that wait
+// for loads. More of them get two launches, in each of which all take about as long. Backward with
+// its delta in fp32, one launch against two (us): heads of 64, 128 workgroups 35 : 48, 680 86 : 100,
+// 848 64 : 74, 1328 138 : 122, 1360 106 : 118, 1744 179 : 159; heads of 128, 128 workgroups
+// 56 : 76, 848 119 : 124, 2632 552 : 497.
 template <typename T, int NT, bool DQ, bool DKV>
 __global__ __launch_bounds__(THREADS, NT > (DKV ? 4 : 8) ? 1 : 2) void attn_generic_backward_kernel(GenArgs f) {
     extern __shared__ float lds[];
@@ -487,10 +491,11 @@ hipError_t backward(const AttnArgs &a, hipStream_t st) {
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if constexpr (NT <= 4) {
-        if (rows + keys <= kMostBlocks) {
+    if constexpr (NT <= 8) {
+        if (rows + keys <= kSideBySide) {
             f.dq_blocks = (int)rows;
-            if (rows + keys) attn_generic_backward_kernel<T, NT, true, true><<<grid_of(rows + keys), THREADS, bytes, st>>>(f);
+            if (rows + keys)
+                attn_generic_backward_kernel<T, NT, true, true><<<(unsigned)(rows + keys), THREADS, bytes, st>>>(f);
             return hipGetLastError();
         }
     }
