@@ -207,6 +207,15 @@ __global__ __launch_bounds__(256) void qk_forward_kernel(QkArgs a, int lpr_, int
         for (int h = max(h0 - first, 0); h < min(h1 - first, n); h += rpw) {
             const int r = h + sub;
             const bool live = r < min(h1 - first, n);
+            if constexpr (COPY) {                    // (bits, so that a NaN keeps its own)
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const int i = li + 64 * v;
+                    if (live && keep && i < nvec)
+                        *(Pack<T, VEC> *)(dst + r * to.sh + i * VEC) = *(const Pack<T, VEC> *)(src + r * from.sh + i * VEC);
+                }
+                continue;
+            }
             float x[NV][VEC], ss = 0.f;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
@@ -218,20 +227,18 @@ __global__ __launch_bounds__(256) void qk_forward_kernel(QkArgs a, int lpr_, int
                     for (int j = 0; j < VEC; ++j) x[v][j] = 0.f;
                 }
             }
-            if (!COPY) {
-                if (weight) {
+            if (weight) {
 #pragma unroll
-                    for (int v = 0; v < NV; ++v)
+                for (int v = 0; v < NV; ++v)
 #pragma unroll
-                        for (int j = 0; j < VEC; ++j) ss = fmaf(x[v][j], x[v][j], ss);
-                    const float rr = inv_root(row_sum<LPR>(ss, lpr), inv_d, a.eps);
+                    for (int j = 0; j < VEC; ++j) ss = fmaf(x[v][j], x[v][j], ss);
+                const float rr = inv_root(row_sum<LPR>(ss, lpr), inv_d, a.eps);
 #pragma unroll
-                    for (int v = 0; v < NV; ++v)
+                for (int v = 0; v < NV; ++v)
 #pragma unroll
-                        for (int j = 0; j < VEC; ++j) x[v][j] = x[v][j] * rr * wt[v][j];
-                }
-                rotate<VEC, NV, LPR, 1>(g, a.rot, a.layout, li, lpr, x);
+                    for (int j = 0; j < VEC; ++j) x[v][j] = x[v][j] * rr * wt[v][j];
             }
+            rotate<VEC, NV, LPR, 1>(g, a.rot, a.layout, li, lpr, x);
             if (live && keep) {
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {

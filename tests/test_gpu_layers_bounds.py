@@ -297,3 +297,13 @@ def test_values_that_not_every_query_sees(prefix, seqs, dtype, how, d, page):
         if c != b:
             s = slice(a.cu[c], a.cu[c + 1])
             assert torch.equal(torch.nan_to_num(got["out"][s], 9.0), torch.nan_to_num(want["out"][s], 9.0))
+
+
+@pytest.mark.parametrize("d", [128, 127])
+def test_values_keep_their_bits(d):
+    """Every bf16 pattern, signalling NaNs and subnormals among them, on its way into a cache."""
+    v = torch.arange(65536, dtype=torch.int32).to(torch.int16).cuda().view(BF16).view(512, 1, 128)[:, :, :d]
+    k = torch.ones_like(v)
+    ko, vo = torch.empty_like(k), torch.zeros(512, 1, 128, dtype=BF16, device="cuda")[:, :, :d]
+    L.olive_qk_norm_rope(L.make_qk_desc(512, 0, 1, d), None, k, None, ko, v=v, v_out=vo)
+    assert torch.equal(vo.contiguous().view(torch.int16), v.contiguous().view(torch.int16))
