@@ -173,9 +173,12 @@ __device__ __forceinline__ void load_weight(const void *w, int li, int nvec,
     }
 }
 
-// 1 / root of the mean square (v_rsq_f32 is off by one unit at most).
+// 1 / root of the mean square (v_rsq_f32 is off by one unit at most, and takes a subnormal number
+// for 0: small ones are scaled).
 __device__ __forceinline__ float inv_root(float ss, float inv_d, float eps) {
-    return __builtin_amdgcn_rsqf(fmaf(ss, inv_d, eps));
+    const float m = fmaf(ss, inv_d, eps);
+    const bool small = m < 0x1p-100f;
+    return __builtin_amdgcn_rsqf(small ? m * 0x1p100f : m) * (small ? 0x1p50f : 1.f);
 }
 
 // Wavefront w of the grid: token w / chunks, rows (w % chunks) * per ... of its q, k and v.
@@ -301,14 +304,15 @@ __global__ __launch_bounds__(256) void qk_backward_kernel(QkArgs a, int lpr_) {
                         }
                     ss = row_sum<LPR>(ss, lpr);
                     sh = row_sum<LPR>(sh, lpr);
-                    const float rr = inv_root(ss, inv_d, a.eps), m = rr * rr * (sh * inv_d);
+                    const float rr = inv_root(ss, inv_d, a.eps), m = rr * (sh * inv_d);
 #pragma unroll
                     for (int v = 0; v < NV; ++v)
 #pragma unroll
                         for (int j = 0; j < VEC; ++j) {
                             // (a row that is not there has x = y = 0, and eps may be 0)
-                            if (live && li + 64 * v < nvec) sum[v][j] = fmaf(y[v][j], x[v][j] * rr, sum[v][j]);
-                            y[v][j] = rr * (y[v][j] * wt[v][j] - x[v][j] * m);
+                            const float n = x[v][j] * rr;
+                            if (live && li + 64 * v < nvec) sum[v][j] = fmaf(y[v][j], n, sum[v][j]);
+                            y[v][j] = rr * (y[v][j] * wt[v][j] - n * m);
                         }
                 }
                 if (live) {

@@ -307,3 +307,24 @@ def test_values_keep_their_bits(d):
     ko, vo = torch.empty_like(k), torch.zeros(512, 1, 128, dtype=BF16, device="cuda")[:, :, :d]
     L.olive_qk_norm_rope(L.make_qk_desc(512, 0, 1, d), None, k, None, ko, v=v, v_out=vo)
     assert torch.equal(vo.contiguous().view(torch.int16), v.contiguous().view(torch.int16))
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64), (F32, 5)])
+def test_mean_squares_below_the_normal_numbers(dtype, d):
+    """Without eps, heads of 1e-20: mean squares of 1e-40 (18 bits are left of them), so each
+    element comes out as 1 and the gradients as those of 1 at the scale of 1e20."""
+    x = torch.full((3, 2, d), 1e-20, device="cuda").to(dtype)
+    x[:, :, ::2] *= -1
+    w = torch.ones(d, dtype=dtype, device="cuda")
+    g = torch.randn(3, 2, d, device="cuda").to(dtype)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    desc = L.make_qk_desc(3, 2, 0, d, weight_q=w, dtype=L.OLIVE_F32 if dtype == F32 else L.OLIVE_BF16, eps=0.0)
+    L.olive_qk_norm_rope(desc, x, None, y, None)
+    L.olive_qk_norm_rope_backward(desc, x, None, g, None, dx, None)
+    r = x.double().square().mean(-1, keepdim=True).rsqrt()
+    n = x.double() * r
+    unit = 2.0 ** -16 + (2.0 ** -8 if dtype == BF16 else 2.0 ** -20)
+    assert bool(((y.double() - n).abs() <= unit).all())
+    want = r * (g.double() - n * (g.double() * n).mean(-1, keepdim=True))
+    size = r * (g.double().abs() + (g.double() * n).abs().mean(-1, keepdim=True))
+    assert bool(((dx.double() - want).abs() <= unit * size).all())
