@@ -20,7 +20,9 @@
  * call on the same inputs gives the same bits.
  *
  * Sums, softmax statistics and norms are held in 32 bits or more whatever the dtype, and
- * an output is rounded to its dtype once. Workspaces are the caller's: a call leaves
+ * an output is rounded to its dtype once. With bf16 the attention's weights, and in its
+ * backward their gradients, are rounded to bf16 too, as operands of the next product.
+ * Workspaces are the caller's: a call leaves
  * nothing in them that a later call reads, and calls that may overlap need one each.
  */
 #ifndef OLIVE_LAYERS_H
@@ -81,7 +83,7 @@ typedef struct {
  * k / k_out when heads_k = 0. A token whose position is out of range gets NaN (its value is
  * copied as it is).
  * Errors: E_NULL, E_SHAPE, E_DTYPE, E_RANGE (size, layout, rot_dim, eps), E_UNSUPPORTED
- * (more than 256 elements or 4096 heads), E_HIP.
+ * (more than 256 elements or 4096 heads; a view that is not aligned to its type), E_HIP.
  */
 olive_status olive_qk_norm_rope(const olive_qk_desc *desc, const olive_heads *q,
                                 const olive_heads *k, const olive_heads *v,
@@ -99,7 +101,8 @@ olive_status olive_qk_norm_rope_workspace(const olive_qk_desc *desc, int64_t *by
  * grad_q and grad_k may be grad_q_out and grad_k_out themselves. grad_weight_q and
  * grad_weight_k: fp32 [head_dim] or NULL; NULL where the weight is. workspace: device,
  * 16-byte aligned, needed where a weight gradient is asked for.
- * Errors: as olive_qk_norm_rope, plus E_SHAPE for a workspace that is too small.
+ * Errors: as olive_qk_norm_rope, plus E_SHAPE for a workspace that is too small and
+ * E_UNSUPPORTED for one that is not aligned.
  */
 olive_status olive_qk_norm_rope_backward(const olive_qk_desc *desc, const olive_heads *q,
                                          const olive_heads *k, const olive_heads *grad_q_out,
@@ -168,7 +171,8 @@ olive_status olive_prefix_attention_workspace(const olive_attn_desc *desc, int32
  * views may be NULL when max_prefix = 0, the suffix views when max_suffix = 0. workspace:
  * device, 16-byte aligned, NULL if 0 bytes are needed.
  * Errors: E_NULL, E_SHAPE (sizes; a workspace that is too small), E_DTYPE, E_RANGE (size,
- * scale), E_UNSUPPORTED (head_dim > 256), E_HIP.
+ * scale), E_UNSUPPORTED (head_dim > 256; a view that is not aligned to its type, a workspace
+ * that is not aligned), E_HIP.
  */
 olive_status olive_prefix_attention(const olive_attn_desc *desc, const olive_heads *q,
                                     const olive_heads *k_prefix, const olive_heads *v_prefix,
@@ -212,9 +216,12 @@ typedef struct {
 
 /*
  * A list of count >= 0 gradients (host array, copied). The context holds the list and the
- * partial sums on the device; init synchronises the stream. It borrows the gradients.
- * Errors: E_NULL, E_SHAPE (a negative count or n), E_DTYPE, E_RANGE (in place with another
- * dtype_out), E_NOMEM, E_HIP.
+ * partial sums on the device; init synchronises the stream. It borrows the gradients: a
+ * program whose gradients stay where they are keeps the context (making one costs more than a
+ * call on small gradients).
+ * Errors: E_NULL, E_SHAPE (a negative count or n, more values than the chunks' count holds),
+ * E_DTYPE, E_RANGE (in place with another dtype_out), E_UNSUPPORTED (a gradient or output that
+ * is not aligned to its type), E_NOMEM, E_HIP.
  */
 olive_status olive_grad_clip_init(olive_clip_ctx **out, const olive_grad_tensor *list,
                                   int32_t count, void *hip_stream);

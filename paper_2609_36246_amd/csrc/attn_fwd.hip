@@ -18,12 +18,16 @@
 //           against its suffix
 // Parts of a row meet in a second kernel through fp32 partial outputs.
 //
+// The weights are rounded to bf16 as operands because fp32 products run at an eighth of the rate
+// (153 against 1200 TFLOP/s in large ones); their sum is formed of the unrounded ones. With it an
+// output is 0.0020 to 0.0024 (2-norm) from the exact one, with its own rounding alone 0.0017.
+//
 // Single tokens are bound by the reading of the keys and values (64 sequences on 4 prefixes of
-// 16000 to 32768 tokens, 32 / 8 heads of 128: 130 us with the join, 4.3 TB/s; 4 sequences on one of 4096, 16
-// heads: 13 us and 5 us for the join, chains of waits). Long runs are bound by the products and
-// the exponentials beside them (8 runs of 1024 tokens on 2 prefixes of 4096, 16 / 8 heads of 128:
-// 348 us, 890 TFLOP/s; prompts of 1200 to 6000 tokens with heads of 64, where a score has half
-// the products: 244 us, 790 TFLOP/s).
+// 16000 to 32768 tokens, 32 / 8 heads of 128: 125 us and 6 us for the join, 4.3 TB/s; 4 sequences on one of
+// 4096, 16 heads: 13 us and 5 us for the join, chains of waits). Long runs are bound by the
+// products and the exponentials beside them (8 runs of 1024 tokens on 2 prefixes of 4096, 16 / 8
+// heads of 128: 337 us, 920 TFLOP/s; prompts of 1200 to 6000 tokens with heads of 64, where a
+// score has half the products: 250 us, 770 TFLOP/s). Kernel times of a trace, clocks settled.
 #include "attn_tile.hpp"
 
 namespace olive {

@@ -9,7 +9,7 @@
 // operand to match.
 //
 // Bound by the waits for the operands: forward and backward of 3 runs of 30 to 90 tokens on a
-// prefix of 150, fp32, 4 / 2 heads of 64: 39 us (13 forward, 4 delta, 24 gradients).
+// prefix of 150, fp32, 4 / 2 heads of 64: 39 us (12 forward, 3 delta, 24 gradients).
 #include "attn_seq.hpp"
 #include "olive_device.hpp"
 

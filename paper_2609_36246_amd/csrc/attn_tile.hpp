@@ -172,7 +172,7 @@ struct DieOrder {
 // The row tiles of a sequence in chunks of a die's run, the last chunk of all sequences and heads
 // first: under a causal mask the last rows see the most keys, and what starts late is short.
 // (Sequence by sequence a fifth of the chip waited for the last ones: ragged prompts of 1200 to
-// 6000 tokens, 16 heads of 64, 269 us, in this order 244.)
+// 6000 tokens, 16 heads of 64, 269 us, in this order 244, both on one card.)
 constexpr int kRowChunk = 16;
 struct RowOrder {
     int tiles, chunks;

@@ -4,7 +4,7 @@
 // neither overflows nor vanishes there, and the sum's error stays below fp32's rounding), a
 // partial sum a workgroup; every workgroup of the second pass adds the partial sums in the
 // same order and scales its chunks. Bound by memory: the values are read twice and written
-// once. 1.45 GB in 41 tensors: 260 us for the norm (5.6 TB/s) and 545 us for the scaling (5.3).
+// once. 1.45 GB in 41 tensors: 258 us for the norm (5.6 TB/s) and 541 us for the scaling (5.4).
 #include "layers_internal.hpp"
 #include "olive_device.hpp"
 

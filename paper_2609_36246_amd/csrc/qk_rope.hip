@@ -6,8 +6,8 @@
 // it walks over heads: the angles and weights of its elements stay in registers.
 //
 // Bound by memory: 7 (backward 14) operations an element for 4 (6) bytes in bf16. 32768 tokens
-// of 40 heads of 128: 160 us, 4.2 TB/s (a large copy: 4.75); the backward of 24 heads 138 us,
-// 4.4 TB/s, of which 7 us the weight gradients' second pass; 8 tokens into a cache 5 us.
+// of 40 heads of 128: 160 us, 4.2 TB/s (a large copy: 4.75); the backward of 24 heads 139 us,
+// 4.4 TB/s, of which 6 us the weight gradients' second pass; 8 tokens into a cache 5 us.
 #include <type_traits>
 
 #include "layers_internal.hpp"
