@@ -128,8 +128,8 @@ olive_status olive_qk_norm_rope_backward(const olive_qk_desc *desc, const olive_
  * work is split; a sequence beyond them, or with rows outside the buffers, gets NaN (with
  * pages: at least the queries that see a token of such a page). One whose cu_q entries are
  * not in order within [0, total_q] is left out; others of a call with such entries, or with
- * group_seqs out of order, get NaN where their rows do not lie between the first and the last
- * entry of their group. Rows that two sequences or groups have get no defined value.
+ * group_seqs out of order, may get NaN where their rows do not lie between the first and the
+ * last entry of their group. Rows that two sequences or groups have get no defined value.
  * Rows of keys and values that no sequence has are never read into a result.
  */
 typedef struct {
