@@ -427,7 +427,8 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(BwdArgs f) {
     part_range(tiles_of<ROWS>(w.rows - r0), w.prefix ? f.np : f.ns, w.part, i0, i1);
     r0 += i0 * ROWS;
     // the first rows that see this lane's key, and this wavefront's last and first one
-    const int from = row_of(key), from_hi = row_of(w.j0 + 32 * wave + 31), from_lo = row_of(w.j0 + 32 * wave);
+    // (of the keys that are there: past them the difference may pass 32 bits)
+    const int from = row_of(key), from_hi = row_of(min(w.j0 + 32 * wave + 31, w.keys - 1)), from_lo = row_of(w.j0 + 32 * wave);
     L load;
     if (i0 < i1) {
         load.open(f, w, r0);
