@@ -1,11 +1,12 @@
-"""ctypes binding of libolive_score.so (the C ABI of include/olive_score.h and
-include/olive_layers.h).
+"""ctypes binding of libolive_score.so (the C ABI of include/olive_score.h,
+include/olive_layers.h and include/olive_tokens.h).
 
 Argument marshalling only: every function has the C name and forwards plain
 pointers, sizes and the HIP stream. Torch tensors are accepted wherever the C
 function takes a device pointer (their data_ptr() is passed); None maps to NULL.
-The layer operators' functions refuse tensors of another type or layout than the
-library would read (ValueError); the sizes of the heads' views are the caller's.
+The layer operators' and the token operators' functions refuse tensors of another type or
+layout than the library would read (ValueError); the sizes of the heads' views are the
+caller's, those of the token operators' matrices are checked.
 The library must have been built (python -m paper_2609_36246_amd.build); loading
 fails loudly otherwise -- there is no fallback path.
 """
@@ -49,6 +50,8 @@ OLIVE_TOPK = 16
 OLIVE_OUT_REGION_ONLY = 1
 OLIVE_ROPE_HALF = 0
 OLIVE_ROPE_PAIRS = 1
+OLIVE_NORM_RMS = 0
+OLIVE_NORM_LAYER = 1
 
 
 class olive_score_desc(ctypes.Structure):
@@ -126,6 +129,25 @@ class olive_grad_tensor(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("dtype_out", ctypes.c_int32)]
 
 
+class olive_embed_desc(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_int32), ("dtype", ctypes.c_int32), ("tokens", ctypes.c_int64),
+                ("vocab", ctypes.c_int64), ("width", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("ids", ctypes.c_void_p)]
+
+
+class olive_norm_desc(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("width", ctypes.c_int32), ("kind", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+
+
+class olive_sample_desc(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("vocab", ctypes.c_int64), ("uniform", ctypes.c_void_p),
+                ("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
+                ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p)]
+
+
 class OliveError(RuntimeError):
     def __init__(self, status: int, what: str):
         self.status = status
@@ -133,7 +155,7 @@ class OliveError(RuntimeError):
 
 
 _lib: Optional[ctypes.CDLL] = None
-_calls = {}              # the layer operators' entries with addresses for every pointer
+_calls = {}              # the layer and token operators' entries with addresses for every pointer
 
 
 def load() -> ctypes.CDLL:
@@ -189,8 +211,10 @@ def load() -> ctypes.CDLL:
     for name, args in (("olive_qk_norm_rope", "p" * 8), ("olive_qk_norm_rope_backward", "p" * 10 + "lp"),
                        ("olive_prefix_attention", "p" * 9 + "lp"),
                        ("olive_prefix_attention_backward", "p" * 15 + "lp"),
-                       ("olive_grad_clip", "pfpp")):
-        kinds = {"p": vp, "l": ctypes.c_int64, "f": ctypes.c_float}
+                       ("olive_grad_clip", "pfpp"), ("olive_embed", "pplplp"),
+                       ("olive_embed_backward", "pplpliiplp"), ("olive_row_norm", "p" + "pl" * 4 + "p"),
+                       ("olive_row_norm_backward", "p" + "pl" * 4 + "ppplp"), ("olive_sample", "pplpppplp")):
+        kinds = {"p": vp, "l": ctypes.c_int64, "f": ctypes.c_float, "i": ctypes.c_int32}
         _calls[name] = ctypes.CFUNCTYPE(st, *(kinds[a] for a in args))((name, lib))
     hp, qp = ctypes.POINTER(olive_heads), ctypes.POINTER(olive_qk_desc)
     ap, i64 = ctypes.POINTER(olive_attn_desc), ctypes.c_int64
@@ -214,6 +238,17 @@ def load() -> ctypes.CDLL:
     lib.olive_grad_clip.restype = st
     lib.olive_grad_clip_free.argtypes = [vp]
     lib.olive_grad_clip_free.restype = st
+    i32 = ctypes.c_int32
+    ep, np_, sp = (ctypes.POINTER(t) for t in (olive_embed_desc, olive_norm_desc, olive_sample_desc))
+    for name, args in (("olive_embed", [ep, vp, i64, vp, i64, vp]), ("olive_embed_workspace", [ep, ctypes.POINTER(i64)]),
+                       ("olive_embed_backward", [ep, vp, i64, vp, i64, i32, i32, vp, i64, vp]),
+                       ("olive_row_norm", [np_] + [vp, i64] * 4 + [vp]),
+                       ("olive_row_norm_workspace", [np_, ctypes.POINTER(i64)]),
+                       ("olive_row_norm_backward", [np_] + [vp, i64] * 4 + [f32p, f32p, vp, i64, vp]),
+                       ("olive_sample_workspace", [sp, ctypes.POINTER(i64)]),
+                       ("olive_sample", [sp, vp, i64, i32p, f32p, i32p, vp, i64, vp])):
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = st
     _lib = lib
     return lib
 
@@ -666,3 +701,138 @@ def olive_grad_clip(ctx, max_norm: float, norm=None, stream=None, check: bool = 
 
 def olive_grad_clip_free(ctx) -> int:
     return load().olive_grad_clip_free(ctx)
+
+
+def _rows(x, dtype, rows: int, width: int, what: str, output: bool = False):
+    """Address and row stride of a [rows, width] tensor of a torch type, contiguous within a row
+    (None: neither); an output's rows do not overlap."""
+    if x is None:
+        return None, 0
+    s, shape = x.stride(), x.shape
+    if x.dtype is not dtype or len(s) != 2 or shape[0] != rows or shape[1] != width or \
+            (s[1] != 1 and width > 1) or (output and s[0] < width and rows > 1):
+        raise ValueError("%s: expected [%d, %d] of %s with contiguous rows%s"
+                         % (what, rows, width, dtype, " apart from each other" if output else ""))
+    return x.data_ptr(), s[0]
+
+
+def _bytes_of(name, desc) -> int:
+    n = ctypes.c_int64(0)
+    _check(getattr(load(), name)(ctypes.byref(desc), ctypes.byref(n)), name)
+    return n.value
+
+
+def make_embed_desc(tokens, vocab, width, ids, dtype=OLIVE_BF16, scale=1.0) -> olive_embed_desc:
+    """ids: contiguous int32 [tokens]; negative ones are padding. The descriptor keeps it alive."""
+    d = olive_embed_desc()
+    d.size = ctypes.sizeof(olive_embed_desc)
+    d.dtype, d.tokens, d.vocab, d.width = int(dtype), int(tokens), int(vocab), int(width)
+    d.scale, d.ids = float(scale), _array(ids, "int32", d.tokens, "ids")
+    d.tensors = (ids,)
+    return d
+
+
+def olive_embed(desc: olive_embed_desc, table, out, stream=None, check: bool = True) -> int:
+    """out [tokens, width] gets scale * table[ids]; table [vocab, width]."""
+    dtype = _dtype(desc.dtype)
+    s = _call("olive_embed")(ctypes.addressof(desc), *_rows(table, dtype, desc.vocab, desc.width, "table"),
+                             *_rows(out, dtype, desc.tokens, desc.width, "out", True), _stream(stream))
+    if check:
+        _check(s, "olive_embed")
+    return s
+
+
+def olive_embed_workspace(desc: olive_embed_desc) -> int:
+    """Bytes of olive_embed_backward's workspace."""
+    return _bytes_of("olive_embed_workspace", desc)
+
+
+def olive_embed_backward(desc: olive_embed_desc, grad_out, grad_table, accumulate: bool = False, workspace=None,
+                         stream=None, check: bool = True) -> int:
+    """grad_table [vocab, width], bf16 or fp32: written whole, or with `accumulate` the sums are
+    added to the rows of the tokens that occur."""
+    if str(grad_table.dtype) not in ("torch.bfloat16", "torch.float32"):
+        raise ValueError("grad_table: expected bf16 or fp32")
+    kind = OLIVE_F32 if str(grad_table.dtype) == "torch.float32" else OLIVE_BF16
+    s = _call("olive_embed_backward")(
+        ctypes.addressof(desc), *_rows(grad_out, _dtype(desc.dtype), desc.tokens, desc.width, "grad_out"),
+        *_rows(grad_table, grad_table.dtype, desc.vocab, desc.width, "grad_table", True), kind, int(accumulate),
+        *_workspace(workspace), _stream(stream))
+    if check:
+        _check(s, "olive_embed_backward")
+    return s
+
+
+def make_norm_desc(rows, width, weight=None, bias=None, dtype=OLIVE_BF16, eps=1e-6,
+                   kind=OLIVE_NORM_RMS) -> olive_norm_desc:
+    """weight and bias: contiguous [width] of the rows' dtype. The descriptor keeps them alive."""
+    d = olive_norm_desc()
+    d.size = ctypes.sizeof(olive_norm_desc)
+    d.dtype, d.rows, d.width, d.kind, d.eps = int(dtype), int(rows), int(width), int(kind), float(eps)
+    d.weight = _array(weight, d.dtype, d.width, "weight")
+    d.bias = _array(bias, d.dtype, d.width, "bias")
+    d.tensors = (weight, bias)
+    return d
+
+
+def olive_row_norm(desc: olive_norm_desc, x, out, residual=None, sum_out=None, stream=None, check: bool = True) -> int:
+    """All [rows, width]: out gets the norm of x + residual, sum_out that sum."""
+    t, n, w = _dtype(desc.dtype), desc.rows, desc.width
+    s = _call("olive_row_norm")(ctypes.addressof(desc), *_rows(x, t, n, w, "x"), *_rows(residual, t, n, w, "residual"),
+                                *_rows(out, t, n, w, "out", True), *_rows(sum_out, t, n, w, "sum_out", True),
+                                _stream(stream))
+    if check:
+        _check(s, "olive_row_norm")
+    return s
+
+
+def olive_row_norm_workspace(desc: olive_norm_desc) -> int:
+    """Bytes of olive_row_norm_backward's workspace."""
+    return _bytes_of("olive_row_norm_workspace", desc)
+
+
+def olive_row_norm_backward(desc: olive_norm_desc, h, grad_out, grad_h, grad_sum=None, grad_weight=None,
+                            grad_bias=None, workspace=None, stream=None, check: bool = True) -> int:
+    """h: the rows that were normed (the forward's sum_out, or x without a residual)."""
+    t, n, w = _dtype(desc.dtype), desc.rows, desc.width
+    s = _call("olive_row_norm_backward")(
+        ctypes.addressof(desc), *_rows(h, t, n, w, "h"), *_rows(grad_out, t, n, w, "grad_out"),
+        *_rows(grad_sum, t, n, w, "grad_sum"), *_rows(grad_h, t, n, w, "grad_h", True),
+        _array(grad_weight, OLIVE_F32, w, "grad_weight"), _array(grad_bias, OLIVE_F32, w, "grad_bias"),
+        *_workspace(workspace), _stream(stream))
+    if check:
+        _check(s, "olive_row_norm_backward")
+    return s
+
+
+def make_sample_desc(rows, vocab, uniform, temperature=None, top_k=None, top_p=None, min_p=None,
+                     dtype=OLIVE_BF16) -> olive_sample_desc:
+    """uniform, temperature, top_p, min_p: contiguous fp32 [rows]; top_k int32 [rows]; None where a
+    setting is not used. The descriptor keeps them alive."""
+    d = olive_sample_desc()
+    d.size = ctypes.sizeof(olive_sample_desc)
+    d.dtype, d.rows, d.vocab = int(dtype), int(rows), int(vocab)
+    d.uniform = _array(uniform, OLIVE_F32, d.rows, "uniform")
+    d.temperature = _array(temperature, OLIVE_F32, d.rows, "temperature")
+    d.top_k = _array(top_k, "int32", d.rows, "top_k")
+    d.top_p, d.min_p = _array(top_p, OLIVE_F32, d.rows, "top_p"), _array(min_p, OLIVE_F32, d.rows, "min_p")
+    d.tensors = (uniform, temperature, top_k, top_p, min_p)
+    return d
+
+
+def olive_sample_workspace(desc: olive_sample_desc) -> int:
+    """Bytes of olive_sample's workspace."""
+    return _bytes_of("olive_sample_workspace", desc)
+
+
+def olive_sample(desc: olive_sample_desc, logits, token, logp=None, kept=None, workspace=None, stream=None,
+                 check: bool = True) -> int:
+    """logits [rows, vocab]; token, kept int32 [rows], logp fp32 [rows]."""
+    n = desc.rows
+    s = _call("olive_sample")(
+        ctypes.addressof(desc), *_rows(logits, _dtype(desc.dtype), n, desc.vocab, "logits"),
+        _array(token, "int32", n, "token"), _array(logp, OLIVE_F32, n, "logp"), _array(kept, "int32", n, "kept"),
+        *_workspace(workspace), _stream(stream))
+    if check:
+        _check(s, "olive_sample")
+    return s

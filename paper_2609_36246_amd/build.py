@@ -15,7 +15,7 @@ SOURCES = ["olive_abi.hip", "prep.hip", "score_simple.hip", "score_mfma.hip", "c
            "fixup.hip", "topk.hip", "gemm_mfma.hip", "backward.hip",
            "filter.hip", "argmax.hip", "score_wide.hip",
            "layers_abi.hip", "qk_rope.hip", "attn_generic.hip", "attn_fwd.hip", "attn_bwd.hip",
-           "grad_clip.hip"]
+           "grad_clip.hip", "tokens_abi.hip", "embed.hip", "row_norm.hip", "sample.hip"]
 ARCH = "gfx950"
 
 

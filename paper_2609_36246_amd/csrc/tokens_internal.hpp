@@ -1,0 +1,68 @@
+// Launchers of the token operators (include/olive_tokens.h) and their argument structs.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "layers_internal.hpp"
+#include "olive_tokens.h"
+
+namespace olive {
+
+struct RowsArg {                     // a [rows][width] matrix
+    char *p;
+    int64_t st;                      // elements between rows
+};
+
+// Whether every matrix that is there can be read `bytes` at a time from the start of each row.
+inline bool rows_aligned(std::initializer_list<RowsArg> all, int bytes, int esz) {
+    for (const RowsArg &m : all)
+        if (m.p && (((uintptr_t)m.p | (uint64_t)(m.st * esz)) % bytes) != 0) return false;
+    return true;
+}
+
+// ---- embedding -----------------------------------------------------------------------------
+struct EmbedArgs {
+    const int32_t *ids;
+    int32_t tokens, vocab, width;
+    float scale;
+    RowsArg table, out;              // backward: the table's gradient, and that of the rows
+    bool accumulate;
+    char *work;
+};
+
+int64_t embed_backward_bytes(const EmbedArgs &a);
+hipError_t launch_embed(const EmbedArgs &a, bool bf16, hipStream_t st);
+hipError_t launch_embed_backward(const EmbedArgs &a, bool bf16, bool table_bf16, hipStream_t st);
+
+// ---- row norms -----------------------------------------------------------------------------
+struct NormArgs {
+    RowsArg x, res, out, sum;        // backward: h, grad_sum, grad_h, grad_out
+    const void *weight, *bias;
+    float *gw, *gb;                  // backward: or NULL
+    float *part;                     // backward: [workgroups][2][width] partial sums
+    int32_t rows, width, layer;
+    float eps;
+};
+
+constexpr int kNormBlocks = 512;     // workgroups of the backward at most (its partial sums)
+
+hipError_t launch_norm(const NormArgs &a, bool bf16, hipStream_t st);
+hipError_t launch_norm_backward(const NormArgs &a, bool bf16, hipStream_t st);
+
+// ---- sampling ------------------------------------------------------------------------------
+struct SampleArgs {
+    RowsArg logits;
+    int32_t rows, vocab;
+    const float *uniform, *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    int32_t *token, *kept;
+    float *logp;
+    char *work;
+};
+
+int64_t sample_bytes(const SampleArgs &a, bool bf16);
+hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t st);
+
+}  // namespace olive

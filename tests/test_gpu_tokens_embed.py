@@ -1,0 +1,190 @@
+"""olive_embed and olive_embed_backward against their fp64 definitions.
+
+Bounds: an output is one product rounded to its dtype: half a step. A row of the table's
+gradient is a sum of n products in fp32 (n roundings of sums, at most u n times the sum of the
+absolute values, in any order), the product with the scale, the addition to what was there,
+and the rounding to its dtype.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import tokens_oracle as O
+from paper_2609_36246_amd import _lib as L
+from tests.tokens_harness import BF16, F32, U32, f64, graph_of, kind, matrix, unit
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def gpu():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    L.load()
+
+
+def tokens(n, vocab, how="mixed", seed=0):
+    r = np.random.RandomState(seed)
+    if how == "one":
+        ids = np.full(n, vocab // 2)
+    elif how == "uniform":
+        ids = r.randint(0, vocab, n)
+    elif how == "distinct":
+        ids = r.permutation(vocab)[:n]
+    else:
+        ids = np.minimum((np.exp(r.uniform(0, np.log(vocab + 1), n))).astype(np.int64) - 1, vocab - 1)
+        ids[r.uniform(size=n) < 0.1] = -1
+    return torch.tensor(ids, dtype=torch.int32).cuda()
+
+
+def forward(ids, table, scale=1.0, how="plain", stream=None):
+    out = matrix(len(ids), table.shape[1], table.dtype, how)
+    d = L.make_embed_desc(len(ids), len(table), table.shape[1], ids, dtype=kind(table.dtype), scale=scale)
+    L.olive_embed(d, table, out, stream=stream)
+    torch.cuda.synchronize()
+    return out
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,vocab,width,how,scale", [
+    (1, 1, 1, "plain", 1.0), (8, 1000, 2048, "plain", 1.0), (7, 50, 40, "plain", 2.5), (700, 333, 8, "plain", 1.0),
+    (65, 77, 1600, "part", 0.3), (33, 100, 515, "plain", -1.5), (129, 64, 136, "odd", 45.25),
+    (3, 5, 65536, "plain", 1.0), (5000, 4000, 64, "part", 8.0)])
+def test_forward(dtype, n, vocab, width, how, scale):
+    gen = torch.Generator().manual_seed(n + width)
+    table = matrix(vocab, width, dtype, how, gen)
+    ids = tokens(n, vocab, seed=n)
+    out = forward(ids, table, scale, how)
+    want = O.embed(ids.cpu().numpy(), f64(table), np.float32(scale).astype(np.float64))
+    assert np.all(np.abs(f64(out) - want) <= unit(dtype) * np.abs(want))
+    if scale == 1.0:
+        assert np.array_equal(f64(out), want)
+
+
+def test_tokens_that_are_not_there():
+    gen = torch.Generator().manual_seed(1)
+    table = matrix(10, 72, BF16, gen=gen)
+    ids = torch.tensor([3, -1, 10, -(1 << 31), (1 << 31) - 1, 9, 0], dtype=torch.int32).cuda()
+    out = f64(forward(ids, table))
+    np.testing.assert_array_equal(out, O.embed(ids.cpu().numpy(), f64(table), 1.0))
+    assert np.isnan(out[[2, 4]]).all() and not out[[1, 3]].any()
+
+
+def test_values_that_are_not_finite_keep_to_their_rows():
+    table = matrix(6, 64, F32, gen=torch.Generator().manual_seed(2))
+    table[2] = float("inf")
+    table[4] = float("nan")
+    ids = torch.tensor([0, 2, 4, 5, -1], dtype=torch.int32).cuda()
+    np.testing.assert_array_equal(f64(forward(ids, table)), O.embed(ids.cpu().numpy(), f64(table), 1.0))
+
+
+def backward(ids, grad, vocab, scale=1.0, into=None, gdtype=F32, how="plain", stream=None):
+    """`into`: the table's gradient that the sums are added to (None: a poisoned one, written whole)."""
+    table = matrix(vocab, grad.shape[1], gdtype, how) if into is None else into
+    d = L.make_embed_desc(len(ids), vocab, grad.shape[1], ids, dtype=kind(grad.dtype), scale=scale)
+    work = torch.full((L.olive_embed_workspace(d),), 0xff, dtype=torch.uint8, device="cuda")
+    L.olive_embed_backward(d, grad, table, accumulate=into is not None, workspace=work, stream=stream)
+    torch.cuda.synchronize()
+    return table
+
+
+def check(ids, grad, vocab, scale, got, before=None):
+    want, size, terms = O.embed_backward(ids.cpu().numpy(), f64(grad), vocab, float(np.float32(scale)), before)
+    bound = U32 * (terms[:, None] + 3) * size + unit(got.dtype) * np.abs(want) + 1e-37
+    bad = ~(np.abs(f64(got) - want) <= bound)
+    assert not bad.any(), "%d values off, first at %s" % (bad.sum(), np.argwhere(bad)[0])
+    if before is not None:                      # rows of tokens that do not occur keep their bits
+        assert np.array_equal(f64(got)[terms == 0], before[terms == 0])
+    else:
+        assert not f64(got)[terms == 0].any()
+
+
+BACKWARD = [(1, 1, 1, "mixed", "plain"), (2, 3, 2048, "one", "plain"), (64, 50, 24, "uniform", "plain"),
+            (65, 2000, 136, "distinct", "part"), (333, 40, 515, "mixed", "plain"), (1000, 7, 64, "mixed", "odd"),
+            (2048, 3000, 128, "mixed", "plain"), (2049, 3000, 96, "uniform", "part"), (4097, 20000, 72, "mixed", "plain"),
+            (9000, 100, 40, "one", "plain"), (20000, 151936, 8, "mixed", "plain"), (20000, 151936, 16, "distinct", "plain"),
+            (300, 10, 5000, "mixed", "plain"), (70000, 1 << 20, 4, "mixed", "plain"), (70001, 1000, 3, "uniform", "odd")]
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("dtype,gdtype", [(BF16, F32), (BF16, BF16), (F32, F32), (F32, BF16)])
+@pytest.mark.parametrize("n,vocab,width,ids,how", BACKWARD, ids=lambda v: str(v))
+def test_backward(n, vocab, width, ids, how, dtype, gdtype, accumulate):
+    gen = torch.Generator().manual_seed(n + width)
+    grad = matrix(n, width, dtype, how, gen, std=1e-2)
+    i = tokens(n, vocab, ids, seed=n)
+    into = matrix(vocab, width, gdtype, how, gen) if accumulate else None
+    before = f64(into) if accumulate else None
+    got = backward(i, grad, vocab, 1.75, into, gdtype, how)
+    check(i, grad, vocab, 1.75, got, before)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_tokens_out_of_range_have_no_gradient(accumulate):
+    gen = torch.Generator().manual_seed(3)
+    ids = torch.tensor([4, -1, 9, 10, 4, -(1 << 31), (1 << 31) - 1, 0, 4], dtype=torch.int32).cuda()
+    grad = matrix(9, 48, BF16, gen=gen)
+    grad[[1, 3, 5, 6]] = float("nan")
+    into = matrix(10, 48, F32, gen=gen) if accumulate else None
+    before = f64(into) if accumulate else None
+    check(ids, torch.where(torch.isnan(grad), 0.0, grad), 10, 1.0, backward(ids, grad, 10, into=into), before)
+    nothing = torch.full((500,), -1, dtype=torch.int32, device="cuda")
+    got = backward(nothing, matrix(500, 48, BF16), 10, into=None if not accumulate else matrix(10, 48, F32, fill=7.0))
+    assert bool((got == (7.0 if accumulate else 0.0)).all())
+
+
+def test_no_tokens():
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    assert forward(none, matrix(5, 8, F32, fill=1.0)).shape == (0, 8)
+    got = backward(none, matrix(0, 8, F32), 5)
+    assert not bool(got.any()) and bool((backward(none, matrix(0, 8, F32), 5, into=matrix(5, 8, F32, fill=3.0)) == 3.0).all())
+
+
+def test_a_gradient_row_that_is_read_again():
+    """grad_out as the same row for every token (stride 0), as the gradient of a sum is."""
+    ids = tokens(3000, 50, seed=9)
+    row = matrix(1, 64, F32, gen=torch.Generator().manual_seed(4))
+    check(ids, row.expand(3000, 64), 50, 1.0, backward(ids, row.expand(3000, 64), 50))
+
+
+def test_gradient_against_differences():
+    """The loss sum(out * g) moves by the gradient where one value of the table moves (it is linear:
+    the difference is exact but for roundings)."""
+    gen = torch.Generator().manual_seed(5)
+    table, ids = matrix(30, 16, F32, gen=gen), tokens(200, 30, seed=5)
+    g = matrix(200, 16, F32, gen=gen)
+    grad = f64(backward(ids, g, 30, 0.5))
+    for v, c in ((0, 0), (1, 7), (5, 15), (29, 3)):
+        other = table.clone()
+        other[v, c] += 1.0
+        step = float(other[v, c].double() - table[v, c].double())
+        diff = (f64(forward(ids, other, 0.5)) - f64(forward(ids, table, 0.5))) * f64(g)
+        terms = int((ids == v).sum())
+        # each output is rounded (2^-24 of values below 8), the gradient's sum too
+        assert abs(diff.sum() - step * grad[v, c]) <= 16 * U32 * (terms + 3) * np.abs(f64(g)[:, c]).sum() + 1e-12
+
+
+def test_same_bits_on_another_stream_and_in_a_graph():
+    gen = torch.Generator().manual_seed(6)
+    table = matrix(5000, 256, BF16, gen=gen)
+    grad, ids = matrix(6000, 256, BF16, gen=gen), tokens(6000, 5000, seed=6)
+    out, first = forward(ids, table, 2.0), backward(ids, grad, 5000)
+    s = torch.cuda.Stream()
+    assert torch.equal(out, forward(ids, table, 2.0, stream=s))
+    assert torch.equal(first, backward(ids, grad, 5000, stream=s))
+    d = L.make_embed_desc(6000, 5000, 256, ids, scale=2.0)
+    o, t = torch.empty_like(out), torch.empty_like(first)
+    work = torch.empty(L.olive_embed_workspace(d), dtype=torch.uint8, device="cuda")
+
+    def call():
+        L.olive_embed(d, table, o)
+        L.olive_embed_backward(d, grad, t, workspace=work)
+
+    g = graph_of(call)
+    for seed in (7, 8, 9):
+        ids.copy_(tokens(6000, 5000, "uniform" if seed == 8 else "mixed", seed))
+        grad.mul_(1.5)
+        o.fill_(float("nan"))
+        t.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, forward(ids, table, 2.0)) and torch.equal(t, backward(ids, grad, 5000, 2.0))

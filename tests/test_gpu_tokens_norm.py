@@ -1,0 +1,261 @@
+"""olive_row_norm and olive_row_norm_backward against their fp64 definitions.
+
+Bounds, u = 2^-24: the sum h is one rounding to the dtype and is checked for its bits. A sum
+over the width d in fp32 is off by at most u (log2(d) + 16) times the sum of the absolute values
+(lanes add 32 values in a row at most, then a tree), so mean and mean square are, and the
+inverse root by half of that and a unit of its own. y = n w + b: relative to |n w| + |b|, and for the
+layer norm the mean's error relative to the mean of |h|, which n's scale is 1/std of.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import tokens_oracle as O
+from paper_2609_36246_amd import _lib as L
+from tests.tokens_harness import BF16, F32, U32, f64, graph_of, kind, matrix, unit
+
+pytestmark = pytest.mark.gpu
+RMS, LAYER = L.OLIVE_NORM_RMS, L.OLIVE_NORM_LAYER
+EPS = 1e-6
+
+
+@pytest.fixture(scope="module", autouse=True)
+def gpu():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    L.load()
+
+
+def sums(width):
+    return U32 * (np.log2(width) + 36)
+
+
+class Norm:
+    def __init__(self, rows, width, dtype, k, how="plain", weight=True, bias=False, residual=False, seed=0, std=1.5,
+                 mean=0.3, eps=EPS):
+        gen = torch.Generator().manual_seed(seed + rows + width)
+        self.rows, self.width, self.dtype, self.k, self.how, self.eps = rows, width, dtype, k, how, eps
+        self.x = matrix(rows, width, dtype, how, gen, std, mean)
+        self.res = matrix(rows, width, dtype, how, gen, std) if residual else None
+        vec = lambda m, s: (torch.randn(width, generator=gen) * s + m).to(dtype).cuda()  # noqa: E731
+        self.w, self.b = vec(1.0, 0.3) if weight else None, vec(0.0, 0.5) if bias else None
+        self.dy = matrix(rows, width, dtype, how, gen, 1e-2)
+        self.dsum = matrix(rows, width, dtype, how, gen, 1e-2) if residual else None
+        self.desc = L.make_norm_desc(rows, width, self.w, self.b, kind(dtype), eps, k)
+
+    def forward(self, out=None, total=None, stream=None):
+        out = matrix(self.rows, self.width, self.dtype, self.how) if out is None else out
+        if total is None and self.res is not None:
+            total = matrix(self.rows, self.width, self.dtype, self.how)
+        L.olive_row_norm(self.desc, self.x, out, self.res, total, stream=stream)
+        torch.cuda.synchronize()
+        return out, total
+
+    def h(self):
+        return self.x if self.res is None else (self.x.float() + self.res.float()).to(self.dtype)
+
+    def check_forward(self):
+        out, total = self.forward()
+        if total is not None:
+            assert torch.equal(total, self.h())
+        h = f64(self.h())
+        w, b = (None if t is None else f64(t) for t in (self.w, self.b))
+        want = O.row_norm(h, w, b, self.eps, self.k == LAYER)
+        plain = np.abs(O.row_norm(h, w, None, self.eps, self.k == LAYER))
+        tol = (sums(self.width) + 6 * U32) * plain + 2 * U32 * np.abs(want)
+        if self.k == LAYER:
+            c = h - h.mean(1, keepdims=True)
+            std = np.sqrt((c * c).mean(1, keepdims=True) + self.eps)
+            tol = tol + sums(self.width) * np.abs(h).mean(1, keepdims=True) / std * (1.0 if w is None else np.abs(w)) * \
+                (1.0 + np.abs(c) / std)
+        bad = ~(np.abs(f64(out) - want) <= tol + unit(self.dtype) * np.abs(want) + 2.0 ** -133)
+        assert not bad.any(), "%d off, first at %s" % (bad.sum(), np.argwhere(bad)[0])
+
+    def backward(self, grad_h=None, weights=True, stream=None):
+        gh = matrix(self.rows, self.width, self.dtype, self.how) if grad_h is None else grad_h
+        gw, gb = (torch.full((self.width,), float("nan"), device="cuda") for _ in range(2)) if weights else (None, None)
+        work = torch.full((L.olive_row_norm_workspace(self.desc),), 0xff, dtype=torch.uint8, device="cuda")
+        L.olive_row_norm_backward(self.desc, self.h().contiguous() if self.res is not None else self.x, self.dy, gh,
+                                  self.dsum, gw, gb, work if weights else None, stream=stream)
+        torch.cuda.synchronize()
+        return gh, gw, gb
+
+    def check_backward(self):
+        gh, gw, gb = self.backward()
+        h, layer = f64(self.h()), self.k == LAYER
+        ds = None if self.dsum is None else f64(self.dsum)
+        w = None if self.w is None else f64(self.w)
+        want, size, ww, ws, bw, bs = O.row_norm_backward(h, w, self.eps, layer, f64(self.dy), ds)
+        rel = 3 * sums(self.width) + 12 * U32
+        if layer:           # the mean's error, relative to the standard deviation, is n's
+            c = h - h.mean(1, keepdims=True)
+            std = np.sqrt((c * c).mean(1, keepdims=True) + self.eps)
+            extra = sums(self.width) * (np.abs(h).mean(1, keepdims=True) / std + 1.0)
+            size = size * (1.0 + np.abs(c / std).max(1, keepdims=True))
+            rel = rel + 3 * extra
+            wrel = 2 * extra.max() * (1.0 + 1.0 / max(1e-9, np.abs(c / std).mean()))
+        else:
+            wrel = 0.0
+        tol = rel * size + unit(self.dtype) * np.abs(want) + 2.0 ** -133
+        bad = ~(np.abs(f64(gh) - want) <= tol)
+        assert not bad.any(), "%d off, first at %s" % (bad.sum(), np.argwhere(bad)[0])
+        # sums over the rows: at most so many roundings in a row as there are rows
+        n = U32 * (self.rows + 4)
+        scale = np.abs(f64(self.dy)).sum(0)
+        assert np.all(np.abs(f64(gw) - ww) <= (n + sums(self.width) + 6 * U32) * ws + wrel * scale + 1e-37)
+        assert np.all(np.abs(f64(gb) - bw) <= n * bs + 1e-37)
+
+
+SIZES = [(1, 1, "plain"), (3, 2, "plain"), (5, 7, "plain"), (9, 64, "plain"), (4, 257, "odd"), (70, 512, "part"),
+         (33, 1000, "plain"), (8, 1600, "part"), (17, 2048, "plain"), (6, 2049, "plain"), (130, 2056, "plain"),
+         (5, 3584, "plain"), (21, 4096, "part"), (3, 5120, "odd"), (4, 8192, "plain"), (2, 16384, "plain"), (3, 16383, "plain"),
+         (2, 12296, "plain"), (600, 72, "plain"), (2500, 24, "odd")]
+
+
+@pytest.mark.parametrize("k", [RMS, LAYER])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,width,how", SIZES)
+def test_forward(rows, width, how, dtype, k):
+    if k == LAYER and width == 1:
+        pytest.skip("a layer norm of one element is its bias")
+    Norm(rows, width, dtype, k, how, bias=True, residual=True).check_forward()
+    Norm(rows, width, dtype, k, how, weight=rows % 2 == 0, seed=1).check_forward()
+
+
+@pytest.mark.parametrize("k", [RMS, LAYER])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,width,how", SIZES)
+def test_backward(rows, width, how, dtype, k):
+    if k == LAYER and width <= 2:
+        pytest.skip("a layer norm of two elements is a sign: its gradient is a difference of equal numbers")
+    Norm(rows, width, dtype, k, how, bias=True, residual=True).check_backward()
+    Norm(rows, width, dtype, k, how, weight=rows % 2 == 0, seed=1).check_backward()
+
+
+@pytest.mark.parametrize("k", [RMS, LAYER])
+def test_many_rows(k):
+    Norm(9001, 256, BF16, k, bias=True).check_forward()
+    Norm(9001, 256, BF16, k, bias=True).check_backward()
+
+
+@pytest.mark.parametrize("width", [7, 512, 4096])
+def test_one_element_and_rows_of_zeros(width):
+    n = Norm(4, width, F32, LAYER, bias=True)
+    n.x[1] = 0.0
+    n.x[2] = 5.0
+    out = f64(n.forward()[0])
+    assert np.array_equal(out[1], f64(n.b)) and np.array_equal(out[2], f64(n.b))
+    n.check_backward()
+    z = Norm(3, width, BF16, RMS, eps=0.0)
+    z.x[0] = 0.0                                   # 0 / 0 with eps 0: NaN, in that row alone
+    out = f64(z.forward()[0])
+    assert np.isfinite(out[1:]).all()
+    one = Norm(2, 1, F32, LAYER, bias=True)
+    assert np.array_equal(f64(one.forward()[0]), np.repeat(f64(one.b)[None], 2, 0))
+
+
+@pytest.mark.parametrize("scale", [1e-17, 1e17])
+def test_small_and_large_values(scale):
+    Norm(5, 640, F32, RMS, std=scale, mean=0.0, eps=0.0).check_forward()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("width", [40, 2048, 6000])
+def test_values_that_are_not_finite_keep_to_their_rows(value, width):
+    for k in (RMS, LAYER):
+        n = Norm(6, width, BF16, k, bias=True)
+        clean = f64(n.forward()[0])
+        gclean = f64(n.backward()[0])
+        n.x[3, width // 2] = value
+        out, gh = f64(n.forward()[0]), f64(n.backward()[0])
+        keep = [0, 1, 2, 4, 5]
+        assert np.array_equal(out[keep], clean[keep]) and np.array_equal(gh[keep], gclean[keep])
+        assert np.isnan(out[3]).any()
+
+
+@pytest.mark.parametrize("width", [100, 1024, 5000])
+@pytest.mark.parametrize("k", [RMS, LAYER])
+def test_in_place(k, width):
+    n = Norm(37, width, BF16, k, bias=True, residual=True)
+    out, total = n.forward()
+    x, r = n.x.clone(), n.res.clone()
+    n.forward(out=n.x, total=n.res)
+    assert torch.equal(n.x, out) and torch.equal(n.res, total)
+    n.x, n.res = x.clone(), r.clone()
+    n.forward(out=n.res, total=n.x)
+    assert torch.equal(n.res, out) and torch.equal(n.x, total)
+    n.x, n.res = x.clone(), r.clone()
+    gh, _, _ = n.backward()
+    n2 = Norm(37, width, BF16, k, bias=True, residual=True)
+    assert torch.equal(n2.backward(grad_h=n2.dy)[0], gh)
+    n3 = Norm(37, width, BF16, k, bias=True, residual=True)
+    assert torch.equal(n3.backward(grad_h=n3.dsum)[0], gh)
+
+
+def test_rows_behind_the_last_are_left_as_they_were():
+    n = Norm(5, 256, BF16, RMS, residual=True)
+    out, total = (torch.full((9, 256), 3.0, dtype=BF16, device="cuda") for _ in range(2))
+    n.forward(out=out[:5], total=total[:5])
+    n.backward(grad_h=out[:5])
+    assert bool((out[5:] == 3.0).all()) and bool((total[5:] == 3.0).all())
+
+
+def test_no_rows():
+    n = Norm(0, 300, BF16, LAYER, bias=True)
+    n.forward()
+    _, gw, gb = n.backward()
+    assert not bool(gw.any()) and not bool(gb.any())
+
+
+def test_without_weight_gradients_and_with_one():
+    n = Norm(50, 384, F32, LAYER, weight=False)
+    gh, gw, gb = n.backward()
+    assert torch.equal(n.backward(weights=False)[0], gh)
+    other = torch.full((384,), float("nan"), device="cuda")
+    work = torch.empty(L.olive_row_norm_workspace(n.desc), dtype=torch.uint8, device="cuda")
+    L.olive_row_norm_backward(n.desc, n.x, n.dy, gh, grad_bias=other, workspace=work)
+    assert torch.equal(other, gb)
+    L.olive_row_norm_backward(n.desc, n.x, n.dy, gh, grad_weight=other, workspace=work)
+    assert torch.equal(other, gw)
+
+
+@pytest.mark.parametrize("k", [RMS, LAYER])
+def test_gradient_against_differences(k):
+    """sum(y g) in 64 bits around h: the error of a central difference with step s is of s^2."""
+    n = Norm(3, 24, F32, k, std=1.0)
+    gh, gw, _ = n.backward()
+    h, w, g = f64(n.x), f64(n.w), f64(n.dy)
+    loss = lambda a, b: float((O.row_norm(a, b, None, EPS, k == LAYER) * g).sum())  # noqa: E731
+    s = 1e-4
+    for r, c in ((0, 0), (1, 11), (2, 23)):
+        e = np.zeros_like(h)
+        e[r, c] = s
+        assert abs((loss(h + e, w) - loss(h - e, w)) / (2 * s) - f64(gh)[r, c]) <= 1e-6 * np.abs(g).max() * 10
+        v = np.zeros_like(w)
+        v[c] = s
+        assert abs((loss(h, w + v) - loss(h, w - v)) / (2 * s) - f64(gw)[c]) <= 1e-6 * np.abs(g).max() * 10
+
+
+@pytest.mark.parametrize("width", [2048, 4096, 77])
+def test_same_bits_on_another_stream_and_in_a_graph(width):
+    n = Norm(3000, width, BF16, LAYER, bias=True, residual=True)
+    (out, total), (gh, gw, gb) = n.forward(), n.backward()
+    s = torch.cuda.Stream()
+    out2, total2 = n.forward(stream=s)
+    again = n.backward(stream=s)
+    assert torch.equal(out, out2) and torch.equal(total, total2)
+    assert all(torch.equal(a, b) for a, b in zip((gh, gw, gb), again))
+    work = torch.empty(L.olive_row_norm_workspace(n.desc), dtype=torch.uint8, device="cuda")
+
+    def call():
+        L.olive_row_norm(n.desc, n.x, out2, n.res, total2)
+        L.olive_row_norm_backward(n.desc, total2, n.dy, again[0], n.dsum, again[1], again[2], work)
+
+    g = graph_of(call)
+    for _ in range(3):
+        n.x.mul_(1.25)
+        n.dy.mul_(0.5)
+        for t in (out2, total2) + again:
+            t.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((out2, total2) + again, n.forward() + n.backward()))
