@@ -13,18 +13,22 @@
 //    edge, so that the sum does not depend on its order. Inside the last bin the run's end is
 //    found digit by digit of (value, index).
 //
+// Code is kept short where a workgroup runs it once (loops over a lane's tokens are rolled): instructions come
+// from the L2 cache a line at a time, and with unrolled loops that was half of the time of a call
+// of few rows.
+//
 // Masses are 64-bit: a token changes where the error of the sums passes u times their total over a
 // border, and a row has as many borders as tokens.
 #include <type_traits>
 
 #include "rows.hpp"
 #include "tokens_internal.hpp"
+#include "wave_ops.hpp"
 
 namespace olive {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kCell = 512;                       // tokens that a wavefront looks at together, 8 a lane
 
 // ---------------------------------------------------------------------- bins of bf16 values
 // Magnitudes in [2^-40, 2^15) have a bin of their own each, in blocks of 128 (one power of two):
@@ -53,40 +57,94 @@ __device__ __forceinline__ float value_of(int bin) {
 }
 
 // ------------------------------------------------------------------------------------ parts
+// A part of a row: its counts, or of a row that keeps every token its mass alone.
 struct PartHead {
     uint64_t blocks[2];                          // blocks that hold counts
+    double mass;                                 // relative to the largest value
+    float top;
+    int32_t n;                                   // tokens that are not -inf
     int32_t flags;                               // bit 0: a bad value, bit 1: one without a bin
-    int32_t pad;
+    int32_t pad[7];
 };
-constexpr int64_t kPartBytes = kBins * 2 + 64;   // head, then 16-bit counts
-constexpr int kMostParts = 64, kMostPart = 65024;
+static_assert(sizeof(PartHead) == 64, "");
+constexpr int kPartThreads = 512;
+constexpr int kMostParts = 64, kMostPart = 65024;            // (16-bit counts)
+constexpr int kWhole = kPartThreads * 8 * 4;                 // tokens of a part whose mass is formed at once
 
-struct Parts { int32_t count, len; };
+struct Parts {
+    int32_t count, len;
+    int32_t bytes;                               // of a part in the workspace
+};
 
-Parts parts_of(int32_t rows, int32_t vocab) {
-    int64_t s = 1024 / rows, least = (vocab + kMostPart - 1) / kMostPart;
-    if (vocab <= 16384) s = 1;
-    if (s > (vocab + 4095) / 4096) s = (vocab + 4095) / 4096;
-    if (s > kMostParts) s = kMostParts;
+// Rows of up to 16384 tokens are counted by the workgroup that does the rest (one launch: 32 rows of
+// 16384 take 15 us, in two launches 19). Else about 512 workgroups count, each 4096 tokens at least.
+Parts parts_of(const SampleArgs &a) {
+    // (every row keeps every token, or the first alone)
+    const bool plain = !a.top_k && !a.top_p && !a.min_p && a.vocab <= kMostParts * kWhole;
+    int64_t s = (plain ? 1024 : 512) / a.rows, least = (a.vocab + kMostPart - 1) / kMostPart;
+    if (plain) least = (a.vocab + kWhole - 1) / kWhole;
+    const int64_t most = plain ? (a.vocab + 2047) / 2048 : (a.vocab + 4095) / 4096;
+    if (a.vocab <= 16384) s = least = 1;
+    if (s > most) s = most;
+    if (s > (plain ? kMostParts : 16)) s = plain ? kMostParts : 16;
     if (s < least) s = least;
-    const int64_t len = ((vocab + s - 1) / s + kCell - 1) / kCell * kCell;
-    return Parts{(int32_t)((vocab + len - 1) / len), (int32_t)len};
+    const int64_t len = ((a.vocab + s - 1) / s + 511) / 512 * 512;
+    return Parts{(int32_t)((a.vocab + len - 1) / len), (int32_t)len, plain ? 64 : kBins * 2 + 64};
 }
 
-// 8 values from i on (none past `end`), at any alignment of their type
-template <typename T>
-struct __attribute__((packed, aligned(sizeof(T)))) Eight { T v[8]; };
+// A lane's tokens: 16 bytes from i on, at any alignment of their type; -inf past `end`.
+struct Lot { uint32_t w[4]; };
+template <typename T> constexpr int kLot = 16 / (int)sizeof(T);
+template <typename T> constexpr int kCell = 64 * kLot<T>;    // tokens of a wavefront's lots
 
 template <typename T>
-__device__ __forceinline__ Eight<T> load_eight(const T *z, int i, int end) {
-    if (i + 8 <= end) return *(const Eight<T> *)(z + i);
-    Eight<T> x;
+__device__ __forceinline__ Lot load_lot(const T *z, int i, int end) {
+    struct __attribute__((packed, aligned(sizeof(T)))) Loose { uint32_t w[4]; };
+    constexpr int kBits = 8 * (int)sizeof(T);
+    constexpr uint32_t kFill = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+    Lot x{{kFill, kFill, kFill, kFill}};
+    if (i >= end) return x;
+    const auto drop = [&](uint32_t in) {         // the first token goes, `in` comes last
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        if constexpr (sizeof(T) == 2) x.v[j] = i + j < end ? z[i + j] : (T)0xff80u;
-        else x.v[j] = i + j < end ? z[i + j] : kNegInf;
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t above = j < 3 ? x.w[j + 1] : in;
+            x.w[j] = kBits == 32 ? above : x.w[j] >> 16 | above << 16;
+        }
+    };
+    const int from = min(i, end - kLot<T>);      // (at a row's end the 16 bytes before it, shifted)
+    if (from >= 0) {
+        const Loose y = *(const Loose *)(z + from);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x.w[j] = y.w[j];
+#pragma unroll 1
+        for (int j = from; j < i; ++j) drop(kFill);
+    } else {
+#pragma unroll 1
+        for (int j = i; j < i + kLot<T>; ++j) {
+            uint32_t v = kFill;
+            if (j < end) memcpy(&v, z + j, sizeof(T));
+            drop(v);
+        }
     }
     return x;
+}
+// fn(j, bits) for each token j of a lot.
+template <typename T, typename F>
+__device__ __forceinline__ void each_token(Lot x, F fn) {
+#pragma unroll 1
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (sizeof(T) == 2) {
+            fn(2 * k, x.w[0] & 0xffffu);
+            fn(2 * k + 1, x.w[0] >> 16);
+        } else {
+            fn(k, x.w[0]);
+        }
+        x.w[0] = x.w[1], x.w[1] = x.w[2], x.w[2] = x.w[3];
+    }
+}
+template <typename T>
+__device__ __forceinline__ float token_value(uint32_t bits) {
+    return sizeof(T) == 2 ? bf16_bits_to_f32(bits) : __uint_as_float(bits);
 }
 
 // Counts of [begin, end) of a row into 16-bit bins (two to a word); the flags of its odd values.
@@ -94,10 +152,10 @@ template <int THREADS>
 __device__ __forceinline__ int count_bins(const uint16_t *z, int begin, int end, uint32_t *hist) {
     int flags = 0;
     for (int i = begin + (int)threadIdx.x * 8; i < end; i += THREADS * 8) {
-        const Eight<uint16_t> x = load_eight(z, i, end);
+        const Lot x = load_lot(z, i, end);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int b = bin_of(x.v[j]);
+            const int b = bin_of(j & 1 ? x.w[j >> 1] >> 16 : x.w[j >> 1] & 0xffffu);
             if (b >= 0) atomicAdd(hist + (b >> 1), 1u << ((b & 1) * 16));
             else flags |= b == kBad ? 1 : b == kOdd ? 2 : 0;
         }
@@ -105,69 +163,10 @@ __device__ __forceinline__ int count_bins(const uint16_t *z, int begin, int end,
     return flags;
 }
 
-constexpr int kPartThreads = 512;
-
-__global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(SampleArgs a, Parts p) {
-    __shared__ uint32_t hist[kBins / 2];
-    __shared__ uint32_t used[4], flags;
-    const int64_t row = blockIdx.x;
-    const int part = blockIdx.y;
-    for (int i = threadIdx.x; i < kBins / 2; i += kPartThreads) hist[i] = 0;
-    if (threadIdx.x < 4) used[threadIdx.x] = 0;
-    if (threadIdx.x == 4) flags = 0;
-    __syncthreads();
-    const int begin = part * p.len, end = min(a.vocab, begin + p.len);
-    const int f = count_bins<kPartThreads>((const uint16_t *)a.logits.p + row * a.logits.st, begin, end, hist);
-    if (f) atomicOr(&flags, (uint32_t)f);
-    __syncthreads();
-    char *to = a.work + (row * p.count + part) * kPartBytes;
-    const int lane = threadIdx.x & 63;
-    for (int b = threadIdx.x >> 6; b < kBlocks; b += kPartThreads / 64) {
-        const uint32_t c = hist[b * 64 + lane];
-        if (!__ballot(c != 0)) continue;
-        ((uint32_t *)(to + 64))[b * 64 + lane] = c;
-        if (lane == 0) atomicOr(used + (b >> 5), 1u << (b & 31));
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        PartHead *h = (PartHead *)to;
-        h->blocks[0] = used[0] | (uint64_t)used[1] << 32;
-        h->blocks[1] = used[2] | (uint64_t)used[3] << 32;
-        h->flags = (int32_t)flags;
-    }
-}
-
-// ------------------------------------------------------------------------- block-wide steps
-// The sums over the threads before this one, and over all, of a count and a mass.
-__device__ __forceinline__ void block_scan(int c, double m, int &cb, double &mb, int &call, double &mall) {
-    __shared__ int jc[kWaves];
-    __shared__ double jm[kWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int cs = c;
-    double ms = m;
-    for (int o = 1; o < 64; o <<= 1) {
-        const int u = __shfl_up(cs, o);
-        const double v = __shfl_up(ms, o);
-        if (lane >= o) cs += u, ms += v;
-    }
-    __syncthreads();
-    if (lane == 63) jc[wave] = cs, jm[wave] = ms;
-    __syncthreads();
-    cb = cs - c, call = 0;
-    double before = 0.0;
-    mall = 0.0;
-    for (int i = 0; i < kWaves; ++i) {
-        if (i < wave) cb += jc[i], before += jm[i];
-        call += jc[i], mall += jm[i];
-    }
-    mb = before + __shfl_up(ms, 1);
-    if (lane == 0) mb = before;
-}
-
 struct Settings {
     float u, temp, p, mp;
     int k;
-    bool ok;
+    bool ok, greedy;                             // greedy: the first token alone
 };
 
 __device__ __forceinline__ Settings settings_of(const SampleArgs &a, int row) {
@@ -178,9 +177,116 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs &a, int row) {
     s.mp = a.min_p ? a.min_p[row] : 0.f;
     s.k = a.top_k ? a.top_k[row] : 0;
     s.ok = s.u >= 0.f && s.u <= 1.f && s.temp >= 0.f && s.temp < __builtin_inff() && s.p == s.p && s.mp == s.mp;
-    if (s.temp == 0.f || s.mp > 1.f) s.k = 1, s.p = 1.f, s.mp = 0.f;   // the first token alone
+    s.greedy = s.temp == 0.f || s.mp > 1.f || s.k == 1;
+    if (s.greedy) s.k = 1, s.p = 1.f, s.mp = 0.f;
     if (s.temp == 0.f) s.temp = 1.f;
     return s;
+}
+
+// Of calls without cuts: a part's largest value, and its mass relative to that.
+__global__ __launch_bounds__(kPartThreads) void sample_masses_kernel(SampleArgs a, Parts p) {
+    constexpr int kPartWaves = kPartThreads / 64;
+    const int64_t row = blockIdx.x;
+    const int part = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int begin = part * p.len, end = min(a.vocab, begin + p.len);
+    const uint16_t *z = (const uint16_t *)a.logits.p + row * a.logits.st;
+    PartHead *head = (PartHead *)(a.work + (row * p.count + part) * p.bytes);
+    const Settings s = settings_of(a, row);
+    if (!s.ok) return;
+    __shared__ Lot lots[kWhole / 8];             // (a thread's own)
+    const int mine = (end - begin + kPartThreads * 8 - 1) / (kPartThreads * 8);
+#pragma unroll
+    for (int i = 0; i < kWhole / 8 / kPartThreads; ++i)
+        if (i < mine) lots[i * kPartThreads + tid] = load_lot(z, begin + (tid + i * kPartThreads) * 8, end);
+    uint32_t top = 0, bad = 0;
+    int n = 0;
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i)
+        each_token<uint16_t>(lots[i * kPartThreads + tid], [&](int, uint32_t bits) {
+            const float v = bf16_bits_to_f32(bits);
+            bad |= !(v < __builtin_inff());
+            n += v > kNegInf;
+            top = max(top, f2ord(v));
+        });
+    __shared__ uint32_t tops[kPartWaves], bads[kPartWaves];
+    __shared__ int ns[kPartWaves];
+    __shared__ double masses[kPartWaves];
+    top = wave_max(top);
+    n = wave_sum(n);
+    if (lane == 0) tops[wave] = top, ns[wave] = n, bads[wave] = 0;
+    if (__ballot(bad) && lane == 0) bads[wave] = 1;
+    __syncthreads();
+    for (int i = 0; i < kPartWaves; ++i) top = max(top, tops[i]);
+    const double first = (double)ord2f(top), t = (double)s.temp;
+    double mass = 0.0;
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i)
+        each_token<uint16_t>(lots[i * kPartThreads + tid], [&](int, uint32_t bits) {
+            const float v = bf16_bits_to_f32(bits);
+            mass += v > kNegInf ? exp(((double)v - first) / t) : 0.0;
+        });
+    mass = wave_sum(mass);
+    if (lane == 0) masses[wave] = mass;
+    __syncthreads();
+    if (tid == 0) {
+        PartHead h{};
+        h.top = (float)first;
+        for (int i = 0; i < kPartWaves; ++i) h.mass += masses[i], h.n += ns[i], h.flags |= (int)bads[i];
+        *head = h;
+    }
+}
+
+// Of the others: the counts of a part's bins, and which blocks of them hold any.
+__global__ __launch_bounds__(kPartThreads) void sample_counts_kernel(SampleArgs a, Parts p) {
+    __shared__ uint32_t hist[kBins / 2];
+    __shared__ uint32_t used[4], flags;
+    constexpr int kPartWaves = kPartThreads / 64;
+    const int64_t row = blockIdx.x;
+    const int part = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int begin = part * p.len, end = min(a.vocab, begin + p.len);
+    const uint16_t *z = (const uint16_t *)a.logits.p + row * a.logits.st;
+    char *to = a.work + (row * p.count + part) * p.bytes;
+    PartHead *head = (PartHead *)to;
+    for (int i = tid; i < kBins / 8; i += kPartThreads) ((uint4 *)hist)[i] = make_uint4(0, 0, 0, 0);
+    if (tid < 4) used[tid] = 0;
+    if (tid == 4) flags = 0;
+    __syncthreads();
+    const int f = count_bins<kPartThreads>(z, begin, end, hist);
+    if (f) atomicOr(&flags, (uint32_t)f);
+    __syncthreads();
+    for (int b = wave; b < kBlocks; b += kPartWaves) {
+        const uint32_t c = hist[b * 64 + lane];
+        if (!__ballot(c != 0)) continue;
+        ((uint32_t *)(to + 64))[b * 64 + lane] = c;
+        if (lane == 0) atomicOr(used + (b >> 5), 1u << (b & 31));
+    }
+    __syncthreads();
+    if (tid == 0) {
+        head->blocks[0] = used[0] | (uint64_t)used[1] << 32;
+        head->blocks[1] = used[2] | (uint64_t)used[3] << 32;
+        head->flags = (int32_t)flags;
+    }
+}
+
+// ------------------------------------------------------------------------- block-wide steps
+// The sums over the threads before this one, and over all, of a count and a mass.
+__device__ __forceinline__ void block_scan(int c, double m, int &cb, double &mb, int &call, double &mall) {
+    __shared__ int jc[kWaves];
+    __shared__ double jm[kWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int cs = wave_scan(c);
+    const double ms = wave_scan(m);
+    __syncthreads();
+    if (lane == 63) jc[wave] = cs, jm[wave] = ms;
+    __syncthreads();
+    cb = cs - c, call = 0;
+    double before = 0.0;
+    mall = 0.0;
+    for (int i = 0; i < kWaves; ++i) {
+        if (i < wave) cb += jc[i], before += jm[i];
+        call += jc[i], mall += jm[i];
+    }
+    mb = before + wave_before(ms);
 }
 
 __device__ __forceinline__ void no_answer(const SampleArgs &a, int row) {
@@ -191,8 +297,8 @@ __device__ __forceinline__ void no_answer(const SampleArgs &a, int row) {
 }
 
 // Where the token lies: ranges of [begin, end) by their kept masses, at most 128 at a time, then
-// the 512 tokens of one. `src(i, end, f)` calls f(j, kept, tie, weight) for the 8 tokens of a lane
-// from i on; of the ties the first `ties` in order are kept.
+// the lots of one. `item(i, bits, fn)` calls fn(kept, tie, weight) for a token; of the ties the
+// first `ties` in order are kept, with `tie_weight`.
 struct Range { double mass; int kept, ties; };
 constexpr int kRanges = 128;
 
@@ -215,12 +321,7 @@ __device__ __forceinline__ int pick_range(const Range *r, int n, double w, Drawn
         x[i] = 2 * lane + i < n ? r[2 * lane + i] : Range{0.0, 0, 0};
         t += x[i].ties;
     }
-    int before = t;
-    for (int o = 1; o < 64; o <<= 1) {
-        const int u = __shfl_up(before, o);
-        if (lane >= o) before += u;
-    }
-    before -= t;
+    int before = wave_scan(t) - t;
     double own = 0.0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -230,13 +331,7 @@ __device__ __forceinline__ int pick_range(const Range *r, int n, double w, Drawn
         mass[i] = x[i].mass + ties[i] * w;
         own += mass[i];
     }
-    double run = own;
-    for (int o = 1; o < 64; o <<= 1) {
-        const double u = __shfl_up(run, o);
-        if (lane >= o) run += u;
-    }
-    double at = __shfl_up(run, 1);
-    if (lane == 0) at = 0.0;
+    double at = wave_before(wave_scan(own));
     int found = 1 << 30, last = -1;
     double left = 0.0, left_last = 0.0;
 #pragma unroll
@@ -260,77 +355,96 @@ __device__ __forceinline__ int pick_range(const Range *r, int n, double w, Drawn
         found = last;
         left = left_last;
     }
-    found = __shfl(found, src);
-    d.want = __shfl(left, src);
-    d.ties = __shfl(found & 1 ? ties[1] : ties[0], src);
+    found = wave_read(found, src);
+    d.want = wave_read(left, src);
+    d.ties = wave_read(found & 1 ? ties[1] : ties[0], src);
     return found;
 }
 
-template <typename Src>
-__device__ __forceinline__ int locate(const Src &src, int begin, int end, double tie_weight, Drawn d, Range *ranges) {
+template <typename T, typename Item>
+__device__ __forceinline__ int locate(const T *z, const Item &item, int begin, int end, double tie_weight, Drawn d,
+                                      Range *ranges) {
+    constexpr int kC = kCell<T>, kL = kLot<T>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    while (end - begin > kCell) {
-        const int step = max(kCell, ((end - begin + kRanges - 1) / kRanges + kCell - 1) / kCell * kCell);
-        const int n = (end - begin + step - 1) / step;
+#pragma unroll 1
+    while (end - begin > kC) {
+        const int step = max(kC, ((end - begin + kRanges - 1) / kRanges + kC - 1) / kC * kC);
+        const int n = (end - begin + step - 1) / step, cells = step / kC;
         __syncthreads();                         // (the ranges before are read)
-        for (int r = wave; r < n; r += kWaves) {
-            Range x{0.0, 0, 0};
-            const int e = min(end, begin + (r + 1) * step);
-            for (int i = begin + r * step; i < e; i += kCell)
-                src(i + lane * 8, e, [&](int, bool kept, bool tie, double w) {
-                    x.mass += kept ? w : 0.0;
+        // this wavefront's cells, those of the ranges wave, wave + 16, ..: three are on their way
+        Lot ahead[3];
+        int at = begin + wave * step, left = cells, r = wave;
+        int next = at, next_left = cells;
+        const auto load_next = [&]() {
+            const Lot x = load_lot(z, next + lane * kL, end);
+            next += kC;
+            if (--next_left == 0) next += (kWaves - 1) * step, next_left = cells;
+            next = min(next, end);
+            return x;
+        };
+#pragma unroll
+        for (int j = 0; j < 3; ++j) ahead[j] = load_next();
+        Range x{0.0, 0, 0};
+#pragma unroll 1
+        while (r < n) {
+            const Lot y = ahead[0];
+            ahead[0] = ahead[1], ahead[1] = ahead[2];
+            ahead[2] = load_next();
+            each_token<T>(y, [&](int j, uint32_t bits) {
+                item(at + lane * kL + j, bits, [&](bool kept, bool tie, double w) {
+                    x.mass += w;
                     x.kept += kept;
                     x.ties += tie;
                 });
-            for (int o = 32; o > 0; o >>= 1) {
-                x.mass += __shfl_xor(x.mass, o);
-                x.kept += __shfl_xor(x.kept, o);
-                x.ties += __shfl_xor(x.ties, o);
-            }
+            });
+            at += kC;
+            if (--left > 0) continue;
+            x.mass = wave_sum(x.mass);
+            x.kept = wave_sum(x.kept);
+            x.ties = wave_sum(x.ties);
             if (lane == 0) ranges[r] = x;
+            x = Range{0.0, 0, 0};
+            r += kWaves, at += (kWaves - 1) * step, left = cells;
         }
         __syncthreads();
-        const int r = max(0, pick_range(ranges, n, tie_weight, d));
+        r = max(0, pick_range(ranges, n, tie_weight, d));
         begin += r * step;
         end = min(end, begin + step);
     }
-    // 8 tokens a lane, every wavefront for itself
-    Range own{0.0, 0, 0};
-    src(begin + lane * 8, end, [&](int, bool kept, bool tie, double w) {
-        own.mass += kept ? w : 0.0;
-        own.ties += tie;
-    });
-    int before = own.ties;
-    for (int o = 1; o < 64; o <<= 1) {
-        const int u = __shfl_up(before, o);
-        if (lane >= o) before += u;
+    // a lot a lane, every wavefront for itself: its mass, then its tokens one by one
+    const Lot y = load_lot(z, begin + lane * kL, end);
+    int before = 0, found = -1, last = -1;
+    double at = 0.0;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        each_token<T>(y, [&](int j, uint32_t bits) {
+            const int i = begin + lane * kL + j;
+            item(i, bits, [&](bool kept, bool tie, double w) {
+                const bool keep = i < end && (kept || (tie && before < d.ties));
+                before += tie;
+                if (!keep) return;
+                at += tie ? tie_weight : w;
+                last = i;
+                if (found < 0 && (d.u == 0.f || (d.u < 1.f && at > d.want))) found = i;
+            });
+        });
+        if (pass) break;
+        // (of the lane's ties in the first pass as many were added as it has before the limit)
+        const int ties = before, first = wave_scan(ties) - ties;
+        at += (min(max(d.ties - first, 0), ties) - min(ties, d.ties)) * tie_weight;
+        at = wave_before(wave_scan(at));
+        before = first;
+        found = last = -1;
     }
-    before -= own.ties;
-    own.mass += min(max(d.ties - before, 0), own.ties) * tie_weight;
-    double at = own.mass;
-    for (int o = 1; o < 64; o <<= 1) {
-        const double u = __shfl_up(at, o);
-        if (lane >= o) at += u;
-    }
-    at = __shfl_up(at, 1);
-    if (lane == 0) at = 0.0;
-    int found = -1, last = -1;
-    src(begin + lane * 8, end, [&](int j, bool kept, bool tie, double w) {
-        const bool keep = kept || (tie && before < d.ties);
-        before += tie;
-        if (!keep) return;
-        at += tie ? tie_weight : w;
-        last = begin + lane * 8 + j;
-        if (found < 0 && (d.u == 0.f || (d.u < 1.f && at > d.want))) found = last;
-    });
     uint64_t hit = __ballot(found >= 0);
-    if (hit) return __shfl(found, __builtin_ctzll(hit));
+    if (hit) return wave_read(found, __builtin_ctzll(hit));
     hit = __ballot(last >= 0);
-    return __shfl(last, hit ? 63 - __builtin_clzll(hit) : 0);
+    return wave_read(last, hit ? 63 - __builtin_clzll(hit) : 0);
 }
 
 // ------------------------------------------------------------------------------ fine bins
 constexpr int kFineBins = 2048, kFineList = 4096;
+constexpr int kFew = 256, kFewList = 1024;       // top_k of which the kept tokens are put in order
 
 __device__ __forceinline__ double exp_small(double x) {      // e^-x for 0 <= x <= 1/32, to 2^-53
     double r = -1.0 / 5040;
@@ -347,14 +461,13 @@ struct FinePool {
     uint32_t count[kFineBins];
     uint64_t mass[kFineBins];                    // in fixed point, relative to the bin's edge
     double edge[kFineBins];                      // e^(-b / 32)
-    uint32_t key[kFineList], index[kFineList];
+    uint32_t key[kFineList], index[kFineList];   // (of few tokens: their places in order, and weights)
     uint32_t dcount[256];
     uint64_t dmass[256];
     Range ranges[kRanges];
     uint32_t top, n, bad, listed, least;
-    int bin, bin_p;
+    int bin, above, first, last;
     double before;                               // mass above a bin
-    int above;                                   // tokens above it
 };
 
 // An end of the run: tokens of the bins before `bin`, and those of it at or above `comp`.
@@ -365,22 +478,80 @@ struct Edge {
     double mass;
 };
 
+__device__ __forceinline__ double b_mass(const FinePool &f, int b, double back) { return (double)f.mass[b] * back * f.edge[b]; }
+__device__ __forceinline__ uint64_t comp_of(uint32_t key, int i) {
+    return (uint64_t)key << 24 | (0xffffff - (uint32_t)i);
+}
+
+// The run's end among `n` tokens at least `k` of which are known to be the first of the row: they are put
+// in order by counting for each the ones before it, k <= 256 are kept.
+template <typename T, typename Scaled>
+__device__ __forceinline__ void sample_few(const SampleArgs &a, int row, const Settings &s, FinePool &f, int n,
+                                           const Scaled &scaled) {
+    const int tid = threadIdx.x, k = s.k;
+    uint64_t *comp = f.mass, *sorted = f.mass + kFewList;
+    double *weight = f.edge;
+    static_assert(2 * kFewList <= kFineBins, "");
+    if (tid < n) comp[tid] = comp_of(f.key[tid], (int)f.index[tid]);
+    if (tid == 0) f.first = 0x7fffffff, f.last = -1;
+    __syncthreads();
+    if (tid < n) {
+        const uint64_t own = comp[tid];
+        int rank = 0;
+#pragma unroll 8
+        for (int i = 0; i < n; ++i) rank += comp[i] > own;
+        sorted[rank] = own;
+    }
+    __syncthreads();
+    const uint64_t own = tid < k ? sorted[tid] : 0;
+    const int index = 0xffffff - (int)(own & 0xffffff);
+    const double w = tid < k ? exp(-scaled(ord2f((uint32_t)(own >> 24)))) : 0.0;
+    if (tid < k) weight[tid] = w;
+    int cb, call;
+    double mb, all;
+    block_scan(0, w, cb, mb, call, all);
+    // (the run's tokens are counted: what lies above either limit is the first part of the order)
+    const bool in_p = tid < k && (tid == 0 || !(s.p < 1.f) || mb < (double)s.p * all);
+    const bool in_m = tid < k && (tid == 0 || !(s.mp > 0.f) || w >= (double)s.mp);
+    const bool in = in_p && in_m;
+    double total;
+    int kept;
+    block_scan(in, in ? w : 0.0, cb, mb, kept, total);
+    const double want = (double)s.u * total;
+    if (in) {
+        double at = 0.0;
+#pragma unroll 4
+        for (int i = 0; i < kept; ++i) at += 0xffffff - (int)(sorted[i] & 0xffffff) <= index ? weight[i] : 0.0;
+        atomicMax(&f.last, index);
+        if (s.u == 0.f || (s.u < 1.f && at > want)) atomicMin(&f.first, index);
+    }
+    __syncthreads();
+    if (tid == 0) {
+        const int token = f.first == 0x7fffffff ? f.last : f.first;
+        a.token[row] = token;
+        const float v = RowElem<T>::get(((const T *)a.logits.p + row * a.logits.st)[token]);
+        if (a.logp) a.logp[row] = (float)(-scaled(v) - log(total));
+        if (a.kept) a.kept[row] = kept;
+    }
+}
+
 template <typename T>
-__device__ void sample_fine(const SampleArgs &a, int row, const Settings &s, FinePool &f) {
+__device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const Settings &s, FinePool &f) {
     const T *z = (const T *)a.logits.p + row * a.logits.st;
     const int tid = threadIdx.x, V = a.vocab;
     const auto each = [&](auto fn) {             // every token that is not -inf: fn(value, index)
-        for (int i = tid * 8; i < V; i += kThreads * 8) {
-            const Eight<T> x = load_eight(z, i, V);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float v = RowElem<T>::get(x.v[j]) + 0.f;     // (-0 and 0 are the same value)
+        Lot next = load_lot(z, tid * kLot<T>, V);
+#pragma unroll 1
+        for (int i = tid * kLot<T>; i < V; i += kThreads * kLot<T>) {
+            const Lot x = next;
+            next = load_lot(z, min(i + kThreads * kLot<T>, V), V);
+            each_token<T>(x, [&](int j, uint32_t bits) {
+                const float v = token_value<T>(bits) + 0.f;        // (-0 and 0 are the same value)
                 if (!(v == kNegInf)) fn(v, i + j);
-            }
+            });
         }
     };
-    for (int i = tid; i < kFineBins; i += kThreads) f.count[i] = 0, f.mass[i] = 0, f.edge[i] = exp(-i / 32.0);
-    if (tid == 0) f.top = 0, f.n = 0, f.bad = 0;
+    if (tid == 0) f.top = 0, f.n = 0, f.bad = 0, f.listed = 0, f.least = 0xffffffffu;
     __syncthreads();
     uint32_t top = 0, n = 0, bad = 0;
     each([&](float v, int) {
@@ -388,10 +559,16 @@ __device__ void sample_fine(const SampleArgs &a, int row, const Settings &s, Fin
         top = max(top, f2ord(v));
         ++n;
     });
-    for (int o = 32; o > 0; o >>= 1) {
-        top = max(top, (uint32_t)__shfl_xor((int)top, o));
-        n += __shfl_xor((int)n, o);
+    if (s.k > 0 && s.k <= kFew) {
+        // the least of the largest values of k groups of threads or more: k tokens at least reach it
+        uint32_t group = top;
+        for (int o = 1; o * 2 <= (s.k <= 64 ? 16 : s.k <= 128 ? 8 : 4); o <<= 1)
+            group = max(group, (uint32_t)__shfl_xor((int)group, o));
+        const uint32_t least = ~wave_max(~group);
+        if ((tid & 63) == 0) atomicMin(&f.least, least);
     }
+    top = wave_max(top);
+    n = wave_sum(n);
     if ((tid & 63) == 0) {
         atomicMax(&f.top, top);
         atomicAdd(&f.n, n);
@@ -399,23 +576,36 @@ __device__ void sample_fine(const SampleArgs &a, int row, const Settings &s, Fin
     if (bad) atomicOr(&f.bad, 1u);
     __syncthreads();
     if (f.bad || f.n == 0 || !s.ok) return no_answer(a, row);
-
     const double zmax = (double)ord2f(f.top), inv = 1.0 / (double)s.temp;
+    const auto scaled = [&](float v) { return (zmax - (double)v) * inv; };
     const int total = (int)f.n;
+    if (s.k > 0 && s.k <= kFew && s.k < total) {
+        const uint32_t least = f.least;
+        each([&](float v, int i) {
+            const uint32_t key = f2ord(v);
+            if (key < least) return;
+            const uint32_t at = atomicAdd(&f.listed, 1u);
+            if (at < (uint32_t)kFewList) f.key[at] = key, f.index[at] = i;
+        });
+        __syncthreads();
+        if (f.listed <= (uint32_t)kFewList) return sample_few<T>(a, row, s, f, (int)f.listed, scaled);
+    }
+
+    for (int i = tid; i < kFineBins; i += kThreads) f.count[i] = 0, f.mass[i] = 0, f.edge[i] = exp(-i / 32.0);
+    __syncthreads();
     int bits = 0;
     while ((V >> bits) > 0) ++bits;
     const double unit = ldexp(1.0, 62 - bits), back = ldexp(1.0, bits - 62);
-    const auto scaled = [&](float v) { return (zmax - (double)v) * inv; };
     const auto bin_at = [&](double t) { return t < 63.96875 ? (int)(t * 32.0) : kFineBins - 1; };
-    const auto rel = [&](double t, int b) {      // weight relative to the bin's edge
-        const double x = t - b * 0.03125;
-        return b < kFineBins - 1 ? exp_small(x) : exp(-x);
-    };
+    // a weight relative to its bin's edge, in fixed point (of the last bin, whose mass is less than the sums'
+    // roundings, none)
+    const auto rel = [&](double t, int b) { return b < kFineBins - 1 ? exp_small(t - b * 0.03125) : 0.0; };
+    const auto fixed = [&](double t, int b) { return (unsigned long long)(rel(t, b) * unit + 0.5); };
     each([&](float v, int) {
         const double t = scaled(v);
         const int b = bin_at(t);
         atomicAdd(f.count + b, 1u);
-        if (b < kFineBins - 1) atomicAdd((unsigned long long *)f.mass + b, (unsigned long long)(rel(t, b) * unit + 0.5));
+        atomicAdd((unsigned long long *)f.mass + b, fixed(t, b));
     });
     __syncthreads();
     int c[2], cb, call;
@@ -423,16 +613,31 @@ __device__ void sample_fine(const SampleArgs &a, int row, const Settings &s, Fin
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         c[i] = (int)f.count[2 * tid + i];
-        m[i] = (double)f.mass[2 * tid + i] * back * f.edge[2 * tid + i];
+        m[i] = b_mass(f, 2 * tid + i, back);
     }
     block_scan(c[0] + c[1], m[0] + m[1], cb, mb, call, mall);
 
-    // The tokens of bin b in order until `count` of them, or until their mass is `mass` (relative to the bin's
-    // edge): the last one's value and index, how many they are and their mass.
-    const auto refine = [&](int b, bool by_mass, int count, double mass) {
-        const bool list = f.count[b] <= (uint32_t)kFineList;
-        if (tid == 0) f.listed = 0;
+    // Where the run ends: by the count of top_k, then by the mass of top_p. The bin is the first that
+    // reaches it; inside, the digits of value and index are found one after the other.
+    Edge end{kFineBins, 0, total, mall};
+#pragma unroll 1
+    for (int by_mass = 0; by_mass < 2; ++by_mass) {
+        if (by_mass ? !(s.p < 1.f) : !(s.k > 0 && s.k < total)) continue;
+        const double share = (double)s.p * end.mass;
         __syncthreads();
+        if (tid == 0) f.bin = kFineBins, f.listed = 0;
+        __syncthreads();
+        const bool in0 = c[0] && (by_mass ? mb + m[0] >= share : cb + c[0] >= s.k);
+        const bool in1 = c[1] && (by_mass ? mb + m[0] + m[1] >= share : cb + c[0] + c[1] >= s.k);
+        if (in0 || in1) atomicMin(&f.bin, 2 * tid + !in0);
+        __syncthreads();
+        const int b = f.bin;
+        if (by_mass && (b >= kFineBins - 1 || b > end.bin)) continue;
+        if (tid == b >> 1) {
+            f.above = cb + (b & 1 ? c[0] : 0);
+            f.before = mb + (b & 1 ? m[0] : 0.0);
+        }
+        const bool list = f.count[b] <= (uint32_t)kFineList;
         if (list) {
             each([&](float v, int i) {
                 if (bin_at(scaled(v)) != b) return;
@@ -441,23 +646,24 @@ __device__ void sample_fine(const SampleArgs &a, int row, const Settings &s, Fin
                 f.index[at] = i;
             });
         }
+        __syncthreads();
+        const int above = f.above, count = s.k - above;
+        const double before = f.before, want = (share - before) / f.edge[b] * unit;
         uint64_t prefix = 0, most = 0;
         Edge e{b, 0, 0, 0.0};
-        const double want = mass * unit;
+#pragma unroll 1
         for (int shift = 48; shift >= 0; shift -= 8) {
             if (tid < 256) f.dcount[tid] = 0, f.dmass[tid] = 0;
             __syncthreads();
-            const auto add = [&](uint32_t key, int i) {
-                const uint64_t comp = (uint64_t)key << 24 | (0xffffff - (uint32_t)i);
+            const auto add = [&](float v, int i) {
+                const uint64_t comp = comp_of(f2ord(v), i);
                 if ((comp >> shift >> 8) != prefix) return;
                 const int d = 255 - (int)(comp >> shift & 255);
                 atomicAdd(f.dcount + d, 1u);
-                if (b < kFineBins - 1)
-                    atomicAdd((unsigned long long *)f.dmass + d,
-                              (unsigned long long)(rel(scaled(ord2f(key)), b) * unit + 0.5));
+                atomicAdd((unsigned long long *)f.dmass + d, fixed(scaled(v), b));
             };
-            if (list) for (int i = tid; i < (int)f.listed; i += kThreads) add(f.key[i], f.index[i]);
-            else each([&](float v, int i) { if (bin_at(scaled(v)) == b) add(f2ord(v), i); });
+            if (list) for (int i = tid; i < (int)f.listed; i += kThreads) add(ord2f(f.key[i]), (int)f.index[i]);
+            else each([&](float v, int i) { if (bin_at(scaled(v)) == b) add(v, i); });
             __syncthreads();
             // every wavefront for itself: 4 digits a lane
             const int lane = tid & 63;
@@ -468,41 +674,26 @@ __device__ void sample_fine(const SampleArgs &a, int row, const Settings &s, Fin
                 cs += dc[i] = (int)f.dcount[4 * lane + i];
                 ms += dm[i] = f.dmass[4 * lane + i];
             }
-            int cr = cs;
-            uint64_t mr = ms;
-            for (int o = 1; o < 64; o <<= 1) {
-                const int u = __shfl_up(cr, o);
-                const uint64_t v = __shfl_up((unsigned long long)mr, o);
-                if (lane >= o) cr += u, mr += v;
-            }
-            cr -= cs, mr -= ms;
-            int digit = -1, there = -1;          // where it ends; the last digit that has any
-            int c_at = 0, c_there = 0, n_at = 0, n_there = 0;
-            uint64_t m_at = 0, m_there = 0, w_at = 0, w_there = 0;
+            int cr = wave_scan(cs) - cs;
+            uint64_t mr = wave_scan(ms) - ms;
+            bool ends = false;
+            int digit = -1, c_at = 0, n_at = 0;  // where it ends, or the lane's last digit that has any
+            uint64_t m_at = 0, w_at = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (dc[i] > 0) {
-                    there = 4 * lane + i, c_there = cr, m_there = mr, n_there = dc[i], w_there = dm[i];
-                    const bool ends = by_mass ? (double)(most + mr + dm[i]) >= want : e.kept + cr + dc[i] >= count;
-                    if (digit < 0 && ends) digit = there, c_at = cr, m_at = mr, n_at = dc[i], w_at = dm[i];
+                if (dc[i] > 0 && !ends) {
+                    ends = by_mass ? (double)(most + mr + dm[i]) >= want : e.kept + cr + dc[i] >= count;
+                    digit = 4 * lane + i, c_at = cr, m_at = mr, n_at = dc[i], w_at = dm[i];
                 }
                 cr += dc[i], mr += dm[i];
             }
-            uint64_t hit = __ballot(digit >= 0);
-            int src;
-            if (hit) {
-                src = __builtin_ctzll(hit);
-            } else {
-                hit = __ballot(there >= 0);
-                src = 63 - __builtin_clzll(hit);
-                digit = there, c_at = c_there, m_at = m_there, n_at = n_there, w_at = w_there;
-            }
-            digit = __shfl(digit, src);
-            e.kept += __shfl(c_at, src);
-            most += __shfl((unsigned long long)m_at, src);
-            n_at = __shfl(n_at, src);
-            w_at = __shfl((unsigned long long)w_at, src);
-            prefix = prefix << 8 | (uint64_t)(255 - digit);
+            const uint64_t hit = __ballot(ends), any = __ballot(digit >= 0);
+            const int src = hit ? __builtin_ctzll(hit) : any ? 63 - __builtin_clzll(any) : 0;
+            prefix = prefix << 8 | (uint64_t)(255 - wave_read(digit, src));
+            e.kept += wave_read(c_at, src);
+            most += wave_read(m_at, src);
+            n_at = wave_read(n_at, src);
+            w_at = wave_read(w_at, src);
             __syncthreads();
             if (n_at == 1 || (!by_mass && e.kept + n_at == count)) {     // all of this digit
                 e.comp = prefix << shift;
@@ -511,90 +702,40 @@ __device__ void sample_fine(const SampleArgs &a, int row, const Settings &s, Fin
                 break;
             }
         }
-        e.mass = (double)most * back * f.edge[b];
-        return e;
-    };
-    // the cumulative count and mass before bin b
-    const auto before = [&](int b, int &above, double &mass) {
-        __syncthreads();
-        if (tid == b >> 1) {
-            f.above = cb + (b & 1 ? c[0] : 0);
-            f.before = mb + (b & 1 ? m[0] : 0.0);
-        }
-        __syncthreads();
-        above = f.above;
-        mass = f.before;
-    };
-    Edge end{kFineBins, 0, total, mall};
-    const auto cut = [&](const Edge &e) {
-        if (e.bin < end.bin || (e.bin == end.bin && e.comp > end.comp)) end = e;
-    };
-    if (s.k > 0 && s.k < total) {
-        if (tid == 0) f.bin = 0;
-        __syncthreads();
-        if (cb < s.k && cb + c[0] + c[1] >= s.k) f.bin = 2 * tid + (cb + c[0] < s.k);
-        __syncthreads();
-        const int b = f.bin;
-        int above;
-        double mass;
-        before(b, above, mass);
-        Edge e = refine(b, false, s.k - above, 0.0);
+        e.mass = (double)most * back * f.edge[b] + before;
         e.kept += above;
-        e.mass += mass;
-        cut(e);
-    }
-    if (s.p < 1.f) {
-        const double want = (double)s.p * end.mass;
-        __syncthreads();
-        if (tid == 0) f.bin_p = kFineBins;
-        __syncthreads();
-        const int b0 = mb + m[0] >= want && c[0] ? 2 * tid : mb + m[0] + m[1] >= want && c[1] ? 2 * tid + 1 : kFineBins;
-        if (b0 < kFineBins) atomicMin(&f.bin_p, b0);
-        __syncthreads();
-        const int b = f.bin_p;
-        if (b < kFineBins - 1 && b <= end.bin) {
-            int above;
-            double mass;
-            before(b, above, mass);
-            Edge e = refine(b, true, 0, (want - mass) / f.edge[b]);
-            e.kept += above;
-            e.mass += mass;
-            cut(e);
-        }
+        if (e.bin < end.bin || e.comp > end.comp) end = e;
     }
     if (s.mp > 0.f) {
         const int b = bin_at(-log((double)s.mp));
         __syncthreads();
         if (tid == 0) f.least = 0xffffffffu, f.listed = 0, f.dmass[0] = 0;
+        if (tid == b >> 1) {
+            f.above = cb + (b & 1 ? c[0] : 0);
+            f.before = mb + (b & 1 ? m[0] : 0.0);
+        }
         __syncthreads();
         each([&](float v, int) {
             const double t = scaled(v);
             if (bin_at(t) != b || !(exp(-t) >= (double)s.mp)) return;
             atomicMin(&f.least, f2ord(v));
             atomicAdd(&f.listed, 1u);
-            if (b < kFineBins - 1) atomicAdd((unsigned long long *)f.dmass, (unsigned long long)(rel(t, b) * unit + 0.5));
+            atomicAdd((unsigned long long *)f.dmass, fixed(t, b));
         });
         __syncthreads();
-        int above;
-        double mass;
-        before(b, above, mass);
         // (a comp that no token reaches where the bin has none)
-        Edge e{b, f.listed ? (uint64_t)f.least << 24 : ~0ull, above + (int)f.listed, mass + (double)f.dmass[0] * back * f.edge[b]};
-        __syncthreads();
-        cut(e);
+        const Edge e{b, f.listed ? (uint64_t)f.least << 24 : ~0ull, f.above + (int)f.listed,
+                     f.before + (double)f.dmass[0] * back * f.edge[b]};
+        if (e.bin < end.bin || (e.bin == end.bin && e.comp > end.comp)) end = e;
     }
-    const auto src = [&](int i, int e, auto fn) {
-        const Eight<T> x = load_eight(z, i, e);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float v = RowElem<T>::get(x.v[j]) + 0.f;
-            const double t = scaled(v);
-            const int b = bin_at(t);
-            const bool kept = v > kNegInf && (b < end.bin || (b == end.bin && ((uint64_t)f2ord(v) << 24 | (0xffffff - (uint32_t)(i + j))) >= end.comp));
-            fn(j, kept, false, kept && b < kFineBins - 1 ? f.edge[b] * rel(t, b) : 0.0);
-        }
+    const auto item = [&](int i, uint32_t bits, auto fn) {
+        const float v = token_value<T>(bits) + 0.f;
+        const double t = scaled(v);
+        const int b = v > kNegInf ? bin_at(t) : kFineBins;
+        const bool kept = b < end.bin || (b == end.bin && b < kFineBins && comp_of(f2ord(v), i) >= end.comp);
+        fn(kept, false, kept ? f.edge[b] * rel(t, b) : 0.0);
     };
-    const int token = locate(src, 0, V, 0.0, Drawn{(double)s.u * end.mass, s.u, 0}, f.ranges);
+    const int token = locate(z, item, 0, V, 0.0, Drawn{(double)s.u * end.mass, s.u, 0}, f.ranges);
     if (tid == 0) {
         a.token[row] = token;
         if (a.logp) a.logp[row] = (float)(-scaled(RowElem<T>::get(z[token])) - log(end.mass));
@@ -608,34 +749,102 @@ __global__ __launch_bounds__(kThreads) void sample_fine_kernel(SampleArgs a) {
     sample_fine<T>(a, blockIdx.x, settings_of(a, blockIdx.x), f);
 }
 
+// The rows that the coarse bins have left: those whose token is kLeft.
+constexpr int kLeft = -2;
+
+__global__ __launch_bounds__(kThreads) void sample_left_kernel(SampleArgs a) {
+    __shared__ FinePool f;
+    __shared__ int left;
+    for (int64_t r0 = 0; r0 < a.rows; r0 += (int64_t)gridDim.x * kThreads) {
+        const int64_t r = r0 + (int64_t)threadIdx.x * gridDim.x + blockIdx.x;
+        bool mine = r < a.rows && a.token[r] == kLeft;
+        while (__syncthreads_or(mine)) {
+            if (threadIdx.x == 0) left = 0x7fffffff;
+            __syncthreads();
+            if (mine) atomicMin(&left, (int)r);
+            __syncthreads();
+            const int row = left;
+            if (mine && r == row) mine = false;
+            sample_fine<uint16_t>(a, row, settings_of(a, row), f);
+            __syncthreads();
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------- coarse bins
 struct CoarsePool {
-    double weight[kSlots * 128];
+    double weight[kSlots * 128 + 256];           // 0 past the bins in use, and after the cut past the run
     uint32_t count[kSlots * 128];
     uint64_t blocks[kMostParts][2];
     Range ranges[kRanges];
     uint32_t used[4], flags;
-    uint8_t slot[kBlocks], block[kSlots];
+    int16_t place[512];                          // of a value's sign and exponent: its block's first bin here
+    uint8_t block[kSlots];
     int first, bin_k, ties_k, bin_p, bin_m, above;
     double mass;
 };
 struct CoarseRow : CoarsePool { uint32_t hist[kBins / 2]; };   // of a row that is counted here
 
+// A row that keeps every token, from its parts' masses: the part, then the token by its own weights.
+// A greedy row: the first of its largest.
+__global__ __launch_bounds__(kThreads) void sample_all_kernel(SampleArgs a, Parts parts) {
+    __shared__ Range ranges[kRanges];
+    const int row = blockIdx.x, lane = threadIdx.x & 63, S = parts.count;
+    const uint16_t *z = (const uint16_t *)a.logits.p + row * a.logits.st;
+    const Settings s = settings_of(a, row);
+    if (!s.ok) return no_answer(a, row);
+    float top = kNegInf;
+    double mass = 0.0;
+    int n = 0, flags = 0;
+    if (lane < S) {
+        const PartHead *h = (const PartHead *)(a.work + ((int64_t)row * S + lane) * parts.bytes);
+        top = h->top;
+        mass = h->mass;
+        n = h->n;
+        flags = h->flags;
+    }
+    if (__ballot(flags != 0)) return no_answer(a, row);
+    const int there = wave_sum(n);
+    if (there == 0) return no_answer(a, row);
+    const double zmax = (double)ord2f(wave_max(f2ord(n > 0 ? top : kNegInf))), t = (double)s.temp;
+    mass = n > 0 ? mass * exp(((double)top - zmax) / t) : 0.0;
+    const double all = wave_sum(mass);
+    if (threadIdx.x < S) ranges[lane] = Range{mass, s.greedy ? n > 0 && (double)top == zmax : n, 0};
+    __syncthreads();
+    Drawn d{(double)s.u * all, s.greedy ? 0.f : s.u, 0};
+    const int q = max(0, pick_range(ranges, S, 0.0, d)), begin = q * parts.len;
+    const auto item = [&](int, uint32_t bits, auto fn) {
+        const float v = bf16_bits_to_f32(bits);
+        const bool in = s.greedy ? (double)v == zmax : v > kNegInf;
+        fn(in, false, in ? exp(((double)v - zmax) / t) : 0.0);
+    };
+    const int token = locate(z, item, begin, min(a.vocab, begin + parts.len), 0.0, d, ranges);
+    if (threadIdx.x == 0) {
+        a.token[row] = token;
+        if (a.logp) a.logp[row] = (float)(((double)bf16_bits_to_f32(z[token]) - zmax) / t - (s.greedy ? 0.0 : log(all)));
+        if (a.kept) a.kept[row] = s.greedy ? 1 : there;
+    }
+}
+
+// (64 registers: two workgroups a compute unit where there are rows enough)
 template <bool SPLIT>
-__global__ __launch_bounds__(kThreads) void sample_coarse_kernel(SampleArgs a, Parts parts) {
-    using Pool = std::conditional_t<SPLIT, CoarsePool, CoarseRow>;
-    __shared__ union Shared {
-        Pool c;
-        FinePool f;
-        __device__ Shared() {}
-    } pool;
-    Pool &f = pool.c;
+__global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(SampleArgs a, Parts parts) {
+    __shared__ std::conditional_t<SPLIT, CoarsePool, CoarseRow> f;
     constexpr int kPer = kSlots * 128 / kThreads;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int V = a.vocab, S = parts.count;
     const uint16_t *z = (const uint16_t *)a.logits.p + row * a.logits.st;
-    const char *part = a.work + (int64_t)row * S * kPartBytes;
+    const char *part = a.work + (int64_t)row * S * parts.bytes;
     const Settings s = settings_of(a, row);
+    if (!s.ok) return no_answer(a, row);
+
+    // a part's two counts, 0 where it has none of the block (its memory is not written)
+    const auto counts_of = [&](int q, int b, int pair) {
+        const bool there = q < S && f.blocks[q][b >> 6] >> (b & 63) & 1;
+        const uint32_t *p = (const uint32_t *)(part + (there ? q * parts.bytes + 64 : 0)) + (there ? b * 64 + pair : 0);
+        const uint32_t x = *p;
+        return there ? x : 0;
+    };
 
     // ---- the blocks in use, and the counts of their bins
     if (tid < 4) f.used[tid] = 0;
@@ -645,7 +854,7 @@ __global__ __launch_bounds__(kThreads) void sample_coarse_kernel(SampleArgs a, P
     __syncthreads();
     if constexpr (SPLIT) {
         if (tid < S) {
-            const PartHead h = *(const PartHead *)(part + tid * kPartBytes);
+            const PartHead h = *(const PartHead *)(part + tid * parts.bytes);
             f.blocks[tid][0] = h.blocks[0];
             f.blocks[tid][1] = h.blocks[1];
             for (int i = 0; i < 4; ++i) atomicOr(f.used + i, (uint32_t)(h.blocks[i >> 1] >> (i & 1) * 32));
@@ -661,34 +870,41 @@ __global__ __launch_bounds__(kThreads) void sample_coarse_kernel(SampleArgs a, P
     __syncthreads();
     int slots = 0;
     for (int i = 0; i < 4; ++i) slots += __popc(f.used[i]);
-    if ((f.flags & 1) || slots == 0 || !s.ok) return no_answer(a, row);
-    bool fine = (f.flags & 2) || slots > kSlots;
+    if ((f.flags & 1) || slots == 0) return no_answer(a, row);
+    // (u = 0 and 1 ask for the first and the last token kept, whatever they weigh)
+    bool fine = (f.flags & 2) || slots > kSlots || s.u == 0.f || s.u == 1.f;
     const int bins = slots * 128;
     if (!fine) {
-        if (tid < kBlocks) {
+        if (tid < 512) f.place[tid] = kSlots * 128;
+        __syncthreads();
+        if (tid < kBlocks && f.used[tid >> 5] >> (tid & 31) & 1) {
             int at = 0;
             for (int i = 0; i < 4; ++i) {
                 const int from = tid - 32 * i;
                 at += from >= 32 ? __popc(f.used[i]) : from > 0 ? __popc(f.used[i] & ((1u << from) - 1)) : 0;
             }
-            const bool in = f.used[tid >> 5] >> (tid & 31) & 1;
-            f.slot[tid] = in ? at : 255;
-            if (in) f.block[at] = tid;
+            f.block[at] = tid;
+            // a positive value's bin is 127 - its mantissa after its place, a negative one's its mantissa
+            if (tid < kSide >> 7) f.place[(kHigh >> 7) - 1 - tid] = at * 128;
+            else if (tid == kZeroBin >> 7) f.place[0] = at * 128 - 127, f.place[256] = at * 128;
+            else if (tid < kBelow >> 7) f.place[256 + (kLow >> 7) + tid - (kNegative >> 7)] = at * 128;
         }
         __syncthreads();
+#pragma unroll 1
         for (int i = tid; i < slots * 64; i += kThreads) {
-            const int b = f.block[i >> 6], pair = b * 64 + (i & 63);
+            const int b = f.block[i >> 6];
             uint32_t c0 = 0, c1 = 0;
             if constexpr (SPLIT) {
-                for (int q = 0; q < S; ++q) {
-                    if (!(f.blocks[q][b >> 6] >> (b & 63) & 1)) continue;
-                    const uint32_t x = ((const uint32_t *)(part + q * kPartBytes + 64))[pair];
-                    c0 += x & 0xffffu;
-                    c1 += x >> 16;
+                for (int q0 = 0; q0 < S; q0 += 8) {          // (8 loads in flight)
+                    uint32_t x[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = counts_of(q0 + j, b, i & 63);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) c0 += x[j] & 0xffffu, c1 += x[j] >> 16;
                 }
             } else {
-                c0 = f.hist[pair] & 0xffffu;
-                c1 = f.hist[pair] >> 16;
+                c0 = f.hist[b * 64 + (i & 63)] & 0xffffu;
+                c1 = f.hist[b * 64 + (i & 63)] >> 16;
             }
             f.count[2 * i] = c0;
             f.count[2 * i + 1] = c1;
@@ -710,9 +926,10 @@ __global__ __launch_bounds__(kThreads) void sample_coarse_kernel(SampleArgs a, P
         fine = top == kBelow || (below && (zmax + 32768.0) / t < 800.0);
     }
     if (!fine) {
-        for (int i = tid; i < bins; i += kThreads) {
-            const int b = bin_at(i);
-            f.weight[i] = f.count[i] && b != kBelow ? exp(((double)value_of(b) - zmax) / t) : 0.0;
+#pragma unroll 1
+        for (int i = tid; i < kSlots * 128 + 256; i += kThreads) {
+            const int b = i < bins ? bin_at(i) : kBelow;
+            f.weight[i] = b != kBelow && f.count[i] ? exp(((double)value_of(b) - zmax) / t) : 0.0;
         }
         __syncthreads();
 #pragma unroll
@@ -794,35 +1011,36 @@ __global__ __launch_bounds__(kThreads) void sample_coarse_kernel(SampleArgs a, P
             if (f.bin_m < end) end = f.bin_m, ties = (int)f.count[end];
         }
         measure();
-        // some of the values below -2^15, and they matter for the token: their order does
-        fine = end < bins && bin_at(end) == kBelow && (s.u == 0.f || s.u == 1.f) && ties < (int)f.count[end];
     }
     if (fine) {
-        __syncthreads();
-        return sample_fine<uint16_t>(a, row, s, pool.f);
+        if (tid == 0) a.token[row] = kLeft;
+        return;
     }
     const int kept = f.above;
     const double tie_weight = end < bins ? f.weight[end] : 0.0;
+    __syncthreads();
+    for (int i = end + tid; i < bins; i += kThreads) f.weight[i] = 0.0;
+    __syncthreads();
     Drawn d{(double)s.u * all, s.u, ties};
     int begin = 0, stop = V;
     if constexpr (SPLIT) {
         for (int q = wave; q < S; q += kWaves) {
             Range x{0.0, 0, 0};
-            const uint32_t *hist = (const uint32_t *)(part + q * kPartBytes + 64);
-            for (int i = lane; i < slots * 64 && 2 * (i - lane) <= end; i += 64) {
-                const int b = f.block[i >> 6];
-                if (!(f.blocks[q][b >> 6] >> (b & 63) & 1)) continue;
-                const uint32_t y = hist[b * 64 + (i & 63)];
-                const int n0 = (int)(y & 0xffffu), n1 = (int)(y >> 16);
-                if (2 * i < end && n0) x.mass += n0 * f.weight[2 * i], x.kept += n0;
-                if (2 * i + 1 < end && n1) x.mass += n1 * f.weight[2 * i + 1], x.kept += n1;
-                x.ties += 2 * i == end ? n0 : 2 * i + 1 == end ? n1 : 0;
+            const int blocks = min(slots, (end >> 7) + 1);
+            for (int i0 = 0; i0 < blocks; i0 += 4) {
+                uint32_t y[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = i0 + j < blocks ? counts_of(q, f.block[i0 + j], lane) : 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int at = (i0 + j) * 128 + 2 * lane, n0 = (int)(y[j] & 0xffffu), n1 = (int)(y[j] >> 16);
+                    x.mass += n0 * f.weight[at] + n1 * f.weight[at + 1];
+                    x.ties += at == end ? n0 : at + 1 == end ? n1 : 0;
+                }
             }
-            for (int o = 32; o > 0; o >>= 1) {
-                x.mass += __shfl_xor(x.mass, o);
-                x.kept += __shfl_xor(x.kept, o);
-                x.ties += __shfl_xor(x.ties, o);
-            }
+            x.mass = wave_sum(x.mass);
+            x.ties = wave_sum(x.ties);
+            x.kept = x.mass > 0.0;
             if (lane == 0) f.ranges[q] = x;
         }
         __syncthreads();
@@ -830,16 +1048,13 @@ __global__ __launch_bounds__(kThreads) void sample_coarse_kernel(SampleArgs a, P
         begin = q * parts.len;
         stop = min(V, begin + parts.len);
     }
-    const auto src = [&](int i, int e, auto fn) {
-        const Eight<uint16_t> x = load_eight(z, i, e);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int b = bin_of(x.v[j]);
-            const int at = b >= 0 ? f.slot[b >> 7] * 128 + (b & 127) : 1 << 20;
-            fn(j, at < end, at == end, at < end ? f.weight[at] : 0.0);
-        }
+    // (values below -2^15 and -inf have a place past the bins, whose weights are 0)
+    const auto item = [&](int, uint32_t bits, auto fn) {
+        const int at = f.place[bits >> 7] + (int)((bits & 127) ^ (bits & 0x8000u ? 0 : 127));
+        const double w = f.weight[at];
+        fn(w > 0.0, at == end, w);
     };
-    const int token = locate(src, begin, stop, tie_weight, d, f.ranges);
+    const int token = locate(z, item, begin, stop, tie_weight, d, f.ranges);
     if (tid == 0) {
         a.token[row] = token;
         if (a.logp) a.logp[row] = (float)(((double)bf16_bits_to_f32(z[token]) - zmax) / t - log(all));
@@ -851,8 +1066,8 @@ __global__ __launch_bounds__(kThreads) void sample_coarse_kernel(SampleArgs a, P
 
 int64_t sample_bytes(const SampleArgs &a, bool bf16) {
     if (!bf16 || a.rows == 0) return 0;
-    const Parts p = parts_of(a.rows, a.vocab);
-    return p.count == 1 || p.count > kMostParts ? 0 : (int64_t)a.rows * p.count * kPartBytes;
+    const Parts p = parts_of(a);
+    return p.count == 1 || p.count > kMostParts ? 0 : (int64_t)a.rows * p.count * p.bytes;
 }
 
 hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t st) {
@@ -860,19 +1075,26 @@ hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t st) {
         sample_fine_kernel<float><<<a.rows, kThreads, 0, st>>>(a);
         return hipGetLastError();
     }
-    const Parts p = parts_of(a.rows, a.vocab);
-    if (p.count > kMostParts) {
+    const Parts p = parts_of(a);
+    if (p.count > kMostParts) {                  // (rows of more than 4 million tokens)
         sample_fine_kernel<uint16_t><<<a.rows, kThreads, 0, st>>>(a);
         return hipGetLastError();
     }
     if (p.count == 1) {
         sample_coarse_kernel<false><<<a.rows, kThreads, 0, st>>>(a, p);
-        return hipGetLastError();
+    } else {
+        const bool plain = p.bytes == sizeof(PartHead);
+        if (plain) sample_masses_kernel<<<dim3(a.rows, p.count), kPartThreads, 0, st>>>(a, p);
+        else sample_counts_kernel<<<dim3(a.rows, p.count), kPartThreads, 0, st>>>(a, p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (plain) sample_all_kernel<<<a.rows, kThreads, 0, st>>>(a, p);
+        else sample_coarse_kernel<true><<<a.rows, kThreads, 0, st>>>(a, p);
+        if (plain) return hipGetLastError();     // (every row is answered)
     }
-    sample_parts_kernel<<<dim3(a.rows, p.count), kPartThreads, 0, st>>>(a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    sample_coarse_kernel<true><<<a.rows, kThreads, 0, st>>>(a, p);
+    sample_left_kernel<<<a.rows < kChipUnits ? a.rows : kChipUnits, kThreads, 0, st>>>(a);
     return hipGetLastError();
 }
 
