@@ -129,9 +129,9 @@ __device__ __forceinline__ Lot load_lot(const T *z, int i, int end) {
     return x;
 }
 // fn(j, bits) for each token j of a lot.
-template <typename T, typename F>
+template <typename T, int UNROLL = 1, typename F>
 __device__ __forceinline__ void each_token(Lot x, F fn) {
-#pragma unroll 1
+#pragma unroll UNROLL
     for (int k = 0; k < 4; ++k) {
         if constexpr (sizeof(T) == 2) {
             fn(2 * k, x.w[0] & 0xffffu);
@@ -148,16 +148,25 @@ __device__ __forceinline__ float token_value(uint32_t bits) {
 }
 
 // Counts of [begin, end) of a row into 16-bit bins (two to a word); the flags of its odd values.
+// Four lots a thread are on their way together.
 template <int THREADS>
 __device__ __forceinline__ int count_bins(const uint16_t *z, int begin, int end, uint32_t *hist) {
+    constexpr int kAhead = 4;
     int flags = 0;
-    for (int i = begin + (int)threadIdx.x * 8; i < end; i += THREADS * 8) {
-        const Lot x = load_lot(z, i, end);
+#pragma unroll 1
+    for (int i0 = begin + (int)threadIdx.x * 8; i0 < end; i0 += kAhead * THREADS * 8) {
+        Lot x[kAhead];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int b = bin_of(j & 1 ? x.w[j >> 1] >> 16 : x.w[j >> 1] & 0xffffu);
-            if (b >= 0) atomicAdd(hist + (b >> 1), 1u << ((b & 1) * 16));
-            else flags |= b == kBad ? 1 : b == kOdd ? 2 : 0;
+        for (int k = 0; k < kAhead; ++k) x[k] = load_lot(z, i0 + k * THREADS * 8, end);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (i0 + k * THREADS * 8 >= end) break;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int b = bin_of(j & 1 ? x[k].w[j >> 1] >> 16 : x[k].w[j >> 1] & 0xffffu);
+                if (b >= 0) atomicAdd(hist + (b >> 1), 1u << ((b & 1) * 16));
+                else flags |= b == kBad ? 1 : b == kOdd ? 2 : 0;
+            }
         }
     }
     return flags;
@@ -361,7 +370,7 @@ __device__ __forceinline__ int pick_range(const Range *r, int n, double w, Drawn
     return found;
 }
 
-template <typename T, typename Item>
+template <typename T, int UNROLL = 1, typename Item>
 __device__ __forceinline__ int locate(const T *z, const Item &item, int begin, int end, double tie_weight, Drawn d,
                                       Range *ranges) {
     constexpr int kC = kCell<T>, kL = kLot<T>;
@@ -390,7 +399,7 @@ __device__ __forceinline__ int locate(const T *z, const Item &item, int begin, i
             const Lot y = ahead[0];
             ahead[0] = ahead[1], ahead[1] = ahead[2];
             ahead[2] = load_next();
-            each_token<T>(y, [&](int j, uint32_t bits) {
+            each_token<T, UNROLL>(y, [&](int j, uint32_t bits) {
                 item(at + lane * kL + j, bits, [&](bool kept, bool tie, double w) {
                     x.mass += w;
                     x.kept += kept;
@@ -417,7 +426,7 @@ __device__ __forceinline__ int locate(const T *z, const Item &item, int begin, i
     double at = 0.0;
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
-        each_token<T>(y, [&](int j, uint32_t bits) {
+        each_token<T, UNROLL>(y, [&](int j, uint32_t bits) {
             const int i = begin + lane * kL + j;
             item(i, bits, [&](bool kept, bool tie, double w) {
                 const bool keep = i < end && (kept || (tie && before < d.ties));
@@ -743,32 +752,14 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void sample_fine_kernel(SampleArgs a) {
-    __shared__ FinePool f;
-    sample_fine<T>(a, blockIdx.x, settings_of(a, blockIdx.x), f);
-}
-
-// The rows that the coarse bins have left: those whose token is kLeft.
+// LEFT: of the rows only those that the coarse bins have left (their token is kLeft).
 constexpr int kLeft = -2;
 
-__global__ __launch_bounds__(kThreads) void sample_left_kernel(SampleArgs a) {
+template <typename T, bool LEFT>
+__global__ __launch_bounds__(kThreads) void sample_fine_kernel(SampleArgs a) {
     __shared__ FinePool f;
-    __shared__ int left;
-    for (int64_t r0 = 0; r0 < a.rows; r0 += (int64_t)gridDim.x * kThreads) {
-        const int64_t r = r0 + (int64_t)threadIdx.x * gridDim.x + blockIdx.x;
-        bool mine = r < a.rows && a.token[r] == kLeft;
-        while (__syncthreads_or(mine)) {
-            if (threadIdx.x == 0) left = 0x7fffffff;
-            __syncthreads();
-            if (mine) atomicMin(&left, (int)r);
-            __syncthreads();
-            const int row = left;
-            if (mine && r == row) mine = false;
-            sample_fine<uint16_t>(a, row, settings_of(a, row), f);
-            __syncthreads();
-        }
-    }
+    if (LEFT && a.token[blockIdx.x] != kLeft) return;
+    sample_fine<T>(a, blockIdx.x, settings_of(a, blockIdx.x), f);
 }
 
 // ---------------------------------------------------------------------------- coarse bins
@@ -836,6 +827,9 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
     const uint16_t *z = (const uint16_t *)a.logits.p + row * a.logits.st;
     const char *part = a.work + (int64_t)row * S * parts.bytes;
     const Settings s = settings_of(a, row);
+    PartHead own{};
+    if constexpr (SPLIT)
+        if (tid < S) own = *(const PartHead *)(part + tid * parts.bytes);
     if (!s.ok) return no_answer(a, row);
 
     // a part's two counts, 0 where it has none of the block (its memory is not written)
@@ -854,7 +848,7 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
     __syncthreads();
     if constexpr (SPLIT) {
         if (tid < S) {
-            const PartHead h = *(const PartHead *)(part + tid * parts.bytes);
+            const PartHead &h = own;
             f.blocks[tid][0] = h.blocks[0];
             f.blocks[tid][1] = h.blocks[1];
             for (int i = 0; i < 4; ++i) atomicOr(f.used + i, (uint32_t)(h.blocks[i >> 1] >> (i & 1) * 32));
@@ -890,25 +884,39 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
             else if (tid < kBelow >> 7) f.place[256 + (kLow >> 7) + tid - (kNegative >> 7)] = at * 128;
         }
         __syncthreads();
+        constexpr int kRounds = kSlots * 64 / kThreads;
+        uint32_t c0[kRounds] = {}, c1[kRounds] = {};
+        if constexpr (SPLIT) {
 #pragma unroll 1
-        for (int i = tid; i < slots * 64; i += kThreads) {
-            const int b = f.block[i >> 6];
-            uint32_t c0 = 0, c1 = 0;
-            if constexpr (SPLIT) {
-                for (int q0 = 0; q0 < S; q0 += 8) {          // (8 loads in flight)
-                    uint32_t x[8];
+            for (int q0 = 0; q0 < S; q0 += 8) {              // (24 loads on their way together)
+                uint32_t x[kRounds][8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = counts_of(q0 + j, b, i & 63);
+                for (int k = 0; k < kRounds; ++k) {
+                    const int i = tid + k * kThreads, b = f.block[min(i >> 6, slots - 1)];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) c0 += x[j] & 0xffffu, c1 += x[j] >> 16;
+                    for (int j = 0; j < 8; ++j) x[k][j] = counts_of(i < slots * 64 ? q0 + j : S, b, i & 63);
                 }
-            } else {
-                c0 = f.hist[b * 64 + (i & 63)] & 0xffffu;
-                c1 = f.hist[b * 64 + (i & 63)] >> 16;
+#pragma unroll
+                for (int k = 0; k < kRounds; ++k)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) c0[k] += x[k][j] & 0xffffu, c1[k] += x[k][j] >> 16;
             }
-            f.count[2 * i] = c0;
-            f.count[2 * i + 1] = c1;
-            if (c0 | c1) atomicMin(&f.first, 2 * i + (c0 == 0));
+        } else {
+#pragma unroll
+            for (int k = 0; k < kRounds; ++k) {
+                const int i = tid + k * kThreads;
+                if (i >= slots * 64) break;
+                const uint32_t x = f.hist[f.block[i >> 6] * 64 + (i & 63)];
+                c0[k] = x & 0xffffu, c1[k] = x >> 16;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kRounds; ++k) {
+            const int i = tid + k * kThreads;
+            if (i >= slots * 64) break;
+            f.count[2 * i] = c0[k];
+            f.count[2 * i + 1] = c1[k];
+            if (c0[k] | c1[k]) atomicMin(&f.first, 2 * i + (c0[k] == 0));
         }
         __syncthreads();
     }
@@ -1024,16 +1032,22 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
     Drawn d{(double)s.u * all, s.u, ties};
     int begin = 0, stop = V;
     if constexpr (SPLIT) {
-        for (int q = wave; q < S; q += kWaves) {
+        // (two wavefronts a part where there are few)
+        const int twice = 2 * S <= kWaves, blocks = min(slots, (end >> 7) + 1);
+        for (int q = wave >> twice; q < S; q += kWaves >> twice) {
             Range x{0.0, 0, 0};
-            const int blocks = min(slots, (end >> 7) + 1);
-            for (int i0 = 0; i0 < blocks; i0 += 4) {
-                uint32_t y[4];
+#pragma unroll 1
+            for (int i0 = twice ? wave & 1 : 0; i0 < blocks; i0 += 8 << twice) {
+                uint32_t y[8];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = i0 + j < blocks ? counts_of(q, f.block[i0 + j], lane) : 0;
+                for (int j = 0; j < 8; ++j) {
+                    const int i = i0 + (j << twice);
+                    y[j] = counts_of(i < blocks ? q : S, f.block[min(i, slots - 1)], lane);
+                }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int at = (i0 + j) * 128 + 2 * lane, n0 = (int)(y[j] & 0xffffu), n1 = (int)(y[j] >> 16);
+                for (int j = 0; j < 8; ++j) {
+                    const int at = min(i0 + (j << twice), kSlots) * 128 + 2 * lane;
+                    const int n0 = (int)(y[j] & 0xffffu), n1 = (int)(y[j] >> 16);
                     x.mass += n0 * f.weight[at] + n1 * f.weight[at + 1];
                     x.ties += at == end ? n0 : at + 1 == end ? n1 : 0;
                 }
@@ -1041,7 +1055,14 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
             x.mass = wave_sum(x.mass);
             x.ties = wave_sum(x.ties);
             x.kept = x.mass > 0.0;
-            if (lane == 0) f.ranges[q] = x;
+            if (lane == 0) f.ranges[twice ? 64 + wave : q] = x;
+        }
+        if (twice) {
+            __syncthreads();
+            if (tid < S) {
+                const Range x = f.ranges[64 + 2 * tid], y = f.ranges[65 + 2 * tid];
+                f.ranges[tid] = Range{x.mass + y.mass, x.kept | y.kept, x.ties + y.ties};
+            }
         }
         __syncthreads();
         const int q = max(0, pick_range(f.ranges, S, tie_weight, d));
@@ -1054,7 +1075,7 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
         const double w = f.weight[at];
         fn(w > 0.0, at == end, w);
     };
-    const int token = locate(z, item, begin, stop, tie_weight, d, f.ranges);
+    const int token = locate<uint16_t, 4>(z, item, begin, stop, tie_weight, d, f.ranges);
     if (tid == 0) {
         a.token[row] = token;
         if (a.logp) a.logp[row] = (float)(((double)bf16_bits_to_f32(z[token]) - zmax) / t - log(all));
@@ -1072,12 +1093,12 @@ int64_t sample_bytes(const SampleArgs &a, bool bf16) {
 
 hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t st) {
     if (!bf16) {
-        sample_fine_kernel<float><<<a.rows, kThreads, 0, st>>>(a);
+        sample_fine_kernel<float, false><<<a.rows, kThreads, 0, st>>>(a);
         return hipGetLastError();
     }
     const Parts p = parts_of(a);
     if (p.count > kMostParts) {                  // (rows of more than 4 million tokens)
-        sample_fine_kernel<uint16_t><<<a.rows, kThreads, 0, st>>>(a);
+        sample_fine_kernel<uint16_t, false><<<a.rows, kThreads, 0, st>>>(a);
         return hipGetLastError();
     }
     if (p.count == 1) {
@@ -1094,7 +1115,7 @@ hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t st) {
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    sample_left_kernel<<<a.rows < kChipUnits ? a.rows : kChipUnits, kThreads, 0, st>>>(a);
+    sample_fine_kernel<uint16_t, true><<<a.rows, kThreads, 0, st>>>(a);
     return hipGetLastError();
 }
 
