@@ -1,117 +1,491 @@
-// Rows of an embedding table by tokens, and the table's gradient.
+// Rows of an embedding table by tokens, and the table's gradient by sorted tokens.
+//
+// The gradient: tokens are sorted with their positions (in tiles of 4096 in LDS, then up to 64 sorted
+// segments are merged at a time), the sorted list is cut into blocks of equal length, and a wavefront adds
+// the rows of a block, 16 bytes a lane, run by run. A run inside a block goes to the table at once;
+// of one that crosses a border each block leaves a partial row, which a last pass adds in order. So a
+// token that is everywhere is shared by many wavefronts, and the order of additions is the order of
+// the tokens' positions whatever runs when. Bound by memory: 32768 rows of 2048 bf16 are read
+// once, the table's rows are written once.
 #include "rows.hpp"
 #include "tokens_internal.hpp"
+#include "wave_ops.hpp"
 
 namespace olive {
 namespace {
 
-// Wavefront w: token w / chunks, vectors (w % chunks) * per ... of its row.
-template <typename T, int VEC>
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+// ------------------------------------------------------------------------------------ rows
+// Wavefront w: token w / chunks, lots (w % chunks) * per ... of its row.
+template <typename T, bool TAIL>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, int chunks, int per) {
+    constexpr int L = kLot<T>;
     const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)block_index() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t w = (int64_t)block_index() * 4 + wave_index();
     const int64_t t = w / chunks;
     if (t >= a.tokens) return;
-    const int nvec = a.width / VEC, v0 = (int)(w % chunks) * per, v1 = min(v0 + per, nvec);
+    const int begin = (int)(w % chunks) * per, end = min(a.width, begin + per);
     const int id = a.ids[t];
     const bool there = id >= 0 && id < a.vocab;
     const T *src = (const T *)a.table.p + (there ? id : 0) * a.table.st;
     T *dst = (T *)a.out.p + t * a.out.st;
-    for (int v = v0 + lane; v < v1; v += 64) {
-        float x[VEC];
+    for (int i = begin + lane * L; i < end; i += 64 * L) {
+        float x[L];
         if (there) {
-            get_vec<T, VEC>(src + v * VEC, x);
+            if constexpr (TAIL) unpack_lot<T>(load_lot(src, i, end, 0), x);
+            else unpack_lot<T>(read_lot(src + i), x);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) x[j] *= a.scale;
+            for (int j = 0; j < L; ++j) x[j] *= a.scale;
         } else {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) x[j] = id < 0 ? 0.f : __builtin_nanf("");
+            for (int j = 0; j < L; ++j) x[j] = id < 0 ? 0.f : __builtin_nanf("");
         }
-        put_vec<T, VEC>(dst + v * VEC, x);
+        if constexpr (TAIL) store_lot(dst, i, end, pack_lot<T>(x));
+        else write_lot(dst + i, pack_lot<T>(x));
     }
 }
 
-template <typename TT, int VEC>
-__global__ __launch_bounds__(256) void embed_zero_kernel(EmbedArgs a) {
-    const int nvec = a.width / VEC;
-    const float zero[VEC] = {};
-    for (int64_t r = block_index(); r < a.vocab; r += (int64_t)gridDim.x * gridDim.y)
-        for (int v = threadIdx.x; v < nvec; v += 256) put_vec<TT, VEC>((TT *)a.table.p + r * a.table.st + v * VEC, zero);
+// ------------------------------------------------------------------------------------ sort
+constexpr int kTile = 4096, kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kFan = 64;                         // segments that a pass merges into one
+
+// A token's place in the order: its id, `vocab` for those that have no gradient.
+__device__ __forceinline__ uint32_t key_of(const EmbedArgs &a, int id) {
+    return id >= 0 && id < a.vocab ? (uint32_t)id : (uint32_t)a.vocab;
 }
 
-// The wavefront of a token's first occurrence finds the others and adds their rows in order.
-template <typename T, typename TT, int VEC>
-__global__ __launch_bounds__(256) void embed_grad_kernel(EmbedArgs a, int chunks) {
-    const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)block_index() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t t = w / chunks;
-    if (t >= a.tokens) return;
-    const int id = a.ids[t];
-    if (id < 0 || id >= a.vocab) return;
-    for (int64_t s = 0; s < t; s += 64)
-        if (__ballot(s + lane < t && a.ids[s + lane] == id)) return;
-    const int nvec = a.width / VEC, v = (int)(w % chunks) * 64 + lane;
-    float sum[VEC] = {};
-    for (int64_t s = t; s < a.tokens; s += 64) {
-        uint64_t m = __ballot(s + lane < a.tokens && a.ids[s + lane] == id);
-        for (; m; m &= m - 1) {
-            const int64_t r = s + __builtin_ctzll(m);
-            if (v < nvec) {
-                float x[VEC];
-                get_vec<T, VEC>((const T *)a.out.p + r * a.out.st + v * VEC, x);
+// Sorts a tile by 8 bits of the key at a time, stably: a wavefront has 256 tokens, ranks 64 of them at a
+// time by comparing digits (a ballot a bit), and keeps its own counts.
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedArgs a, uint32_t *keys, int32_t *places, int bits) {
+    __shared__ uint32_t key[2][kTile];
+    __shared__ uint16_t place[2][kTile];
+    __shared__ uint32_t count[kSortWaves][256];
+    __shared__ uint32_t join[kSortWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_index();
+    const int first = blockIdx.x * kTile, n = min(kTile, a.tokens - first);
+    for (int i = tid; i < kTile; i += kSortThreads) {
+        key[0][i] = i < n ? key_of(a, a.ids[first + i]) : 0xffffffffu;
+        place[0][i] = (uint16_t)i;
+    }
+    int from = 0;
+    for (int shift = 0; shift < bits; shift += 8, from ^= 1) {
+        for (int i = tid; i < kSortWaves * 256; i += kSortThreads) (&count[0][0])[i] = 0;
+        __syncthreads();
+        uint32_t k[4], rank[4];
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) sum[j] += x[j];
+        for (int r = 0; r < 4; ++r) {
+            k[r] = key[from][wave * 256 + r * 64 + lane];
+            const uint32_t d = k[r] >> shift & 255;
+            uint64_t same = ~0ull;
+#pragma unroll
+            for (int b = 0; b < 8; ++b) {
+                const bool set = d >> b & 1;
+                const uint64_t m = __ballot(set);
+                same &= set ? m : ~m;
+            }
+            const int lead = __builtin_ctzll(same);
+            uint32_t before = 0;
+            if (lane == lead) before = atomicAdd(&count[wave][d], (uint32_t)__popcll(same));
+            rank[r] = __shfl(before, lead) + (uint32_t)__popcll(same & ((1ull << lane) - 1));
+        }
+        __syncthreads();
+        // counts before: of smaller digits, then of the same digit in wavefronts before
+        uint32_t c[4], s = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s += c[i] = count[(tid & 3) * 4 + i][tid >> 2];
+        uint32_t at = wave_scan(s);
+        if (lane == 63) join[wave] = at;
+        __syncthreads();
+        at -= s;
+        for (int i = 0; i < wave; ++i) at += join[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            count[(tid & 3) * 4 + i][tid >> 2] = at;
+            at += c[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const uint32_t to = count[wave][k[r] >> shift & 255] + rank[r];
+            key[from ^ 1][to] = k[r];
+            place[from ^ 1][to] = place[from][wave * 256 + r * 64 + lane];
+        }
+        __syncthreads();
+    }
+    for (int i = tid; i < n; i += kSortThreads) {
+        keys[first + i] = key[from][i];
+        places[first + i] = first + place[from][i];
+    }
+}
+
+// Merges groups of up to kFan sorted segments of `len`: a token moves on by the number of tokens of
+// the group's other segments before it, which is looked up once for a run of equal keys.
+__global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(EmbedArgs a, const uint32_t *keys,
+                                                                   const int32_t *places, uint32_t *keys_to,
+                                                                   int32_t *places_to, int64_t len) {
+    __shared__ int32_t moves[kTile];
+    __shared__ int32_t join[kSortWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_index();
+    const int64_t first = (int64_t)blockIdx.x * kTile, group = first / (len * kFan) * (len * kFan);
+    const int n = (int)min((int64_t)kTile, a.tokens - first);
+    const int own = (int)((first - group) / len);
+    const int segments = (int)min((int64_t)kFan, (a.tokens - group + len - 1) / len);
+    // 4 tokens in a row a thread; the first of a run within this workgroup's looks up
+    uint32_t k[4];
+    int head[4], newest = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int p = tid * 4 + i;
+        k[i] = p < n ? keys[first + p] : 0xffffffffu;
+    }
+    const uint32_t before = tid == 0 || tid * 4 >= n ? ~k[0] : keys[first + tid * 4 - 1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int p = tid * 4 + i;
+        if (p < n && k[i] != (i ? k[i - 1] : before)) {
+            newest = p;
+            int move = 0;
+            for (int s0 = 0; s0 < segments; s0 += 4) {       // 4 searches side by side
+                int64_t start[4];
+                int lo[4], left[4];
+                uint32_t want[4];
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const bool there = s0 + s < segments && s0 + s != own;
+                    start[s] = group + (there ? s0 + s : own) * len;
+                    lo[s] = 0;
+                    left[s] = there ? (int)min(len, a.tokens - start[s]) : 0;
+                    want[s] = k[i] + (s0 + s < own);         // (of the segments before also the equal ones)
+                }
+                while (left[0] | left[1] | left[2] | left[3]) {
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        const int half = left[s] >> 1;
+                        const bool less = left[s] > 0 && keys[start[s] + lo[s] + half] < want[s];
+                        lo[s] = less ? lo[s] + half + 1 : lo[s];
+                        left[s] = less ? left[s] - half - 1 : half;
+                    }
+                }
+                move += lo[0] + lo[1] + lo[2] + lo[3];
+            }
+            moves[p] = move;
+        }
+        head[i] = newest;
+    }
+    // the latest first of a run at or before each token
+    uint32_t seen = (uint32_t)newest;
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t u = (uint32_t)__shfl_up((int)seen, o);
+        if (lane >= o) seen = max(seen, u);
+    }
+    if (lane == 63) join[wave] = (int)seen;
+    __syncthreads();
+    int prev = __shfl_up((int)seen, 1);
+    if (lane == 0) prev = 0;
+    for (int i = 0; i < wave; ++i) prev = max(prev, join[i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int p = tid * 4 + i;
+        if (p >= n) break;
+        const int64_t to = first + p - own * len + moves[max(head[i], prev)];
+        keys_to[to] = k[i];
+        places_to[to] = places[first + p];
+    }
+}
+
+// ------------------------------------------------------------------------------------ sums
+// N elements of TT at any alignment.
+template <typename TT, int N>
+struct Piece {
+    static constexpr int kWords = N * (int)sizeof(TT) / 4;
+    struct __attribute__((packed, aligned(sizeof(TT)))) Loose { uint32_t w[kWords]; };
+    static __device__ __forceinline__ void get(const TT *p, float (&x)[N]) {
+        const Loose u = *(const Loose *)p;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if constexpr (sizeof(TT) == 4) x[j] = __uint_as_float(u.w[j]);
+            else x[j] = __uint_as_float(j & 1 ? u.w[j >> 1] & 0xffff0000u : u.w[j >> 1] << 16);
+        }
+    }
+    static __device__ __forceinline__ void put(TT *p, const float (&x)[N]) {
+        Loose u;
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) {
+            if constexpr (sizeof(TT) == 4) u.w[j] = __float_as_uint(x[j]);
+            else u.w[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
+        }
+        *(Loose *)p = u;
+    }
+};
+
+// What a lane does with the N columns from c on of a table's row: scale * sum (+ what is there).
+template <typename TT, int N, bool TAIL>
+__device__ __forceinline__ void to_table(const EmbedArgs &a, uint32_t id, int c, const float (&sum)[N]) {
+    TT *row = (TT *)a.table.p + id * a.table.st;
+    if (!TAIL || c + N <= a.width) {
+        if (c >= a.width) return;
+        float x[N] = {};
+        if (a.accumulate) Piece<TT, N>::get(row + c, x);
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = fmaf(sum[j], a.scale, x[j]);
+        Piece<TT, N>::put(row + c, x);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < N - 1; ++j)
+        if (c + j < a.width)
+            row[c + j] = RowElem<TT>::put(fmaf(sum[j], a.scale, a.accumulate ? RowElem<TT>::get(row[c + j]) : 0.f));
+}
+
+template <typename T, bool TAIL>
+__device__ __forceinline__ Lot load_grad(const EmbedArgs &a, int place, int c) {
+    const T *row = (const T *)a.out.p + place * a.out.st;
+    if constexpr (TAIL) return load_lot(row, c, a.width, 0);
+    if (c < a.width) return read_lot(row + c);
+    return Lot{{0, 0, 0, 0}};
+}
+
+struct Sorted {
+    const uint32_t *keys;
+    const int32_t *places;
+    float *part;                                 // [blocks][2][width rounded up to a lane's columns]
+    int rows, blocks, chunks;                    // sorted tokens a block; columns' chunks
+    int64_t sums;                                // workgroups of sums, before those that write zeros
+};
+
+// A wavefront: the sums of one block's runs in one chunk of the columns. Behind them, wavefronts that
+// write zeros into the rows of 64 ids each that do not occur.
+template <typename T, typename TT, bool TAIL>
+__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, Sorted s) {
+    constexpr int L = kLot<T>;
+    const int lane = threadIdx.x & 63;
+    const int64_t g = block_index();
+    if (g >= s.sums) {
+        const int64_t r0 = ((g - s.sums) * 4 + wave_index()) * 64, r = r0 + lane;
+        if (r0 >= a.vocab) return;
+        int lo = 0, left = a.tokens;
+        while (left > 0) {
+            const int half = left >> 1;
+            const bool less = s.keys[lo + half] < (uint32_t)r;
+            lo = less ? lo + half + 1 : lo;
+            left = less ? left - half - 1 : half;
+        }
+        uint64_t absent = __ballot(r < a.vocab && !(lo < a.tokens && s.keys[lo] == (uint32_t)r));
+        constexpr int N = 16 / (int)sizeof(TT);
+        for (; absent; absent &= absent - 1) {
+            TT *row = (TT *)a.table.p + (r0 + __builtin_ctzll(absent)) * a.table.st;
+            for (int c = lane * N; c < a.width; c += 64 * N) {
+                if (c + N <= a.width) {
+                    write_lot(row + c, Lot{{0, 0, 0, 0}});
+                } else {
+                    for (int j = c; j < a.width; ++j) row[j] = (TT)0;
+                }
+            }
+        }
+        return;
+    }
+    const int64_t w = g * 4 + wave_index();
+    const int b = (int)(w / s.chunks), c = ((int)(w % s.chunks) * 64 + lane) * L;
+    if (b >= s.blocks) return;
+    const int64_t p0 = (int64_t)b * s.rows;
+    const int n = (int)min((int64_t)s.rows, a.tokens - p0);
+    const uint32_t key = lane < n ? s.keys[p0 + lane] : 0xffffffffu;
+    const int place = lane < n ? s.places[p0 + lane] : 0;
+    const uint32_t prev = p0 > 0 ? s.keys[p0 - 1] : 0xffffffffu, next = p0 + n < a.tokens ? s.keys[p0 + n] : 0xffffffffu;
+    const int there = __popcll(__ballot(key < (uint32_t)a.vocab));       // (the others are at the end)
+    if (there == 0) return;
+    constexpr int kAhead = 8;
+    float sum[L] = {};
+    uint32_t run = wave_read(key, 0);
+    const auto leave = [&](bool last) {
+        const bool from_before = run == prev, goes_on = last && run == next;
+        if (from_before || goes_on) {
+            float *to = s.part + ((int64_t)b * 2 + !from_before) * s.chunks * 64 * L + c;
+            Piece<float, L>::put(to, sum);
+        } else {
+            to_table<TT, L, TAIL>(a, run, c, sum);
+        }
+    };
+#pragma unroll 1
+    for (int e0 = 0; e0 < there; e0 += kAhead) {
+        Lot x[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) x[j] = load_grad<T, TAIL>(a, wave_read(place, min(e0 + j, there - 1)), c);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (e0 + j >= there) break;
+            const uint32_t k = wave_read(key, e0 + j);
+            float v[L];
+            unpack_lot<T>(x[j], v);
+            if (k != run) {
+                leave(false);
+                run = k;
+#pragma unroll
+                for (int i = 0; i < L; ++i) sum[i] = v[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < L; ++i) sum[i] += v[i];
             }
         }
     }
-    if (v >= nvec) return;
-    TT *dst = (TT *)a.table.p + id * a.table.st + v * VEC;
-    float old[VEC] = {};
-    if (a.accumulate) get_vec<TT, VEC>(dst, old);
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) sum[j] = fmaf(sum[j], a.scale, old[j]);
-    put_vec<TT, VEC>(dst, sum);
+    leave(there == n);
 }
 
-template <typename T, int VEC>
+// The runs that cross a border: the block where one begins adds what the blocks have left of it.
+template <typename T, typename TT, bool TAIL>
+__global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a, Sorted s) {
+    constexpr int L = kLot<T>;
+    const int64_t g = block_index();
+    const int b = (int)(g / s.chunks), lane = threadIdx.x & 63, wave = wave_index();
+    const int c = ((int)(g % s.chunks) * 64 + lane) * L;
+    if (b + 1 >= s.blocks) return;
+    const int64_t p0 = (int64_t)b * s.rows, p1 = p0 + s.rows;
+    const uint32_t run = s.keys[p1 - 1];
+    if (run >= (uint32_t)a.vocab || s.keys[p1] != run || (p0 > 0 && s.keys[p0 - 1] == run)) return;
+    // blocks after this one whose first token is of the run
+    int more = 1;
+    for (int64_t i = b + 2; i < s.blocks; i += 64) {
+        const uint64_t in = __ballot(i + lane < s.blocks && s.keys[(i + lane) * s.rows] == run);
+        more += __popcll(in);
+        if (in != ~0ull) break;
+    }
+    const auto part = [&](int64_t block, int slot) { return s.part + (block * 2 + slot) * s.chunks * 64 * L + c; };
+    float sum[L] = {};
+    if (wave == 0) Piece<float, L>::get(part(b, 1), sum);
+#pragma unroll 4
+    for (int i = wave; i < more; i += 4) {
+        float x[L];
+        Piece<float, L>::get(part(b + 1 + i, 0), x);
+#pragma unroll
+        for (int j = 0; j < L; ++j) sum[j] += x[j];
+    }
+    __shared__ float join[3][64][L + 1];
+    if (wave)
+#pragma unroll
+        for (int j = 0; j < L; ++j) join[wave - 1][lane][j] = sum[j];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+#pragma unroll
+        for (int j = 0; j < L; ++j) sum[j] += join[i][lane][j];
+    to_table<TT, L, TAIL>(a, run, c, sum);
+}
+
+// Few tokens: the wavefront of a token's first occurrence finds the others and adds their rows in order.
+template <typename TT>
+__global__ __launch_bounds__(256) void embed_zero_kernel(EmbedArgs a) {
+    constexpr int N = 16 / (int)sizeof(TT);
+    for (int64_t r = blockIdx.x; r < a.vocab; r += gridDim.x) {
+        TT *row = (TT *)a.table.p + r * a.table.st;
+        for (int c = threadIdx.x * N; c < a.width; c += 256 * N) store_lot(row, c, a.width, Lot{{0, 0, 0, 0}});
+    }
+}
+template <typename T, typename TT, bool TAIL>
+__global__ __launch_bounds__(256) void embed_few_kernel(EmbedArgs a, int chunks) {
+    constexpr int L = kLot<T>;
+    const int lane = threadIdx.x & 63;
+    const int64_t w = (int64_t)block_index() * 4 + wave_index();
+    const int t = (int)(w / chunks), c = ((int)(w % chunks) * 64 + lane) * L;
+    if (t >= a.tokens) return;
+    const int id = a.ids[t];
+    if (id < 0 || id >= a.vocab) return;
+    for (int s = 0; s < t; s += 64)
+        if (__ballot(s + lane < t && a.ids[s + lane] == id)) return;
+    float sum[L] = {};
+    for (int s = t; s < a.tokens; s += 64) {
+        uint64_t m = __ballot(s + lane < a.tokens && a.ids[s + lane] == id);
+        for (; m; m &= m - 1) {
+            float x[L];
+            unpack_lot<T>(load_grad<T, TAIL>(a, s + __builtin_ctzll(m), c), x);
+#pragma unroll
+            for (int j = 0; j < L; ++j) sum[j] += x[j];
+        }
+    }
+    to_table<TT, L, TAIL>(a, (uint32_t)id, c, sum);
+}
+
+// ---------------------------------------------------------------------------------- launches
+constexpr int kFew = 1024;                       // tokens up to which the first occurrences are looked for
+
+int block_rows(int64_t tokens) { return tokens >= 32768 ? 64 : tokens >= 8192 ? 32 : 16; }
+int64_t up16(int64_t n) { return (n + 15) & ~(int64_t)15; }
+
+struct Layout { int64_t keys[2], places[2], part, bytes; };
+
+Layout layout_of(const EmbedArgs &a) {
+    Layout l{};
+    if (a.tokens <= kFew) return l;
+    const int64_t n = up16((int64_t)a.tokens * 4), rows = block_rows(a.tokens);
+    const int64_t blocks = (a.tokens + rows - 1) / rows, columns = ((int64_t)a.width + 511) / 512 * 512;
+    l.keys[0] = 0, l.places[0] = n, l.keys[1] = 2 * n, l.places[1] = 3 * n;
+    l.part = 4 * n;
+    l.bytes = l.part + blocks * 2 * columns * (int64_t)sizeof(float);
+    return l;
+}
+
+template <typename T>
 hipError_t forward(const EmbedArgs &a, hipStream_t st) {
-    const int nvec = a.width / VEC;
-    const int per = 64, chunks = (nvec + per - 1) / per;
-    embed_kernel<T, VEC><<<grid_of(((int64_t)a.tokens * chunks + 3) / 4), 256, 0, st>>>(a, chunks, per);
+    constexpr int per = 64 * kLot<T>;
+    const int chunks = (a.width + per - 1) / per;
+    const dim3 grid = grid_of(((int64_t)a.tokens * chunks + 3) / 4);
+    if (a.width % kLot<T>) embed_kernel<T, true><<<grid, 256, 0, st>>>(a, chunks, per);
+    else embed_kernel<T, false><<<grid, 256, 0, st>>>(a, chunks, per);
     return hipGetLastError();
 }
 
-template <typename T, typename TT, int VEC>
+template <typename T, typename TT, bool TAIL>
 hipError_t backward(const EmbedArgs &a, hipStream_t st) {
-    if (!a.accumulate) {
-        embed_zero_kernel<TT, VEC><<<a.vocab < 4096 ? a.vocab : 4096, 256, 0, st>>>(a);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess || a.tokens == 0) return e;
+    const int per = 64 * kLot<T>, chunks = (a.width + per - 1) / per;
+    if (a.tokens <= kFew) {
+        if (!a.accumulate) {
+            embed_zero_kernel<TT><<<a.vocab < 8192 ? a.vocab : 8192, 256, 0, st>>>(a);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess || a.tokens == 0) return e;
+        }
+        embed_few_kernel<T, TT, TAIL><<<grid_of(((int64_t)a.tokens * chunks + 3) / 4), 256, 0, st>>>(a, chunks);
+        return hipGetLastError();
     }
-    const int chunks = (a.width / VEC + 63) / 64;
-    embed_grad_kernel<T, TT, VEC><<<grid_of(((int64_t)a.tokens * chunks + 3) / 4), 256, 0, st>>>(a, chunks);
+    const Layout l = layout_of(a);
+    uint32_t *keys[2] = {(uint32_t *)(a.work + l.keys[0]), (uint32_t *)(a.work + l.keys[1])};
+    int32_t *places[2] = {(int32_t *)(a.work + l.places[0]), (int32_t *)(a.work + l.places[1])};
+    int bits = 0;
+    while (((int64_t)a.vocab >> bits) > 0) ++bits;
+    const int tiles = (a.tokens + kTile - 1) / kTile;
+    embed_sort_kernel<<<tiles, kSortThreads, 0, st>>>(a, keys[0], places[0], bits);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    int at = 0;
+    for (int64_t len = kTile; len < a.tokens; len *= kFan, at ^= 1) {
+        embed_merge_kernel<<<tiles, kSortThreads, 0, st>>>(a, keys[at], places[at], keys[at ^ 1], places[at ^ 1], len);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    Sorted s{};
+    s.keys = keys[at];
+    s.places = places[at];
+    s.part = (float *)(a.work + l.part);
+    s.rows = block_rows(a.tokens);
+    s.blocks = (a.tokens + s.rows - 1) / s.rows;
+    s.chunks = chunks;
+    s.sums = ((int64_t)s.blocks * chunks + 3) / 4;
+    const int64_t zeros = a.accumulate ? 0 : ((int64_t)a.vocab + 255) / 256;
+    embed_sum_kernel<T, TT, TAIL><<<grid_of(s.sums + zeros), 256, 0, st>>>(a, s);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    embed_join_kernel<T, TT, TAIL><<<grid_of((int64_t)s.blocks * chunks), 256, 0, st>>>(a, s);
     return hipGetLastError();
 }
 
 template <typename T, typename TT>
 hipError_t backward(const EmbedArgs &a, hipStream_t st) {
-    constexpr int WIDE = 4;
-    if (a.width % WIDE == 0 && rows_aligned({a.out}, WIDE * sizeof(T), sizeof(T)) &&
-        rows_aligned({a.table}, WIDE * sizeof(TT), sizeof(TT)))
-        return backward<T, TT, WIDE>(a, st);
-    return backward<T, TT, 1>(a, st);
-}
-
-template <typename T>
-hipError_t forward(const EmbedArgs &a, hipStream_t st) {
-    constexpr int WIDE = 16 / sizeof(T);
-    if (a.width % WIDE == 0 && rows_aligned({a.table, a.out}, 16, sizeof(T))) return forward<T, WIDE>(a, st);
-    return forward<T, 1>(a, st);
+    return a.width % kLot<T> ? backward<T, TT, true>(a, st) : backward<T, TT, false>(a, st);
 }
 
 }  // namespace
 
-int64_t embed_backward_bytes(const EmbedArgs &) { return 0; }
+int64_t embed_backward_bytes(const EmbedArgs &a) { return layout_of(a).bytes; }
 
 hipError_t launch_embed(const EmbedArgs &a, bool bf16, hipStream_t st) {
     return bf16 ? forward<uint16_t>(a, st) : forward<float>(a, st);

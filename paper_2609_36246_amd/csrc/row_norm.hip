@@ -1,9 +1,12 @@
 // Layer norm and RMS norm of rows, with the residual added before, and their backward.
 //
-// A row lies in the registers of WAVES wavefronts, VEC * NV elements a lane, so that it is read
-// once: mean and mean square of what is left are two sums over the registers.
+// A row lies in the registers of WAVES wavefronts, NV vectors of 16 bytes a lane, so that it is read
+// once: mean and mean square of what is left are sums over the registers. One wavefront holds up to
+// 4096 bf16 elements (backward 2048, with the sums of the weight's gradients beside them), so that most
+// rows need no barrier; what is read of a row is asked for at once.
 #include "rows.hpp"
 #include "tokens_internal.hpp"
+#include "wave_ops.hpp"
 
 namespace olive {
 namespace {
@@ -11,8 +14,7 @@ namespace {
 // The sum over a row's lanes, the same in all of them. `join`: LDS of the row, WAVES values.
 template <int WAVES>
 __device__ __forceinline__ float row_total(float v, float *join) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    v = wave_sum(v);
     if constexpr (WAVES > 1) {
         __syncthreads();                     // (the values of the sum before are read)
         if ((threadIdx.x & 63) == 0) join[threadIdx.x >> 6] = v;
@@ -31,37 +33,42 @@ __device__ __forceinline__ float inverse_root(float m) {
     return __builtin_amdgcn_rsqf(small ? m * 0x1p100f : m) * (small ? 0x1p50f : 1.f);
 }
 
-constexpr int threads_of(int waves) { return waves > 4 ? 64 * waves : 256; }
+// Rows of one wavefront share a workgroup of four; else a workgroup has one row.
+constexpr int threads_of(int waves) { return waves == 1 ? 256 : 64 * waves; }
 
-template <typename T, int VEC, int NV, int WAVES>
+// TAIL: the width is no multiple of a vector (any alignment is read the same).
+template <typename T, int NV, int WAVES, bool TAIL>
 struct Rows {
-    static constexpr int kThreads = threads_of(WAVES);
-    static constexpr int kRows = kThreads / (64 * WAVES);      // rows of a workgroup at a time
+    static constexpr int VEC = 16 / (int)sizeof(T);
+    static constexpr int kRows = threads_of(WAVES) / (64 * WAVES);   // rows of a workgroup at a time
+    using Vec = Lot;
     static __device__ __forceinline__ int lane() { return threadIdx.x % (64 * WAVES); }
-    static __device__ __forceinline__ int sub() { return threadIdx.x / (64 * WAVES); }
+    static __device__ __forceinline__ int sub() {
+        return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WAVES;
+    }
+    static __device__ __forceinline__ int vec(int i) { return lane() + 64 * WAVES * i; }
 
-    // elements of a row that this lane holds (0 past its end)
-    static __device__ __forceinline__ void load(const char *p, int64_t at, int nvec, float (&x)[NV][VEC]) {
+    static __device__ __forceinline__ void load(const char *p, int64_t at, int width, Vec (&x)[NV]) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int v = lane() + 64 * WAVES * i;
-            if (v < nvec) {
-                get_vec<T, VEC>((const T *)p + at + v * VEC, x[i]);
+            if constexpr (TAIL) {
+                x[i] = load_lot((const T *)p + at, vec(i) * VEC, width, 0);
             } else {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) x[i][j] = 0.f;
+                x[i] = Lot{{0, 0, 0, 0}};
+                if (vec(i) * VEC < width) x[i] = read_lot((const T *)p + at + vec(i) * VEC);
             }
         }
     }
-    static __device__ __forceinline__ void store(char *p, int64_t at, int nvec, const float (&x)[NV][VEC]) {
+    static __device__ __forceinline__ void store(char *p, int64_t at, int width, const float (&x)[NV][VEC]) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int v = lane() + 64 * WAVES * i;
-            if (v < nvec) put_vec<T, VEC>((T *)p + at + v * VEC, x[i]);
-        }
+        for (int i = 0; i < NV; ++i) store(p, at, width, i, pack_lot<T>(x[i]));
     }
-    // h - mean (layer norm) in place; the inverse root of its mean square
-    static __device__ __forceinline__ float normed(const NormArgs &a, int nvec, float (&h)[NV][VEC], float *join) {
+    static __device__ __forceinline__ void store(char *p, int64_t at, int width, int i, const Lot &x) {
+        if constexpr (TAIL) store_lot((T *)p + at, vec(i) * VEC, width, x);
+        else if (vec(i) * VEC < width) write_lot((T *)p + at + vec(i) * VEC, x);
+    }
+    // h - mean (layer norm) in place, 0 past the row's end; the inverse root of its mean square
+    static __device__ __forceinline__ float normed(const NormArgs &a, float (&h)[NV][VEC], float *join) {
         if (a.layer) {
             float s = 0.f;
 #pragma unroll
@@ -72,7 +79,7 @@ struct Rows {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) h[i][j] = lane() + 64 * WAVES * i < nvec ? h[i][j] - mean : 0.f;
+                for (int j = 0; j < VEC; ++j) h[i][j] = vec(i) * VEC + j < a.width ? h[i][j] - mean : 0.f;
         }
         float s = 0.f;
 #pragma unroll
@@ -83,138 +90,222 @@ struct Rows {
     }
 };
 
-template <typename T, int VEC, int NV, int WAVES>
+template <typename T, int NV, int WAVES, bool TAIL>
 __global__ __launch_bounds__(threads_of(WAVES)) void norm_kernel(NormArgs a) {
-    using R = Rows<T, VEC, NV, WAVES>;
+    using R = Rows<T, NV, WAVES, TAIL>;
+    constexpr int VEC = R::VEC;
     __shared__ float join[WAVES];
-    const int nvec = a.width / VEC;
+    const int width = a.width;
     for (int64_t r = (int64_t)blockIdx.x * R::kRows + R::sub(); r < a.rows; r += (int64_t)gridDim.x * R::kRows) {
-        float h[NV][VEC], w[NV][VEC];
-        R::load(a.x.p, r * a.x.st, nvec, h);
+        float h[NV][VEC];
+        typename R::Vec x[NV], y[NV], w[NV];
+        R::load(a.x.p, r * a.x.st, width, x);
+        if (a.res.p) R::load(a.res.p, r * a.res.st, width, y);
+        if (a.weight) R::load((const char *)a.weight, 0, width, w);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) unpack_lot<T>(x[i], h[i]);
         if (a.res.p) {
-            R::load(a.res.p, r * a.res.st, nvec, w);
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < NV; ++i) {
+                float t[VEC];
+                unpack_lot<T>(y[i], t);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) h[i][j] = RowElem<T>::get(RowElem<T>::put(h[i][j] + w[i][j]));
+                for (int j = 0; j < VEC; ++j) t[j] += h[i][j];
+                x[i] = pack_lot<T>(t);
+                unpack_lot<T>(x[i], h[i]);
+            }
         }
-        if (a.sum.p) R::store(a.sum.p, r * a.sum.st, nvec, h);
-        const float rr = R::normed(a, nvec, h, join);
-        if (a.weight) R::load((const char *)a.weight, 0, nvec, w);
+        if (a.sum.p) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) h[i][j] = h[i][j] * rr * (a.weight ? w[i][j] : 1.f);
-        if (a.bias) {
-            R::load((const char *)a.bias, 0, nvec, w);
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) h[i][j] += w[i][j];
+            for (int i = 0; i < NV; ++i) R::store(a.sum.p, r * a.sum.st, width, i, x[i]);
         }
-        R::store(a.out.p, r * a.out.st, nvec, h);
+        const float rr = R::normed(a, h, join);
+        if (a.bias) R::load((const char *)a.bias, 0, width, y);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float u[VEC], v[VEC];
+            if (a.weight) unpack_lot<T>(w[i], u);
+            if (a.bias) unpack_lot<T>(y[i], v);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                h[i][j] = h[i][j] * rr * (a.weight ? u[j] : 1.f);
+                if (a.bias) h[i][j] += v[j];
+            }
+        }
+        R::store(a.out.p, r * a.out.st, width, h);
     }
 }
 
 // Persistent workgroups over rows; a lane sums its columns' weight and bias gradients over its
-// rows, and each group of WAVES wavefronts writes one partial row of both.
-template <typename T, int VEC, int NV, int WAVES>
+// rows, the workgroup joins them in a fixed order and writes one partial row of both.
+template <typename T, int NV, int WAVES, bool TAIL, bool BIAS>
 __global__ __launch_bounds__(threads_of(WAVES)) void norm_backward_kernel(NormArgs a) {
-    using R = Rows<T, VEC, NV, WAVES>;
+    using R = Rows<T, NV, WAVES, TAIL>;
+    constexpr int VEC = R::VEC;
     __shared__ float join[WAVES];
-    const int nvec = a.width / VEC;
-    const float inv = 1.f / (float)a.width;
-    float gw[NV][VEC] = {}, gb[NV][VEC] = {};
+    const int width = a.width;
+    const float inv = 1.f / (float)width;
+    float gw[NV][VEC] = {}, gb[BIAS ? NV : 1][VEC] = {};
     for (int64_t r = (int64_t)blockIdx.x * R::kRows + R::sub(); r < a.rows; r += (int64_t)gridDim.x * R::kRows) {
-        float h[NV][VEC], g[NV][VEC], w[NV][VEC];
-        R::load(a.x.p, r * a.x.st, nvec, h);
-        R::load(a.sum.p, r * a.sum.st, nvec, g);
-        if (a.weight) R::load((const char *)a.weight, 0, nvec, w);
-        const float rr = R::normed(a, nvec, h, join);
+        float h[NV][VEC], g[NV][VEC];
+        typename R::Vec x[NV], y[NV], z[NV], w[NV];
+        R::load(a.x.p, r * a.x.st, width, x);
+        R::load(a.sum.p, r * a.sum.st, width, y);
+        if (a.res.p) R::load(a.res.p, r * a.res.st, width, z);
+        if (a.weight) R::load((const char *)a.weight, 0, width, w);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) unpack_lot<T>(x[i], h[i]);
+        const float rr = R::normed(a, h, join);
         float sg = 0.f, sn = 0.f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+            float u[VEC];
+            unpack_lot<T>(y[i], g[i]);
+            if (a.weight) unpack_lot<T>(w[i], u);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 h[i][j] *= rr;
-                if (R::lane() + 64 * WAVES * i < nvec) {
-                    gw[i][j] = fmaf(g[i][j], h[i][j], gw[i][j]);
-                    gb[i][j] += g[i][j];
-                }
-                if (a.weight) g[i][j] *= w[i][j];
+                // (past the row's end x = y = 0, and eps may be 0)
+                if (R::vec(i) * VEC + j < width) gw[i][j] = fmaf(g[i][j], h[i][j], gw[i][j]);
+                if constexpr (BIAS) gb[i][j] += g[i][j];
+                if (a.weight) g[i][j] *= u[j];
                 sg += g[i][j];
                 sn = fmaf(g[i][j], h[i][j], sn);
             }
+        }
         sn = row_total<WAVES>(sn, join) * inv;
         sg = a.layer ? row_total<WAVES>(sg, join) * inv : 0.f;
-        if (a.res.p) R::load(a.res.p, r * a.res.st, nvec, w);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+            float u[VEC];
+            if (a.res.p) unpack_lot<T>(z[i], u);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 g[i][j] = rr * (g[i][j] - h[i][j] * sn - sg);
-                if (a.res.p) g[i][j] += w[i][j];
-            }
-        R::store(a.out.p, r * a.out.st, nvec, g);
-    }
-    if (!a.gw && !a.gb) return;
-    float *part = a.part + ((int64_t)blockIdx.x * R::kRows + R::sub()) * 2 * a.width;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int v = R::lane() + 64 * WAVES * i;
-        if (v < nvec) {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                part[v * VEC + j] = gw[i][j];
-                part[a.width + v * VEC + j] = gb[i][j];
+                if (a.res.p) g[i][j] += u[j];
             }
         }
+        R::store(a.out.p, r * a.out.st, width, g);
+    }
+    if (!a.gw && !a.gb) return;
+    float *part = a.part + (int64_t)blockIdx.x * 2 * width;
+    const auto put = [&](const float (&s)[VEC], int i, float *to) {
+        float v[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) v[j] = s[j];
+        if constexpr (R::kRows > 1) {
+            __shared__ float rows[R::kRows][64 * VEC];
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) rows[R::sub()][j * 64 + R::lane()] = v[j];
+            __syncthreads();
+            if (R::sub()) return;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+#pragma unroll
+                for (int k = 1; k < R::kRows; ++k) v[j] += rows[k][j * 64 + R::lane()];
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+            if (R::vec(i) * VEC + j < width) to[R::vec(i) * VEC + j] = v[j];
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        put(gw[i], i, part);
+        if constexpr (BIAS) put(gb[i], i, part + width);
     }
 }
 
-__global__ __launch_bounds__(256) void norm_weight_kernel(NormArgs a, int parts) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= 2 * a.width) return;
+// Sums the partial rows: 64 columns a workgroup, every 16th row a wavefront.
+constexpr int kJoinWaves = 16;
+
+__global__ __launch_bounds__(64 * kJoinWaves) void norm_weight_kernel(NormArgs a, int parts) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+    float *out = blockIdx.y ? a.gb : a.gw;
+    if (!out) return;
+    const float *from = a.part + (int64_t)blockIdx.y * a.width + c;
     float s = 0.f;
-    for (int i = 0; i < parts; ++i) s += a.part[(int64_t)i * 2 * a.width + c];
-    float *out = c < a.width ? a.gw : a.gb;
-    if (out) out[c < a.width ? c : c - a.width] = s;
+    if (c < a.width)
+#pragma unroll 8
+        for (int i = wave; i < parts; i += kJoinWaves) s += from[(int64_t)i * 2 * a.width];
+    __shared__ float join[kJoinWaves][64];
+    join[wave][lane] = s;
+    __syncthreads();
+    if (wave || c >= a.width) return;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kJoinWaves; ++i) s += join[i][lane];
+    out[c] = s;
 }
 
-template <typename T, int VEC, int NV, int WAVES>
-hipError_t go(const NormArgs &a, bool backward, hipStream_t st) {
-    using R = Rows<T, VEC, NV, WAVES>;
+template <typename T, int NV, int WAVES>
+hipError_t forward(const NormArgs &a, hipStream_t st) {
+    using R = Rows<T, NV, WAVES, false>;
     const int64_t groups = ((int64_t)a.rows + R::kRows - 1) / R::kRows;
-    if (!backward) {
-        norm_kernel<T, VEC, NV, WAVES><<<(int)(groups < 2048 ? groups : 2048), R::kThreads, 0, st>>>(a);
-        return hipGetLastError();
-    }
-    const int most = kNormBlocks / R::kRows, blocks = (int)(groups < most ? (groups > 0 ? groups : 1) : most);
-    norm_backward_kernel<T, VEC, NV, WAVES><<<blocks, R::kThreads, 0, st>>>(a);
+    const int blocks = (int)(groups < (1 << 20) ? groups : 1 << 20);
+    if (a.width % R::VEC) norm_kernel<T, NV, WAVES, true><<<blocks, threads_of(WAVES), 0, st>>>(a);
+    else norm_kernel<T, NV, WAVES, false><<<blocks, threads_of(WAVES), 0, st>>>(a);
+    return hipGetLastError();
+}
+
+// Wavefronts of a row in the backward, and its workgroups at most: 8 wavefronts a compute unit.
+int waves_of(int width) {
+    int w = 1;
+    while (w * 2048 < width) w *= 2;             // (32 values of each kind a lane)
+    return w;
+}
+int blocks_of(int width) { return width <= 2048 ? 512 : 2048 / waves_of(width); }
+
+template <typename T, int NV, int WAVES>
+hipError_t backward(const NormArgs &a, hipStream_t st) {
+    using R = Rows<T, NV, WAVES, false>;
+    const int64_t groups = ((int64_t)a.rows + R::kRows - 1) / R::kRows, most = blocks_of(a.width);
+    const int blocks = (int)(groups < most ? (groups > 0 ? groups : 1) : most);
+    const auto run = [&](auto kernel) { kernel<<<blocks, threads_of(WAVES), 0, st>>>(a); };
+    if (a.width % R::VEC) run(norm_backward_kernel<T, NV, WAVES, true, true>);       // (bias or not)
+    else if (a.gb) run(norm_backward_kernel<T, NV, WAVES, false, true>);
+    else run(norm_backward_kernel<T, NV, WAVES, false, false>);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || (!a.gw && !a.gb)) return e;
-    norm_weight_kernel<<<(2 * a.width + 255) / 256, 256, 0, st>>>(a, blocks * R::kRows);
+    norm_weight_kernel<<<dim3((a.width + 63) / 64, a.gb ? 2 : 1), 64 * kJoinWaves, 0, st>>>(a, blocks);
     return hipGetLastError();
 }
 
 template <typename T>
-hipError_t pick(const NormArgs &a, bool backward, hipStream_t st) {
-    constexpr int WIDE = 16 / sizeof(T);
-    const bool wide = a.width % WIDE == 0 && rows_aligned({a.x, a.res, a.out, a.sum}, 16, sizeof(T)) &&
-                      (((uintptr_t)a.weight | (uintptr_t)a.bias) & 15) == 0;
-    if (wide && a.width <= 64 * WIDE * 4) return go<T, WIDE, 4, 1>(a, backward, st);
-    if (wide) return go<T, WIDE, 16 / WIDE, 16>(a, backward, st);
-    if (a.width <= 64 * 4 * 4) return go<T, 1, 4, 4>(a, backward, st);
-    return go<T, 1, 16, 16>(a, backward, st);
+hipError_t pick_forward(const NormArgs &a, hipStream_t st) {
+    constexpr int one = 64 * 16 / (int)sizeof(T);                // elements of a vector a lane
+    if (a.width <= one) return forward<T, 1, 1>(a, st);
+    if (a.width <= 2 * one) return forward<T, 2, 1>(a, st);
+    if (a.width <= 4 * one) return forward<T, 4, 1>(a, st);
+    if (a.width <= 8 * one) return forward<T, 8, 1>(a, st);
+    if (a.width <= 16 * one) return forward<T, 4, 4>(a, st);
+    return forward<T, 4, 16>(a, st);
+}
+
+template <typename T>
+hipError_t pick_backward(const NormArgs &a, hipStream_t st) {
+    constexpr int one = 64 * 16 / (int)sizeof(T), full = 2048 / one;
+    if (a.width <= one) return backward<T, 1, 1>(a, st);
+    if (a.width <= 2 * one) return backward<T, 2, 1>(a, st);
+    switch (waves_of(a.width)) {
+        case 1: return backward<T, full, 1>(a, st);
+        case 2: return backward<T, full, 2>(a, st);
+        case 4: return backward<T, full, 4>(a, st);
+        default: return backward<T, full, 8>(a, st);
+    }
 }
 
 }  // namespace
 
+int64_t norm_backward_bytes(const NormArgs &a) {
+    return (int64_t)blocks_of(a.width) * 2 * a.width * (int64_t)sizeof(float);
+}
+
 hipError_t launch_norm(const NormArgs &a, bool bf16, hipStream_t st) {
-    return bf16 ? pick<uint16_t>(a, false, st) : pick<float>(a, false, st);
+    return bf16 ? pick_forward<uint16_t>(a, st) : pick_forward<float>(a, st);
 }
 hipError_t launch_norm_backward(const NormArgs &a, bool bf16, hipStream_t st) {
-    return bf16 ? pick<uint16_t>(a, true, st) : pick<float>(a, true, st);
+    return bf16 ? pick_backward<uint16_t>(a, st) : pick_backward<float>(a, st);
 }
 
 }  // namespace olive

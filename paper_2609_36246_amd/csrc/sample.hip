@@ -92,41 +92,12 @@ Parts parts_of(const SampleArgs &a) {
     return Parts{(int32_t)((a.vocab + len - 1) / len), (int32_t)len, plain ? 64 : kBins * 2 + 64};
 }
 
-// A lane's tokens: 16 bytes from i on, at any alignment of their type; -inf past `end`.
-struct Lot { uint32_t w[4]; };
-template <typename T> constexpr int kLot = 16 / (int)sizeof(T);
 template <typename T> constexpr int kCell = 64 * kLot<T>;    // tokens of a wavefront's lots
 
+// A lane's tokens from i on, -inf past `end`.
 template <typename T>
-__device__ __forceinline__ Lot load_lot(const T *z, int i, int end) {
-    struct __attribute__((packed, aligned(sizeof(T)))) Loose { uint32_t w[4]; };
-    constexpr int kBits = 8 * (int)sizeof(T);
-    constexpr uint32_t kFill = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
-    Lot x{{kFill, kFill, kFill, kFill}};
-    if (i >= end) return x;
-    const auto drop = [&](uint32_t in) {         // the first token goes, `in` comes last
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t above = j < 3 ? x.w[j + 1] : in;
-            x.w[j] = kBits == 32 ? above : x.w[j] >> 16 | above << 16;
-        }
-    };
-    const int from = min(i, end - kLot<T>);      // (at a row's end the 16 bytes before it, shifted)
-    if (from >= 0) {
-        const Loose y = *(const Loose *)(z + from);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x.w[j] = y.w[j];
-#pragma unroll 1
-        for (int j = from; j < i; ++j) drop(kFill);
-    } else {
-#pragma unroll 1
-        for (int j = i; j < i + kLot<T>; ++j) {
-            uint32_t v = kFill;
-            if (j < end) memcpy(&v, z + j, sizeof(T));
-            drop(v);
-        }
-    }
-    return x;
+__device__ __forceinline__ Lot load_tokens(const T *z, int i, int end) {
+    return load_lot(z, i, end, sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u);
 }
 // fn(j, bits) for each token j of a lot.
 template <typename T, int UNROLL = 1, typename F>
@@ -157,7 +128,7 @@ __device__ __forceinline__ int count_bins(const uint16_t *z, int begin, int end,
     for (int i0 = begin + (int)threadIdx.x * 8; i0 < end; i0 += kAhead * THREADS * 8) {
         Lot x[kAhead];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) x[k] = load_lot(z, i0 + k * THREADS * 8, end);
+        for (int k = 0; k < kAhead; ++k) x[k] = load_tokens(z, i0 + k * THREADS * 8, end);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (i0 + k * THREADS * 8 >= end) break;
@@ -206,7 +177,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_masses_kernel(SampleArgs 
     const int mine = (end - begin + kPartThreads * 8 - 1) / (kPartThreads * 8);
 #pragma unroll
     for (int i = 0; i < kWhole / 8 / kPartThreads; ++i)
-        if (i < mine) lots[i * kPartThreads + tid] = load_lot(z, begin + (tid + i * kPartThreads) * 8, end);
+        if (i < mine) lots[i * kPartThreads + tid] = load_tokens(z, begin + (tid + i * kPartThreads) * 8, end);
     uint32_t top = 0, bad = 0;
     int n = 0;
 #pragma unroll 1
@@ -385,7 +356,7 @@ __device__ __forceinline__ int locate(const T *z, const Item &item, int begin, i
         int at = begin + wave * step, left = cells, r = wave;
         int next = at, next_left = cells;
         const auto load_next = [&]() {
-            const Lot x = load_lot(z, next + lane * kL, end);
+            const Lot x = load_tokens(z, next + lane * kL, end);
             next += kC;
             if (--next_left == 0) next += (kWaves - 1) * step, next_left = cells;
             next = min(next, end);
@@ -421,7 +392,7 @@ __device__ __forceinline__ int locate(const T *z, const Item &item, int begin, i
         end = min(end, begin + step);
     }
     // a lot a lane, every wavefront for itself: its mass, then its tokens one by one
-    const Lot y = load_lot(z, begin + lane * kL, end);
+    const Lot y = load_tokens(z, begin + lane * kL, end);
     int before = 0, found = -1, last = -1;
     double at = 0.0;
 #pragma unroll 1
@@ -549,11 +520,11 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
     const T *z = (const T *)a.logits.p + row * a.logits.st;
     const int tid = threadIdx.x, V = a.vocab;
     const auto each = [&](auto fn) {             // every token that is not -inf: fn(value, index)
-        Lot next = load_lot(z, tid * kLot<T>, V);
+        Lot next = load_tokens(z, tid * kLot<T>, V);
 #pragma unroll 1
         for (int i = tid * kLot<T>; i < V; i += kThreads * kLot<T>) {
             const Lot x = next;
-            next = load_lot(z, min(i + kThreads * kLot<T>, V), V);
+            next = load_tokens(z, min(i + kThreads * kLot<T>, V), V);
             each_token<T>(x, [&](int j, uint32_t bits) {
                 const float v = token_value<T>(bits) + 0.f;        // (-0 and 0 are the same value)
                 if (!(v == kNegInf)) fn(v, i + j);

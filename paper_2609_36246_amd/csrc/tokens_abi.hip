@@ -171,7 +171,7 @@ olive_status olive_row_norm_workspace(const olive_norm_desc *desc, int64_t *byte
     if (!bytes) return OLIVE_E_NULL;
     const olive_status s = check_norm(desc);
     if (s != OLIVE_OK) return s;
-    *bytes = (int64_t)kNormBlocks * 2 * desc->width * (int64_t)sizeof(float);
+    *bytes = norm_backward_bytes(norm_args(desc));
     return OLIVE_OK;
 }
 

@@ -45,8 +45,7 @@ struct NormArgs {
     float eps;
 };
 
-constexpr int kNormBlocks = 512;     // workgroups of the backward at most (its partial sums)
-
+int64_t norm_backward_bytes(const NormArgs &a);
 hipError_t launch_norm(const NormArgs &a, bool bf16, hipStream_t st);
 hipError_t launch_norm_backward(const NormArgs &a, bool bf16, hipStream_t st);
 

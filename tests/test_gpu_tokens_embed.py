@@ -39,6 +39,7 @@ def tokens(n, vocab, how="mixed", seed=0):
 def forward(ids, table, scale=1.0, how="plain", stream=None):
     out = matrix(len(ids), table.shape[1], table.dtype, how)
     d = L.make_embed_desc(len(ids), len(table), table.shape[1], ids, dtype=kind(table.dtype), scale=scale)
+    torch.cuda.synchronize()                    # (what is made here, before another stream's call)
     L.olive_embed(d, table, out, stream=stream)
     torch.cuda.synchronize()
     return out
@@ -82,6 +83,7 @@ def backward(ids, grad, vocab, scale=1.0, into=None, gdtype=F32, how="plain", st
     table = matrix(vocab, grad.shape[1], gdtype, how) if into is None else into
     d = L.make_embed_desc(len(ids), vocab, grad.shape[1], ids, dtype=kind(grad.dtype), scale=scale)
     work = torch.full((L.olive_embed_workspace(d),), 0xff, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
     L.olive_embed_backward(d, grad, table, accumulate=into is not None, workspace=work, stream=stream)
     torch.cuda.synchronize()
     return table
@@ -116,6 +118,15 @@ def test_backward(n, vocab, width, ids, how, dtype, gdtype, accumulate):
     before = f64(into) if accumulate else None
     got = backward(i, grad, vocab, 1.75, into, gdtype, how)
     check(i, grad, vocab, 1.75, got, before)
+
+
+def test_more_tokens_than_one_merge_takes():
+    gen = torch.Generator().manual_seed(11)
+    n = 4096 * 64 + 5001
+    for how, vocab in (("mixed", 3000), ("uniform", 100000)):
+        grad = matrix(n, 4, F32, gen=gen, std=1e-2)
+        ids = tokens(n, vocab, how, seed=11)
+        check(ids, grad, vocab, 1.0, backward(ids, grad, vocab))
 
 
 @pytest.mark.parametrize("accumulate", [False, True])

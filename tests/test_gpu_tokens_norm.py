@@ -46,6 +46,7 @@ class Norm:
         out = matrix(self.rows, self.width, self.dtype, self.how) if out is None else out
         if total is None and self.res is not None:
             total = matrix(self.rows, self.width, self.dtype, self.how)
+        torch.cuda.synchronize()                # (what is made here, before another stream's call)
         L.olive_row_norm(self.desc, self.x, out, self.res, total, stream=stream)
         torch.cuda.synchronize()
         return out, total
@@ -74,8 +75,9 @@ class Norm:
         gh = matrix(self.rows, self.width, self.dtype, self.how) if grad_h is None else grad_h
         gw, gb = (torch.full((self.width,), float("nan"), device="cuda") for _ in range(2)) if weights else (None, None)
         work = torch.full((L.olive_row_norm_workspace(self.desc),), 0xff, dtype=torch.uint8, device="cuda")
-        L.olive_row_norm_backward(self.desc, self.h().contiguous() if self.res is not None else self.x, self.dy, gh,
-                                  self.dsum, gw, gb, work if weights else None, stream=stream)
+        h = self.h().contiguous() if self.res is not None else self.x
+        torch.cuda.synchronize()
+        L.olive_row_norm_backward(self.desc, h, self.dy, gh, self.dsum, gw, gb, work if weights else None, stream=stream)
         torch.cuda.synchronize()
         return gh, gw, gb
 
