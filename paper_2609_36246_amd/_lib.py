@@ -261,13 +261,23 @@ def _ptr(x) -> Optional[int]:
     return x.data_ptr()
 
 
+_device = None           # torch's own entry for the current device, once torch has set up its devices
+
+
 def _stream(stream) -> Optional[int]:
+    global _device
     if stream is None:
         import torch
         # torch's bare handle where this torch has it: the public call makes a Stream object each
         # time, of the same handle
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
+        if raw is None:
+            return torch.cuda.current_stream().cuda_stream
+        if _device is None:
+            device = torch.cuda.current_device()
+            _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+            return raw(device)
+        return raw(_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -708,12 +718,12 @@ def _rows(x, dtype, rows: int, width: int, what: str, output: bool = False):
     (None: neither); an output's rows do not overlap."""
     if x is None:
         return None, 0
-    s, shape = x.stride(), x.shape
-    if x.dtype is not dtype or len(s) != 2 or shape[0] != rows or shape[1] != width or \
-            (s[1] != 1 and width > 1) or (output and s[0] < width and rows > 1):
-        raise ValueError("%s: expected [%d, %d] of %s with contiguous rows%s"
-                         % (what, rows, width, dtype, " apart from each other" if output else ""))
-    return x.data_ptr(), s[0]
+    if x.dtype is dtype and x.shape == (rows, width):
+        apart, step = x.stride()
+        if (step == 1 or width <= 1) and not (output and apart < width and rows > 1):
+            return x.data_ptr(), apart
+    raise ValueError("%s: expected [%d, %d] of %s with contiguous rows%s"
+                     % (what, rows, width, dtype, " apart from each other" if output else ""))
 
 
 def _bytes_of(name, desc) -> int:

@@ -1,6 +1,6 @@
 // Rows of an embedding table by tokens, and the table's gradient by sorted tokens.
 //
-// The gradient: tokens are sorted with their positions (in tiles of 4096 in LDS, then up to 64 sorted
+// The gradient: tokens are sorted with their positions (in tiles of 2048 in LDS, then up to 64 sorted
 // segments are merged at a time), the sorted list is cut into blocks of equal length, and a wavefront adds
 // the rows of a block, 16 bytes a lane, run by run. A run inside a block goes to the table at once;
 // of one that crosses a border each block leaves a partial row, which a last pass adds in order. So a
@@ -47,7 +47,8 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, int chunks, int
 }
 
 // ------------------------------------------------------------------------------------ sort
-constexpr int kTile = 4096, kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kTile = 2048, kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kRounds = kTile / kSortThreads, kDigit = 9;
 constexpr int kFan = 64;                         // segments that a pass merges into one
 
 // A token's place in the order: its id, `vocab` for those that have no gradient.
@@ -55,31 +56,39 @@ __device__ __forceinline__ uint32_t key_of(const EmbedArgs &a, int id) {
     return id >= 0 && id < a.vocab ? (uint32_t)id : (uint32_t)a.vocab;
 }
 
-// Sorts a tile by 8 bits of the key at a time, stably: a wavefront has 256 tokens, ranks 64 of them at a
-// time by comparing digits (a ballot a bit), and keeps its own counts.
-__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedArgs a, uint32_t *keys, int32_t *places, int bits) {
+// Sorts a tile by a digit of the key at a time (at most 9 bits, as many each), stably: a wavefront has 128
+// tokens, ranks 64 of them at a time by comparing digits (a ballot a bit), and keeps its own
+// counts. 18 bits take two passes of 2.5 us; a chain of waits, of which fewer and longer ones are less.
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedArgs a, uint32_t *keys, int32_t *places, int bits,
+                                                                  int digit) {
     __shared__ uint32_t key[2][kTile];
     __shared__ uint16_t place[2][kTile];
-    __shared__ uint32_t count[kSortWaves][256];
+    __shared__ uint32_t count[kSortWaves][1 << kDigit];
     __shared__ uint32_t join[kSortWaves];
+    constexpr int kPer = (kSortWaves << kDigit) / kSortThreads, kSplit = kSortWaves / kPer;
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_index();
     const int first = blockIdx.x * kTile, n = min(kTile, a.tokens - first);
+    const uint32_t mask = (1u << digit) - 1;
     for (int i = tid; i < kTile; i += kSortThreads) {
         key[0][i] = i < n ? key_of(a, a.ids[first + i]) : 0xffffffffu;
         place[0][i] = (uint16_t)i;
     }
     int from = 0;
-    for (int shift = 0; shift < bits; shift += 8, from ^= 1) {
-        for (int i = tid; i < kSortWaves * 256; i += kSortThreads) (&count[0][0])[i] = 0;
+    for (int shift = 0; shift < bits; shift += digit, from ^= 1) {
+        for (int i = tid; i < kSortWaves << kDigit; i += kSortThreads) (&count[0][0])[i] = 0;
         __syncthreads();
-        uint32_t k[4], rank[4];
+        uint32_t k[kRounds], p[kRounds], rank[kRounds];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            k[r] = key[from][wave * 256 + r * 64 + lane];
-            const uint32_t d = k[r] >> shift & 255;
+        for (int r = 0; r < kRounds; ++r) {
+            k[r] = key[from][(wave * kRounds + r) * 64 + lane];
+            p[r] = place[from][(wave * kRounds + r) * 64 + lane];
+        }
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const uint32_t d = k[r] >> shift & mask;
             uint64_t same = ~0ull;
 #pragma unroll
-            for (int b = 0; b < 8; ++b) {
+            for (int b = 0; b < kDigit; ++b) {
                 const bool set = d >> b & 1;
                 const uint64_t m = __ballot(set);
                 same &= set ? m : ~m;
@@ -91,25 +100,26 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedArgs a, u
         }
         __syncthreads();
         // counts before: of smaller digits, then of the same digit in wavefronts before
-        uint32_t c[4], s = 0;
+        uint32_t c[kPer], s = 0;
+        const int d0 = tid / kSplit, w0 = tid % kSplit * kPer;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s += c[i] = count[(tid & 3) * 4 + i][tid >> 2];
+        for (int i = 0; i < kPer; ++i) s += c[i] = count[w0 + i][d0];
         uint32_t at = wave_scan(s);
         if (lane == 63) join[wave] = at;
         __syncthreads();
         at -= s;
         for (int i = 0; i < wave; ++i) at += join[i];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            count[(tid & 3) * 4 + i][tid >> 2] = at;
+        for (int i = 0; i < kPer; ++i) {
+            count[w0 + i][d0] = at;
             at += c[i];
         }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const uint32_t to = count[wave][k[r] >> shift & 255] + rank[r];
+        for (int r = 0; r < kRounds; ++r) {
+            const uint32_t to = count[wave][k[r] >> shift & mask] + rank[r];
             key[from ^ 1][to] = k[r];
-            place[from ^ 1][to] = place[from][wave * 256 + r * 64 + lane];
+            place[from ^ 1][to] = (uint16_t)p[r];
         }
         __syncthreads();
     }
@@ -120,78 +130,51 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedArgs a, u
 }
 
 // Merges groups of up to kFan sorted segments of `len`: a token moves on by the number of tokens of
-// the group's other segments before it, which is looked up once for a run of equal keys.
-__global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(EmbedArgs a, const uint32_t *keys,
-                                                                   const int32_t *places, uint32_t *keys_to,
-                                                                   int32_t *places_to, int64_t len) {
-    __shared__ int32_t moves[kTile];
-    __shared__ int32_t join[kSortWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = wave_index();
-    const int64_t first = (int64_t)blockIdx.x * kTile, group = first / (len * kFan) * (len * kFan);
-    const int n = (int)min((int64_t)kTile, a.tokens - first);
+// the group's other segments before it. A workgroup has kWindow tokens of one segment; four threads a
+// token search a quarter of the segments each, two side by side. (A search is a chain of waits: 16
+// segments of 2048 take 11 waits of 0.6 us.)
+constexpr int kWindow = 256;
+
+__global__ __launch_bounds__(4 * kWindow) void embed_merge_kernel(EmbedArgs a, const uint32_t *keys, const int32_t *places,
+                                                                  uint32_t *keys_to, int32_t *places_to, int64_t len) {
+    __shared__ int32_t moves[4][kWindow];
+    const int p = threadIdx.x % kWindow, quarter = threadIdx.x / kWindow;
+    const int64_t first = (int64_t)blockIdx.x * kWindow, group = first / (len * kFan) * (len * kFan);
     const int own = (int)((first - group) / len);
     const int segments = (int)min((int64_t)kFan, (a.tokens - group + len - 1) / len);
-    // 4 tokens in a row a thread; the first of a run within this workgroup's looks up
-    uint32_t k[4];
-    int head[4], newest = 0;
+    const bool live = first + p < a.tokens;
+    const uint32_t k = live ? keys[first + p] : 0;
+    int move = 0;
+    if (live)
+        for (int s0 = quarter; s0 < segments; s0 += 8) {
+            int64_t start[2];
+            int lo[2] = {}, left[2];
+            uint32_t want[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int p = tid * 4 + i;
-        k[i] = p < n ? keys[first + p] : 0xffffffffu;
-    }
-    const uint32_t before = tid == 0 || tid * 4 >= n ? ~k[0] : keys[first + tid * 4 - 1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int p = tid * 4 + i;
-        if (p < n && k[i] != (i ? k[i - 1] : before)) {
-            newest = p;
-            int move = 0;
-            for (int s0 = 0; s0 < segments; s0 += 4) {       // 4 searches side by side
-                int64_t start[4];
-                int lo[4], left[4];
-                uint32_t want[4];
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const bool there = s0 + s < segments && s0 + s != own;
-                    start[s] = group + (there ? s0 + s : own) * len;
-                    lo[s] = 0;
-                    left[s] = there ? (int)min(len, a.tokens - start[s]) : 0;
-                    want[s] = k[i] + (s0 + s < own);         // (of the segments before also the equal ones)
-                }
-                while (left[0] | left[1] | left[2] | left[3]) {
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        const int half = left[s] >> 1;
-                        const bool less = left[s] > 0 && keys[start[s] + lo[s] + half] < want[s];
-                        lo[s] = less ? lo[s] + half + 1 : lo[s];
-                        left[s] = less ? left[s] - half - 1 : half;
-                    }
-                }
-                move += lo[0] + lo[1] + lo[2] + lo[3];
+            for (int i = 0; i < 2; ++i) {
+                const int s = s0 + 4 * i;
+                const bool there = s < segments && s != own;
+                start[i] = group + (there ? s : own) * len;
+                left[i] = there ? (int)min(len, a.tokens - start[i]) : 0;
+                want[i] = k + (s < own);                     // (of the segments before also the equal ones)
             }
-            moves[p] = move;
-        }
-        head[i] = newest;
-    }
-    // the latest first of a run at or before each token
-    uint32_t seen = (uint32_t)newest;
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t u = (uint32_t)__shfl_up((int)seen, o);
-        if (lane >= o) seen = max(seen, u);
-    }
-    if (lane == 63) join[wave] = (int)seen;
-    __syncthreads();
-    int prev = __shfl_up((int)seen, 1);
-    if (lane == 0) prev = 0;
-    for (int i = 0; i < wave; ++i) prev = max(prev, join[i]);
+            while (left[0] | left[1]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int p = tid * 4 + i;
-        if (p >= n) break;
-        const int64_t to = first + p - own * len + moves[max(head[i], prev)];
-        keys_to[to] = k[i];
-        places_to[to] = places[first + p];
-    }
+                for (int i = 0; i < 2; ++i) {
+                    const int half = left[i] >> 1;
+                    const bool less = left[i] > 0 && keys[start[i] + lo[i] + half] < want[i];
+                    lo[i] = less ? lo[i] + half + 1 : lo[i];
+                    left[i] = less ? left[i] - half - 1 : half;
+                }
+            }
+            move += lo[0] + lo[1];
+        }
+    moves[quarter][p] = move;
+    __syncthreads();
+    if (quarter || !live) return;
+    const int64_t to = first + p - own * len + moves[0][p] + moves[1][p] + moves[2][p] + moves[3][p];
+    keys_to[to] = k;
+    places_to[to] = places[first + p];
 }
 
 // ------------------------------------------------------------------------------------ sums
@@ -453,12 +436,13 @@ hipError_t backward(const EmbedArgs &a, hipStream_t st) {
     int bits = 0;
     while (((int64_t)a.vocab >> bits) > 0) ++bits;
     const int tiles = (a.tokens + kTile - 1) / kTile;
-    embed_sort_kernel<<<tiles, kSortThreads, 0, st>>>(a, keys[0], places[0], bits);
+    const int passes = (bits + kDigit - 1) / kDigit, digit = (bits + passes - 1) / passes;
+    embed_sort_kernel<<<tiles, kSortThreads, 0, st>>>(a, keys[0], places[0], bits, digit);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     int at = 0;
     for (int64_t len = kTile; len < a.tokens; len *= kFan, at ^= 1) {
-        embed_merge_kernel<<<tiles, kSortThreads, 0, st>>>(a, keys[at], places[at], keys[at ^ 1], places[at ^ 1], len);
+        embed_merge_kernel<<<(a.tokens + kWindow - 1) / kWindow, 4 * kWindow, 0, st>>>(a, keys[at], places[at], keys[at ^ 1], places[at ^ 1], len);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
