@@ -202,23 +202,30 @@ struct Piece {
     }
 };
 
-// What a lane does with the N columns from c on of a table's row: scale * sum (+ what is there).
+// A lane's N columns from c on of a table's row: what is there, where the sums are added to it.
 template <typename TT, int N, bool TAIL>
-__device__ __forceinline__ void to_table(const EmbedArgs &a, uint32_t id, int c, const float (&sum)[N]) {
-    TT *row = (TT *)a.table.p + id * a.table.st;
-    if (!TAIL || c + N <= a.width) {
-        if (c >= a.width) return;
-        float x[N] = {};
-        if (a.accumulate) Piece<TT, N>::get(row + c, x);
+__device__ __forceinline__ void from_table(const EmbedArgs &a, uint32_t id, int c, float (&x)[N]) {
+    const TT *row = (const TT *)a.table.p + id * a.table.st;
+    if (c + N <= a.width) {
+        Piece<TT, N>::get(row + c, x);
+    } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j) x[j] = fmaf(sum[j], a.scale, x[j]);
-        Piece<TT, N>::put(row + c, x);
-        return;
+        for (int j = 0; j < N; ++j) x[j] = TAIL && j < N - 1 && c + j < a.width ? RowElem<TT>::get(row[c + j]) : 0.f;
     }
+}
+// And what goes there: scale * sum + x.
+template <typename TT, int N, bool TAIL>
+__device__ __forceinline__ void to_table(const EmbedArgs &a, uint32_t id, int c, const float (&sum)[N], float (&x)[N]) {
+    TT *row = (TT *)a.table.p + id * a.table.st;
 #pragma unroll
-    for (int j = 0; j < N - 1; ++j)
-        if (c + j < a.width)
-            row[c + j] = RowElem<TT>::put(fmaf(sum[j], a.scale, a.accumulate ? RowElem<TT>::get(row[c + j]) : 0.f));
+    for (int j = 0; j < N; ++j) x[j] = fmaf(sum[j], a.scale, x[j]);
+    if (c + N <= a.width) {
+        Piece<TT, N>::put(row + c, x);
+    } else if (TAIL) {
+#pragma unroll
+        for (int j = 0; j < N - 1; ++j)
+            if (c + j < a.width) row[c + j] = RowElem<TT>::put(x[j]);
+    }
 }
 
 template <typename T, bool TAIL>
@@ -278,41 +285,43 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, Sorted s) {
     const uint32_t prev = p0 > 0 ? s.keys[p0 - 1] : 0xffffffffu, next = p0 + n < a.tokens ? s.keys[p0 + n] : 0xffffffffu;
     const int there = __popcll(__ballot(key < (uint32_t)a.vocab));       // (the others are at the end)
     if (there == 0) return;
+    // 8 rows on their way together, and the table's rows of the runs that end among them
     constexpr int kAhead = 8;
     float sum[L] = {};
-    uint32_t run = wave_read(key, 0);
-    const auto leave = [&](bool last) {
-        const bool from_before = run == prev, goes_on = last && run == next;
-        if (from_before || goes_on) {
-            float *to = s.part + ((int64_t)b * 2 + !from_before) * s.chunks * 64 * L + c;
-            Piece<float, L>::put(to, sum);
-        } else {
-            to_table<TT, L, TAIL>(a, run, c, sum);
-        }
-    };
 #pragma unroll 1
     for (int e0 = 0; e0 < there; e0 += kAhead) {
         Lot x[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) x[j] = load_grad<T, TAIL>(a, wave_read(place, min(e0 + j, there - 1)), c);
+        float old[kAhead][L];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            if (e0 + j >= there) break;
-            const uint32_t k = wave_read(key, e0 + j);
+            const int e = min(e0 + j, there - 1);
+            x[j] = load_grad<T, TAIL>(a, wave_read(place, e), c);
+            const uint32_t k = wave_read(key, e);
+#pragma unroll
+            for (int i = 0; i < L; ++i) old[j][i] = 0.f;
+            if (a.accumulate && (e == there - 1 || wave_read(key, min(e + 1, 63)) != k))
+                from_table<TT, L, TAIL>(a, k, c, old[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int e = e0 + j;
+            if (e >= there) break;
+            const uint32_t k = wave_read(key, e);
             float v[L];
             unpack_lot<T>(x[j], v);
-            if (k != run) {
-                leave(false);
-                run = k;
 #pragma unroll
-                for (int i = 0; i < L; ++i) sum[i] = v[i];
+            for (int i = 0; i < L; ++i) sum[i] += v[i];
+            if (e < there - 1 && wave_read(key, e + 1) == k) continue;
+            const bool from_before = k == prev, goes_on = e == n - 1 && k == next;
+            if (from_before || goes_on) {
+                Piece<float, L>::put(s.part + ((int64_t)b * 2 + !from_before) * s.chunks * 64 * L + c, sum);
             } else {
-#pragma unroll
-                for (int i = 0; i < L; ++i) sum[i] += v[i];
+                to_table<TT, L, TAIL>(a, k, c, sum, old[j]);
             }
+#pragma unroll
+            for (int i = 0; i < L; ++i) sum[i] = 0.f;
         }
     }
-    leave(there == n);
 }
 
 // The runs that cross a border: the block where one begins adds what the blocks have left of it.
@@ -353,7 +362,9 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a, Sorted s) 
     for (int i = 0; i < 3; ++i)
 #pragma unroll
         for (int j = 0; j < L; ++j) sum[j] += join[i][lane][j];
-    to_table<TT, L, TAIL>(a, run, c, sum);
+    float x[L] = {};
+    if (a.accumulate) from_table<TT, L, TAIL>(a, run, c, x);
+    to_table<TT, L, TAIL>(a, run, c, sum, x);
 }
 
 // Few tokens: the wavefront of a token's first occurrence finds the others and adds their rows in order.
@@ -386,7 +397,9 @@ __global__ __launch_bounds__(256) void embed_few_kernel(EmbedArgs a, int chunks)
             for (int j = 0; j < L; ++j) sum[j] += x[j];
         }
     }
-    to_table<TT, L, TAIL>(a, (uint32_t)id, c, sum);
+    float x[L] = {};
+    if (a.accumulate) from_table<TT, L, TAIL>(a, (uint32_t)id, c, x);
+    to_table<TT, L, TAIL>(a, (uint32_t)id, c, sum, x);
 }
 
 // ---------------------------------------------------------------------------------- launches
