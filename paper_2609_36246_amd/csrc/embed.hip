@@ -131,32 +131,44 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedArgs a, u
 
 // Merges groups of up to kFan sorted segments of `len`: a token moves on by the number of tokens of
 // the group's other segments before it. A workgroup has kWindow tokens of one segment; four threads a
-// token search a quarter of the segments each, two side by side. (A search is a chain of waits: 16
-// segments of 2048 take 11 waits of 0.6 us.)
-constexpr int kWindow = 256;
+// token search a quarter of the segments each, two side by side: first among 64 keys of each segment
+// that lie in LDS, then between two of them. (A search is a chain of waits: of 16 segments of 2048 without
+// the keys in LDS 12.6 us a pass.)
+constexpr int kWindow = 256, kSamples = 64;
 
 __global__ __launch_bounds__(4 * kWindow) void embed_merge_kernel(EmbedArgs a, const uint32_t *keys, const int32_t *places,
                                                                   uint32_t *keys_to, int32_t *places_to, int64_t len) {
+    __shared__ uint32_t samples[kFan][kSamples + 1];
     __shared__ int32_t moves[4][kWindow];
     const int p = threadIdx.x % kWindow, quarter = threadIdx.x / kWindow;
     const int64_t first = (int64_t)blockIdx.x * kWindow, group = first / (len * kFan) * (len * kFan);
-    const int own = (int)((first - group) / len);
+    const int own = (int)((first - group) / len), stride = (int)(len / kSamples);
     const int segments = (int)min((int64_t)kFan, (a.tokens - group + len - 1) / len);
     const bool live = first + p < a.tokens;
     const uint32_t k = live ? keys[first + p] : 0;
+    for (int i = threadIdx.x; i < segments * kSamples; i += 4 * kWindow) {
+        const int64_t at = group + i / kSamples * len + i % kSamples * stride;
+        samples[i / kSamples][i % kSamples] = at < a.tokens ? keys[at] : 0xffffffffu;
+    }
+    __syncthreads();
     int move = 0;
     if (live)
         for (int s0 = quarter; s0 < segments; s0 += 8) {
             int64_t start[2];
-            int lo[2] = {}, left[2];
+            int lo[2], left[2];
             uint32_t want[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int s = s0 + 4 * i;
                 const bool there = s < segments && s != own;
                 start[i] = group + (there ? s : own) * len;
-                left[i] = there ? (int)min(len, a.tokens - start[i]) : 0;
                 want[i] = k + (s < own);                     // (of the segments before also the equal ones)
+                int m = 0;                                   // samples before
+#pragma unroll
+                for (int step = kSamples; step > 0; step >>= 1)
+                    if (there && m + step <= kSamples && samples[s][m + step - 1] < want[i]) m += step;
+                lo[i] = m > 0 ? (m - 1) * stride + 1 : 0;
+                left[i] = m > 0 ? max(0, (int)min((int64_t)stride - 1, min(len, a.tokens - start[i]) - lo[i])) : 0;
             }
             while (left[0] | left[1]) {
 #pragma unroll

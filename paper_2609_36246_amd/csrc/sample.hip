@@ -92,18 +92,30 @@ Parts parts_of(const SampleArgs &a) {
     return Parts{(int32_t)((a.vocab + len - 1) / len), (int32_t)len, plain ? 64 : kBins * 2 + 64};
 }
 
-template <typename T> constexpr int kCell = 64 * kLot<T>;    // tokens of a wavefront's lots
-
 // A lane's tokens from i on, -inf past `end`.
 template <typename T>
 __device__ __forceinline__ Lot load_tokens(const T *z, int i, int end) {
     return load_lot(z, i, end, sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u);
 }
+// The same of WORDS words: 1, two bf16 tokens, in the first.
+template <typename T, int WORDS>
+__device__ __forceinline__ Lot load_some(const T *z, int i, int end) {
+    if constexpr (WORDS == 4) {
+        return load_tokens(z, i, end);
+    } else {
+        static_assert(WORDS == 1 && sizeof(T) == 2, "");
+        struct __attribute__((packed, aligned(2))) Loose { uint32_t w; };
+        Lot x{{0xff80ff80u}};
+        if (i + 2 <= end) x.w[0] = ((const Loose *)(z + i))->w;
+        else if (i < end) x.w[0] = 0xff800000u | z[i];
+        return x;
+    }
+}
 // fn(j, bits) for each token j of a lot.
-template <typename T, int UNROLL = 1, typename F>
+template <typename T, int UNROLL = 1, int WORDS = 4, typename F>
 __device__ __forceinline__ void each_token(Lot x, F fn) {
 #pragma unroll UNROLL
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < WORDS; ++k) {
         if constexpr (sizeof(T) == 2) {
             fn(2 * k, x.w[0] & 0xffffu);
             fn(2 * k + 1, x.w[0] >> 16);
@@ -141,6 +153,25 @@ __device__ __forceinline__ int count_bins(const uint16_t *z, int begin, int end,
         }
     }
     return flags;
+}
+
+// e^x for x <= 0: 2^n e^r with n the nearest whole number to x / ln 2, by the series of e^r (|r| <= ln 2 / 2:
+// r^13 / 13! is 2^-52), its even and odd terms side by side.
+__device__ __forceinline__ double exp_below(double x) {
+    x = fmax(x, -1100.0);
+    const double n = rint(x * 1.4426950408889634);
+    const double r = fma(n, -1.9082149292705877e-10, fma(n, -0.6931471803691238, x)), q = r * r;
+    double even = fma(q, 1.0 / 479001600, 1.0 / 3628800), odd = fma(q, 1.0 / 39916800, 1.0 / 362880);
+    even = fma(q, even, 1.0 / 40320);
+    odd = fma(q, odd, 1.0 / 5040);
+    even = fma(q, even, 1.0 / 720);
+    odd = fma(q, odd, 1.0 / 120);
+    even = fma(q, even, 1.0 / 24);
+    odd = fma(q, odd, 1.0 / 6);
+    even = fma(q, even, 0.5);
+    odd = fma(q, odd, 1.0);
+    even = fma(q, even, 1.0);
+    return ldexp(fma(r, odd, even), (int)n);
 }
 
 struct Settings {
@@ -197,13 +228,13 @@ __global__ __launch_bounds__(kPartThreads) void sample_masses_kernel(SampleArgs 
     if (__ballot(bad) && lane == 0) bads[wave] = 1;
     __syncthreads();
     for (int i = 0; i < kPartWaves; ++i) top = max(top, tops[i]);
-    const double first = (double)ord2f(top), t = (double)s.temp;
+    const double first = (double)ord2f(top), inv = 1.0 / (double)s.temp;
     double mass = 0.0;
 #pragma unroll 1
     for (int i = 0; i < mine; ++i)
         each_token<uint16_t>(lots[i * kPartThreads + tid], [&](int, uint32_t bits) {
             const float v = bf16_bits_to_f32(bits);
-            mass += v > kNegInf ? exp(((double)v - first) / t) : 0.0;
+            mass += v > kNegInf ? exp_below(((double)v - first) * inv) : 0.0;
         });
     mass = wave_sum(mass);
     if (lane == 0) masses[wave] = mass;
@@ -341,10 +372,10 @@ __device__ __forceinline__ int pick_range(const Range *r, int n, double w, Drawn
     return found;
 }
 
-template <typename T, int UNROLL = 1, typename Item>
+template <typename T, int UNROLL = 1, int WORDS = 4, typename Item>
 __device__ __forceinline__ int locate(const T *z, const Item &item, int begin, int end, double tie_weight, Drawn d,
                                       Range *ranges) {
-    constexpr int kC = kCell<T>, kL = kLot<T>;
+    constexpr int kL = WORDS * 4 / (int)sizeof(T), kC = 64 * kL;     // tokens of a lane and of a cell
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll 1
     while (end - begin > kC) {
@@ -356,7 +387,7 @@ __device__ __forceinline__ int locate(const T *z, const Item &item, int begin, i
         int at = begin + wave * step, left = cells, r = wave;
         int next = at, next_left = cells;
         const auto load_next = [&]() {
-            const Lot x = load_tokens(z, next + lane * kL, end);
+            const Lot x = load_some<T, WORDS>(z, next + lane * kL, end);
             next += kC;
             if (--next_left == 0) next += (kWaves - 1) * step, next_left = cells;
             next = min(next, end);
@@ -370,7 +401,7 @@ __device__ __forceinline__ int locate(const T *z, const Item &item, int begin, i
             const Lot y = ahead[0];
             ahead[0] = ahead[1], ahead[1] = ahead[2];
             ahead[2] = load_next();
-            each_token<T, UNROLL>(y, [&](int j, uint32_t bits) {
+            each_token<T, UNROLL, WORDS>(y, [&](int j, uint32_t bits) {
                 item(at + lane * kL + j, bits, [&](bool kept, bool tie, double w) {
                     x.mass += w;
                     x.kept += kept;
@@ -392,12 +423,12 @@ __device__ __forceinline__ int locate(const T *z, const Item &item, int begin, i
         end = min(end, begin + step);
     }
     // a lot a lane, every wavefront for itself: its mass, then its tokens one by one
-    const Lot y = load_tokens(z, begin + lane * kL, end);
+    const Lot y = load_some<T, WORDS>(z, begin + lane * kL, end);
     int before = 0, found = -1, last = -1;
     double at = 0.0;
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
-        each_token<T, UNROLL>(y, [&](int j, uint32_t bits) {
+        each_token<T, UNROLL, WORDS>(y, [&](int j, uint32_t bits) {
             const int i = begin + lane * kL + j;
             item(i, bits, [&](bool kept, bool tie, double w) {
                 const bool keep = i < end && (kept || (tie && before < d.ties));
@@ -485,7 +516,7 @@ __device__ __forceinline__ void sample_few(const SampleArgs &a, int row, const S
     __syncthreads();
     const uint64_t own = tid < k ? sorted[tid] : 0;
     const int index = 0xffffff - (int)(own & 0xffffff);
-    const double w = tid < k ? exp(-scaled(ord2f((uint32_t)(own >> 24)))) : 0.0;
+    const double w = tid < k ? exp_below(-scaled(ord2f((uint32_t)(own >> 24)))) : 0.0;
     if (tid < k) weight[tid] = w;
     int cb, call;
     double mb, all;
@@ -571,7 +602,7 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
         if (f.listed <= (uint32_t)kFewList) return sample_few<T>(a, row, s, f, (int)f.listed, scaled);
     }
 
-    for (int i = tid; i < kFineBins; i += kThreads) f.count[i] = 0, f.mass[i] = 0, f.edge[i] = exp(-i / 32.0);
+    for (int i = tid; i < kFineBins; i += kThreads) f.count[i] = 0, f.mass[i] = 0, f.edge[i] = exp_below(i * -0.03125);
     __syncthreads();
     int bits = 0;
     while ((V >> bits) > 0) ++bits;
@@ -697,7 +728,7 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
         __syncthreads();
         each([&](float v, int) {
             const double t = scaled(v);
-            if (bin_at(t) != b || !(exp(-t) >= (double)s.mp)) return;
+            if (bin_at(t) != b || !(exp_below(-t) >= (double)s.mp)) return;
             atomicMin(&f.least, f2ord(v));
             atomicAdd(&f.listed, 1u);
             atomicAdd((unsigned long long *)f.dmass, fixed(t, b));
@@ -768,8 +799,8 @@ __global__ __launch_bounds__(kThreads) void sample_all_kernel(SampleArgs a, Part
     if (__ballot(flags != 0)) return no_answer(a, row);
     const int there = wave_sum(n);
     if (there == 0) return no_answer(a, row);
-    const double zmax = (double)ord2f(wave_max(f2ord(n > 0 ? top : kNegInf))), t = (double)s.temp;
-    mass = n > 0 ? mass * exp(((double)top - zmax) / t) : 0.0;
+    const double zmax = (double)ord2f(wave_max(f2ord(n > 0 ? top : kNegInf))), inv = 1.0 / (double)s.temp;
+    mass = n > 0 ? mass * exp_below(((double)top - zmax) * inv) : 0.0;
     const double all = wave_sum(mass);
     if (threadIdx.x < S) ranges[lane] = Range{mass, s.greedy ? n > 0 && (double)top == zmax : n, 0};
     __syncthreads();
@@ -778,12 +809,12 @@ __global__ __launch_bounds__(kThreads) void sample_all_kernel(SampleArgs a, Part
     const auto item = [&](int, uint32_t bits, auto fn) {
         const float v = bf16_bits_to_f32(bits);
         const bool in = s.greedy ? (double)v == zmax : v > kNegInf;
-        fn(in, false, in ? exp(((double)v - zmax) / t) : 0.0);
+        fn(in, false, in ? exp_below(((double)v - zmax) * inv) : 0.0);
     };
-    const int token = locate(z, item, begin, min(a.vocab, begin + parts.len), 0.0, d, ranges);
+    const int token = locate<uint16_t, 1, 1>(z, item, begin, min(a.vocab, begin + parts.len), 0.0, d, ranges);
     if (threadIdx.x == 0) {
         a.token[row] = token;
-        if (a.logp) a.logp[row] = (float)(((double)bf16_bits_to_f32(z[token]) - zmax) / t - (s.greedy ? 0.0 : log(all)));
+        if (a.logp) a.logp[row] = (float)(((double)bf16_bits_to_f32(z[token]) - zmax) * inv - (s.greedy ? 0.0 : log(all)));
         if (a.kept) a.kept[row] = s.greedy ? 1 : there;
     }
 }
@@ -802,14 +833,6 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
     if constexpr (SPLIT)
         if (tid < S) own = *(const PartHead *)(part + tid * parts.bytes);
     if (!s.ok) return no_answer(a, row);
-
-    // a part's two counts, 0 where it has none of the block (its memory is not written)
-    const auto counts_of = [&](int q, int b, int pair) {
-        const bool there = q < S && f.blocks[q][b >> 6] >> (b & 63) & 1;
-        const uint32_t *p = (const uint32_t *)(part + (there ? q * parts.bytes + 64 : 0)) + (there ? b * 64 + pair : 0);
-        const uint32_t x = *p;
-        return there ? x : 0;
-    };
 
     // ---- the blocks in use, and the counts of their bins
     if (tid < 4) f.used[tid] = 0;
@@ -855,45 +878,58 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
             else if (tid < kBelow >> 7) f.place[256 + (kLow >> 7) + tid - (kNegative >> 7)] = at * 128;
         }
         __syncthreads();
-        constexpr int kRounds = kSlots * 64 / kThreads;
+        // a wavefront has every 16th block, two counts a lane; 8 parts of each of its blocks are on their way together
+        constexpr int kRounds = kSlots / kWaves;
         uint32_t c0[kRounds] = {}, c1[kRounds] = {};
         if constexpr (SPLIT) {
+            uint64_t has[kRounds];               // parts that have counts of the block
+            const uint32_t *from[kRounds];
+#pragma unroll
+            for (int k = 0; k < kRounds; ++k) {
+                const int slot = wave + k * kWaves;
+                const int b = __builtin_amdgcn_readfirstlane(f.block[min(slot, slots - 1)]);
+                has[k] = slot < slots ? __ballot(lane < S && (f.blocks[lane][b >> 6] >> (b & 63) & 1)) : 0;
+                from[k] = (const uint32_t *)(part + 64) + b * 64 + lane;
+            }
 #pragma unroll 1
-            for (int q0 = 0; q0 < S; q0 += 8) {              // (24 loads on their way together)
+            while (has[0] | has[1] | has[2]) {
                 uint32_t x[kRounds][8];
 #pragma unroll
-                for (int k = 0; k < kRounds; ++k) {
-                    const int i = tid + k * kThreads, b = f.block[min(i >> 6, slots - 1)];
+                for (int j = 0; j < 8; ++j)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) x[k][j] = counts_of(i < slots * 64 ? q0 + j : S, b, i & 63);
-                }
+                    for (int k = 0; k < kRounds; ++k) {
+                        x[k][j] = 0;
+                        if (has[k]) x[k][j] = from[k][__builtin_ctzll(has[k]) * (parts.bytes / 4)];
+                        has[k] &= has[k] - 1;
+                    }
 #pragma unroll
-                for (int k = 0; k < kRounds; ++k)
+                for (int j = 0; j < 8; ++j)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) c0[k] += x[k][j] & 0xffffu, c1[k] += x[k][j] >> 16;
+                    for (int k = 0; k < kRounds; ++k) c0[k] += x[k][j] & 0xffffu, c1[k] += x[k][j] >> 16;
             }
         } else {
 #pragma unroll
             for (int k = 0; k < kRounds; ++k) {
-                const int i = tid + k * kThreads;
-                if (i >= slots * 64) break;
-                const uint32_t x = f.hist[f.block[i >> 6] * 64 + (i & 63)];
+                const int slot = wave + k * kWaves;
+                if (slot >= slots) break;
+                const uint32_t x = f.hist[f.block[slot] * 64 + lane];
                 c0[k] = x & 0xffffu, c1[k] = x >> 16;
             }
         }
 #pragma unroll
         for (int k = 0; k < kRounds; ++k) {
-            const int i = tid + k * kThreads;
+            const int i = (wave + k * kWaves) * 64 + lane;
             if (i >= slots * 64) break;
             f.count[2 * i] = c0[k];
             f.count[2 * i + 1] = c1[k];
-            if (c0[k] | c1[k]) atomicMin(&f.first, 2 * i + (c0[k] == 0));
+            const uint64_t any = __ballot((c0[k] | c1[k]) != 0);
+            if (any && lane == __builtin_ctzll(any)) atomicMin(&f.first, 2 * i + (c0[k] == 0));
         }
         __syncthreads();
     }
     const auto bin_at = [&](int i) { return f.block[i >> 7] * 128 + (i & 127); };
     double zmax = 0.0;
-    const double t = (double)s.temp;
+    const double inv = 1.0 / (double)s.temp;
     int c[kPer], cs = 0, cb = 0, n = 0;
     double ms = 0.0, mb = 0.0, mall = 0.0;
     const int b0 = tid * kPer;
@@ -902,13 +938,13 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
         zmax = (double)value_of(top);
         // values below -2^15 are counted only: their weights vanish, or the row is not for these bins
         const bool below = f.used[kBelow >> 12] >> (kBelow >> 7 & 31) & 1;
-        fine = top == kBelow || (below && (zmax + 32768.0) / t < 800.0);
+        fine = top == kBelow || (below && (zmax + 32768.0) * inv < 800.0);
     }
     if (!fine) {
 #pragma unroll 1
         for (int i = tid; i < kSlots * 128 + 256; i += kThreads) {
             const int b = i < bins ? bin_at(i) : kBelow;
-            f.weight[i] = b != kBelow && f.count[i] ? exp(((double)value_of(b) - zmax) / t) : 0.0;
+            f.weight[i] = b != kBelow && f.count[i] ? exp_below(((double)value_of(b) - zmax) * inv) : 0.0;
         }
         __syncthreads();
 #pragma unroll
@@ -1007,20 +1043,35 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
         const int twice = 2 * S <= kWaves, blocks = min(slots, (end >> 7) + 1);
         for (int q = wave >> twice; q < S; q += kWaves >> twice) {
             Range x{0.0, 0, 0};
+            // the part's blocks up to the run's end, by their places here
+            bool in = false;
+            if (lane < blocks) {
+                const int b = f.block[lane];
+                in = f.blocks[q][b >> 6] >> (b & 63) & 1;
+            }
+            uint64_t has = __ballot(in);
+            if (twice) has &= wave & 1 ? 0xaaaaaaaaaaaaaaaaull : 0x5555555555555555ull;
+            const uint32_t *from = (const uint32_t *)(part + (int64_t)q * parts.bytes + 64) + lane;
 #pragma unroll 1
-            for (int i0 = twice ? wave & 1 : 0; i0 < blocks; i0 += 8 << twice) {
+            while (has) {
                 uint32_t y[8];
+                int at[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const int i = i0 + (j << twice);
-                    y[j] = counts_of(i < blocks ? q : S, f.block[min(i, slots - 1)], lane);
+                    y[j] = 0;
+                    at[j] = kSlots * 128;
+                    if (has) {
+                        const int i = __builtin_ctzll(has);
+                        y[j] = from[__builtin_amdgcn_readfirstlane(f.block[i]) * 64];
+                        at[j] = i * 128;
+                    }
+                    has &= has - 1;
                 }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const int at = min(i0 + (j << twice), kSlots) * 128 + 2 * lane;
-                    const int n0 = (int)(y[j] & 0xffffu), n1 = (int)(y[j] >> 16);
-                    x.mass += n0 * f.weight[at] + n1 * f.weight[at + 1];
-                    x.ties += at == end ? n0 : at + 1 == end ? n1 : 0;
+                    const int i = at[j] + 2 * lane, n0 = (int)(y[j] & 0xffffu), n1 = (int)(y[j] >> 16);
+                    x.mass += n0 * f.weight[i] + n1 * f.weight[i + 1];
+                    x.ties += i == end ? n0 : i + 1 == end ? n1 : 0;
                 }
             }
             x.mass = wave_sum(x.mass);
@@ -1049,7 +1100,7 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
     const int token = locate<uint16_t, 4>(z, item, begin, stop, tie_weight, d, f.ranges);
     if (tid == 0) {
         a.token[row] = token;
-        if (a.logp) a.logp[row] = (float)(((double)bf16_bits_to_f32(z[token]) - zmax) / t - log(all));
+        if (a.logp) a.logp[row] = (float)(((double)bf16_bits_to_f32(z[token]) - zmax) * inv - log(all));
         if (a.kept) a.kept[row] = kept;
     }
 }
