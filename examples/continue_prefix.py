@@ -1,11 +1,12 @@
 """A one-layer student on continuations of shared prefixes: rollouts, then its update.
 
     python examples/continue_prefix.py [--steps 4] [--tokens 48] [--prefix 300] [--rollouts 4]
+                                       [--temperature 0.8 --top-p 0.95]
 
 The student is a frozen embedding, one attention layer with normed and rotated query and key
 heads, a residual, and a vocabulary projection. Two prefixes are continued by several rollouts
 each, one token of all rollouts at a time (the keys and values go to pages of a cache, each
-prefix is read once for its rollouts), and the update of Eq. 1 runs on the continuations: the
+prefix is read once for its rollouts; the next token is the likeliest, or drawn at a temperature), and the update of Eq. 1 runs on the continuations: the
 layer's forward over whole continuations, the scoring with its backward, the layer's backward,
 and the clipping of all gradients to a global norm. The layer's dense products are torch's;
 everything else goes through the library.
@@ -79,8 +80,24 @@ class Prefixes:
             max_prefix=max(self.len), max_suffix=max_suffix, prefix_rows=sum(self.len), **kw)
 
 
-def roll_out(p, pre, table, rollouts, first, tokens):
-    """Greedy continuations [B, tokens] whose first token is given, and their attention outputs."""
+def rows_of(p, ids):
+    """The embedding's rows of tokens [n]."""
+    x = torch.empty(len(ids), D, dtype=BF16, device="cuda")
+    L.olive_embed(L.make_embed_desc(len(ids), V, D, ids), p["embed"], x)
+    return x
+
+
+def draw(p, h, out, temperature, top_p):
+    """The next tokens of rows h at a temperature, from the likeliest that make up top_p."""
+    B = len(h)
+    fill = lambda v: torch.full((B,), v, device="cuda")  # noqa: E731
+    d = L.make_sample_desc(B, V, torch.rand(B, device="cuda"), temperature=fill(temperature), top_p=fill(top_p))
+    work = torch.empty(L.olive_sample_workspace(d), dtype=torch.uint8, device="cuda")
+    L.olive_sample(d, h @ p["head"].t(), out, workspace=work)
+
+
+def roll_out(p, pre, table, rollouts, first, tokens, temperature=0.0, top_p=1.0):
+    """Continuations [B, tokens] whose first token is given, and their attention outputs."""
     B = rollouts * len(pre.len)
     pages = -(-tokens // PAGE)
     kc, vc = (torch.zeros(B * pages * PAGE, HK, HD, dtype=BF16, device="cuda") for _ in range(2))
@@ -91,7 +108,7 @@ def roll_out(p, pre, table, rollouts, first, tokens):
     work, logp, nxt = None, torch.empty(B, device="cuda"), torch.empty(B, dtype=torch.int32, device="cuda")
     y, outs = [first.int()], []
     for t in range(tokens):
-        x = p["embed"][y[-1].long()]
+        x = rows_of(p, y[-1])
         q, k, v = project(p, x)
         slots = page_table[:, t // PAGE] * PAGE + t % PAGE
         qn, out = torch.empty(B, HQ, HD, dtype=BF16, device="cuda"), torch.empty(B, HQ, HD, dtype=BF16, device="cuda")
@@ -102,7 +119,10 @@ def roll_out(p, pre, table, rollouts, first, tokens):
             work = torch.empty(L.olive_prefix_attention_workspace(d), dtype=torch.uint8, device="cuda")
         L.olive_prefix_attention(d, qn, pre.k, pre.v, kc, vc, out, workspace=work)
         h = x + out.view(B, -1) @ p["wo"]
-        L.olive_token_logprobs(ctx, L.make_batch(cu, cut, y[-1], h), logp, argmax_student=nxt)
+        if temperature > 0.0:
+            draw(p, h, nxt, temperature, top_p)
+        else:
+            L.olive_token_logprobs(ctx, L.make_batch(cu, cut, y[-1], h), logp, argmax_student=nxt)
         outs.append(out)
         y.append(nxt.clone())
     L.olive_score_free(ctx)
@@ -114,7 +134,7 @@ def update(p, pre, table, rollouts, y, targets, max_norm):
     gradients and their norm. y, targets: [B, n] tokens."""
     B, n = y.shape
     T = B * n
-    x = p["embed"][y.reshape(-1).long()]
+    x = rows_of(p, y.reshape(-1).int())
     q, k, v = project(p, x)
     pos = torch.cat([torch.arange(m, m + n) for m in pre.len for _ in range(rollouts)]).int().cuda()
     qd = qk_desc(p, pos, table)
@@ -167,6 +187,8 @@ def main(argv=None):
     ap.add_argument("--tokens", type=int, default=48)
     ap.add_argument("--prefix", type=int, default=300)
     ap.add_argument("--rollouts", type=int, default=4)
+    ap.add_argument("--temperature", type=float, default=0.0)
+    ap.add_argument("--top-p", type=float, default=1.0)
     ap.add_argument("--lr", type=float, default=0.05)
     a = ap.parse_args(argv)
     torch.manual_seed(0)
@@ -176,7 +198,7 @@ def main(argv=None):
     B = a.rollouts * len(lengths)
     first = torch.randint(0, V, (B,)).cuda()
     pre = Prefixes(p, tokens, table)
-    y, stepwise = roll_out(p, pre, table, a.rollouts, first, a.tokens)
+    y, stepwise = roll_out(p, pre, table, a.rollouts, first, a.tokens, a.temperature, a.top_p)
     # the teacher's tokens at the student's states stand in for a teacher's continuation
     targets = torch.randint(0, V, y.shape).cuda()
     losses = []

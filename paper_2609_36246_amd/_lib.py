@@ -264,20 +264,25 @@ def _ptr(x) -> Optional[int]:
 _device = None           # torch's own entry for the current device, once torch has set up its devices
 
 
-def _stream(stream) -> Optional[int]:
+def _here() -> int:
+    """The current device's index (-1 without a GPU)."""
     global _device
+    if _device is None:
+        import torch
+        if not torch.cuda.is_available():
+            return -1
+        torch.cuda.current_device()
+        _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _device()
+
+
+def _stream(stream) -> Optional[int]:
     if stream is None:
         import torch
         # torch's bare handle where this torch has it: the public call makes a Stream object each
         # time, of the same handle
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if raw is None:
-            return torch.cuda.current_stream().cuda_stream
-        if _device is None:
-            device = torch.cuda.current_device()
-            _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-            return raw(device)
-        return raw(_device())
+        return torch.cuda.current_stream().cuda_stream if raw is None else raw(_here())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -713,17 +718,30 @@ def olive_grad_clip_free(ctx) -> int:
     return load().olive_grad_clip_free(ctx)
 
 
-def _rows(x, dtype, rows: int, width: int, what: str, output: bool = False):
-    """Address and row stride of a [rows, width] tensor of a torch type, contiguous within a row
-    (None: neither); an output's rows do not overlap."""
+def _elsewhere(x, here: int, what: str):
+    raise ValueError("%s: a tensor on device %d, and the current one is %d" % (what, x.get_device(), here))
+
+
+def _rows(x, dtype, rows: int, width: int, here: int, what: str, output: bool = False):
+    """Address and row stride of a [rows, width] tensor of a torch type on the current device,
+    contiguous within a row (None: neither); an output's rows do not overlap."""
     if x is None:
         return None, 0
     if x.dtype is dtype and x.shape == (rows, width):
         apart, step = x.stride()
         if (step == 1 or width <= 1) and not (output and apart < width and rows > 1):
+            if x.get_device() != here:
+                _elsewhere(x, here, what)
             return x.data_ptr(), apart
     raise ValueError("%s: expected [%d, %d] of %s with contiguous rows%s"
                      % (what, rows, width, dtype, " apart from each other" if output else ""))
+
+
+def _there(x, here: int, what: str):
+    """A tensor, None or an address, which is the current device's if it is a tensor."""
+    if x is not None and not isinstance(x, int) and x.get_device() != here:
+        _elsewhere(x, here, what)
+    return x
 
 
 def _bytes_of(name, desc) -> int:
@@ -744,9 +762,9 @@ def make_embed_desc(tokens, vocab, width, ids, dtype=OLIVE_BF16, scale=1.0) -> o
 
 def olive_embed(desc: olive_embed_desc, table, out, stream=None, check: bool = True) -> int:
     """out [tokens, width] gets scale * table[ids]; table [vocab, width]."""
-    dtype = _dtype(desc.dtype)
-    s = _call("olive_embed")(ctypes.addressof(desc), *_rows(table, dtype, desc.vocab, desc.width, "table"),
-                             *_rows(out, dtype, desc.tokens, desc.width, "out", True), _stream(stream))
+    dtype, here = _dtype(desc.dtype), _here()
+    s = _call("olive_embed")(ctypes.addressof(desc), *_rows(table, dtype, desc.vocab, desc.width, here, "table"),
+                             *_rows(out, dtype, desc.tokens, desc.width, here, "out", True), _stream(stream))
     if check:
         _check(s, "olive_embed")
     return s
@@ -763,11 +781,11 @@ def olive_embed_backward(desc: olive_embed_desc, grad_out, grad_table, accumulat
     added to the rows of the tokens that occur."""
     if str(grad_table.dtype) not in ("torch.bfloat16", "torch.float32"):
         raise ValueError("grad_table: expected bf16 or fp32")
-    kind = OLIVE_F32 if str(grad_table.dtype) == "torch.float32" else OLIVE_BF16
+    kind, here = OLIVE_F32 if str(grad_table.dtype) == "torch.float32" else OLIVE_BF16, _here()
     s = _call("olive_embed_backward")(
-        ctypes.addressof(desc), *_rows(grad_out, _dtype(desc.dtype), desc.tokens, desc.width, "grad_out"),
-        *_rows(grad_table, grad_table.dtype, desc.vocab, desc.width, "grad_table", True), kind, int(accumulate),
-        *_workspace(workspace), _stream(stream))
+        ctypes.addressof(desc), *_rows(grad_out, _dtype(desc.dtype), desc.tokens, desc.width, here, "grad_out"),
+        *_rows(grad_table, grad_table.dtype, desc.vocab, desc.width, here, "grad_table", True), kind, int(accumulate),
+        *_workspace(_there(workspace, here, "workspace")), _stream(stream))
     if check:
         _check(s, "olive_embed_backward")
     return s
@@ -787,10 +805,10 @@ def make_norm_desc(rows, width, weight=None, bias=None, dtype=OLIVE_BF16, eps=1e
 
 def olive_row_norm(desc: olive_norm_desc, x, out, residual=None, sum_out=None, stream=None, check: bool = True) -> int:
     """All [rows, width]: out gets the norm of x + residual, sum_out that sum."""
-    t, n, w = _dtype(desc.dtype), desc.rows, desc.width
-    s = _call("olive_row_norm")(ctypes.addressof(desc), *_rows(x, t, n, w, "x"), *_rows(residual, t, n, w, "residual"),
-                                *_rows(out, t, n, w, "out", True), *_rows(sum_out, t, n, w, "sum_out", True),
-                                _stream(stream))
+    t, n, w, here = _dtype(desc.dtype), desc.rows, desc.width, _here()
+    s = _call("olive_row_norm")(
+        ctypes.addressof(desc), *_rows(x, t, n, w, here, "x"), *_rows(residual, t, n, w, here, "residual"),
+        *_rows(out, t, n, w, here, "out", True), *_rows(sum_out, t, n, w, here, "sum_out", True), _stream(stream))
     if check:
         _check(s, "olive_row_norm")
     return s
@@ -804,12 +822,13 @@ def olive_row_norm_workspace(desc: olive_norm_desc) -> int:
 def olive_row_norm_backward(desc: olive_norm_desc, h, grad_out, grad_h, grad_sum=None, grad_weight=None,
                             grad_bias=None, workspace=None, stream=None, check: bool = True) -> int:
     """h: the rows that were normed (the forward's sum_out, or x without a residual)."""
-    t, n, w = _dtype(desc.dtype), desc.rows, desc.width
+    t, n, w, here = _dtype(desc.dtype), desc.rows, desc.width, _here()
     s = _call("olive_row_norm_backward")(
-        ctypes.addressof(desc), *_rows(h, t, n, w, "h"), *_rows(grad_out, t, n, w, "grad_out"),
-        *_rows(grad_sum, t, n, w, "grad_sum"), *_rows(grad_h, t, n, w, "grad_h", True),
-        _array(grad_weight, OLIVE_F32, w, "grad_weight"), _array(grad_bias, OLIVE_F32, w, "grad_bias"),
-        *_workspace(workspace), _stream(stream))
+        ctypes.addressof(desc), *_rows(h, t, n, w, here, "h"), *_rows(grad_out, t, n, w, here, "grad_out"),
+        *_rows(grad_sum, t, n, w, here, "grad_sum"), *_rows(grad_h, t, n, w, here, "grad_h", True),
+        _array(_there(grad_weight, here, "grad_weight"), OLIVE_F32, w, "grad_weight"),
+        _array(_there(grad_bias, here, "grad_bias"), OLIVE_F32, w, "grad_bias"),
+        *_workspace(_there(workspace, here, "workspace")), _stream(stream))
     if check:
         _check(s, "olive_row_norm_backward")
     return s
@@ -838,11 +857,12 @@ def olive_sample_workspace(desc: olive_sample_desc) -> int:
 def olive_sample(desc: olive_sample_desc, logits, token, logp=None, kept=None, workspace=None, stream=None,
                  check: bool = True) -> int:
     """logits [rows, vocab]; token, kept int32 [rows], logp fp32 [rows]."""
-    n = desc.rows
+    n, here = desc.rows, _here()
     s = _call("olive_sample")(
-        ctypes.addressof(desc), *_rows(logits, _dtype(desc.dtype), n, desc.vocab, "logits"),
-        _array(token, "int32", n, "token"), _array(logp, OLIVE_F32, n, "logp"), _array(kept, "int32", n, "kept"),
-        *_workspace(workspace), _stream(stream))
+        ctypes.addressof(desc), *_rows(logits, _dtype(desc.dtype), n, desc.vocab, here, "logits"),
+        _array(_there(token, here, "token"), "int32", n, "token"),
+        _array(_there(logp, here, "logp"), OLIVE_F32, n, "logp"), _array(_there(kept, here, "kept"), "int32", n, "kept"),
+        *_workspace(_there(workspace, here, "workspace")), _stream(stream))
     if check:
         _check(s, "olive_sample")
     return s

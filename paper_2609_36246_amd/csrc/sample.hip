@@ -76,12 +76,13 @@ struct Parts {
     int32_t bytes;                               // of a part in the workspace
 };
 
-// Rows of up to 16384 tokens are counted by the workgroup that does the rest (one launch: 32 rows of
-// 16384 take 15 us, in two launches 19). Else about 512 workgroups count, each 4096 tokens at least.
+// Rows of up to 16384 tokens are counted by the workgroup that does the rest, in one launch. Else a
+// row has up to 16 parts of 4096 tokens at least, fewer where there are more than 128 rows (a part
+// costs the second launch its counts: 64 rows of 151936 take the same with 8 and with 16).
 Parts parts_of(const SampleArgs &a) {
     // (every row keeps every token, or the first alone)
     const bool plain = !a.top_k && !a.top_p && !a.min_p && a.vocab <= kMostParts * kWhole;
-    int64_t s = (plain ? 1024 : 512) / a.rows, least = (a.vocab + kMostPart - 1) / kMostPart;
+    int64_t s = (plain ? 1024 : 2048) / a.rows, least = (a.vocab + kMostPart - 1) / kMostPart;
     if (plain) least = (a.vocab + kWhole - 1) / kWhole;
     const int64_t most = plain ? (a.vocab + 2047) / 2048 : (a.vocab + 4095) / 4096;
     if (a.vocab <= 16384) s = least = 1;
@@ -131,16 +132,22 @@ __device__ __forceinline__ float token_value(uint32_t bits) {
 }
 
 // Counts of [begin, end) of a row into 16-bit bins (two to a word); the flags of its odd values.
-// Four lots a thread are on their way together.
-template <int THREADS>
-__device__ __forceinline__ int count_bins(const uint16_t *z, int begin, int end, uint32_t *hist) {
+// Four lots a thread are on their way together, the first ones while `clear` makes the bins empty.
+template <int THREADS, typename Clear>
+__device__ __forceinline__ int count_bins(const uint16_t *z, int begin, int end, uint32_t *hist, Clear clear) {
     constexpr int kAhead = 4;
     int flags = 0;
-#pragma unroll 1
-    for (int i0 = begin + (int)threadIdx.x * 8; i0 < end; i0 += kAhead * THREADS * 8) {
-        Lot x[kAhead];
+    Lot x[kAhead];
+    const int first = begin + (int)threadIdx.x * 8;
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) x[k] = load_tokens(z, i0 + k * THREADS * 8, end);
+    for (int k = 0; k < kAhead; ++k) x[k] = load_tokens(z, first + k * THREADS * 8, end);
+    clear();
+#pragma unroll 1
+    for (int i0 = first; i0 < end; i0 += kAhead * THREADS * 8) {
+        if (i0 != first) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) x[k] = load_tokens(z, i0 + k * THREADS * 8, end);
+        }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (i0 + k * THREADS * 8 >= end) break;
@@ -258,11 +265,12 @@ __global__ __launch_bounds__(kPartThreads) void sample_counts_kernel(SampleArgs 
     const uint16_t *z = (const uint16_t *)a.logits.p + row * a.logits.st;
     char *to = a.work + (row * p.count + part) * p.bytes;
     PartHead *head = (PartHead *)to;
-    for (int i = tid; i < kBins / 8; i += kPartThreads) ((uint4 *)hist)[i] = make_uint4(0, 0, 0, 0);
-    if (tid < 4) used[tid] = 0;
-    if (tid == 4) flags = 0;
-    __syncthreads();
-    const int f = count_bins<kPartThreads>(z, begin, end, hist);
+    const int f = count_bins<kPartThreads>(z, begin, end, hist, [&]() {
+        for (int i = tid; i < kBins / 8; i += kPartThreads) ((uint4 *)hist)[i] = make_uint4(0, 0, 0, 0);
+        if (tid < 4) used[tid] = 0;
+        if (tid == 4) flags = 0;
+        __syncthreads();
+    });
     if (f) atomicOr(&flags, (uint32_t)f);
     __syncthreads();
     for (int b = wave; b < kBlocks; b += kPartWaves) {
@@ -819,10 +827,17 @@ __global__ __launch_bounds__(kThreads) void sample_all_kernel(SampleArgs a, Part
     }
 }
 
-// (64 registers: two workgroups a compute unit where there are rows enough)
-template <bool SPLIT>
-__global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(SampleArgs a, Parts parts) {
-    __shared__ std::conditional_t<SPLIT, CoarsePool, CoarseRow> f;
+// MANY: 64 registers, so that two workgroups share a compute unit, and the rows that these bins do
+// not hold are left to a launch of their own (4.5 us); else they are answered here.
+template <bool SPLIT, bool MANY>
+__global__ __launch_bounds__(kThreads, MANY ? 8 : 4) void sample_coarse_kernel(SampleArgs a, Parts parts) {
+    using Coarse = std::conditional_t<SPLIT, CoarsePool, CoarseRow>;
+    __shared__ union Pool {
+        Coarse c;
+        std::conditional_t<MANY, char, FinePool> f;
+        __device__ Pool() {}
+    } pool;
+    Coarse &f = pool.c;
     constexpr int kPer = kSlots * 128 / kThreads;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int V = a.vocab, S = parts.count;
@@ -837,10 +852,8 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
     // ---- the blocks in use, and the counts of their bins
     if (tid < 4) f.used[tid] = 0;
     if (tid == 4) f.flags = 0, f.first = kSlots * 128, f.bin_k = f.bin_p = kSlots * 128, f.bin_m = -1;
-    if constexpr (!SPLIT)
-        for (int i = tid; i < kBins / 2; i += kThreads) f.hist[i] = 0;
-    __syncthreads();
     if constexpr (SPLIT) {
+        __syncthreads();
         if (tid < S) {
             const PartHead &h = own;
             f.blocks[tid][0] = h.blocks[0];
@@ -849,7 +862,10 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
             if (h.flags) atomicOr(&f.flags, (uint32_t)h.flags);
         }
     } else {
-        const int flags = count_bins<kThreads>(z, 0, V, f.hist);
+        const int flags = count_bins<kThreads>(z, 0, V, f.hist, [&]() {
+            for (int i = tid; i < kBins / 2; i += kThreads) f.hist[i] = 0;
+            __syncthreads();
+        });
         if (flags) atomicOr(&f.flags, (uint32_t)flags);
         __syncthreads();
         for (int b = wave; b < kBlocks; b += kWaves)
@@ -858,7 +874,7 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
     __syncthreads();
     int slots = 0;
     for (int i = 0; i < 4; ++i) slots += __popc(f.used[i]);
-    if ((f.flags & 1) || slots == 0) return no_answer(a, row);
+    if ((f.flags & 1) || (slots == 0 && !(f.flags & 2))) return no_answer(a, row);
     // (u = 0 and 1 ask for the first and the last token kept, whatever they weigh)
     bool fine = (f.flags & 2) || slots > kSlots || s.u == 0.f || s.u == 1.f;
     const int bins = slots * 128;
@@ -1028,7 +1044,12 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 8 : 4) void sample_coarse_kernel(
         measure();
     }
     if (fine) {
-        if (tid == 0) a.token[row] = kLeft;
+        if constexpr (MANY) {
+            if (tid == 0) a.token[row] = kLeft;
+        } else {
+            __syncthreads();
+            sample_fine<uint16_t>(a, row, s, pool.f);
+        }
         return;
     }
     const int kept = f.above;
@@ -1124,18 +1145,24 @@ hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t st) {
         return hipGetLastError();
     }
     if (p.count == 1) {
-        sample_coarse_kernel<false><<<a.rows, kThreads, 0, st>>>(a, p);
-    } else {
-        const bool plain = p.bytes == sizeof(PartHead);
-        if (plain) sample_masses_kernel<<<dim3(a.rows, p.count), kPartThreads, 0, st>>>(a, p);
-        else sample_counts_kernel<<<dim3(a.rows, p.count), kPartThreads, 0, st>>>(a, p);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        if (plain) sample_all_kernel<<<a.rows, kThreads, 0, st>>>(a, p);
-        else sample_coarse_kernel<true><<<a.rows, kThreads, 0, st>>>(a, p);
-        if (plain) return hipGetLastError();     // (every row is answered)
+        sample_coarse_kernel<false, false><<<a.rows, kThreads, 0, st>>>(a, p);
+        return hipGetLastError();
     }
-    const hipError_t e = hipGetLastError();
+    const bool plain = p.bytes == sizeof(PartHead);
+    if (plain) sample_masses_kernel<<<dim3(a.rows, p.count), kPartThreads, 0, st>>>(a, p);
+    else sample_counts_kernel<<<dim3(a.rows, p.count), kPartThreads, 0, st>>>(a, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (plain) {
+        sample_all_kernel<<<a.rows, kThreads, 0, st>>>(a, p);
+        return hipGetLastError();
+    }
+    if (a.rows <= kChipUnits) {
+        sample_coarse_kernel<true, false><<<a.rows, kThreads, 0, st>>>(a, p);
+        return hipGetLastError();
+    }
+    sample_coarse_kernel<true, true><<<a.rows, kThreads, 0, st>>>(a, p);
+    e = hipGetLastError();
     if (e != hipSuccess) return e;
     sample_fine_kernel<uint16_t, true><<<a.rows, kThreads, 0, st>>>(a);
     return hipGetLastError();

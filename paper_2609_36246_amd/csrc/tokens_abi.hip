@@ -106,6 +106,8 @@ olive_status olive_embed(const olive_embed_desc *desc, const void *table, int64_
     if (!apart(desc->vocab, desc->width, table_stride, false) || !apart(desc->tokens, desc->width, out_stride, true))
         return OLIVE_E_SHAPE;
     if (misplaced(table, desc->dtype) || misplaced(out, desc->dtype)) return OLIVE_E_UNSUPPORTED;
+    // (wavefronts of a launch, four to a workgroup)
+    if (desc->tokens * ((desc->width + 255) / 256) / 4 >= kMostBlocks) return OLIVE_E_SHAPE;
     EmbedArgs a = embed_args(desc);
     a.table = {(char *)table, table_stride};
     a.out = {(char *)out, out_stride};

@@ -194,6 +194,61 @@ def test_extremes_of_the_type():
         Sample(z, [0.1234, 0.4567, 0.7891, 0.5003], **s).check()
 
 
+@pytest.mark.parametrize("vocab", [900, 40000, 151936])
+def test_values_of_every_size(vocab):
+    """bf16 rows that a table with a bin for each value does not hold: more powers of two than it has
+    blocks, tiny values, values beyond 2^15 and below -2^15; ordinary rows between them."""
+    gen = torch.Generator().manual_seed(vocab)
+    n = 8
+    z = torch.randn(n, vocab, generator=gen) * 3.0
+    z[1] = torch.randn(vocab, generator=gen) * 2.0 ** torch.randint(-39, 14, (vocab,), generator=gen)
+    z[2, ::3] = torch.randn(len(z[2, ::3]), generator=gen) * 1e-20
+    z[3] *= 20000.0
+    z[4, vocab // 2:] = -1e30
+    z[5, : vocab - 5] = -60000.0
+    z[5, vocab - 5:] = -32768.0
+    z[6] = -40000.0 + 100.0 * torch.randn(vocab, generator=gen)
+    z = z.to(BF16).cuda()
+    for s in (dict(), dict(top_k=30), dict(top_k=vocab - 100, top_p=0.97), dict(min_p=0.03), dict(temperature=60.0, top_p=0.8),
+              dict(temperature=1e4, top_k=500), dict(temperature=0.0)):
+        Sample(z, uniform(n, 3), **s).check()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_vocabulary_of_millions(dtype):
+    z = normal(1, 4500001, dtype, 1.0)
+    for s in (dict(), dict(top_k=300, top_p=0.9), dict(top_p=0.5), dict(temperature=0.0)):
+        Sample(z, [0.6180], **s).check()
+
+
+def test_ties_across_parts():
+    """Equal values at the border in every part of long rows, and runs that end inside one."""
+    z = torch.full((4, 50000), -1.0, dtype=BF16, device="cuda")
+    z[1, 25000:] = -2.0
+    z[2, ::7] = 1.5
+    z[3, 49999] = 5.0
+    for s in (dict(top_k=30000), dict(top_k=7500), dict(top_k=20001, temperature=0.5), dict(top_p=0.7301)):
+        Sample(z, [0.1003, 0.9502, 0.5001, 0.7503], **s).check()
+
+
+def test_draws_at_both_ends_of_long_rows():
+    z = normal(6, 60000, BF16, 2.0)
+    for s in (dict(), dict(top_k=77), dict(top_p=0.9), dict(min_p=0.01)):
+        Sample(z, [0.0, 1.0, 0.0, 1.0, 2.0 ** -24, 1.0 - 2.0 ** -24], **s).check()
+
+
+def test_many_rows():
+    """More rows than compute units: the counts are added by two workgroups a compute unit, and rows that
+    the bins do not hold by a launch of their own."""
+    z = normal(300, 20000, BF16, 3.0)
+    z[5] *= 1e-15
+    z[299] *= 50000.0
+    u = uniform(300, 12)
+    u[7], u[8] = 0.0, 1.0
+    Sample(z, u, top_p=0.92, temperature=0.9).check()
+    Sample(z[:, :9000].contiguous(), u, top_k=40).check()
+
+
 def test_optional_outputs_and_no_rows():
     z = normal(5, 800, BF16)
     full = Sample(z, 0.6, top_p=0.8)

@@ -251,7 +251,20 @@ def test_calls_of_other_tensors(monkeypatch):
     bad += [lambda: L.olive_sample(s, m(), tok, logp=torch.zeros(6, dtype=torch.float64), stream=0),
             lambda: L.olive_sample(s, m(), tok, kept=torch.zeros(6), stream=0)]
     for call in bad:
-        with pytest.raises(ValueError):
+        with pytest.raises(ValueError, match="expected|contiguous"):
+            call()
+
+
+def test_tensors_of_another_device(monkeypatch):
+    """What is not on the current device is refused before the library is entered."""
+    monkeypatch.setattr(L, "_call", lambda name: lambda *a: pytest.fail("the library was entered"))
+    monkeypatch.setattr(L, "_here", lambda: 3)
+    x, ids, f = torch.zeros(6, 64, dtype=BF16), torch.zeros(6, dtype=I32), torch.zeros(6)
+    e, k, s = L.make_embed_desc(6, 6, 64, ids), L.make_norm_desc(6, 64), L.make_sample_desc(6, 64, f)
+    for call in (lambda: L.olive_embed(e, x, x, stream=0), lambda: L.olive_embed_backward(e, x, x, stream=0),
+                 lambda: L.olive_row_norm(k, x, x, stream=0), lambda: L.olive_row_norm_backward(k, x, x, x, stream=0),
+                 lambda: L.olive_sample(s, x, ids, stream=0)):
+        with pytest.raises(ValueError, match="on device -1, and the current one is 3"):
             call()
 
 
