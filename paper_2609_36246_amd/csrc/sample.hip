@@ -69,7 +69,7 @@ struct PartHead {
 static_assert(sizeof(PartHead) == 64, "");
 constexpr int kPartThreads = 512;
 constexpr int kMostParts = 64, kMostPart = 65024;            // (16-bit counts)
-constexpr int kWhole = kPartThreads * 8 * 4;                 // tokens of a part whose mass is formed at once
+template <typename T> constexpr int kWhole = kPartThreads * kLot<T> * 4;     // tokens of a part whose mass is formed at once
 
 struct Parts {
     int32_t count, len;
@@ -79,13 +79,16 @@ struct Parts {
 // Rows of up to 16384 tokens are counted by the workgroup that does the rest, in one launch. Else a
 // row has up to 16 parts of 4096 tokens at least, fewer where there are more than 128 rows (a part
 // costs the second launch its counts: 64 rows of 151936 take the same with 8 and with 16).
-Parts parts_of(const SampleArgs &a) {
+// Rows of fp32 that are cut are not split (count 0).
+Parts parts_of(const SampleArgs &a, bool bf16) {
+    const int whole = bf16 ? kWhole<uint16_t> : kWhole<float>;
     // (every row keeps every token, or the first alone)
-    const bool plain = !a.top_k && !a.top_p && !a.min_p && a.vocab <= kMostParts * kWhole;
+    const bool plain = !a.top_k && !a.top_p && !a.min_p && a.vocab <= kMostParts * whole;
+    if (!bf16 && (!plain || a.vocab <= 4096)) return Parts{0, 0, 0};
     int64_t s = (plain ? 1024 : 2048) / a.rows, least = (a.vocab + kMostPart - 1) / kMostPart;
-    if (plain) least = (a.vocab + kWhole - 1) / kWhole;
+    if (plain) least = (a.vocab + whole - 1) / whole;
     const int64_t most = plain ? (a.vocab + 2047) / 2048 : (a.vocab + 4095) / 4096;
-    if (a.vocab <= 16384) s = least = 1;
+    if (bf16 && a.vocab <= 16384) s = least = 1;
     if (s > most) s = most;
     if (s > (plain ? kMostParts : 16)) s = plain ? kMostParts : 16;
     if (s < least) s = least;
@@ -98,17 +101,21 @@ template <typename T>
 __device__ __forceinline__ Lot load_tokens(const T *z, int i, int end) {
     return load_lot(z, i, end, sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u);
 }
-// The same of WORDS words: 1, two bf16 tokens, in the first.
+// The same of WORDS words: 4, or 1 (two bf16 tokens or one of fp32), the first.
 template <typename T, int WORDS>
 __device__ __forceinline__ Lot load_some(const T *z, int i, int end) {
     if constexpr (WORDS == 4) {
         return load_tokens(z, i, end);
     } else {
-        static_assert(WORDS == 1 && sizeof(T) == 2, "");
-        struct __attribute__((packed, aligned(2))) Loose { uint32_t w; };
-        Lot x{{0xff80ff80u}};
-        if (i + 2 <= end) x.w[0] = ((const Loose *)(z + i))->w;
-        else if (i < end) x.w[0] = 0xff800000u | z[i];
+        static_assert(WORDS == 1, "");
+        Lot x{{sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u}};
+        if constexpr (sizeof(T) == 2) {
+            struct __attribute__((packed, aligned(2))) Loose { uint32_t w; };
+            if (i + 2 <= end) x.w[0] = ((const Loose *)(z + i))->w;
+            else if (i < end) x.w[0] = 0xff800000u | z[i];
+        } else {
+            if (i < end) x.w[0] = __float_as_uint(z[i]);
+        }
         return x;
     }
 }
@@ -202,26 +209,27 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs &a, int row) {
 }
 
 // Of calls without cuts: a part's largest value, and its mass relative to that.
+template <typename T>
 __global__ __launch_bounds__(kPartThreads) void sample_masses_kernel(SampleArgs a, Parts p) {
     constexpr int kPartWaves = kPartThreads / 64;
     const int64_t row = blockIdx.x;
     const int part = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int begin = part * p.len, end = min(a.vocab, begin + p.len);
-    const uint16_t *z = (const uint16_t *)a.logits.p + row * a.logits.st;
+    const T *z = (const T *)a.logits.p + row * a.logits.st;
     PartHead *head = (PartHead *)(a.work + (row * p.count + part) * p.bytes);
     const Settings s = settings_of(a, row);
     if (!s.ok) return;
-    __shared__ Lot lots[kWhole / 8];             // (a thread's own)
-    const int mine = (end - begin + kPartThreads * 8 - 1) / (kPartThreads * 8);
+    __shared__ Lot lots[kWhole<T> / kLot<T>];    // (a thread's own)
+    const int mine = (end - begin + kPartThreads * kLot<T> - 1) / (kPartThreads * kLot<T>);
 #pragma unroll
-    for (int i = 0; i < kWhole / 8 / kPartThreads; ++i)
-        if (i < mine) lots[i * kPartThreads + tid] = load_tokens(z, begin + (tid + i * kPartThreads) * 8, end);
+    for (int i = 0; i < 4; ++i)
+        if (i < mine) lots[i * kPartThreads + tid] = load_tokens(z, begin + (tid + i * kPartThreads) * kLot<T>, end);
     uint32_t top = 0, bad = 0;
     int n = 0;
 #pragma unroll 1
     for (int i = 0; i < mine; ++i)
-        each_token<uint16_t>(lots[i * kPartThreads + tid], [&](int, uint32_t bits) {
-            const float v = bf16_bits_to_f32(bits);
+        each_token<T>(lots[i * kPartThreads + tid], [&](int, uint32_t bits) {
+            const float v = token_value<T>(bits);
             bad |= !(v < __builtin_inff());
             n += v > kNegInf;
             top = max(top, f2ord(v));
@@ -239,8 +247,8 @@ __global__ __launch_bounds__(kPartThreads) void sample_masses_kernel(SampleArgs 
     double mass = 0.0;
 #pragma unroll 1
     for (int i = 0; i < mine; ++i)
-        each_token<uint16_t>(lots[i * kPartThreads + tid], [&](int, uint32_t bits) {
-            const float v = bf16_bits_to_f32(bits);
+        each_token<T>(lots[i * kPartThreads + tid], [&](int, uint32_t bits) {
+            const float v = token_value<T>(bits);
             mass += v > kNegInf ? exp_below(((double)v - first) * inv) : 0.0;
         });
     mass = wave_sum(mass);
@@ -558,13 +566,20 @@ template <typename T>
 __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const Settings &s, FinePool &f) {
     const T *z = (const T *)a.logits.p + row * a.logits.st;
     const int tid = threadIdx.x, V = a.vocab;
-    const auto each = [&](auto fn) {             // every token that is not -inf: fn(value, index)
-        Lot next = load_tokens(z, tid * kLot<T>, V);
+    // every token that is not -inf: fn(value, index); `light`: a few instructions, worth their unrolling
+    const auto each = [&](auto fn, auto light) {
+        constexpr int kStep = kThreads * kLot<T>, kAhead = 4;
+        const int first = tid * kLot<T>;
+        Lot ahead[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) ahead[j] = load_tokens(z, min(first + j * kStep, V), V);
 #pragma unroll 1
-        for (int i = tid * kLot<T>; i < V; i += kThreads * kLot<T>) {
-            const Lot x = next;
-            next = load_tokens(z, min(i + kThreads * kLot<T>, V), V);
-            each_token<T>(x, [&](int j, uint32_t bits) {
+        for (int i = first; i < V; i += kStep) {
+            const Lot x = ahead[0];
+#pragma unroll
+            for (int j = 0; j + 1 < kAhead; ++j) ahead[j] = ahead[j + 1];
+            ahead[kAhead - 1] = load_tokens(z, min(i + kAhead * kStep, V), V);
+            each_token<T, decltype(light)::value ? 4 : 1>(x, [&](int j, uint32_t bits) {
                 const float v = token_value<T>(bits) + 0.f;        // (-0 and 0 are the same value)
                 if (!(v == kNegInf)) fn(v, i + j);
             });
@@ -577,7 +592,7 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
         bad |= !(v < __builtin_inff());
         top = max(top, f2ord(v));
         ++n;
-    });
+    }, std::true_type{});
     if (s.k > 0 && s.k <= kFew) {
         // the least of the largest values of k groups of threads or more: k tokens at least reach it
         uint32_t group = top;
@@ -605,7 +620,7 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
             if (key < least) return;
             const uint32_t at = atomicAdd(&f.listed, 1u);
             if (at < (uint32_t)kFewList) f.key[at] = key, f.index[at] = i;
-        });
+        }, std::true_type{});
         __syncthreads();
         if (f.listed <= (uint32_t)kFewList) return sample_few<T>(a, row, s, f, (int)f.listed, scaled);
     }
@@ -625,7 +640,7 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
         const int b = bin_at(t);
         atomicAdd(f.count + b, 1u);
         atomicAdd((unsigned long long *)f.mass + b, fixed(t, b));
-    });
+    }, std::false_type{});
     __syncthreads();
     int c[2], cb, call;
     double m[2], mb, mall;
@@ -663,7 +678,7 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
                 const uint32_t at = atomicAdd(&f.listed, 1u);
                 f.key[at] = f2ord(v);
                 f.index[at] = i;
-            });
+            }, std::false_type{});
         }
         __syncthreads();
         const int above = f.above, count = s.k - above;
@@ -682,7 +697,7 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
                 atomicAdd((unsigned long long *)f.dmass + d, fixed(scaled(v), b));
             };
             if (list) for (int i = tid; i < (int)f.listed; i += kThreads) add(ord2f(f.key[i]), (int)f.index[i]);
-            else each([&](float v, int i) { if (bin_at(scaled(v)) == b) add(v, i); });
+            else each([&](float v, int i) { if (bin_at(scaled(v)) == b) add(v, i); }, std::false_type{});
             __syncthreads();
             // every wavefront for itself: 4 digits a lane
             const int lane = tid & 63;
@@ -740,7 +755,7 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
             atomicMin(&f.least, f2ord(v));
             atomicAdd(&f.listed, 1u);
             atomicAdd((unsigned long long *)f.dmass, fixed(t, b));
-        });
+        }, std::false_type{});
         __syncthreads();
         // (a comp that no token reaches where the bin has none)
         const Edge e{b, f.listed ? (uint64_t)f.least << 24 : ~0ull, f.above + (int)f.listed,
@@ -788,10 +803,11 @@ struct CoarseRow : CoarsePool { uint32_t hist[kBins / 2]; };   // of a row that 
 
 // A row that keeps every token, from its parts' masses: the part, then the token by its own weights.
 // A greedy row: the first of its largest.
+template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_all_kernel(SampleArgs a, Parts parts) {
     __shared__ Range ranges[kRanges];
     const int row = blockIdx.x, lane = threadIdx.x & 63, S = parts.count;
-    const uint16_t *z = (const uint16_t *)a.logits.p + row * a.logits.st;
+    const T *z = (const T *)a.logits.p + row * a.logits.st;
     const Settings s = settings_of(a, row);
     if (!s.ok) return no_answer(a, row);
     float top = kNegInf;
@@ -815,14 +831,14 @@ __global__ __launch_bounds__(kThreads) void sample_all_kernel(SampleArgs a, Part
     Drawn d{(double)s.u * all, s.greedy ? 0.f : s.u, 0};
     const int q = max(0, pick_range(ranges, S, 0.0, d)), begin = q * parts.len;
     const auto item = [&](int, uint32_t bits, auto fn) {
-        const float v = bf16_bits_to_f32(bits);
+        const float v = token_value<T>(bits);
         const bool in = s.greedy ? (double)v == zmax : v > kNegInf;
         fn(in, false, in ? exp_below(((double)v - zmax) * inv) : 0.0);
     };
-    const int token = locate<uint16_t, 1, 1>(z, item, begin, min(a.vocab, begin + parts.len), 0.0, d, ranges);
+    const int token = locate<T, 1, 1>(z, item, begin, min(a.vocab, begin + parts.len), 0.0, d, ranges);
     if (threadIdx.x == 0) {
         a.token[row] = token;
-        if (a.logp) a.logp[row] = (float)(((double)bf16_bits_to_f32(z[token]) - zmax) * inv - (s.greedy ? 0.0 : log(all)));
+        if (a.logp) a.logp[row] = (float)(((double)RowElem<T>::get(z[token]) - zmax) * inv - (s.greedy ? 0.0 : log(all)));
         if (a.kept) a.kept[row] = s.greedy ? 1 : there;
     }
 }
@@ -1129,43 +1145,36 @@ __global__ __launch_bounds__(kThreads, MANY ? 8 : 4) void sample_coarse_kernel(S
 }  // namespace
 
 int64_t sample_bytes(const SampleArgs &a, bool bf16) {
-    if (!bf16 || a.rows == 0) return 0;
-    const Parts p = parts_of(a);
-    return p.count == 1 || p.count > kMostParts ? 0 : (int64_t)a.rows * p.count * p.bytes;
+    if (a.rows == 0) return 0;
+    const Parts p = parts_of(a, bf16);
+    return p.count <= 1 || p.count > kMostParts ? 0 : (int64_t)a.rows * p.count * p.bytes;
 }
 
 hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t st) {
-    if (!bf16) {
-        sample_fine_kernel<float, false><<<a.rows, kThreads, 0, st>>>(a);
+    const Parts p = parts_of(a, bf16);
+    const auto run = [&](auto kernel) {
+        kernel<<<a.rows, kThreads, 0, st>>>(a);
         return hipGetLastError();
-    }
-    const Parts p = parts_of(a);
-    if (p.count > kMostParts) {                  // (rows of more than 4 million tokens)
-        sample_fine_kernel<uint16_t, false><<<a.rows, kThreads, 0, st>>>(a);
+    };
+    const auto run_parts = [&](auto first, auto second) {
+        first<<<dim3(a.rows, p.count), kPartThreads, 0, st>>>(a, p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        second<<<a.rows, kThreads, 0, st>>>(a, p);
         return hipGetLastError();
-    }
+    };
+    if (p.count > 1 && p.bytes == sizeof(PartHead))
+        return bf16 ? run_parts(sample_masses_kernel<uint16_t>, sample_all_kernel<uint16_t>)
+                    : run_parts(sample_masses_kernel<float>, sample_all_kernel<float>);
+    if (!bf16) return run(sample_fine_kernel<float, false>);
+    if (p.count > kMostParts) return run(sample_fine_kernel<uint16_t, false>);   // (more than 4 million tokens)
     if (p.count == 1) {
         sample_coarse_kernel<false, false><<<a.rows, kThreads, 0, st>>>(a, p);
         return hipGetLastError();
     }
-    const bool plain = p.bytes == sizeof(PartHead);
-    if (plain) sample_masses_kernel<<<dim3(a.rows, p.count), kPartThreads, 0, st>>>(a, p);
-    else sample_counts_kernel<<<dim3(a.rows, p.count), kPartThreads, 0, st>>>(a, p);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (plain) {
-        sample_all_kernel<<<a.rows, kThreads, 0, st>>>(a, p);
-        return hipGetLastError();
-    }
-    if (a.rows <= kChipUnits) {
-        sample_coarse_kernel<true, false><<<a.rows, kThreads, 0, st>>>(a, p);
-        return hipGetLastError();
-    }
-    sample_coarse_kernel<true, true><<<a.rows, kThreads, 0, st>>>(a, p);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    sample_fine_kernel<uint16_t, true><<<a.rows, kThreads, 0, st>>>(a);
-    return hipGetLastError();
+    if (a.rows <= kChipUnits) return run_parts(sample_counts_kernel, sample_coarse_kernel<true, false>);
+    const hipError_t e = run_parts(sample_counts_kernel, sample_coarse_kernel<true, true>);
+    return e != hipSuccess ? e : run(sample_fine_kernel<uint16_t, true>);
 }
 
 }  // namespace olive
