@@ -486,9 +486,9 @@ __device__ __forceinline__ double exp_small(double x) {      // e^-x for 0 <= x 
 
 struct FinePool {
     uint32_t count[kFineBins];
-    uint64_t mass[kFineBins];                    // in fixed point, relative to the bin's edge
+    alignas(16) uint64_t mass[kFineBins];        // in fixed point, relative to the bin's edge
     double edge[kFineBins];                      // e^(-b / 32)
-    uint32_t key[kFineList], index[kFineList];   // (of few tokens: their places in order, and weights)
+    uint32_t key[kFineList], index[kFineList];
     uint32_t dcount[256];
     uint64_t dmass[256];
     Range ranges[kRanges];
@@ -519,15 +519,18 @@ __device__ __forceinline__ void sample_few(const SampleArgs &a, int row, const S
     uint64_t *comp = f.mass, *sorted = f.mass + kFewList;
     double *weight = f.edge;
     static_assert(2 * kFewList <= kFineBins, "");
-    if (tid < n) comp[tid] = comp_of(f.key[tid], (int)f.index[tid]);
+    const uint64_t mine = tid < n ? comp_of(f.key[tid], (int)f.index[tid]) : 0;
+    if (tid < (n + 7 & ~7)) comp[tid] = mine;                // (0 behind the last, to a multiple of 8)
     if (tid == 0) f.first = 0x7fffffff, f.last = -1;
     __syncthreads();
     if (tid < n) {
-        const uint64_t own = comp[tid];
         int rank = 0;
-#pragma unroll 8
-        for (int i = 0; i < n; ++i) rank += comp[i] > own;
-        sorted[rank] = own;
+#pragma unroll 2
+        for (int i = 0; i < n; i += 4) {
+            const ulonglong2 x = *(const ulonglong2 *)(comp + i), y = *(const ulonglong2 *)(comp + i + 2);
+            rank += (x.x > mine) + (x.y > mine) + (y.x > mine) + (y.y > mine);
+        }
+        sorted[rank] = mine;
     }
     __syncthreads();
     const uint64_t own = tid < k ? sorted[tid] : 0;
@@ -566,7 +569,8 @@ template <typename T>
 __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const Settings &s, FinePool &f) {
     const T *z = (const T *)a.logits.p + row * a.logits.st;
     const int tid = threadIdx.x, V = a.vocab;
-    // every token that is not -inf: fn(value, index); `light`: a few instructions, worth their unrolling
+    // every token that is not -inf: fn(value, index). `light`: all of them, for a few instructions each that
+    // are worth their unrolling
     const auto each = [&](auto fn, auto light) {
         constexpr int kStep = kThreads * kLot<T>, kAhead = 4;
         const int first = tid * kLot<T>;
@@ -581,18 +585,20 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
             ahead[kAhead - 1] = load_tokens(z, min(i + kAhead * kStep, V), V);
             each_token<T, decltype(light)::value ? 4 : 1>(x, [&](int j, uint32_t bits) {
                 const float v = token_value<T>(bits) + 0.f;        // (-0 and 0 are the same value)
-                if (!(v == kNegInf)) fn(v, i + j);
+                if (decltype(light)::value || !(v == kNegInf)) fn(v, i + j);
             });
         }
     };
     if (tid == 0) f.top = 0, f.n = 0, f.bad = 0, f.listed = 0, f.least = 0xffffffffu;
     __syncthreads();
-    uint32_t top = 0, n = 0, bad = 0;
+    uint32_t n = 0, bad = 0;
+    float most = kNegInf;
     each([&](float v, int) {
         bad |= !(v < __builtin_inff());
-        top = max(top, f2ord(v));
-        ++n;
+        most = fmaxf(most, v);
+        n += v > kNegInf;
     }, std::true_type{});
+    uint32_t top = f2ord(most);
     if (s.k > 0 && s.k <= kFew) {
         // the least of the largest values of k groups of threads or more: k tokens at least reach it
         uint32_t group = top;
@@ -613,13 +619,12 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
     const double zmax = (double)ord2f(f.top), inv = 1.0 / (double)s.temp;
     const auto scaled = [&](float v) { return (zmax - (double)v) * inv; };
     const int total = (int)f.n;
-    if (s.k > 0 && s.k <= kFew && s.k < total) {
-        const uint32_t least = f.least;
+    if (s.k > 0 && s.k <= kFew && s.k < total && f.least > f2ord(kNegInf)) {
+        const float least = ord2f(f.least);
         each([&](float v, int i) {
-            const uint32_t key = f2ord(v);
-            if (key < least) return;
+            if (!(v >= least)) return;
             const uint32_t at = atomicAdd(&f.listed, 1u);
-            if (at < (uint32_t)kFewList) f.key[at] = key, f.index[at] = i;
+            if (at < (uint32_t)kFewList) f.key[at] = f2ord(v), f.index[at] = i;
         }, std::true_type{});
         __syncthreads();
         if (f.listed <= (uint32_t)kFewList) return sample_few<T>(a, row, s, f, (int)f.listed, scaled);
