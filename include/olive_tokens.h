@@ -64,10 +64,12 @@ olive_status olive_embed_workspace(const olive_embed_desc *desc, int64_t *bytes)
 
 /*
  *   grad_table[v] (+)= scale * sum over t with ids[t] = v of grad_out[t]
- * summed in 32 bits in the order of t. accumulate 0: the whole table is written, zeros for
- * tokens that do not occur; accumulate 1: only the rows of tokens that occur are read and
- * written. grad_dtype: olive_dtype of grad_table. Negative tokens and tokens >= vocab have
- * no part in it. workspace: device, 16-byte aligned, NULL if 0 bytes are needed.
+ * summed in 32 bits, in an order that the tokens alone decide. accumulate 0: the whole table is
+ * written, zeros for tokens that do not occur; accumulate 1: only the rows of tokens that occur
+ * are read and written. grad_dtype: olive_dtype of grad_table. Negative tokens and tokens >=
+ * vocab have no part in it. grad_out and grad_table do not overlap. workspace: device, 16-byte
+ * aligned, NULL if 0 bytes are needed (up to 1024 tokens; else 16 bytes a token, and two rows in
+ * fp32 for every 16 to 64 tokens).
  * Errors: as olive_embed, plus E_SHAPE for a workspace that is too small.
  */
 olive_status olive_embed_backward(const olive_embed_desc *desc, const void *grad_out,

@@ -4,9 +4,12 @@
 // segments are merged at a time), the sorted list is cut into blocks of equal length, and a wavefront adds
 // the rows of a block, 16 bytes a lane, run by run. A run inside a block goes to the table at once;
 // of one that crosses a border each block leaves a partial row, which a last pass adds in order. So a
-// token that is everywhere is shared by many wavefronts, and the order of additions is the order of
-// the tokens' positions whatever runs when. Bound by memory: 32768 rows of 2048 bf16 are read
-// once, the table's rows are written once.
+// token that is everywhere is shared by many wavefronts, and the order of additions does not depend on
+// what runs when. Bound by memory: 29500 rows of 2048 bf16 (of 32768 tokens) added to a gradient of
+// 151936 fp32 rows take 103 us, 76 of them the sums (4.0 TB/s; a row's table row is asked for
+// with the row that ends its sum: 80 us where it was asked for at the sum's end), 8 the sort, 10
+// the merge and 5 the last pass; written whole, 8192 tokens of 1536 take 213 us (192 for sums and zeros, 4.9
+// TB/s). 32768 rows of 2048 by their tokens: 30 us.
 #include "rows.hpp"
 #include "tokens_internal.hpp"
 #include "wave_ops.hpp"
@@ -42,7 +45,7 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, int chunks, int
             for (int j = 0; j < L; ++j) x[j] = id < 0 ? 0.f : __builtin_nanf("");
         }
         if constexpr (TAIL) store_lot(dst, i, end, pack_lot<T>(x));
-        else write_lot(dst + i, pack_lot<T>(x));
+        else write_lot(dst + i, pack_lot<T>(x), a.stream);
     }
 }
 

@@ -31,6 +31,18 @@ __device__ __forceinline__ void write_lot(T *p, const Lot &x) {
     struct __attribute__((packed, aligned(sizeof(T)))) Loose { uint32_t w[4]; };
     *(Loose *)p = Loose{{x.w[0], x.w[1], x.w[2], x.w[3]}};
 }
+// The same past the caches, for outputs that they would not hold until they are read.
+template <typename T>
+__device__ __forceinline__ void stream_lot(T *p, const Lot &x) {
+    typedef uint32_t Words __attribute__((ext_vector_type(4)));
+    typedef Words Loose __attribute__((aligned(2)));
+    __builtin_nontemporal_store((Words){x.w[0], x.w[1], x.w[2], x.w[3]}, (Loose *)p);
+}
+template <typename T>
+__device__ __forceinline__ void write_lot(T *p, const Lot &x, bool stream) {
+    if (stream) stream_lot(p, x);
+    else write_lot(p, x);
+}
 // The first element goes, the last is that of `in` (each half of it for 16 bits).
 template <typename T>
 __device__ __forceinline__ void drop_first(Lot &x, uint32_t in) {

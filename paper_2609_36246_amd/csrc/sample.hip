@@ -13,9 +13,11 @@
 //    edge, so that the sum does not depend on its order. Inside the last bin the run's end is
 //    found digit by digit of (value, index).
 //
-// Code is kept short where a workgroup runs it once (loops over a lane's tokens are rolled): instructions come
-// from the L2 cache a line at a time, and with unrolled loops that was half of the time of a call
-// of few rows.
+// A call of few rows is a chain of waits and of steps that all threads join. Code is kept short where a
+// workgroup runs it once (loops over a lane's tokens are rolled): instructions come from the L2 cache
+// a line at a time (8 fp32 rows of 32000 with top-k 50: 52 us unrolled, 25 rolled, with the kept ones put in
+// order). Of bf16 rows of 151936: 4 without cuts 13 us, 64 with settings of their own 40, 512 with a nucleus
+// 90, of which half is the counting (3.6 tokens a clock and compute unit, the rate of LDS atomics).
 //
 // Masses are 64-bit: a token changes where the error of the sums passes u times their total over a
 // border, and a row has as many borders as tokens.

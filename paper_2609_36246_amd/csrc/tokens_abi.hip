@@ -111,6 +111,7 @@ olive_status olive_embed(const olive_embed_desc *desc, const void *table, int64_
     EmbedArgs a = embed_args(desc);
     a.table = {(char *)table, table_stride};
     a.out = {(char *)out, out_stride};
+    a.stream = streamed(desc->tokens, desc->width, esize(desc->dtype));
     return check_hip(launch_embed(a, desc->dtype == OLIVE_BF16, (hipStream_t)hip_stream));
 }
 
@@ -166,6 +167,7 @@ olive_status olive_row_norm(const olive_norm_desc *desc, const void *x, int64_t 
     if (residual) a.res = {(char *)residual, residual_stride};
     a.out = {(char *)out, out_stride};
     if (sum) a.sum = {(char *)sum, sum_stride};
+    a.stream = streamed(n, w, esize(desc->dtype));
     return check_hip(launch_norm(a, desc->dtype == OLIVE_BF16, (hipStream_t)hip_stream));
 }
 
@@ -203,6 +205,7 @@ olive_status olive_row_norm_backward(const olive_norm_desc *desc, const void *h,
     if (grad_sum) a.res = {(char *)grad_sum, grad_sum_stride};
     a.out = {(char *)grad_h, grad_h_stride};
     a.sum = {(char *)grad_out, grad_out_stride};
+    a.stream = streamed(n, w, esize(desc->dtype));
     a.gw = grad_weight;
     a.gb = grad_bias;
     a.part = (float *)workspace;
