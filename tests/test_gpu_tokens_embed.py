@@ -104,7 +104,8 @@ BACKWARD = [(1, 1, 1, "mixed", "plain"), (2, 3, 2048, "one", "plain"), (64, 50, 
             (65, 2000, 136, "distinct", "part"), (333, 40, 515, "mixed", "plain"), (1000, 7, 64, "mixed", "odd"),
             (2048, 3000, 128, "mixed", "plain"), (2049, 3000, 96, "uniform", "part"), (4097, 20000, 72, "mixed", "plain"),
             (9000, 100, 40, "one", "plain"), (20000, 151936, 8, "mixed", "plain"), (20000, 151936, 16, "distinct", "plain"),
-            (300, 10, 5000, "mixed", "plain"), (70000, 1 << 20, 4, "mixed", "plain"), (70001, 1000, 3, "uniform", "odd")]
+            (300, 10, 5000, "mixed", "plain"), (70000, 1 << 20, 4, "mixed", "plain"), (70001, 1000, 3, "uniform", "odd"),
+            (1100, 30, 20000, "mixed", "plain"), (1030, 5, 2047, "one", "odd")]
 
 
 @pytest.mark.parametrize("accumulate", [False, True])
@@ -141,6 +142,49 @@ def test_tokens_out_of_range_have_no_gradient(accumulate):
     nothing = torch.full((500,), -1, dtype=torch.int32, device="cuda")
     got = backward(nothing, matrix(500, 48, BF16), 10, into=None if not accumulate else matrix(10, 48, F32, fill=7.0))
     assert bool((got == (7.0 if accumulate else 0.0)).all())
+
+
+@pytest.mark.parametrize("how", ["plain", "odd"])
+def test_outputs_that_are_written_past_the_caches(how):
+    gen = torch.Generator().manual_seed(12)
+    table, ids = matrix(5000, 1024, BF16, gen=gen), tokens(50000, 5000, seed=12)
+    out = forward(ids, table, how=how)
+    want = torch.where((ids >= 0)[:, None], table[ids.long().clamp(min=0)], 0.0)
+    assert torch.equal(out.contiguous(), want)
+
+
+def test_rows_further_apart_than_32_bits_count():
+    gen = torch.Generator().manual_seed(13)
+    far = lambda x: torch.empty(2 * 1200000000 + 4096, dtype=x.dtype, device="cuda").as_strided(  # noqa: E731
+        x.shape, (1200000000, 1)).copy_(x)
+    table, ids = matrix(3, 264, BF16, gen=gen), torch.tensor([2, 0, 2], dtype=torch.int32).cuda()
+    out = far(torch.zeros(3, 264, dtype=BF16, device="cuda"))
+    d = L.make_embed_desc(3, 3, 264, ids, scale=2.0)
+    L.olive_embed(d, far(table), out)
+    assert torch.equal(out.contiguous(), forward(ids, table, 2.0))
+    for n in (3, 1500):
+        i = ids.repeat(n)[:n].contiguous()
+        g = matrix(n, 264, BF16, gen=gen)
+        into = far(torch.zeros(3, 264, device="cuda"))
+        backward(i, g, 3, into=into)
+        assert torch.equal(into.contiguous(), backward(i, g, 3))
+
+
+def test_two_calls_at_once():
+    """On two streams, each with a workspace of its own."""
+    gen = torch.Generator().manual_seed(14)
+    calls = []
+    for k in range(2):
+        ids, g = tokens(9000, 4000, seed=k), matrix(9000, 256, BF16, gen=gen)
+        d = L.make_embed_desc(9000, 4000, 256, ids)
+        work = torch.empty(L.olive_embed_workspace(d), dtype=torch.uint8, device="cuda")
+        calls.append((d, g, matrix(4000, 256, F32), work, backward(ids, g, 4000), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for d, g, t, work, _, s in calls:
+            L.olive_embed_backward(d, g, t, workspace=work, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, want) for _, _, t, _, want, _ in calls)
 
 
 def test_no_tokens():

@@ -201,6 +201,33 @@ def test_rows_behind_the_last_are_left_as_they_were():
     assert bool((out[5:] == 3.0).all()) and bool((total[5:] == 3.0).all())
 
 
+@pytest.mark.parametrize("how", ["plain", "odd"])
+def test_outputs_that_are_written_past_the_caches(how):
+    n = Norm(50000, 1024, BF16, LAYER, how, bias=True, residual=True)
+    (out, total), (gh, _, _) = n.forward(), n.backward()
+    for at in (0, 31999, 49000):
+        s = slice(at, at + 1000)
+        d = L.make_norm_desc(1000, 1024, n.w, n.b, L.OLIVE_BF16, EPS, LAYER)
+        o, t, g = (torch.empty(1000, 1024, dtype=BF16, device="cuda") for _ in range(3))
+        L.olive_row_norm(d, n.x[s], o, n.res[s], t)
+        L.olive_row_norm_backward(d, t, n.dy[s], g, n.dsum[s])
+        assert torch.equal(out[s], o) and torch.equal(total[s], t) and torch.equal(gh[s], g)
+
+
+def test_rows_further_apart_than_32_bits_count():
+    n = Norm(3, 2056, BF16, RMS, residual=True)
+    (out, total), (gh, gw, gb) = n.forward(), n.backward()
+    far = lambda x: torch.empty(2 * 1200000000 + 4096, dtype=x.dtype, device="cuda").as_strided(  # noqa: E731
+        x.shape, (1200000000, 1)).copy_(x)
+    o, t, g = (far(torch.zeros(3, 2056, dtype=BF16, device="cuda")) for _ in range(3))
+    w, b = torch.empty_like(gw), torch.empty_like(gb)
+    work = torch.empty(L.olive_row_norm_workspace(n.desc), dtype=torch.uint8, device="cuda")
+    L.olive_row_norm(n.desc, far(n.x), o, far(n.res), t)
+    L.olive_row_norm_backward(n.desc, t, far(n.dy), g, far(n.dsum), w, b, work)
+    assert torch.equal(o.contiguous(), out) and torch.equal(t.contiguous(), total) and torch.equal(g.contiguous(), gh)
+    assert torch.equal(w, gw) and torch.equal(b, gb)
+
+
 def test_no_rows():
     n = Norm(0, 300, BF16, LAYER, bias=True)
     n.forward()

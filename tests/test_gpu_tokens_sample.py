@@ -95,7 +95,7 @@ def test_settings(vocab, how, dtype, settings):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,vocab,spread", [(1, 151936, 1.0), (3, 151936, 4.0), (2, 151936, 0.01), (2, 64007, 30.0),
-                                               (40, 8192, 2.0), (300, 513, 1.0), (2, 300001, 2.0)])
+                                               (40, 8192, 2.0), (300, 513, 1.0), (2, 300001, 2.0), (1, 1200001, 1.0)])
 def test_sizes(rows, vocab, spread, dtype):
     z = normal(rows, vocab, dtype, spread)
     for k, s in enumerate((dict(), dict(top_p=0.95), dict(top_k=1000, top_p=0.9, temperature=0.8), dict(min_p=0.02, temperature=1.3))):
@@ -247,6 +247,30 @@ def test_many_rows():
     u[7], u[8] = 0.0, 1.0
     Sample(z, u, top_p=0.92, temperature=0.9).check()
     Sample(z[:, :9000].contiguous(), u, top_k=40).check()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_further_apart_than_32_bits_count(dtype):
+    z = normal(3, 30000, dtype, 3.0)
+    apart = torch.empty(2 * 1200000000 + 30000, dtype=dtype, device="cuda").as_strided((3, 30000), (1200000000, 1))
+    apart.copy_(z)
+    for s in (dict(), dict(top_p=0.9), dict(top_k=20, temperature=0.7)):
+        want, got = Sample(z, [0.11, 0.52, 0.93], **s).run(), Sample(apart, [0.11, 0.52, 0.93], **s).run()
+        assert all(np.array_equal(a, b) for a, b in zip(want, got))
+
+
+def test_two_calls_at_once():
+    """On two streams, each with a workspace of its own."""
+    calls = [Sample(normal(40, 40000, BF16, 2.0, seed=i), uniform(40, i), top_p=0.9) for i in range(2)]
+    want = [[t.copy() for t in c.run()] for c in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, s in zip(calls, streams):
+            c.call(s)
+    torch.cuda.synchronize()
+    for c, w in zip(calls, want):
+        assert all(np.array_equal(a, b) for a, b in zip(w, (c.token.cpu().numpy(), f64(c.logp), c.kept.cpu().numpy())))
 
 
 def test_optional_outputs_and_no_rows():
