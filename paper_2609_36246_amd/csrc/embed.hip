@@ -7,7 +7,7 @@
 // token that is everywhere is shared by many wavefronts, and the order of additions does not depend on
 // what runs when. Bound by memory: 29500 rows of 2048 bf16 (of 32768 tokens) added to a gradient of
 // 151936 fp32 rows take 103 us, 76 of them the sums (4.0 TB/s; a row's table row is asked for
-// with the row that ends its sum: 80 us where it was asked for at the sum's end), 8 the sort, 10
+// with the row that ends its sum: the call takes 109 where it is asked for at the sum's end), 8 the sort, 10
 // the merge and 5 the last pass; written whole, 8192 tokens of 1536 take 213 us (192 for sums and zeros, 4.9
 // TB/s). 32768 rows of 2048 by their tokens: 30 us.
 #include "rows.hpp"
@@ -61,7 +61,7 @@ __device__ __forceinline__ uint32_t key_of(const EmbedArgs &a, int id) {
 
 // Sorts a tile by a digit of the key at a time (at most 9 bits, as many each), stably: a wavefront has 128
 // tokens, ranks 64 of them at a time by comparing digits (a ballot a bit), and keeps its own
-// counts. 18 bits take two passes of 2.5 us; a chain of waits, of which fewer and longer ones are less.
+// counts. 18 bits take two passes, 8 us in all (three passes on tiles of 4096: 15): a chain of waits.
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedArgs a, uint32_t *keys, int32_t *places, int bits,
                                                                   int digit) {
     __shared__ uint32_t key[2][kTile];
@@ -251,6 +251,8 @@ __device__ __forceinline__ Lot load_grad(const EmbedArgs &a, int place, int c) {
     return Lot{{0, 0, 0, 0}};
 }
 
+constexpr int kAhead = 8;
+
 struct Sorted {
     const uint32_t *keys;
     const int32_t *places;
@@ -300,8 +302,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, Sorted s) {
     const uint32_t prev = p0 > 0 ? s.keys[p0 - 1] : 0xffffffffu, next = p0 + n < a.tokens ? s.keys[p0 + n] : 0xffffffffu;
     const int there = __popcll(__ballot(key < (uint32_t)a.vocab));       // (the others are at the end)
     if (there == 0) return;
-    // 8 rows on their way together, and the table's rows of the runs that end among them
-    constexpr int kAhead = 8;
+    // kAhead rows on their way together, and the table's rows of the runs that end among them
     float sum[L] = {};
 #pragma unroll 1
     for (int e0 = 0; e0 < there; e0 += kAhead) {
@@ -339,6 +340,23 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, Sorted s) {
     }
 }
 
+// Adds the sums of a workgroup's four wavefronts, in order, in the first one (of which it says so).
+template <int L>
+__device__ __forceinline__ bool add_waves(float (&sum)[L]) {
+    __shared__ float join[3][64][L + 1];
+    const int lane = threadIdx.x & 63, wave = wave_index();
+    if (wave)
+#pragma unroll
+        for (int j = 0; j < L; ++j) join[wave - 1][lane][j] = sum[j];
+    __syncthreads();
+    if (wave) return false;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+#pragma unroll
+        for (int j = 0; j < L; ++j) sum[j] += join[i][lane][j];
+    return true;
+}
+
 // The runs that cross a border: the block where one begins adds what the blocks have left of it.
 template <typename T, typename TT, bool TAIL>
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a, Sorted s) {
@@ -367,22 +385,12 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a, Sorted s) 
 #pragma unroll
         for (int j = 0; j < L; ++j) sum[j] += x[j];
     }
-    __shared__ float join[3][64][L + 1];
-    if (wave)
-#pragma unroll
-        for (int j = 0; j < L; ++j) join[wave - 1][lane][j] = sum[j];
-    __syncthreads();
-    if (wave) return;
-#pragma unroll
-    for (int i = 0; i < 3; ++i)
-#pragma unroll
-        for (int j = 0; j < L; ++j) sum[j] += join[i][lane][j];
+    if (!add_waves(sum)) return;
     float x[L] = {};
     if (a.accumulate) from_table<TT, L, TAIL>(a, run, c, x);
     to_table<TT, L, TAIL>(a, run, c, sum, x);
 }
 
-// Few tokens: the wavefront of a token's first occurrence finds the others and adds their rows in order.
 template <typename TT>
 __global__ __launch_bounds__(256) void embed_zero_kernel(EmbedArgs a) {
     constexpr int N = 16 / (int)sizeof(TT);
@@ -391,27 +399,40 @@ __global__ __launch_bounds__(256) void embed_zero_kernel(EmbedArgs a) {
         for (int c = threadIdx.x * N; c < a.width; c += 256 * N) store_lot(row, c, a.width, Lot{{0, 0, 0, 0}});
     }
 }
+// Few tokens: the workgroup of a token's first occurrence finds the others, 64 tokens a wavefront, and adds
+// their rows. Bound by waits: 1024 drawn of 32000 as text is, 2048 wide, 8 us, all the same 27 (by
+// one wavefront, a row at a time, 16 and 193; sorted, 22 and 18).
 template <typename T, typename TT, bool TAIL>
 __global__ __launch_bounds__(256) void embed_few_kernel(EmbedArgs a, int chunks) {
     constexpr int L = kLot<T>;
-    const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)block_index() * 4 + wave_index();
-    const int t = (int)(w / chunks), c = ((int)(w % chunks) * 64 + lane) * L;
-    if (t >= a.tokens) return;
+    const int lane = threadIdx.x & 63, wave = wave_index();
+    const int t = (int)blockIdx.x / chunks, c = ((int)blockIdx.x % chunks * 64 + lane) * L;
     const int id = a.ids[t];
     if (id < 0 || id >= a.vocab) return;
-    for (int s = 0; s < t; s += 64)
-        if (__ballot(s + lane < t && a.ids[s + lane] == id)) return;
+    bool before = false;
+    for (int s = wave * 64; s < t; s += 256) before |= s + lane < t && a.ids[s + lane] == id;
+    if (__syncthreads_or(before)) return;
     float sum[L] = {};
-    for (int s = t; s < a.tokens; s += 64) {
+    for (int s = t + wave * 64; s < a.tokens; s += 256) {
         uint64_t m = __ballot(s + lane < a.tokens && a.ids[s + lane] == id);
-        for (; m; m &= m - 1) {
-            float x[L];
-            unpack_lot<T>(load_grad<T, TAIL>(a, s + __builtin_ctzll(m), c), x);
+        while (m) {
+            Lot x[kAhead];
 #pragma unroll
-            for (int j = 0; j < L; ++j) sum[j] += x[j];
+            for (int j = 0; j < kAhead; ++j) {
+                x[j] = Lot{{0, 0, 0, 0}};
+                if (m) x[j] = load_grad<T, TAIL>(a, s + __builtin_ctzll(m), c);
+                m &= m - 1;
+            }
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                float v[L];
+                unpack_lot<T>(x[j], v);
+#pragma unroll
+                for (int i = 0; i < L; ++i) sum[i] += v[i];
+            }
         }
     }
+    if (!add_waves(sum)) return;
     float x[L] = {};
     if (a.accumulate) from_table<TT, L, TAIL>(a, (uint32_t)id, c, x);
     to_table<TT, L, TAIL>(a, (uint32_t)id, c, sum, x);
@@ -455,7 +476,7 @@ hipError_t backward(const EmbedArgs &a, hipStream_t st) {
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess || a.tokens == 0) return e;
         }
-        embed_few_kernel<T, TT, TAIL><<<grid_of(((int64_t)a.tokens * chunks + 3) / 4), 256, 0, st>>>(a, chunks);
+        embed_few_kernel<T, TT, TAIL><<<a.tokens * chunks, 256, 0, st>>>(a, chunks);
         return hipGetLastError();
     }
     const Layout l = layout_of(a);

@@ -14,13 +14,6 @@ struct RowsArg {                     // a [rows][width] matrix
     int64_t st;                      // elements between rows
 };
 
-// Whether every matrix that is there can be read `bytes` at a time from the start of each row.
-inline bool rows_aligned(std::initializer_list<RowsArg> all, int bytes, int esz) {
-    for (const RowsArg &m : all)
-        if (m.p && (((uintptr_t)m.p | (uint64_t)(m.st * esz)) % bytes) != 0) return false;
-    return true;
-}
-
 // Whether an output is written past the caches: where the next kernel finds little of it there anyway. Rows of
 // tokens and then their norm, 134 MB each: 88 us for 94 (the rows alone 30 for 45, norms of 268 MB 222
 // for 230); of 34 MB 27 for 25, of 17 MB 18 for 17.

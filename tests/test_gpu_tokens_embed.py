@@ -105,7 +105,8 @@ BACKWARD = [(1, 1, 1, "mixed", "plain"), (2, 3, 2048, "one", "plain"), (64, 50, 
             (2048, 3000, 128, "mixed", "plain"), (2049, 3000, 96, "uniform", "part"), (4097, 20000, 72, "mixed", "plain"),
             (9000, 100, 40, "one", "plain"), (20000, 151936, 8, "mixed", "plain"), (20000, 151936, 16, "distinct", "plain"),
             (300, 10, 5000, "mixed", "plain"), (70000, 1 << 20, 4, "mixed", "plain"), (70001, 1000, 3, "uniform", "odd"),
-            (1100, 30, 20000, "mixed", "plain"), (1030, 5, 2047, "one", "odd")]
+            (1100, 30, 20000, "mixed", "plain"), (1030, 5, 2047, "one", "odd"), (1000, 5, 264, "one", "odd"),
+            (777, 40, 1001, "mixed", "plain")]
 
 
 @pytest.mark.parametrize("accumulate", [False, True])
