@@ -507,6 +507,22 @@ struct Edge {
     double mass;
 };
 
+// Counts a token of mass x into bin b; together where a wavefront's tokens are all alike, which would
+// wait for each other (an fp32 row of 151936 with a nucleus: 606 us for 1699 where all are equal, 148 for
+// 345 at T = 0.01, whose tokens nearly all lie in the last bin, and 181 for 168 at T = 1).
+__device__ __forceinline__ void add_to(uint32_t *count, uint64_t *mass, int b, uint64_t x) {
+    const int b0 = __builtin_amdgcn_readfirstlane(b);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+    const uint64_t here = __ballot(true);
+    uint32_t n = 1;
+    if (__ballot(b == b0 && x == ((uint64_t)hi << 32 | lo)) == here) {
+        if ((int)(threadIdx.x & 63) != __builtin_ctzll(here)) return;
+        n = (uint32_t)__popcll(here);
+    }
+    atomicAdd(count + b, n);
+    atomicAdd((unsigned long long *)mass + b, (unsigned long long)n * x);
+}
+
 __device__ __forceinline__ double b_mass(const FinePool &f, int b, double back) { return (double)f.mass[b] * back * f.edge[b]; }
 __device__ __forceinline__ uint64_t comp_of(uint32_t key, int i) {
     return (uint64_t)key << 24 | (0xffffff - (uint32_t)i);
@@ -645,8 +661,7 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
     each([&](float v, int) {
         const double t = scaled(v);
         const int b = bin_at(t);
-        atomicAdd(f.count + b, 1u);
-        atomicAdd((unsigned long long *)f.mass + b, fixed(t, b));
+        add_to(f.count, f.mass, b, fixed(t, b));
     }, std::false_type{});
     __syncthreads();
     int c[2], cb, call;
@@ -700,8 +715,7 @@ __device__ __forceinline__ void sample_fine(const SampleArgs &a, int row, const 
                 const uint64_t comp = comp_of(f2ord(v), i);
                 if ((comp >> shift >> 8) != prefix) return;
                 const int d = 255 - (int)(comp >> shift & 255);
-                atomicAdd(f.dcount + d, 1u);
-                atomicAdd((unsigned long long *)f.dmass + d, fixed(scaled(v), b));
+                add_to(f.dcount, f.dmass, d, fixed(scaled(v), b));
             };
             if (list) for (int i = tid; i < (int)f.listed; i += kThreads) add(ord2f(f.key[i]), (int)f.index[i]);
             else each([&](float v, int i) { if (bin_at(scaled(v)) == b) add(v, i); }, std::false_type{});
