@@ -13,15 +13,19 @@
 namespace olive {
 namespace {
 
-// The sum over a row's lanes, the same in all of them. `join`: LDS of the row, WAVES values.
+// LDS of a row: a value of each of its wavefronts.
 template <int WAVES>
-__device__ __forceinline__ float row_total(float v, float *join) {
+struct Join { double wide[WAVES]; float narrow[WAVES]; };
+
+// The sum over a row's lanes, the same in all of them.
+template <int WAVES, typename V>
+__device__ __forceinline__ V row_total(V v, V *join) {
     v = wave_sum(v);
     if constexpr (WAVES > 1) {
         __syncthreads();                     // (the values of the sum before are read)
         if ((threadIdx.x & 63) == 0) join[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = 0.f;
+        v = 0;
 #pragma unroll
         for (int i = 0; i < WAVES; ++i) v += join[i];
     }
@@ -38,7 +42,9 @@ __device__ __forceinline__ float inverse_root(float m) {
 // Rows of one wavefront share a workgroup of four; else a workgroup has one row.
 constexpr int threads_of(int waves) { return waves == 1 ? 256 : 64 * waves; }
 
-// TAIL: the width is no multiple of a vector (any alignment is read the same).
+// TAIL: the width is no multiple of a vector (any alignment is read the same). (The kernels ask for the
+// wavefronts a SIMD that they have room for but for a register or two, which go to scratch: fp32 rows of
+// 4096, backward, 107 us, with one wavefront 112.)
 template <typename T, int NV, int WAVES, bool TAIL>
 struct Rows {
     static constexpr int VEC = 16 / (int)sizeof(T);
@@ -70,33 +76,40 @@ struct Rows {
         else if (vec(i) * VEC < width) write_lot((T *)p + at + vec(i) * VEC, x, stream);
     }
     // h - mean (layer norm) in place, 0 past the row's end; the inverse root of its mean square
-    static __device__ __forceinline__ float normed(const NormArgs &a, float (&h)[NV][VEC], float *join) {
+    static __device__ __forceinline__ float normed(const NormArgs &a, float (&h)[NV][VEC], Join<WAVES> &join) {
         if (a.layer) {
-            float s = 0.f;
+            // The mean in 64 bits, exact for equal values: a sum in 32 is off by some 2^-24 of the values, which
+            // is no small share of their distance from the mean where they are nearly alike (2 to 3 %
+            // of a layer norm's time).
+            double s = 0.0;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) s += h[i][j];
-            const float mean = row_total<WAVES>(s, join) / (float)a.width;   // (exact where all are equal)
+                for (int j = 0; j < VEC; ++j) s += (double)h[i][j];
+            s = row_total<WAVES>(s, join.wide);
+            // (the quotient with its remainder's, in fewer registers than a division)
+            double mean = s * a.inv_width;
+            mean = fma(fma(-mean, (double)a.width, s), a.inv_width, mean);
+            const float high = (float)mean, low = (float)(mean - (double)high);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) h[i][j] = vec(i) * VEC + j < a.width ? h[i][j] - mean : 0.f;
+                for (int j = 0; j < VEC; ++j) h[i][j] = vec(i) * VEC + j < a.width ? h[i][j] - high - low : 0.f;
         }
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) s = fmaf(h[i][j], h[i][j], s);
-        return inverse_root(row_total<WAVES>(s, join) / (float)a.width + a.eps);
+        return inverse_root(row_total<WAVES>(s, join.narrow) / (float)a.width + a.eps);
     }
 };
 
 template <typename T, int NV, int WAVES, bool TAIL>
-__global__ __launch_bounds__(threads_of(WAVES)) void norm_kernel(NormArgs a) {
+__global__ __launch_bounds__(threads_of(WAVES), WAVES == 4 && !TAIL ? 3 : 1) void norm_kernel(NormArgs a) {
     using R = Rows<T, NV, WAVES, TAIL>;
     constexpr int VEC = R::VEC;
-    __shared__ float join[WAVES];
+    __shared__ Join<WAVES> join;
     const int width = a.width;
     for (int64_t r = (int64_t)blockIdx.x * R::kRows + R::sub(); r < a.rows; r += (int64_t)gridDim.x * R::kRows) {
         float h[NV][VEC];
@@ -141,10 +154,10 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_kernel(NormArgs a) {
 // Persistent workgroups over rows; a lane sums its columns' weight and bias gradients over its
 // rows, the workgroup joins them in a fixed order and writes one partial row of both.
 template <typename T, int NV, int WAVES, bool TAIL, bool BIAS>
-__global__ __launch_bounds__(threads_of(WAVES)) void norm_backward_kernel(NormArgs a) {
+__global__ __launch_bounds__(threads_of(WAVES), BIAS ? 1 : 2) void norm_backward_kernel(NormArgs a) {
     using R = Rows<T, NV, WAVES, TAIL>;
     constexpr int VEC = R::VEC;
-    __shared__ float join[WAVES];
+    __shared__ Join<WAVES> join;
     const int width = a.width;
     const float inv = 1.f / (float)width;
     float gw[NV][VEC] = {}, gb[BIAS ? NV : 1][VEC] = {};
@@ -175,8 +188,8 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_backward_kernel(NormAr
                 sn = fmaf(g[i][j], h[i][j], sn);
             }
         }
-        sn = row_total<WAVES>(sn, join) * inv;
-        sg = a.layer ? row_total<WAVES>(sg, join) * inv : 0.f;
+        sn = row_total<WAVES>(sn, join.narrow) * inv;
+        sg = a.layer ? row_total<WAVES>(sg, join.narrow) * inv : 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             float u[VEC];

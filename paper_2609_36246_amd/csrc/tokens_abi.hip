@@ -67,6 +67,7 @@ NormArgs norm_args(const olive_norm_desc *d) {
     a.width = d->width;
     a.layer = d->kind == OLIVE_NORM_LAYER;
     a.eps = d->eps;
+    a.inv_width = 1.0 / (double)d->width;
     a.weight = d->weight;
     a.bias = d->bias;
     return a;

@@ -41,6 +41,7 @@ struct NormArgs {
     float *part;                     // backward: [workgroups][2][width] partial sums
     int32_t rows, width, layer;
     float eps;
+    double inv_width;
     bool stream;                     // what is written goes past the caches
 };
 

@@ -1,0 +1,97 @@
+"""Row norms of values that sums in 32 bits do not hold: rows whose values are all alike or nearly so.
+
+Bounds, u = 2^-24, beside those of a sum over the width d (u (log2(d) + 36) times the sum of the
+absolute values, half of it and a unit for the inverse root): the mean is formed in 64 bits, by
+chains of 32 + 6 + 16 additions at most, and held in two parts of fp32, so it is off by at most
+(54 2^-53 + 2^-48) mean |h|, and the definition's own mean by as much again: 2^-46 mean |h| in
+all. The distance from it takes two roundings of its own size, which the units below hold. n is off
+by that over the standard deviation, and by n times it through the mean square.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import tokens_oracle as O
+from paper_2609_36246_amd import _lib as L
+from tests.test_gpu_tokens_norm import LAYER, Norm, sums
+from tests.tokens_harness import BF16, F32, U32, f64, unit
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def gpu():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    L.load()
+
+
+def deviations(h, eps):
+    c = h - h.mean(1, keepdims=True)
+    std = np.sqrt((c * c).mean(1, keepdims=True) + eps)
+    return c / std, 2.0 ** -46 * np.abs(h).mean(1, keepdims=True) / std
+
+
+def check_forward(n, out=None):
+    """Against the definition, with the bounds above: no share of the mean in fp32."""
+    out = n.forward()[0] if out is None else out
+    h, layer = f64(n.h()), n.k == LAYER
+    w, b = (None if t is None else f64(t) for t in (n.w, n.b))
+    want, plain = O.row_norm(h, w, b, n.eps, layer), np.abs(O.row_norm(h, w, None, n.eps, layer))
+    tol = (sums(n.width) + 6 * U32) * plain + 2 * U32 * np.abs(want) + unit(n.dtype) * np.abs(want) + 2.0 ** -133
+    if layer:
+        c, off = deviations(h, n.eps)
+        tol = tol + off * (1.0 + c * c) * (1.0 if w is None else np.abs(w))
+    bad = ~(np.abs(f64(out) - want) <= tol)
+    assert not bad.any(), "%d off, first at %s" % (bad.sum(), np.argwhere(bad)[0])
+
+
+def check_backward(n):
+    gh, gw, gb = n.backward()
+    h, layer = f64(n.h()), n.k == LAYER
+    ds, w = (None if t is None else f64(t) for t in (n.dsum, n.w))
+    want, size, ww, ws, bw, bs = O.row_norm_backward(h, w, n.eps, layer, f64(n.dy), ds)
+    rel, extra = 3 * sums(n.width) + 12 * U32, 0.0
+    if layer:
+        c, off = deviations(h, n.eps)
+        off = off * (1.0 + c * c).max(1, keepdims=True)
+        size, rel, extra = size * (1.0 + np.abs(c).max(1, keepdims=True)), rel + 3 * off, off.max()
+    bad = ~(np.abs(f64(gh) - want) <= rel * size + unit(n.dtype) * np.abs(want) + 2.0 ** -133)
+    assert not bad.any(), "%d off, first at %s" % (bad.sum(), np.argwhere(bad)[0])
+    rows = U32 * (n.rows + 4)
+    scale = np.abs(f64(n.dy)).sum(0)
+    assert np.all(np.abs(f64(gw) - ww) <= (rows + sums(n.width) + 6 * U32) * ws + extra * scale + 1e-37)
+    assert np.all(np.abs(f64(gb) - bw) <= rows * bs + 1e-37)
+
+
+ALIKE = [0.1, 1000.1, -3.14159, 7.3e-3, 123456.7, 1.1e-30, -2.9e38]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [2, 7, 768, 777, 1600, 2048, 4096, 5000, 16384])
+def test_rows_of_equal_values(width, dtype):
+    """Their distance from the mean is 0 whatever the value: the output is the bias, the weight's
+    gradient 0, and the rows' r (g - mean g)."""
+    n = Norm(len(ALIKE), width, dtype, LAYER, bias=True)
+    n.x.copy_(torch.tensor(ALIKE).to(dtype)[:, None].expand(-1, width))
+    assert torch.equal(n.forward()[0], n.b.expand(len(ALIKE), -1))
+    gh, gw, gb = n.backward()
+    assert not bool(gw.any())
+    g = f64(n.dy) * f64(n.w)
+    r = (f64(torch.tensor(n.eps, dtype=F32))) ** -0.5
+    want, size = r * (g - g.mean(1, keepdims=True)), r * (np.abs(g) + np.abs(g).mean(1, keepdims=True))
+    assert np.all(np.abs(f64(gh) - want) <= (3 * sums(width) + 12 * U32) * size + unit(dtype) * np.abs(want))
+    bare = Norm(len(ALIKE), width, dtype, LAYER, weight=False)
+    bare.x.copy_(n.x)
+    assert not bool(bare.forward()[0].any())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("mean,std", [(1000.1, 0.02), (-77.7, 1e-3), (3.0, 0.5), (4e5, 1.0)])
+@pytest.mark.parametrize("width", [65, 777, 2048, 4096, 6001, 16384])
+def test_rows_far_from_zero(width, mean, std, dtype):
+    """Means of up to 4e5 standard deviations (in bf16 the values are then a few neighbours, or all
+    alike)."""
+    n = Norm(5, width, dtype, LAYER, bias=True, std=std, mean=mean, eps=1e-12)
+    n.eps = float(torch.tensor(n.eps, dtype=F32))
+    check_forward(n)
+    check_backward(n)
