@@ -86,6 +86,7 @@ olive_status olive_embed_backward(const olive_embed_desc *desc, const void *grad
 /*
  *   h = x + residual, rounded to the dtype (x itself without a residual)
  *   y = n * weight + bias           (a NULL weight is 1, a NULL bias 0)
+ * for values of any size: squares need not be numbers of fp32, and the mean is summed in 64 bits.
  */
 typedef struct {
     int32_t size;                /* sizeof(olive_norm_desc) (checked) */

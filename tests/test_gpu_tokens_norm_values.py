@@ -1,11 +1,13 @@
-"""Row norms of values that sums in 32 bits do not hold: rows whose values are all alike or nearly so.
+"""Row norms of values that 32-bit sums and squares do not hold: rows whose values are all alike or
+nearly so, whose squares leave fp32, and whose distance from the mean does.
 
 Bounds, u = 2^-24, beside those of a sum over the width d (u (log2(d) + 36) times the sum of the
 absolute values, half of it and a unit for the inverse root): the mean is formed in 64 bits, by
 chains of 32 + 6 + 16 additions at most, and held in two parts of fp32, so it is off by at most
 (54 2^-53 + 2^-48) mean |h|, and the definition's own mean by as much again: 2^-46 mean |h| in
-all. The distance from it takes two roundings of its own size, which the units below hold. n is off
-by that over the standard deviation, and by n times it through the mean square.
+all. The distance from it takes two roundings of its own size, which the units below hold; a subnormal
+distance is a multiple of 2^-149, and the mean's second part with it, half of that off at most. n is off by
+that over the standard deviation, and by n times it through the mean square.
 """
 import numpy as np
 import pytest
@@ -13,7 +15,7 @@ import torch
 
 from oracle import tokens_oracle as O
 from paper_2609_36246_amd import _lib as L
-from tests.test_gpu_tokens_norm import LAYER, Norm, sums
+from tests.test_gpu_tokens_norm import LAYER, RMS, Norm, sums
 from tests.tokens_harness import BF16, F32, U32, f64, unit
 
 pytestmark = pytest.mark.gpu
@@ -28,7 +30,7 @@ def gpu():
 def deviations(h, eps):
     c = h - h.mean(1, keepdims=True)
     std = np.sqrt((c * c).mean(1, keepdims=True) + eps)
-    return c / std, 2.0 ** -46 * np.abs(h).mean(1, keepdims=True) / std
+    return c / std, (2.0 ** -46 * np.abs(h).mean(1, keepdims=True) + 2.0 ** -149) / std
 
 
 def check_forward(n, out=None):
@@ -95,3 +97,68 @@ def test_rows_far_from_zero(width, mean, std, dtype):
     n.eps = float(torch.tensor(n.eps, dtype=F32))
     check_forward(n)
     check_backward(n)
+
+
+SIZES = [(5, 640, "plain"), (3, 7, "plain"), (6, 2056, "odd"), (4, 4096, "part"), (3, 6001, "plain"), (2, 16384, "plain")]
+
+
+@pytest.mark.parametrize("k", [RMS, LAYER])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,width,how", SIZES)
+@pytest.mark.parametrize("scale,eps", [(1e-25, 0.0), (1e-36, 0.0), (1e-21, 1e-42), (1e-25, 1e-6), (1e19, 0.0), (1e25, 1e-6),
+                                       (3e37, 1e-6), (1.5e19, 3e38), (1e3, 3e38)])
+def test_squares_out_of_range(rows, width, how, scale, eps, dtype, k):
+    """eps is stored in fp32: the definition takes it as it is there."""
+    n = Norm(rows, width, dtype, k, how, bias=True, std=scale, mean=0.2 * scale, eps=eps)
+    n.eps = float(torch.tensor(eps, dtype=F32))
+    check_forward(n)
+    check_backward(n)
+
+
+@pytest.mark.parametrize("k", [RMS, LAYER])
+def test_subnormal_values(k):
+    n = Norm(4, 1000, F32, k, std=1e-41, mean=0.0, eps=0.0)
+    check_forward(n)
+    n = Norm(4, 1000, F32, k, std=1e-41, mean=0.0, eps=1e-6)
+    check_forward(n)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [40, 777, 2048, 9000])
+def test_distances_from_the_mean_out_of_range(width, dtype):
+    n = Norm(4, width, dtype, LAYER, bias=True, std=1e37)
+    top = torch.finfo(dtype).max
+    n.x[0], n.x[1], n.x[2] = -top, top, -0.9 * top
+    n.x[0, 1], n.x[1, 0], n.x[2, ::2] = top, -top, 0.9 * top
+    check_forward(n)
+    check_backward(n)
+
+
+@pytest.mark.parametrize("k", [RMS, LAYER])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [100, 1024, 4100, 5000])
+def test_in_place_and_rows_of_every_size(width, dtype, k):
+    """Rows of all sizes in one call give what each gives alone, also where the sum goes to x or to the residual
+    before the row is looked at again."""
+    scales = [1.0, 1e25, 1e-25, 0.0, 1e37, 1e-36, 2.0]
+    n = Norm(len(scales), width, dtype, k, bias=True, residual=True, eps=1e-32)
+    for i, s in enumerate(scales):
+        n.x[i] *= s
+        n.res[i] *= s
+    out, total = n.forward()
+    x, r = n.x.clone(), n.res.clone()
+    for o, t in ((n.x, n.res), (n.res, n.x)):
+        n.x.copy_(x), n.res.copy_(r)
+        n.forward(out=o, total=t)
+        assert torch.equal(o, out) and torch.equal(t, total)
+    n.x.copy_(x), n.res.copy_(r)
+    alone = torch.empty_like(out)
+    L.olive_row_norm(n.desc, n.x, alone, n.res)            # without the sum
+    assert torch.equal(alone, out)
+    gh, _, _ = n.backward()
+    one, d = torch.empty(1, width, dtype=dtype, device="cuda"), L.make_norm_desc(1, width, n.w, n.b, n.desc.dtype, 1e-32, k)
+    for i in range(len(scales)):
+        L.olive_row_norm(d, n.x[i:i + 1], one, n.res[i:i + 1])
+        assert torch.equal(one, out[i:i + 1])
+        L.olive_row_norm_backward(d, total[i:i + 1], n.dy[i:i + 1], one, n.dsum[i:i + 1])
+        assert torch.equal(one, gh[i:i + 1])
