@@ -6,7 +6,7 @@ pointers, sizes and the HIP stream. Torch tensors are accepted wherever the C
 function takes a device pointer (their data_ptr() is passed); None maps to NULL.
 The layer operators' and the token operators' functions refuse tensors of another type or
 layout than the library would read (ValueError); the sizes of the heads' views are the
-caller's, those of the token operators' matrices are checked.
+caller's, those of the token operators' matrices are checked, and the device of their tensors.
 The library must have been built (python -m paper_2609_36246_amd.build); loading
 fails loudly otherwise -- there is no fallback path.
 """
@@ -133,12 +133,14 @@ class olive_embed_desc(ctypes.Structure):
     _fields_ = [("size", ctypes.c_int32), ("dtype", ctypes.c_int32), ("tokens", ctypes.c_int64),
                 ("vocab", ctypes.c_int64), ("width", ctypes.c_int32), ("scale", ctypes.c_float),
                 ("ids", ctypes.c_void_p)]
+    device = None            # of the tensors that the descriptor holds (make_embed_desc)
 
 
 class olive_norm_desc(ctypes.Structure):
     _fields_ = [("size", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rows", ctypes.c_int64),
                 ("width", ctypes.c_int32), ("kind", ctypes.c_int32), ("eps", ctypes.c_float),
                 ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+    device = None            # of the tensors that the descriptor holds (make_norm_desc)
 
 
 class olive_sample_desc(ctypes.Structure):
@@ -146,6 +148,7 @@ class olive_sample_desc(ctypes.Structure):
                 ("vocab", ctypes.c_int64), ("uniform", ctypes.c_void_p),
                 ("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
                 ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p)]
+    device = None            # of the tensors that the descriptor holds (make_sample_desc)
 
 
 class OliveError(RuntimeError):
@@ -737,6 +740,23 @@ def _rows(x, dtype, rows: int, width: int, here: int, what: str, output: bool = 
                      % (what, rows, width, dtype, " apart from each other" if output else ""))
 
 
+def _device_of(what: str, used: bool, *tensors) -> Optional[int]:
+    """The one device of a descriptor's tensors (None: it has none, or addresses, or a call of its
+    sizes reads none of them)."""
+    found = {x.get_device() for x in tensors if x is not None and not isinstance(x, int)} if used else ()
+    if len(found) > 1:
+        raise ValueError("%s: tensors on devices %s" % (what, sorted(found)))
+    return next(iter(found), None)
+
+
+def _current(desc) -> int:
+    """The current device's index, which is that of the descriptor's tensors."""
+    here = _here()
+    if desc.device is not None and desc.device != here:
+        raise ValueError("%s: tensors on device %d, and the current one is %d" % (type(desc).__name__, desc.device, here))
+    return here
+
+
 def _there(x, here: int, what: str):
     """A tensor, None or an address, which is the current device's if it is a tensor."""
     if x is not None and not isinstance(x, int) and x.get_device() != here:
@@ -751,18 +771,19 @@ def _bytes_of(name, desc) -> int:
 
 
 def make_embed_desc(tokens, vocab, width, ids, dtype=OLIVE_BF16, scale=1.0) -> olive_embed_desc:
-    """ids: contiguous int32 [tokens]; negative ones are padding. The descriptor keeps it alive."""
+    """ids: contiguous int32 [tokens]; negative ones are padding. The descriptor keeps it alive
+    and remembers its device, which a call needs to be the current one."""
     d = olive_embed_desc()
     d.size = ctypes.sizeof(olive_embed_desc)
     d.dtype, d.tokens, d.vocab, d.width = int(dtype), int(tokens), int(vocab), int(width)
     d.scale, d.ids = float(scale), _array(ids, "int32", d.tokens, "ids")
-    d.tensors = (ids,)
+    d.tensors, d.device = (ids,), _device_of("make_embed_desc", d.tokens > 0, ids)
     return d
 
 
 def olive_embed(desc: olive_embed_desc, table, out, stream=None, check: bool = True) -> int:
     """out [tokens, width] gets scale * table[ids]; table [vocab, width]."""
-    dtype, here = _dtype(desc.dtype), _here()
+    dtype, here = _dtype(desc.dtype), _current(desc)
     s = _call("olive_embed")(ctypes.addressof(desc), *_rows(table, dtype, desc.vocab, desc.width, here, "table"),
                              *_rows(out, dtype, desc.tokens, desc.width, here, "out", True), _stream(stream))
     if check:
@@ -781,7 +802,7 @@ def olive_embed_backward(desc: olive_embed_desc, grad_out, grad_table, accumulat
     added to the rows of the tokens that occur."""
     if str(grad_table.dtype) not in ("torch.bfloat16", "torch.float32"):
         raise ValueError("grad_table: expected bf16 or fp32")
-    kind, here = OLIVE_F32 if str(grad_table.dtype) == "torch.float32" else OLIVE_BF16, _here()
+    kind, here = OLIVE_F32 if str(grad_table.dtype) == "torch.float32" else OLIVE_BF16, _current(desc)
     s = _call("olive_embed_backward")(
         ctypes.addressof(desc), *_rows(grad_out, _dtype(desc.dtype), desc.tokens, desc.width, here, "grad_out"),
         *_rows(grad_table, grad_table.dtype, desc.vocab, desc.width, here, "grad_table", True), kind, int(accumulate),
@@ -793,19 +814,20 @@ def olive_embed_backward(desc: olive_embed_desc, grad_out, grad_table, accumulat
 
 def make_norm_desc(rows, width, weight=None, bias=None, dtype=OLIVE_BF16, eps=1e-6,
                    kind=OLIVE_NORM_RMS) -> olive_norm_desc:
-    """weight and bias: contiguous [width] of the rows' dtype. The descriptor keeps them alive."""
+    """weight and bias: contiguous [width] of the rows' dtype, on one device, which a call
+    needs to be the current one. The descriptor keeps them alive."""
     d = olive_norm_desc()
     d.size = ctypes.sizeof(olive_norm_desc)
     d.dtype, d.rows, d.width, d.kind, d.eps = int(dtype), int(rows), int(width), int(kind), float(eps)
     d.weight = _array(weight, d.dtype, d.width, "weight")
     d.bias = _array(bias, d.dtype, d.width, "bias")
-    d.tensors = (weight, bias)
+    d.tensors, d.device = (weight, bias), _device_of("make_norm_desc", d.rows > 0, weight, bias)
     return d
 
 
 def olive_row_norm(desc: olive_norm_desc, x, out, residual=None, sum_out=None, stream=None, check: bool = True) -> int:
     """All [rows, width]: out gets the norm of x + residual, sum_out that sum."""
-    t, n, w, here = _dtype(desc.dtype), desc.rows, desc.width, _here()
+    t, n, w, here = _dtype(desc.dtype), desc.rows, desc.width, _current(desc)
     s = _call("olive_row_norm")(
         ctypes.addressof(desc), *_rows(x, t, n, w, here, "x"), *_rows(residual, t, n, w, here, "residual"),
         *_rows(out, t, n, w, here, "out", True), *_rows(sum_out, t, n, w, here, "sum_out", True), _stream(stream))
@@ -822,7 +844,7 @@ def olive_row_norm_workspace(desc: olive_norm_desc) -> int:
 def olive_row_norm_backward(desc: olive_norm_desc, h, grad_out, grad_h, grad_sum=None, grad_weight=None,
                             grad_bias=None, workspace=None, stream=None, check: bool = True) -> int:
     """h: the rows that were normed (the forward's sum_out, or x without a residual)."""
-    t, n, w, here = _dtype(desc.dtype), desc.rows, desc.width, _here()
+    t, n, w, here = _dtype(desc.dtype), desc.rows, desc.width, _current(desc)
     s = _call("olive_row_norm_backward")(
         ctypes.addressof(desc), *_rows(h, t, n, w, here, "h"), *_rows(grad_out, t, n, w, here, "grad_out"),
         *_rows(grad_sum, t, n, w, here, "grad_sum"), *_rows(grad_h, t, n, w, here, "grad_h", True),
@@ -837,7 +859,8 @@ def olive_row_norm_backward(desc: olive_norm_desc, h, grad_out, grad_h, grad_sum
 def make_sample_desc(rows, vocab, uniform, temperature=None, top_k=None, top_p=None, min_p=None,
                      dtype=OLIVE_BF16) -> olive_sample_desc:
     """uniform, temperature, top_p, min_p: contiguous fp32 [rows]; top_k int32 [rows]; None where a
-    setting is not used. The descriptor keeps them alive."""
+    setting is not used; all on one device, which a call needs to be the current one. The
+    descriptor keeps them alive."""
     d = olive_sample_desc()
     d.size = ctypes.sizeof(olive_sample_desc)
     d.dtype, d.rows, d.vocab = int(dtype), int(rows), int(vocab)
@@ -846,6 +869,7 @@ def make_sample_desc(rows, vocab, uniform, temperature=None, top_k=None, top_p=N
     d.top_k = _array(top_k, "int32", d.rows, "top_k")
     d.top_p, d.min_p = _array(top_p, OLIVE_F32, d.rows, "top_p"), _array(min_p, OLIVE_F32, d.rows, "min_p")
     d.tensors = (uniform, temperature, top_k, top_p, min_p)
+    d.device = _device_of("make_sample_desc", d.rows > 0, *d.tensors)
     return d
 
 
@@ -857,7 +881,7 @@ def olive_sample_workspace(desc: olive_sample_desc) -> int:
 def olive_sample(desc: olive_sample_desc, logits, token, logp=None, kept=None, workspace=None, stream=None,
                  check: bool = True) -> int:
     """logits [rows, vocab]; token, kept int32 [rows], logp fp32 [rows]."""
-    n, here = desc.rows, _here()
+    n, here = desc.rows, _current(desc)
     s = _call("olive_sample")(
         ctypes.addressof(desc), *_rows(logits, _dtype(desc.dtype), n, desc.vocab, here, "logits"),
         _array(_there(token, here, "token"), "int32", n, "token"),
