@@ -78,10 +78,13 @@ struct Parts {
     int32_t bytes;                               // of a part in the workspace
 };
 
-// Rows of up to 16384 tokens are counted by the workgroup that does the rest, in one launch. Else a
-// row has up to 16 parts of 4096 tokens at least, fewer where there are more than 128 rows (a part
-// costs the second launch its counts: 64 rows of 151936 take the same with 8 and with 16).
-// Rows of fp32 that are cut are not split (count 0).
+// Rows of up to 16384 bf16 tokens are counted by the workgroup that does the rest, in one launch. So are cut ones
+// of up to 65024 (what counts of 16 bits hold) in calls of more than 1024 rows, which need no workspace
+// then (1100 rows of 65024: 183 us; with two parts 132, and 57 KB a row). Else a call has 2048 parts over its rows
+// (16 a row at most, of 4096 tokens at least, and as many as 65024 tokens a part ask for: a part costs the second
+// launch its counts, 64 rows of 151936 take the same with 8 and with 16); where every token is kept 1024 parts
+// (64 a row at most, of 2048 tokens at least and of kWhole at most). Rows of fp32 that are cut are not
+// split (count 0).
 Parts parts_of(const SampleArgs &a, bool bf16) {
     const int whole = bf16 ? kWhole<uint16_t> : kWhole<float>;
     // (every row keeps every token, or the first alone)
