@@ -101,9 +101,10 @@ typedef struct {
 
 /*
  * x, residual, out, sum: [rows][width]; residual NULL: none; sum: where h goes, or NULL.
- * out or sum may be x or residual themselves, and each other's buffers are distinct; other
- * overlaps are not allowed. The rows are normed as the sum that is stored.
- * Errors: E_NULL, E_SHAPE (sizes, strides), E_DTYPE, E_RANGE (size, kind, eps),
+ * out or sum may be x or residual themselves (with their strides), and each other's buffers
+ * are distinct; other overlaps are not allowed. The rows are normed as the sum that is stored.
+ * Errors: E_NULL, E_SHAPE (sizes, strides, out where sum is, or an output where an input of
+ * other strides is), E_DTYPE, E_RANGE (size, kind, eps),
  * E_UNSUPPORTED (more than 16384 elements; a matrix that is not aligned to its type), E_HIP.
  */
 olive_status olive_row_norm(const olive_norm_desc *desc, const void *x, int64_t x_stride,

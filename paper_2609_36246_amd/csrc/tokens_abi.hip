@@ -23,6 +23,12 @@ bool apart(int64_t rows, int64_t width, int64_t stride, bool output) {
     return stride >= (output ? width : 0) && stride <= ((int64_t)1 << 60) / rows;
 }
 
+// Whether an output that begins where an input does is the same matrix, whose rows are read before they are
+// written; with other strides it would write rows that are still to be read.
+bool same_or_apart(int64_t rows, const void *in, int64_t in_stride, const void *out, int64_t out_stride) {
+    return !in || in != out || rows <= 1 || in_stride == out_stride;
+}
+
 olive_status check_workspace(const void *w, int64_t have, int64_t need) {
     if (need <= 0) return OLIVE_OK;
     if (!w) return OLIVE_E_NULL;
@@ -161,6 +167,10 @@ olive_status olive_row_norm(const olive_norm_desc *desc, const void *x, int64_t 
     if (!apart(n, w, x_stride, false) || (residual && !apart(n, w, residual_stride, false)) ||
         !apart(n, w, out_stride, true) || (sum && !apart(n, w, sum_stride, true)))
         return OLIVE_E_SHAPE;
+    if (out == sum || !same_or_apart(n, x, x_stride, out, out_stride) || !same_or_apart(n, x, x_stride, sum, sum_stride) ||
+        !same_or_apart(n, residual, residual_stride, out, out_stride) ||
+        !same_or_apart(n, residual, residual_stride, sum, sum_stride))
+        return OLIVE_E_SHAPE;
     for (const void *p : {x, residual, (const void *)out, (const void *)sum})
         if (misplaced(p, desc->dtype)) return OLIVE_E_UNSUPPORTED;
     NormArgs a = norm_args(desc);
@@ -191,6 +201,9 @@ olive_status olive_row_norm_backward(const olive_norm_desc *desc, const void *h,
     if (n > 0 && (!h || !grad_out || !grad_h)) return OLIVE_E_NULL;
     if (!apart(n, w, h_stride, false) || !apart(n, w, grad_out_stride, false) ||
         (grad_sum && !apart(n, w, grad_sum_stride, false)) || !apart(n, w, grad_h_stride, true))
+        return OLIVE_E_SHAPE;
+    if (!same_or_apart(n, grad_out, grad_out_stride, grad_h, grad_h_stride) ||
+        !same_or_apart(n, grad_sum, grad_sum_stride, grad_h, grad_h_stride))
         return OLIVE_E_SHAPE;
     for (const void *p : {h, grad_out, grad_sum, (const void *)grad_h})
         if (misplaced(p, desc->dtype)) return OLIVE_E_UNSUPPORTED;

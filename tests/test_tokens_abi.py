@@ -280,3 +280,20 @@ def test_tensors_of_another_device(monkeypatch):
 def test_descriptors_of_other_arrays(make):
     with pytest.raises(ValueError):
         make()
+
+
+def test_norm_outputs_where_other_rows_lie():
+    """An output may be an input itself; at its address with other strides it would overwrite rows
+    that are still to be read."""
+    d, one = norm_desc(), norm_desc(rows=1)
+    Q = 2 * P
+    for inputs in (dict(x=P, xs=0), dict(x=P, xs=128), dict(x=Q, res=P, rs=0), dict(x=Q, res=P, rs=65)):
+        assert norm(d, out=P, os_=64, **inputs) == E.OLIVE_E_SHAPE
+        assert norm(d, out=3 * P, os_=64, total=P, ts=64, **inputs) == E.OLIVE_E_SHAPE
+    assert norm(d, x=Q, out=P, total=P, ts=64) == E.OLIVE_E_SHAPE and norm(one, x=Q, out=P, total=P) == E.OLIVE_E_SHAPE
+    assert norm_backward(d, g=P, gs=0, gh=P) == E.OLIVE_E_SHAPE and norm_backward(d, g=P, gs=128, gh=P) == E.OLIVE_E_SHAPE
+    assert norm_backward(d, g=Q, s=P, ss=0, gh=P) == E.OLIVE_E_SHAPE
+    # (refused for what comes after: the strides are one row's, or the input's own)
+    assert norm_backward(one, g=P, gs=0, gh=P, ghs=64, gw=P + 2) == E.OLIVE_E_UNSUPPORTED
+    assert norm_backward(d, g=P, s=P, ss=64, gh=P, gw=P + 2) == E.OLIVE_E_UNSUPPORTED
+    assert norm(d, x=Q, res=P + 1, rs=64, out=Q) == E.OLIVE_E_UNSUPPORTED
