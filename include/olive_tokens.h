@@ -68,8 +68,9 @@ olive_status olive_embed_workspace(const olive_embed_desc *desc, int64_t *bytes)
  * written, zeros for tokens that do not occur; accumulate 1: only the rows of tokens that occur
  * are read and written. grad_dtype: olive_dtype of grad_table. Negative tokens and tokens >=
  * vocab have no part in it. grad_out and grad_table do not overlap. workspace: device, 16-byte
- * aligned, NULL if 0 bytes are needed (up to 1024 tokens; else 16 bytes a token, and two rows in
- * fp32 for every 16 to 64 tokens).
+ * aligned, of olive_embed_workspace's bytes; NULL if 0 are needed (up to 1024 tokens; else 16
+ * bytes a token, and for every 16 to 64 tokens two rows in fp32, each of the width rounded up to
+ * a multiple of 512).
  * Errors: as olive_embed, plus E_SHAPE for a workspace that is too small.
  */
 olive_status olive_embed_backward(const olive_embed_desc *desc, const void *grad_out,
